@@ -311,6 +311,130 @@ int prefixkv_decode_attn_evict(const pkv_shape *shape, int l0, int l1, const voi
                                int distance, void *out, void *ws, size_t ws_bytes,
                                pkv_stream stream);
 
+/* ==== Packed prompts and paged caches =============================================================
+ * For programs that serve sequences of different lengths.  S sequences are packed one behind the
+ * other into T rows: row_off [dev] i32 [S+1] is non-decreasing, sequence s owns the rows
+ * row_off[s] ... row_off[s+1]-1 (none is a sequence without rows), rows in front of row_off[0] and from
+ * row_off[S] on belong to nobody and are left as they are.  Row tensors are [L, heads, T, D] with
+ * element strides l, h and n (b is not looked at, n may be any multiple of 16 bytes), so that a
+ * projection's token-major [T, heads, D] output is passed as it is.
+ *
+ * The cache of a (sequence, layer) is a list of pages, because every layer keeps another number of
+ * positions.  A page holds page_size entries of one (sequence, layer), all KV heads: kp and vp are
+ * [num_pages, Hkv, page_size, D] dense; entry j of (s,l) is row j % page_size of the page
+ * table[s, l, j / page_size].  lens[s,l] counts the entries.  Entries behind lens are never looked at,
+ * so a page need not be cleared.  A table id outside 0 ... num_pages-1 where an entry is asked for is a
+ * fault of the caller's: such rows are not written, and in attention their keys take no part.
+ *   slot = page * page_size + row names an entry of the pool. */
+typedef struct { int32_t S, L, H, Hkv, T, D; int32_t dtype; } pkv_packed;   /* 1 <= S <= 4096, 1 <= L <= 64, 1 <= T <= 2^22 */
+typedef struct {
+    int32_t num_pages;  /* of the pool */
+    int32_t page_size;  /* 16, 32, 64, 128 or 256 entries */
+    int32_t max_pages;  /* width of a table row; max_pages * page_size < 2^20 */
+    int32_t layers;     /* layers of table and lens: [S, layers, max_pages], [S, layers] */
+} pkv_paging;
+
+/* Why prefixkv_page_resize / _append left everything as it was (*status) */
+enum {
+    PKV_PAGES_SHORT = 1, /* fewer free pages than are needed (and nothing of the kind below) */
+    PKV_PAGES_RANGE = 2  /* a length below 0 or above max_pages*page_size, offsets that descend or pass T,
+                            or ends of the ring that cannot be */
+};
+
+/* ---- Page tables and slots from lengths, on the device: nothing is read back.
+ * Free pages wait in a ring: ring [dev] i32 [num_pages], state [dev] i32 [2] = {head, count}; the free
+ * pages are ring[(head + i) % num_pages], i < count.
+ * prefixkv_page_resize gives every segment the length target[s,l]: with held = ceil(lens / page_size)
+ * and want = ceil(target / page_size) entries held ... want-1 of its table row are taken from the head of
+ * the ring, or entries want ... held-1 go to its end, segments in (s,l) order, entries ascending.  A call
+ * needs as many free pages before it as it takes; what it gives back serves the next one.  All of it is
+ * done, or (*status != 0) nothing.
+ * A new sequence is a row of lens that is 0; target 0 ends one.
+ *   target, lens [dev] i32 [S, layers];  lens_out may be lens, state_out may be state;  status [dev] i32 [1]
+ *   ws [dev]: prefixkv_page_workspace_bytes(S, layers) bytes, any contents, 4-byte aligned
+ * S * layers * max_pages < 2^31. */
+size_t prefixkv_page_workspace_bytes(int S, int layers);
+int prefixkv_page_resize(int S, const pkv_paging *paging, const int32_t *target, const int32_t *lens,
+                         int32_t *table, int32_t *ring, const int32_t *state, int32_t *lens_out,
+                         int32_t *state_out, int32_t *status, void *ws, size_t ws_bytes,
+                         pkv_stream stream);
+/* prefixkv_page_append is the same with target = lens + (row_off[s+1] - row_off[s]) in every layer, and
+ * gives the new rows their slots: slots [dev] i64 [layers, T], row t of sequence s in layer l becomes entry
+ * lens[s,l] + t - row_off[s]; -1 for rows that belong to nobody, and for all rows of a refused call. */
+int prefixkv_page_append(int S, int T, const pkv_paging *paging, const int32_t *row_off,
+                         const int32_t *lens, int32_t *table, const int32_t *ring, const int32_t *state,
+                         int32_t *lens_out, int32_t *state_out, int64_t *slots, int32_t *status, void *ws,
+                         size_t ws_bytes, pkv_stream stream);
+
+/* ---- Rotary positions over several axes (time, height, width of an image or video; one axis for text).
+ * Pair i of the first rot_dim columns of a row is turned by the angle  pos[axis[i], t] * freq[i]:
+ *   (a, b) -> (a cos - b sin, b cos + a sin),
+ * (a, b) = columns (i, i + rot_dim/2), or (2i, 2i+1) if interleaved; columns from rot_dim on stay.
+ *   freq [dev] u64 [rot_dim/2]: the frequency as a fraction of a turn per position, in units of 2^-64 turn.
+ *       A product with a position is then exact modulo a turn, however far out the position is.
+ *       prefixkv_rope_freq fills a host array with theta^(-2i/rot_dim) / 2 pi.
+ *   axis [dev] i32 [rot_dim/2], 0 ... axes-1;  pos [dev] i32 [axes, T], any sign
+ *   rot_dim: a multiple of 16, at most D.  1 <= axes <= 8.
+ * Rotation in fp32, one rounding to the storage type. */
+typedef struct {
+    const uint64_t *freq;
+    const int32_t *axis;
+    int32_t rot_dim, axes, interleaved;
+} pkv_rope;
+int prefixkv_rope_freq(int rot_dim, double theta, uint64_t *freq /* [host] [rot_dim/2] */);
+/* q_out, k_out [dev]: [L,H,T,D] and [L,Hkv,T,D] with strides of their own; they may be q and k themselves
+ * (same strides), and must not overlap them otherwise.  All T rows are rotated. */
+int prefixkv_rope(const pkv_packed *shape, const pkv_rope *rope, const int32_t *pos, const void *q,
+                  pkv_strides qs, const void *k, pkv_strides ks, void *q_out, pkv_strides qos,
+                  void *k_out, pkv_strides kos, pkv_stream stream);
+/* The same, with the rotated keys and the values v [L,Hkv,T,D] stored into the pages at slots [dev] i64
+ * [L,T] (from prefixkv_page_append; a caller with a layer at a time passes the layer's row).  A row whose
+ * slot is negative or past the pool is not stored; slots of one call must differ. */
+int prefixkv_rope_store(const pkv_packed *shape, const pkv_rope *rope, const int32_t *pos,
+                        const void *q, pkv_strides qs, const void *k, pkv_strides ks, const void *v,
+                        pkv_strides vs, void *q_out, pkv_strides qos, const int64_t *slots,
+                        const pkv_paging *paging, void *kp, void *vp, pkv_stream stream);
+
+/* ---- prefixkv_compact into pages: the kept set order[b,l,0..lengths[b,l]) of a rectangular batch is
+ * stored in ascending position as entries 0 ... lengths-1 of (b, l0 + l); pages come from
+ * prefixkv_page_resize with target = lengths.  A length is taken as at most N and at most
+ * max_pages*page_size.
+ *   table [dev] i32 [B, layers, max_pages];  l0 + L <= layers
+ *   kept_pos [dev] i32 [B,L,N] or NULL: the kept positions, ascending, in the first lengths[b,l] places */
+int prefixkv_compact_paged(const pkv_shape *shape, const void *k, pkv_strides ks, const void *v,
+                           pkv_strides vs, const int32_t *order, const int32_t *lengths,
+                           const pkv_paging *paging, int l0, const int32_t *table, void *kp, void *vp,
+                           int32_t *kept_pos, pkv_stream stream);
+
+/* ---- Causal attention of packed prompts: prefixkv_prefill_attn for sequences of different lengths.
+ * Row m of a sequence attends to rows 0 ... m of the same sequence.  bf16 storage only.
+ *   q, out [L,H,T,D] strides qs, os;  k, v [L,Hkv,T,D] strides ks, vs;  scale [dev] fp32 [L]
+ *   lse [dev] fp32 [L*H*T]: natural log; those of sequence s lie together as [L][H][n_s] from element
+ *       L*H*row_off[s] on, so that prefixkv_importance with B = 1 and N = n_s takes them, and the rows of q
+ *       and k, as they are.
+ *   ws [dev]: prefixkv_attn_workspace_bytes(shape, 0) bytes, 16-byte aligned (NULL if that is 0) */
+size_t prefixkv_attn_workspace_bytes(const pkv_packed *shape, int max_rows);
+int prefixkv_prefill_attn_packed(const pkv_packed *shape, const void *q, pkv_strides qs, const void *k,
+                                 pkv_strides ks, const void *v, pkv_strides vs, const int32_t *row_off,
+                                 const float *scale, void *out, pkv_strides os, float *lse, void *ws,
+                                 size_t ws_bytes, pkv_stream stream);
+
+/* ---- Attention of a chunk of new rows over the paged cache, which holds their keys and values already
+ * (prefixkv_page_append, then prefixkv_rope_store): row i of the n rows of sequence s attends in layer l to
+ * the entries 0 ... lens[s,l0+l] - n + i.  One row per sequence is a decode step.  A row that sees no entry
+ * gives zeros.
+ *   q, out [L,H,T,D] strides qs, os (the call's layers only);  scale [dev] fp32 [L]
+ *   table, lens: of all `layers`; the call works on l0 ... l0+L-1;  lens counts the new rows
+ *   max_rows: no sequence has more rows in this call (1 <= max_rows <= T); further rows of a sequence that
+ *       has more are left as they are.  It chooses the kernel: with few rows the cache is read by wavefronts
+ *       that share its entries out evenly.
+ *   ws [dev]: prefixkv_attn_workspace_bytes(shape, max_rows) bytes, 16-byte aligned (NULL if that is 0).
+ *       Calls on different streams need workspaces of their own. */
+int prefixkv_chunk_attn(const pkv_packed *shape, const void *q, pkv_strides qs, const int32_t *row_off,
+                        const pkv_paging *paging, int l0, const void *kp, const void *vp,
+                        const int32_t *table, const int32_t *lens, const float *scale, int max_rows,
+                        void *out, pkv_strides os, void *ws, size_t ws_bytes, pkv_stream stream);
+
 /* Measurement aid, not part of the method: a plain device-to-device copy kernel of a known size
  * (bytes % 16 == 0, 16-byte aligned pointers).  It reads `bytes` and writes `bytes`, which is what
  * hardware byte counters are calibrated against when a kernel's HBM traffic is reported. */

@@ -42,6 +42,19 @@ class _SelectParams(C.Structure):
                 ("fixup", C.c_int32)]
 
 
+class _Packed(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("S", "L", "H", "Hkv", "T", "D", "dtype")]
+
+
+class _Paging(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("num_pages", "page_size", "max_pages", "layers")]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("freq", C.c_void_p), ("axis", C.c_void_p), ("rot_dim", C.c_int32), ("axes", C.c_int32),
+                ("interleaved", C.c_int32)]
+
+
 _lib = None
 
 
@@ -100,6 +113,29 @@ def load(path: Optional[str] = None) -> C.CDLL:
     L.prefixkv_decode_attn_evict.restype = C.c_int
     L.prefixkv_decode_attn_evict.argtypes = [C.POINTER(_Shape), i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                              vp, vp, i32, i32, vp, vp, sz, vp]
+    packed, paging, rope = C.POINTER(_Packed), C.POINTER(_Paging), C.POINTER(_Rope)
+    L.prefixkv_page_workspace_bytes.restype = sz
+    L.prefixkv_page_workspace_bytes.argtypes = [i32, i32]
+    L.prefixkv_page_resize.restype = C.c_int
+    L.prefixkv_page_resize.argtypes = [i32, paging, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.prefixkv_page_append.restype = C.c_int
+    L.prefixkv_page_append.argtypes = [i32, i32, paging, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.prefixkv_rope_freq.restype = C.c_int
+    L.prefixkv_rope_freq.argtypes = [i32, C.c_double, vp]
+    L.prefixkv_rope.restype = C.c_int
+    L.prefixkv_rope.argtypes = [packed, rope, vp, vp, _Strides, vp, _Strides, vp, _Strides, vp, _Strides, vp]
+    L.prefixkv_rope_store.restype = C.c_int
+    L.prefixkv_rope_store.argtypes = [packed, rope, vp, vp, _Strides, vp, _Strides, vp, _Strides, vp, _Strides, vp, paging,
+                                      vp, vp, vp]
+    L.prefixkv_compact_paged.restype = C.c_int
+    L.prefixkv_compact_paged.argtypes = [C.POINTER(_Shape), vp, _Strides, vp, _Strides, vp, vp, paging, i32, vp, vp, vp, vp, vp]
+    L.prefixkv_attn_workspace_bytes.restype = sz
+    L.prefixkv_attn_workspace_bytes.argtypes = [packed, i32]
+    L.prefixkv_prefill_attn_packed.restype = C.c_int
+    L.prefixkv_prefill_attn_packed.argtypes = [packed, vp, _Strides, vp, _Strides, vp, _Strides, vp, vp, vp, _Strides, vp, vp,
+                                               sz, vp]
+    L.prefixkv_chunk_attn.restype = C.c_int
+    L.prefixkv_chunk_attn.argtypes = [packed, vp, _Strides, vp, paging, i32, vp, vp, vp, vp, vp, i32, vp, _Strides, vp, sz, vp]
     L.prefixkv_calibration_copy.restype = C.c_int
     L.prefixkv_calibration_copy.argtypes = [vp, vp, sz, vp]
     _lib = L
@@ -553,6 +589,297 @@ def prefixkv_decode_attn_evict(cache: CompactResult, base_lens: torch.Tensor, q:
         w.numel() * w.element_size(), _stream())
     if rc != 0:
         raise PrefixKVError(rc, "prefixkv_decode_attn_evict")
+    return out
+
+
+# ---- packed prompts and paged caches -----------------------------------------------------------------------
+@dataclass
+class PagedCache:
+    kp: torch.Tensor      # [num_pages,Hkv,page_size,D] storage dtype
+    vp: torch.Tensor
+    table: torch.Tensor   # [S,layers,max_pages] i32
+    lens: torch.Tensor    # [S,layers] i32
+    ring: torch.Tensor    # [num_pages] i32: the free pages, from head on
+    state: torch.Tensor   # [2] i32: head, count
+
+    def __post_init__(self):
+        for t in (self.table, self.lens, self.ring, self.state):
+            if t.dtype != torch.int32 or not t.is_contiguous():
+                raise ValueError("table, lens, ring and state must be contiguous i32")
+        if self.kp.dim() != 4 or self.vp.shape != self.kp.shape or self.vp.dtype != self.kp.dtype:
+            raise ValueError("kp, vp must be [num_pages,Hkv,page_size,D] of one dtype")
+        if (self.table.dim() != 3 or self.lens.shape != self.table.shape[:2] or self.ring.shape != self.kp.shape[:1]
+                or self.state.shape != (2,)):
+            raise ValueError("table must be [S,layers,max_pages], lens [S,layers], ring [num_pages], state [2]")
+        P, Hkv, ps, D = self.kp.shape
+        self._paging = _Paging(P, ps, self.table.shape[2], self.table.shape[1])
+
+
+def paged_cache(S: int, layers: int, Hkv: int, D: int, page_size: int, num_pages: int, max_pages: int,
+                dtype: torch.dtype = torch.bfloat16, device="cuda") -> PagedCache:
+    """An empty cache for S sequences: every page is free."""
+    pool = (num_pages, Hkv, page_size, D)
+    return PagedCache(kp=torch.empty(pool, dtype=dtype, device=device), vp=torch.empty(pool, dtype=dtype, device=device),
+                      table=torch.full((S, layers, max_pages), -1, dtype=torch.int32, device=device),
+                      lens=torch.zeros((S, layers), dtype=torch.int32, device=device),
+                      ring=torch.arange(num_pages, dtype=torch.int32, device=device),
+                      state=torch.tensor([0, num_pages], dtype=torch.int32, device=device))
+
+
+def _i32_like(t: torch.Tensor, shape, what: str) -> torch.Tensor:
+    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous i32 {list(shape)}")
+    return t
+
+
+@lru_cache(maxsize=256, typed=True)
+def page_workspace_bytes(S: int, layers: int) -> int:
+    return int(load().prefixkv_page_workspace_bytes(S, layers))
+
+
+def _page_out(cache: PagedCache, status, lens_out, state_out, ws):
+    _need_cuda(cache.table, cache.lens, cache.ring, cache.state, status, lens_out, state_out, ws)
+    S, layers = cache.lens.shape
+    status = torch.empty(1, dtype=torch.int32, device=cache.lens.device) if status is None else _i32_like(status, (1,), "status")
+    lens_out = cache.lens if lens_out is None else _i32_like(lens_out, (S, layers), "lens_out")
+    state_out = cache.state if state_out is None else _i32_like(state_out, (2,), "state_out")
+    return status, lens_out, state_out, _ws(page_workspace_bytes(S, layers), cache.lens.device, ws)
+
+
+def prefixkv_page_resize(cache: PagedCache, target: torch.Tensor, status: Optional[torch.Tensor] = None,
+                         lens_out: Optional[torch.Tensor] = None, state_out: Optional[torch.Tensor] = None,
+                         ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gives every segment the length target [S,layers] i32: pages come from the ring or go back to it; the cache's lens and
+    state are updated (or lens_out, state_out written in their place).  -> status [1] i32, 0 if it was done."""
+    _need_cuda(target)
+    _i32_like(target, cache.lens.shape, "target")
+    status, lens_out, state_out, w = _page_out(cache, status, lens_out, state_out, ws)
+    rc = load().prefixkv_page_resize(cache.lens.shape[0], C.byref(cache._paging), _ptr(target), _ptr(cache.lens),
+                                     _ptr(cache.table), _ptr(cache.ring), _ptr(cache.state), _ptr(lens_out), _ptr(state_out),
+                                     _ptr(status), _ptr(w), w.numel() * w.element_size(), _stream())
+    if rc != 0:
+        raise PrefixKVError(rc, "prefixkv_page_resize")
+    return status
+
+
+def prefixkv_page_append(cache: PagedCache, row_off: torch.Tensor, T: int, slots: Optional[torch.Tensor] = None,
+                         status: Optional[torch.Tensor] = None, lens_out: Optional[torch.Tensor] = None,
+                         state_out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """Room for the new rows of every sequence, in every layer: row_off [S+1] i32, T packed rows
+    -> (slots [layers,T] i64, status [1] i32)."""
+    S, layers = cache.lens.shape
+    _need_cuda(row_off, slots)
+    _i32_like(row_off, (S + 1,), "row_off")
+    if slots is None:
+        slots = torch.empty((layers, T), dtype=torch.int64, device=cache.lens.device)
+    elif slots.dtype != torch.int64 or tuple(slots.shape) != (layers, T) or not slots.is_contiguous():
+        raise ValueError("slots must be contiguous i64 [layers,T]")
+    status, lens_out, state_out, w = _page_out(cache, status, lens_out, state_out, ws)
+    rc = load().prefixkv_page_append(S, int(T), C.byref(cache._paging), _ptr(row_off), _ptr(cache.lens), _ptr(cache.table),
+                                     _ptr(cache.ring), _ptr(cache.state), _ptr(lens_out), _ptr(state_out), _ptr(slots),
+                                     _ptr(status), _ptr(w), w.numel() * w.element_size(), _stream())
+    if rc != 0:
+        raise PrefixKVError(rc, "prefixkv_page_append")
+    return slots, status
+
+
+@dataclass
+class RopePlan:
+    freq: torch.Tensor    # [rot_dim/2] i64 holding the u64 fractions of a turn
+    axis: torch.Tensor    # [rot_dim/2] i32
+    axes: int
+    interleaved: bool
+
+    def __post_init__(self):
+        if self.freq.dtype != torch.int64 or self.freq.dim() != 1 or not self.freq.is_contiguous():
+            raise ValueError("freq must be contiguous i64 [rot_dim/2]")
+        _i32_like(self.axis, self.freq.shape, "axis")
+        self._struct = _Rope(_ptr(self.freq), _ptr(self.axis), 2 * self.freq.shape[0], self.axes, int(self.interleaved))
+
+
+def rope_plan(rot_dim: int, sections=None, theta: float = 10000.0, interleaved: bool = False, cycled: bool = False,
+              device="cuda") -> RopePlan:
+    """Frequencies theta^(-2i/rot_dim) and the axis of every pair: the first sections[0] pairs turn with axis 0, the next
+    sections[1] with axis 1, ...; cycled: the axes take turns pair by pair until their sections are used up.  Default: one axis."""
+    half = rot_dim // 2
+    sections = [half] if sections is None else [int(x) for x in sections]
+    if sum(sections) != half or any(x < 0 for x in sections):
+        raise ValueError(f"the sections must sum to {half} pairs")
+    freq = (C.c_uint64 * max(half, 1))()
+    rc = load().prefixkv_rope_freq(int(rot_dim), float(theta), freq)
+    if rc != 0:
+        raise PrefixKVError(rc, "prefixkv_rope_freq")
+    if cycled:
+        left, axis = list(sections), []
+        while len(axis) < half:
+            for a in range(len(left)):
+                if left[a] > 0:
+                    left[a] -= 1
+                    axis.append(a)
+    else:
+        axis = [a for a, n in enumerate(sections) for _ in range(n)]
+    signed = [x - (1 << 64) if x >= 1 << 63 else x for x in freq]
+    return RopePlan(freq=torch.tensor(signed, dtype=torch.int64, device=device),
+                    axis=torch.tensor(axis, dtype=torch.int32, device=device), axes=len(sections), interleaved=bool(interleaved))
+
+
+def _strides4(t: torch.Tensor) -> _Strides:
+    """Strides of [L,heads,T,D] rows.  (A dimension of one element may have any stride: its own is not looked at.)"""
+    if t.stride(3) != 1:
+        raise ValueError("the head dimension must be contiguous")
+    a = 16 // t.element_size()
+    st = [a if n == 1 else x for x, n in zip(t.stride(), t.shape)]
+    return _Strides(0, st[0], st[1], st[2])
+
+
+@lru_cache(maxsize=256, typed=True)
+def _packed_of(S, L, H, Hkv, T, D, dtype) -> _Packed:
+    return _Packed(S, L, H, Hkv, T, D, dtype)
+
+
+def _rows(*ts: torch.Tensor):
+    L, _, T, D = ts[0].shape
+    for t in ts:
+        if t.dim() != 4 or t.shape[0] != L or t.shape[2] != T or t.shape[3] != D or t.dtype != ts[0].dtype:
+            raise ValueError("row tensors must be [L,heads,T,D] of one dtype")
+
+
+def _rope_args(q, k, positions, plan):
+    if positions.dtype != torch.int32 or positions.shape != (plan.axes, q.shape[2]) or not positions.is_contiguous():
+        raise ValueError("positions must be contiguous i32 [axes,T]")
+    return _packed_of(1, q.shape[0], q.shape[1], k.shape[1], q.shape[2], q.shape[3], _dtype_code(q))
+
+
+def prefixkv_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, plan: RopePlan,
+                  q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+    """q [L,H,T,D], k [L,Hkv,T,D] (bf16 or f32, any strides with D contiguous), positions [axes,T] i32
+    -> (q_out, k_out), rotated; q_out = q and k_out = k rotate in place."""
+    _need_cuda(q, k, positions, plan.freq, plan.axis, q_out, k_out)
+    q_out = torch.empty_like(q) if q_out is None else q_out
+    k_out = torch.empty_like(k) if k_out is None else k_out
+    _rows(q, k, q_out, k_out)
+    if q_out.shape != q.shape or k_out.shape != k.shape:
+        raise ValueError("outputs must have the shapes of q and k")
+    s = _rope_args(q, k, positions, plan)
+    rc = load().prefixkv_rope(C.byref(s), C.byref(plan._struct), _ptr(positions), _ptr(q), _strides4(q), _ptr(k), _strides4(k),
+                              _ptr(q_out), _strides4(q_out), _ptr(k_out), _strides4(k_out), _stream())
+    if rc != 0:
+        raise PrefixKVError(rc, "prefixkv_rope")
+    return q_out, k_out
+
+
+def prefixkv_rope_store(cache: PagedCache, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor,
+                        plan: RopePlan, slots: torch.Tensor, q_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Rotates q [L,H,T,D] and k [L,Hkv,T,D] and stores k and v into the cache's pages at slots [L,T] i64 -> q_out."""
+    _need_cuda(q, k, v, positions, plan.freq, plan.axis, slots, q_out, cache.kp, cache.vp)
+    q_out = torch.empty_like(q) if q_out is None else q_out
+    _rows(q, k, v, q_out)
+    if q_out.shape != q.shape or v.shape != k.shape:
+        raise ValueError("q_out must have the shape of q, v that of k")
+    if slots.dtype != torch.int64 or slots.shape != (q.shape[0], q.shape[2]) or not slots.is_contiguous():
+        raise ValueError("slots must be contiguous i64 [L,T]")
+    if (cache.kp.dtype != q.dtype or cache.kp.shape[1] != k.shape[1] or cache.kp.shape[3] != q.shape[3]
+            or not cache.kp.is_contiguous() or not cache.vp.is_contiguous()):
+        raise ValueError("the cache must have k's heads, head dimension and dtype, and contiguous pools")
+    s = _rope_args(q, k, positions, plan)
+    rc = load().prefixkv_rope_store(C.byref(s), C.byref(plan._struct), _ptr(positions), _ptr(q), _strides4(q), _ptr(k),
+                                    _strides4(k), _ptr(v), _strides4(v), _ptr(q_out), _strides4(q_out), _ptr(slots),
+                                    C.byref(cache._paging), _ptr(cache.kp), _ptr(cache.vp), _stream())
+    if rc != 0:
+        raise PrefixKVError(rc, "prefixkv_rope_store")
+    return q_out
+
+
+def prefixkv_compact_paged(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, order: torch.Tensor, lengths: torch.Tensor,
+                           kept_pos: Optional[torch.Tensor] = None, l0: int = 0) -> PagedCache:
+    """prefixkv_compact into the cache's pages: k,v [B,L,Hkv,N,D], order [B,L,N] i32, lengths [B,L] i32; sequence b of the
+    batch is sequence b of the cache, layer l its layer l0 + l.  kept_pos [B,L,N] i32, optional output."""
+    _need_cuda(k, v, order, lengths, kept_pos, cache.kp, cache.vp, cache.table)
+    B, L, Hkv, N, D = k.shape
+    if v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError("v must match k")
+    _i32_like(order, (B, L, N), "order")
+    _i32_like(lengths, (B, L), "lengths")
+    if kept_pos is not None:
+        _i32_like(kept_pos, (B, L, N), "kept_pos")
+    if (cache.kp.dtype != k.dtype or cache.kp.shape[1] != Hkv or cache.kp.shape[3] != D or cache.table.shape[0] < B
+            or not cache.kp.is_contiguous() or not cache.vp.is_contiguous()):
+        raise ValueError("the cache must have k's heads, head dimension and dtype, B sequences and contiguous pools")
+    s = _shape_of(B, L, Hkv, Hkv, N, D, _dtype_code(k))
+    rc = load().prefixkv_compact_paged(C.byref(s), _ptr(k), _strides5(k), _ptr(v), _strides5(v), _ptr(order), _ptr(lengths),
+                                       C.byref(cache._paging), int(l0), _ptr(cache.table), _ptr(cache.kp), _ptr(cache.vp),
+                                       _ptr(kept_pos), _stream())
+    if rc != 0:
+        raise PrefixKVError(rc, "prefixkv_compact_paged")
+    return cache
+
+
+@lru_cache(maxsize=256, typed=True)
+def _attn_ws_bytes_of(S, L, H, Hkv, T, D, dtype, max_rows) -> int:
+    s = _packed_of(S, L, H, Hkv, T, D, dtype)
+    return int(load().prefixkv_attn_workspace_bytes(C.byref(s), max_rows))
+
+
+def attn_workspace_bytes(S: int, L: int, H: int, Hkv: int, T: int, D: int, dtype: torch.dtype, max_rows: int = 0) -> int:
+    """Workspace of prefixkv_chunk_attn, or (max_rows = 0) of prefixkv_prefill_attn_packed."""
+    return _attn_ws_bytes_of(S, L, H, Hkv, T, D, PKV_F32 if dtype == torch.float32 else PKV_BF16, max_rows)
+
+
+def _scale_of(scale: torch.Tensor, L: int):
+    if scale.dtype != torch.float32 or scale.shape != (L,) or not scale.is_contiguous():
+        raise ValueError("scale must be contiguous f32 [L]")
+
+
+def prefixkv_prefill_attn_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_off: torch.Tensor, scale: torch.Tensor,
+                                 out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                                 ws: Optional[torch.Tensor] = None):
+    """Causal attention of packed prompts: q [L,H,T,D], k/v [L,Hkv,T,D] (bf16), row_off [S+1] i32, scale [L] f32
+    -> (out [L,H,T,D], lse [L*H*T] f32: [L,H,n] of each sequence one behind the other).  Rows that belong to no sequence are
+    left as they are."""
+    _need_cuda(q, k, v, row_off, scale, out, lse, ws)
+    out = torch.empty_like(q) if out is None else out
+    _rows(q, k, v, out)
+    L, H, T, D = q.shape
+    if k.shape != v.shape or out.shape != q.shape:
+        raise ValueError("v must have the shape of k, out that of q")
+    _i32_like(row_off, (row_off.numel(),), "row_off")
+    _scale_of(scale, L)
+    if lse is None:
+        lse = torch.empty(L * H * T, dtype=torch.float32, device=q.device)
+    elif lse.dtype != torch.float32 or lse.numel() != L * H * T or not lse.is_contiguous():
+        raise ValueError("lse must be contiguous f32 [L*H*T]")
+    dims = (row_off.numel() - 1, L, H, k.shape[1], T, D, _dtype_code(q))
+    w = _ws(_attn_ws_bytes_of(*dims, 0), q.device, ws)
+    rc = load().prefixkv_prefill_attn_packed(C.byref(_packed_of(*dims)), _ptr(q), _strides4(q), _ptr(k), _strides4(k), _ptr(v),
+                                             _strides4(v), _ptr(row_off), _ptr(scale), _ptr(out), _strides4(out), _ptr(lse),
+                                             _ptr(w), w.numel() * w.element_size(), _stream())
+    if rc != 0:
+        raise PrefixKVError(rc, "prefixkv_prefill_attn_packed")
+    return out, lse
+
+
+def prefixkv_chunk_attn(cache: PagedCache, q: torch.Tensor, row_off: torch.Tensor, scale: torch.Tensor, max_rows: int,
+                        l0: int = 0, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of new rows q [L,H,T,D] over the cache's layers l0 ... l0+L-1, which hold their keys and values already:
+    row_off [S+1] i32, scale [L] f32, max_rows = the most rows of a sequence -> out [L,H,T,D]."""
+    _need_cuda(q, row_off, scale, out, ws, cache.kp, cache.vp, cache.table, cache.lens)
+    out = torch.empty_like(q) if out is None else out
+    _rows(q, out)
+    L, H, T, D = q.shape
+    S = cache.lens.shape[0]
+    if out.shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    _i32_like(row_off, (S + 1,), "row_off")
+    _scale_of(scale, L)
+    if (cache.kp.dtype != q.dtype or cache.kp.shape[3] != D or not cache.kp.is_contiguous() or not cache.vp.is_contiguous()):
+        raise ValueError("the cache must have q's head dimension and dtype, and contiguous pools")
+    dims = (S, L, H, cache.kp.shape[1], T, D, _dtype_code(q))
+    w = _ws(_attn_ws_bytes_of(*dims, int(max_rows)), q.device, ws)
+    rc = load().prefixkv_chunk_attn(C.byref(_packed_of(*dims)), _ptr(q), _strides4(q), _ptr(row_off), C.byref(cache._paging),
+                                    int(l0), _ptr(cache.kp), _ptr(cache.vp), _ptr(cache.table), _ptr(cache.lens), _ptr(scale),
+                                    int(max_rows), _ptr(out), _strides4(out), _ptr(w), w.numel() * w.element_size(), _stream())
+    if rc != 0:
+        raise PrefixKVError(rc, "prefixkv_chunk_attn")
     return out
 
 

@@ -3,6 +3,8 @@
 // the compute-unit count, and the address of the built-in scratch array of prefixkv_select_static.
 #include "pkv_common.hpp"
 
+#include <math.h>
+
 using namespace pkv;
 
 namespace {
@@ -26,6 +28,23 @@ bool strides_ok(const pkv_strides& t, int esize) {
            t.n % a == 0;
 }
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+
+bool packed_ok(const pkv_packed* s) {
+    return s->S >= 1 && s->S <= kMaxS && s->L >= 1 && s->L <= kMaxL && s->H >= 1 && s->H <= 2048 && s->Hkv >= 1 &&
+           s->H % s->Hkv == 0 && s->T >= 1 && s->T <= kMaxT && (s->D == 64 || s->D == 128);
+}
+bool row_strides_ok(pkv_strides t, int esize) {
+    t.b = 0;
+    return strides_ok(t, esize);
+}
+bool paging_ok(const pkv_paging* g) {
+    return g->num_pages >= 1 && g->page_size >= 16 && g->page_size <= 256 && (g->page_size & (g->page_size - 1)) == 0 &&
+           g->max_pages >= 1 && (int64_t)g->max_pages * g->page_size < kMaxSegmentSlots && g->layers >= 1 && g->layers <= kMaxL;
+}
+bool page_call_ok(int S, const pkv_paging* g) {
+    return S >= 1 && S <= kMaxS && paging_ok(g) && (int64_t)S * g->layers * g->max_pages < (1ll << 31);
+}
+bool rope_ok(const pkv_rope* r, int D) { return r->rot_dim >= 16 && r->rot_dim <= D && r->rot_dim % 16 == 0 && r->axes >= 1 && r->axes <= 8; }
 
 }  // namespace
 
@@ -252,6 +271,137 @@ int prefixkv_decode_attn_evict(const pkv_shape* s, int l0, int l1, const void* q
     if (need > 0 && (ws == nullptr || ws_bytes < need)) return PKV_ERR_WORKSPACE;
     const hipError_t e = launch_decode_evict(*s, l0, l1, q, k_new, v_new, scale, kc, vc, seg_off, caps, base_lens,
                                              lens, kept_pos, t, distance, out, ws, (hipStream_t)stream);
+    return e == hipSuccess ? PKV_OK : PKV_ERR_HIP;
+}
+
+size_t prefixkv_page_workspace_bytes(int S, int layers) {
+    if (S < 1 || S > kMaxS || layers < 1 || layers > kMaxL) return 0;
+    return page_ws_bytes(S, layers);
+}
+
+int prefixkv_page_resize(int S, const pkv_paging* g, const int32_t* target, const int32_t* lens, int32_t* table, int32_t* ring,
+                         const int32_t* state, int32_t* lens_out, int32_t* state_out, int32_t* status, void* ws,
+                         size_t ws_bytes, pkv_stream stream) {
+    if (!g || !target || !lens || !table || !ring || !state || !lens_out || !state_out || !status) return PKV_ERR_NULL;
+    if (!page_call_ok(S, g)) return PKV_ERR_DIM;
+    if (!ws || ws_bytes < page_ws_bytes(S, g->layers) || ((uintptr_t)ws & 3u)) return PKV_ERR_WORKSPACE;
+    const hipError_t e = launch_pages(S, 0, *g, target, nullptr, lens, table, ring, state, lens_out, state_out, nullptr, status,
+                                      ws, (hipStream_t)stream);
+    return e == hipSuccess ? PKV_OK : PKV_ERR_HIP;
+}
+
+int prefixkv_page_append(int S, int T, const pkv_paging* g, const int32_t* row_off, const int32_t* lens, int32_t* table,
+                         const int32_t* ring, const int32_t* state, int32_t* lens_out, int32_t* state_out, int64_t* slots,
+                         int32_t* status, void* ws, size_t ws_bytes, pkv_stream stream) {
+    if (!g || !row_off || !lens || !table || !ring || !state || !lens_out || !state_out || !slots || !status) return PKV_ERR_NULL;
+    if (!page_call_ok(S, g) || T < 1 || T > kMaxT) return PKV_ERR_DIM;
+    if (!ws || ws_bytes < page_ws_bytes(S, g->layers) || ((uintptr_t)ws & 3u)) return PKV_ERR_WORKSPACE;
+    // (nothing is given back by a call that appends, so the ring is not written)
+    const hipError_t e = launch_pages(S, T, *g, nullptr, row_off, lens, table, const_cast<int32_t*>(ring), state, lens_out,
+                                      state_out, slots, status, ws, (hipStream_t)stream);
+    return e == hipSuccess ? PKV_OK : PKV_ERR_HIP;
+}
+
+int prefixkv_rope_freq(int rot_dim, double theta, uint64_t* freq) {
+    if (!freq) return PKV_ERR_NULL;
+    if (rot_dim < 16 || rot_dim > 128 || rot_dim % 16 != 0 || !(theta >= 1.0) || !(theta < 1e300)) return PKV_ERR_DIM;
+    const long double turn = 6.283185307179586476925286766559005768L;
+    for (int i = 0; i < rot_dim / 2; ++i)   // at most 1 / 2 pi: below 2^62
+        freq[i] = (uint64_t)(ldexpl(powl((long double)theta, -2.0L * i / rot_dim) / turn, 64) + 0.5L);
+    return PKV_OK;
+}
+
+static int rope_checks(const pkv_packed* s, const pkv_rope* r, const int32_t* pos, const void* q, const pkv_strides& qs,
+                       const void* k, const pkv_strides& ks, const void* q_out, const pkv_strides& qos) {
+    if (!s || !r || !r->freq || !r->axis || !pos || !q || !k || !q_out) return PKV_ERR_NULL;
+    if (!packed_ok(s) || !rope_ok(r, s->D)) return PKV_ERR_DIM;
+    if (s->dtype != PKV_F32 && s->dtype != PKV_BF16) return PKV_ERR_DTYPE;
+    const int e = s->dtype == PKV_F32 ? 4 : 2;
+    if (!row_strides_ok(qs, e) || !row_strides_ok(ks, e) || !row_strides_ok(qos, e) || !aligned16(q) || !aligned16(k) ||
+        !aligned16(q_out))
+        return PKV_ERR_STRIDE;
+    return PKV_OK;
+}
+
+int prefixkv_rope(const pkv_packed* s, const pkv_rope* r, const int32_t* pos, const void* q, pkv_strides qs, const void* k,
+                  pkv_strides ks, void* q_out, pkv_strides qos, void* k_out, pkv_strides kos, pkv_stream stream) {
+    if (const int rc = rope_checks(s, r, pos, q, qs, k, ks, q_out, qos)) return rc;
+    if (!k_out) return PKV_ERR_NULL;
+    if (!row_strides_ok(kos, s->dtype == PKV_F32 ? 4 : 2) || !aligned16(k_out)) return PKV_ERR_STRIDE;
+    const hipError_t e = launch_rope(*s, *r, pos, q, to_strides(qs), k, to_strides(ks), nullptr, Strides{}, q_out,
+                                     to_strides(qos), k_out, to_strides(kos), nullptr, nullptr, nullptr, nullptr,
+                                     (hipStream_t)stream);
+    return e == hipSuccess ? PKV_OK : PKV_ERR_HIP;
+}
+
+int prefixkv_rope_store(const pkv_packed* s, const pkv_rope* r, const int32_t* pos, const void* q, pkv_strides qs,
+                        const void* k, pkv_strides ks, const void* v, pkv_strides vs, void* q_out, pkv_strides qos,
+                        const int64_t* slots, const pkv_paging* g, void* kp, void* vp, pkv_stream stream) {
+    if (const int rc = rope_checks(s, r, pos, q, qs, k, ks, q_out, qos)) return rc;
+    if (!v || !slots || !g || !kp || !vp) return PKV_ERR_NULL;
+    if (!paging_ok(g)) return PKV_ERR_DIM;
+    if (!row_strides_ok(vs, s->dtype == PKV_F32 ? 4 : 2) || !aligned16(v) || !aligned16(kp) || !aligned16(vp)) return PKV_ERR_STRIDE;
+    const hipError_t e = launch_rope(*s, *r, pos, q, to_strides(qs), k, to_strides(ks), v, to_strides(vs), q_out,
+                                     to_strides(qos), nullptr, Strides{}, slots, g, kp, vp, (hipStream_t)stream);
+    return e == hipSuccess ? PKV_OK : PKV_ERR_HIP;
+}
+
+int prefixkv_compact_paged(const pkv_shape* s, const void* k, pkv_strides ks, const void* v, pkv_strides vs,
+                           const int32_t* order, const int32_t* lengths, const pkv_paging* g, int l0, const int32_t* table,
+                           void* kp, void* vp, int32_t* kept_pos, pkv_stream stream) {
+    if (!s || !k || !v || !order || !lengths || !g || !table || !kp || !vp) return PKV_ERR_NULL;
+    if (!shape_ok(s) || !paging_ok(g) || l0 < 0 || l0 > g->layers - s->L) return PKV_ERR_DIM;
+    if (!dtype_ok(s)) return PKV_ERR_DTYPE;
+    const int esize = s->dtype == PKV_F32 ? 4 : 2;
+    if (!strides_ok(ks, esize) || !strides_ok(vs, esize) || !aligned16(k) || !aligned16(v) || !aligned16(kp) || !aligned16(vp))
+        return PKV_ERR_STRIDE;
+    if ((size_t)((s->N + 63) / 64) * s->Hkv * s->B * s->L > 0x7fffffffull) return PKV_ERR_UNSUPPORTED;
+    const hipError_t e = launch_compact_paged(*s, k, to_strides(ks), v, to_strides(vs), order, lengths, *g, l0, table, kp, vp,
+                                              kept_pos, (hipStream_t)stream);
+    return e == hipSuccess ? PKV_OK : PKV_ERR_HIP;
+}
+
+size_t prefixkv_attn_workspace_bytes(const pkv_packed* s, int max_rows) {
+    if (!s || !packed_ok(s) || (s->dtype != PKV_F32 && s->dtype != PKV_BF16) || max_rows < 0 || max_rows > s->T) return 0;
+    return packed_attn_ws_bytes(*s, max_rows);
+}
+
+int prefixkv_prefill_attn_packed(const pkv_packed* s, const void* q, pkv_strides qs, const void* k, pkv_strides ks,
+                                 const void* v, pkv_strides vs, const int32_t* row_off, const float* scale, void* out,
+                                 pkv_strides os, float* lse, void* ws, size_t ws_bytes, pkv_stream stream) {
+    if (!s || !q || !k || !v || !row_off || !scale || !out || !lse) return PKV_ERR_NULL;
+    if (!packed_ok(s)) return PKV_ERR_DIM;
+    if (s->dtype != PKV_F32 && s->dtype != PKV_BF16) return PKV_ERR_DTYPE;
+    if (s->dtype != PKV_BF16) return PKV_ERR_UNSUPPORTED;
+    if (!row_strides_ok(qs, 2) || !row_strides_ok(ks, 2) || !row_strides_ok(vs, 2) || !row_strides_ok(os, 2) || !aligned16(q) ||
+        !aligned16(k) || !aligned16(v) || !aligned16(out))
+        return PKV_ERR_STRIDE;
+    const size_t need = packed_attn_ws_bytes(*s, 0);
+    if (need > 0 && (!ws || ws_bytes < need || !aligned16(ws))) return PKV_ERR_WORKSPACE;
+    PackedAttn a{};
+    a.q = q; a.k = k; a.v = v; a.qs = to_strides(qs); a.ks = to_strides(ks); a.vs = to_strides(vs); a.os = to_strides(os);
+    a.row_off = row_off; a.scale = scale; a.out = out; a.lse = lse; a.ws = ws;
+    const hipError_t e = launch_packed_attn(*s, a, (hipStream_t)stream);
+    return e == hipSuccess ? PKV_OK : PKV_ERR_HIP;
+}
+
+int prefixkv_chunk_attn(const pkv_packed* s, const void* q, pkv_strides qs, const int32_t* row_off, const pkv_paging* g, int l0,
+                        const void* kp, const void* vp, const int32_t* table, const int32_t* lens, const float* scale,
+                        int max_rows, void* out, pkv_strides os, void* ws, size_t ws_bytes, pkv_stream stream) {
+    if (!s || !q || !row_off || !g || !kp || !vp || !table || !lens || !scale || !out) return PKV_ERR_NULL;
+    if (!packed_ok(s) || !paging_ok(g) || l0 < 0 || l0 > g->layers - s->L || max_rows < 1 || max_rows > s->T) return PKV_ERR_DIM;
+    if (s->dtype != PKV_F32 && s->dtype != PKV_BF16) return PKV_ERR_DTYPE;
+    const int esize = s->dtype == PKV_F32 ? 4 : 2;
+    if (!row_strides_ok(qs, esize) || !row_strides_ok(os, esize) || !aligned16(q) || !aligned16(kp) || !aligned16(vp) ||
+        !aligned16(out))
+        return PKV_ERR_STRIDE;
+    const size_t need = packed_attn_ws_bytes(*s, max_rows);
+    if (need > 0 && (!ws || ws_bytes < need || !aligned16(ws))) return PKV_ERR_WORKSPACE;
+    PackedAttn a{};
+    a.q = q; a.k = kp; a.v = vp; a.qs = to_strides(qs); a.os = to_strides(os);
+    a.row_off = row_off; a.table = table; a.lens = lens; a.scale = scale; a.out = out; a.g = *g; a.l0 = l0;
+    a.max_rows = max_rows; a.ws = ws;
+    const hipError_t e = launch_packed_attn(*s, a, (hipStream_t)stream);
     return e == hipSuccess ? PKV_OK : PKV_ERR_HIP;
 }
 

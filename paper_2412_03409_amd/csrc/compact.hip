@@ -15,6 +15,9 @@ namespace pkv {
 // they cost up to 20 %), so the launcher chooses.  Nontemporal stores of the cache rows were 2-5 % slower inside
 // the pipeline at every size (and faster only when the same call is repeated back to back), so stores are plain.
 typedef __attribute__((ext_vector_type(4))) unsigned int cu32x4_t;
+
+struct PagedDst { const int32_t* table; int num_pages, max_pages, layers, l0, shift; };   // shift: log2 of the page size
+
 template <bool NT>
 __device__ __forceinline__ uint4 ld_row16(const unsigned char* p) {
     if constexpr (NT) {
@@ -33,13 +36,15 @@ __device__ __forceinline__ uint4 ld_row16(const unsigned char* p) {
 // The redundant plans read `order` (4 bytes per kept row) from the L2 and cost less than the separate planning
 // launch they replace (7B shape, batch 1: 35 -> 31 us; N = 8192: 171 -> 163 us).  Workgroups whose chunk lies
 // beyond the segment's length leave at once; beyond 16 chunks a workgroup walks further chunks.
-template <int LPR, bool NTL>
+// PAGED: row r of a segment goes to row r % page size of the page that the segment's table names; the segments' offsets are
+// not needed.
+template <int LPR, bool NTL, bool PAGED = false>
 __global__ void __launch_bounds__(256)
 compact_fused_kernel(int N, int nchunk, int Hkv, int L, int row_bytes, const unsigned char* __restrict__ k, Strides ks,
                      const unsigned char* __restrict__ v, Strides vs, int esize, const int32_t* __restrict__ order,
                      const int32_t* __restrict__ lengths, int decode_capacity, int64_t* __restrict__ seg_off,
                      int32_t* __restrict__ caps, int32_t* __restrict__ lens, int32_t* __restrict__ kept_pos,
-                     unsigned char* __restrict__ kc, unsigned char* __restrict__ vc) {
+                     unsigned char* __restrict__ kc, unsigned char* __restrict__ vc, PagedDst pg) {
     constexpr int kRows = 64;
     constexpr int RPI = 256 / LPR;
     extern __shared__ int s_dyn[];                  // kept positions (N ints), then the flags (N rounded up to 4 bytes)
@@ -53,26 +58,30 @@ compact_fused_kernel(int N, int nchunk, int Hkv, int L, int row_bytes, const uns
     const int chunk = blockIdx.x % nchunk, h = (blockIdx.x / nchunk) % Hkv, seg = blockIdx.x / (nchunk * Hkv);
     int klen = lengths[seg];
     klen = klen < 0 ? 0 : (klen > N ? N : klen);
-    const bool scribe = h == 0 && chunk == 0;
+    if constexpr (PAGED) klen = min(klen, pg.max_pages << pg.shift);
+    const bool scribe = h == 0 && chunk == 0 && !(PAGED && kept_pos == nullptr);
     if (chunk * kRows >= klen && !scribe) return;
 
     // token offset of the segment = sum of (length + capacity) of all segments before it
     long long acc = 0;
-    for (int i = tid; i < seg; i += 256) acc += (long long)lengths[i] + decode_capacity;
+    if constexpr (!PAGED)
+        for (int i = tid; i < seg; i += 256) acc += (long long)lengths[i] + decode_capacity;
     const int32_t* ord = order + (size_t)seg * N;
     int pos_mine[4];                                 // the first 1024 entries of the list are requested at once
 #pragma unroll
     for (int u = 0; u < 4; ++u) pos_mine[u] = tid + 256 * u < klen ? ord[tid + 256 * u] : -1;
     const int nword = (N + 3) / 4;
     for (int i = tid; i < nword; i += 256) s_flag[i] = 0;
-    for (int d = 32; d > 0; d >>= 1) {
-        const uint32_t lo = __shfl_xor((uint32_t)acc, d, kWave);
-        const uint32_t hi = __shfl_xor((uint32_t)((unsigned long long)acc >> 32), d, kWave);
-        acc += (long long)(((unsigned long long)hi << 32) | lo);
+    if constexpr (!PAGED) {
+        for (int d = 32; d > 0; d >>= 1) {
+            const uint32_t lo = __shfl_xor((uint32_t)acc, d, kWave);
+            const uint32_t hi = __shfl_xor((uint32_t)((unsigned long long)acc >> 32), d, kWave);
+            acc += (long long)(((unsigned long long)hi << 32) | lo);
+        }
+        if (lane == 0) s_off[wv] = acc;
     }
-    if (lane == 0) s_off[wv] = acc;
     __syncthreads();
-    const long long off = s_off[0] + s_off[1] + s_off[2] + s_off[3];
+    const long long off = PAGED ? (long long)seg * N : s_off[0] + s_off[1] + s_off[2] + s_off[3];
     unsigned char* fb = (unsigned char*)s_flag;
 #pragma unroll
     for (int u = 0; u < 4; ++u)
@@ -106,7 +115,7 @@ compact_fused_kernel(int N, int nchunk, int Hkv, int L, int row_bytes, const uns
     __syncthreads();
     if (scribe) {
         for (int j = tid; j < len; j += 256) kept_pos[off + j] = s_kept[j];
-        if (tid == 0) {
+        if (!PAGED && tid == 0) {
             seg_off[seg] = off;
             caps[seg] = klen + decode_capacity;
             lens[seg] = klen;
@@ -117,9 +126,17 @@ compact_fused_kernel(int N, int nchunk, int Hkv, int L, int row_bytes, const uns
     const int sub = tid % LPR, rsel = tid / LPR;
     const unsigned char* kb = k + (ks.b * b + ks.l * l + ks.h * h) * (int64_t)esize;
     const unsigned char* vb = v + (vs.b * b + vs.l * l + vs.h * h) * (int64_t)esize;
-    const int64_t dst0 = ((int64_t)off * Hkv + (int64_t)h * cap) * row_bytes;
+    const int64_t dst0 = PAGED ? 0 : ((int64_t)off * Hkv + (int64_t)h * cap) * row_bytes;
+    const int32_t* pages = PAGED ? pg.table + ((int64_t)b * pg.layers + pg.l0 + l) * pg.max_pages : nullptr;
     for (int r0 = chunk * kRows; r0 < len; r0 += nchunk * kRows) {
         uint4 kr[kRows / RPI], vr[kRows / RPI];
+        int page[kRows / RPI];
+#pragma unroll
+        for (int i = 0; i < kRows / RPI; ++i) {
+            const int r = r0 + i * RPI + rsel;
+            page[i] = PAGED ? -1 : 0;
+            if (PAGED && r < len) page[i] = pages[r >> pg.shift];
+        }
 #pragma unroll
         for (int i = 0; i < kRows / RPI; ++i) {
             const int r = r0 + i * RPI + rsel;
@@ -133,9 +150,11 @@ compact_fused_kernel(int N, int nchunk, int Hkv, int L, int row_bytes, const uns
 #pragma unroll
         for (int i = 0; i < kRows / RPI; ++i) {
             const int r = r0 + i * RPI + rsel;
-            if (r < len) {
-                *(uint4*)(kc + dst0 + (int64_t)r * row_bytes + sub * 16) = kr[i];
-                *(uint4*)(vc + dst0 + (int64_t)r * row_bytes + sub * 16) = vr[i];
+            if (PAGED ? r < len && (uint32_t)page[i] < (uint32_t)pg.num_pages : r < len) {
+                const int64_t at = PAGED ? ((((int64_t)page[i] * Hkv + h) << pg.shift) + (r & ((1 << pg.shift) - 1))) * row_bytes
+                                         : dst0 + (int64_t)r * row_bytes;
+                *(uint4*)(kc + at + sub * 16) = kr[i];
+                *(uint4*)(vc + at + sub * 16) = vr[i];
             }
         }
     }
@@ -313,7 +332,7 @@ hipError_t launch_compact(const pkv_shape& s, const void* k, Strides ks, const v
 #define PKV_FUSED(LPR, NTL)                                                                                        \
     hipLaunchKernelGGL((compact_fused_kernel<LPR, NTL>), grid, dim3(256), lds, st, s.N, nchunk, s.Hkv, s.L, row_bytes, \
                        (const unsigned char*)k, ks, (const unsigned char*)v, vs, esize, order, lengths,            \
-                       decode_capacity, seg_off, caps, lens, kept_pos, (unsigned char*)kc, (unsigned char*)vc)
+                       decode_capacity, seg_off, caps, lens, kept_pos, (unsigned char*)kc, (unsigned char*)vc, PagedDst{})
     if (ntl) {
         if (lpr == 8) PKV_FUSED(8, true);
         else if (lpr == 16) PKV_FUSED(16, true);
@@ -324,6 +343,35 @@ hipError_t launch_compact(const pkv_shape& s, const void* k, Strides ks, const v
         else PKV_FUSED(32, false);
     }
 #undef PKV_FUSED
+    return hipGetLastError();
+}
+
+hipError_t launch_compact_paged(const pkv_shape& s, const void* k, Strides ks, const void* v, Strides vs, const int32_t* order,
+                                const int32_t* lengths, const pkv_paging& g, int l0, const int32_t* table, void* kp, void* vp,
+                                int32_t* kept_pos, hipStream_t st) {
+    const int nseg = s.B * s.L;
+    const int esize = s.dtype == PKV_F32 ? 4 : 2;
+    const int row_bytes = s.D * esize;
+    const int lpr = row_bytes / 16;
+    const int nchunk = gather_chunks(s.N);
+    dim3 grid((uint32_t)((size_t)nchunk * s.Hkv * nseg));
+    const size_t lds = (size_t)s.N * 4 + (size_t)((s.N + 3) / 4) * 4;
+    const bool ntl = 2 * (size_t)nseg * s.Hkv * s.N * row_bytes >= ((size_t)1 << 31);   // as in launch_compact
+    const PagedDst pg{table, g.num_pages, g.max_pages, g.layers, l0, __builtin_ctz((unsigned)g.page_size)};
+#define PKV_PAGED(LPR, NTL)                                                                                            \
+    hipLaunchKernelGGL((compact_fused_kernel<LPR, NTL, true>), grid, dim3(256), lds, st, s.N, nchunk, s.Hkv, s.L, row_bytes, \
+                       (const unsigned char*)k, ks, (const unsigned char*)v, vs, esize, order, lengths, 0, (int64_t*)nullptr, \
+                       (int32_t*)nullptr, (int32_t*)nullptr, kept_pos, (unsigned char*)kp, (unsigned char*)vp, pg)
+    if (ntl) {
+        if (lpr == 8) PKV_PAGED(8, true);
+        else if (lpr == 16) PKV_PAGED(16, true);
+        else PKV_PAGED(32, true);
+    } else {
+        if (lpr == 8) PKV_PAGED(8, false);
+        else if (lpr == 16) PKV_PAGED(16, false);
+        else PKV_PAGED(32, false);
+    }
+#undef PKV_PAGED
     return hipGetLastError();
 }
 

@@ -1,0 +1,197 @@
+"""Packed prompts and paged caches: what the C entry points refuse, before anything is enqueued, and what the binding
+refuses; the rotary frequencies; the plain forms against hand-worked numbers."""
+import ctypes as C
+import math
+from fractions import Fraction
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2412_03409_amd as P
+import serving_reference as R
+from paper_2412_03409_amd import binding as Bd
+
+A = C.c_void_p(4096)          # stands for aligned device memory: no call below gets as far as using it
+ODD = C.c_void_p(4100)
+ST = Bd._Strides(0, 8192, 128, 4096)
+BIG = 1 << 30
+
+
+def packed(**kw):
+    d = dict(S=2, L=1, H=4, Hkv=2, T=10, D=128, dtype=P.PKV_BF16)
+    d.update(kw)
+    return C.byref(Bd._Packed(*[d[k] for k in ("S", "L", "H", "Hkv", "T", "D", "dtype")]))
+
+
+def paging(**kw):
+    d = dict(num_pages=8, page_size=16, max_pages=4, layers=2)
+    d.update(kw)
+    return C.byref(Bd._Paging(*[d[k] for k in ("num_pages", "page_size", "max_pages", "layers")]))
+
+
+def rope(**kw):
+    d = dict(freq=4096, axis=4096, rot_dim=64, axes=3, interleaved=0)
+    d.update(kw)
+    return C.byref(Bd._Rope(*[d[k] for k in ("freq", "axis", "rot_dim", "axes", "interleaved")]))
+
+
+BAD_PAGING = [dict(num_pages=0), dict(page_size=8), dict(page_size=24), dict(page_size=512), dict(max_pages=0),
+              dict(max_pages=1 << 16), dict(layers=0), dict(layers=65)]
+BAD_PACKED = [dict(S=0), dict(S=4097), dict(L=0), dict(L=65), dict(H=3), dict(Hkv=0), dict(H=2050, Hkv=1), dict(T=0),
+              dict(T=(1 << 22) + 1), dict(D=96), dict(D=32)]
+
+
+def with_null(args, optional=()):
+    """The argument lists with one pointer missing each."""
+    for i, a in enumerate(args):
+        if a is A and i not in optional:
+            yield [None if j == i else x for j, x in enumerate(args)]
+
+
+def test_page_calls_refuse():
+    lib = P.load()
+    need = P.page_workspace_bytes(2, 2)
+    assert need >= 2 * 2 * 8 and P.page_workspace_bytes(0, 2) == 0 and P.page_workspace_bytes(4097, 2) == 0
+    resize = [2, paging(), A, A, A, A, A, A, A, A, A, need, None]
+    append = [2, 10, paging(), A, A, A, A, A, A, A, A, A, A, need, None]
+    for f, args, ws in ((lib.prefixkv_page_resize, resize, 10), (lib.prefixkv_page_append, append, 12)):
+        g = args.index(args[1] if f is lib.prefixkv_page_resize else args[2])
+        for bad in with_null(args, optional=(ws,)):
+            assert f(*bad) == 1
+        assert f(*[None if i == g else x for i, x in enumerate(args)]) == 1
+        for kw in BAD_PAGING + [dict(max_pages=1 << 14, layers=64)]:
+            S = 4096 if "layers" in kw and kw["layers"] == 64 else 2
+            assert f(*[S if i == 0 else paging(**kw) if i == g else x for i, x in enumerate(args)]) == 2, kw
+        for S in (0, 4097):
+            assert f(*[S] + args[1:]) == 2
+        for i, x in ((ws, None), (ws, C.c_void_p(4098)), (ws + 1, need - 1)):
+            assert f(*[x if j == i else y for j, y in enumerate(args)]) == 5
+    for T in (0, (1 << 22) + 1):
+        assert lib.prefixkv_page_append(*[T if i == 1 else x for i, x in enumerate(append)]) == 2
+
+
+def test_rope_refuses():
+    lib = P.load()
+    plain = [packed(), rope(), A, A, ST, A, ST, A, ST, A, ST, None]
+    store = [packed(), rope(), A, A, ST, A, ST, A, ST, A, ST, A, paging(), A, A, None]
+    for f, args in ((lib.prefixkv_rope, plain), (lib.prefixkv_rope_store, store)):
+        for bad in with_null(args):
+            assert f(*bad) == 1
+        assert f(*[None] + args[1:]) == 1 and f(*[args[0], None] + args[2:]) == 1
+        for kw in (dict(freq=None), dict(axis=None)):
+            assert f(*[args[0], rope(**kw)] + args[2:]) == 1
+        for kw in BAD_PACKED:
+            assert f(*[packed(**kw)] + args[1:]) == 2, kw
+        for kw in (dict(rot_dim=0), dict(rot_dim=8), dict(rot_dim=24), dict(rot_dim=144), dict(axes=0), dict(axes=9)):
+            assert f(*[args[0], rope(**kw)] + args[2:]) == 2, kw
+        assert f(*[packed(dtype=7)] + args[1:]) == 3
+        for i, x in enumerate(args):
+            if x is ST:
+                for bad in (Bd._Strides(0, 8192, 128, 4100), Bd._Strides(0, -8192, 128, 4096), Bd._Strides(0, 8192, 128, 0)):
+                    assert f(*[bad if j == i else y for j, y in enumerate(args)]) == 4
+        assert f(*[ODD if j == 3 else y for j, y in enumerate(args)]) == 4
+    for kw in BAD_PAGING:
+        assert lib.prefixkv_rope_store(*[paging(**kw) if i == 12 else x for i, x in enumerate(store)]) == 2
+
+
+def test_compact_paged_refuses():
+    lib = P.load()
+    shape = lambda **kw: C.byref(Bd._Shape(*[{**dict(B=1, L=2, H=2, Hkv=2, N=100, D=64, dtype=1), **kw}[k]
+                                            for k in ("B", "L", "H", "Hkv", "N", "D", "dtype")]))
+    st = Bd._Strides(0, 8192, 128, 64)
+    args = [shape(), A, st, A, st, A, A, paging(), 0, A, A, A, A, None]
+    for bad in with_null(args, optional=(12,)):
+        assert lib.prefixkv_compact_paged(*bad) == 1
+    for kw in (dict(N=8193), dict(L=65), dict(D=32), dict(B=0)):
+        assert lib.prefixkv_compact_paged(*[shape(**kw)] + args[1:]) == 2
+    for kw in BAD_PAGING:
+        assert lib.prefixkv_compact_paged(*[paging(**kw) if i == 7 else x for i, x in enumerate(args)]) == 2
+    for l0 in (-1, 1, 1 << 30):
+        assert lib.prefixkv_compact_paged(*[l0 if i == 8 else x for i, x in enumerate(args)]) == 2
+    assert lib.prefixkv_compact_paged(*[shape(dtype=2)] + args[1:]) == 3
+    assert lib.prefixkv_compact_paged(*[ODD if i == 10 else x for i, x in enumerate(args)]) == 4
+
+
+def test_attention_refuses():
+    lib = P.load()
+    plain = [packed(), A, ST, A, ST, A, ST, A, A, A, ST, A, A, BIG, None]
+    chunk = [packed(), A, ST, A, paging(), 0, A, A, A, A, A, 10, A, ST, A, BIG, None]
+    for f, args, ws in ((lib.prefixkv_prefill_attn_packed, plain, 12), (lib.prefixkv_chunk_attn, chunk, 14)):
+        for bad in with_null(args, optional=(ws,)):
+            assert f(*bad) == 1
+        for kw in BAD_PACKED:
+            assert f(*[packed(**kw)] + args[1:]) == 2, kw
+        assert f(*[packed(dtype=5)] + args[1:]) == 3
+        assert f(*[ODD if j == 1 else y for j, y in enumerate(args)]) == 4
+        for i, x in enumerate(args):
+            if x is ST:
+                assert f(*[Bd._Strides(0, 8192, 130, 4096) if j == i else y for j, y in enumerate(args)]) == 4
+    assert lib.prefixkv_prefill_attn_packed(*[packed(dtype=P.PKV_F32)] + plain[1:]) == 7
+    for kw in BAD_PAGING:
+        assert lib.prefixkv_chunk_attn(*[paging(**kw) if i == 4 else x for i, x in enumerate(chunk)]) == 2
+    for i, x in ((5, -1), (5, 2), (11, 0), (11, 11)):
+        assert lib.prefixkv_chunk_attn(*[x if j == i else y for j, y in enumerate(chunk)]) == 2
+    for rows, f, args, ws in ((0, lib.prefixkv_prefill_attn_packed, plain, 12), (10, lib.prefixkv_chunk_attn, chunk, 14)):
+        need = P.attn_workspace_bytes(2, 1, 4, 2, 10, 128, torch.bfloat16, max_rows=rows)
+        if need:
+            for i, x in ((ws, None), (ws, C.c_void_p(4104)), (ws + 1, need - 1)):
+                assert f(*[x if j == i else y for j, y in enumerate(args)]) == 5
+    for bad in (dict(T=0), dict(D=96), dict(S=0)):
+        d = {**dict(S=2, L=1, H=4, Hkv=2, T=10, D=128), **bad}
+        assert P.attn_workspace_bytes(dtype=torch.bfloat16, **d) == 0
+    assert P.attn_workspace_bytes(2, 1, 4, 2, 10, 128, torch.bfloat16, max_rows=11) == 0
+
+
+def test_binding_refuses():
+    x = torch.zeros((1, 4, 10, 64), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="GPU"):
+        P.prefixkv_rope(x, x, torch.zeros((1, 10), dtype=torch.int32), P.rope_plan(64, device="cpu"))
+    c = P.paged_cache(2, 3, 4, 64, 16, 5, 2, device="cpu")
+    assert int(c.state[1]) == 5 and c.lens.shape == (2, 3) and bool((c.table == -1).all())
+    with pytest.raises(ValueError, match="GPU"):
+        P.prefixkv_page_resize(c, c.lens)
+    with pytest.raises(ValueError):
+        P.PagedCache(kp=c.kp, vp=c.vp, table=c.table.long(), lens=c.lens, ring=c.ring, state=c.state)
+    with pytest.raises(ValueError):
+        P.PagedCache(kp=c.kp, vp=c.vp, table=c.table, lens=c.lens[:1], ring=c.ring, state=c.state)
+    with pytest.raises(ValueError):
+        P.PagedCache(kp=c.kp, vp=c.vp[:4], table=c.table, lens=c.lens, ring=c.ring, state=c.state)
+    with pytest.raises(ValueError, match="sections"):
+        P.rope_plan(64, [16, 15], device="cpu")
+    with pytest.raises(P.PrefixKVError):
+        P.rope_plan(24, device="cpu")
+    with pytest.raises(P.PrefixKVError):
+        P.rope_plan(64, theta=0.5, device="cpu")
+
+
+def test_rope_plan():
+    plan = P.rope_plan(64, [8, 12, 12], theta=10000.0, device="cpu")
+    assert plan.axis.tolist() == [0] * 8 + [1] * 12 + [2] * 12
+    assert P.rope_plan(16, [2, 3, 3], cycled=True, device="cpu").axis.tolist() == [0, 1, 2, 0, 1, 2, 1, 2]
+    for theta in (10000.0, 500000.0, 1.0):
+        plan = P.rope_plan(128, theta=theta, device="cpu")
+        for i in (0, 1, 17, 63):
+            turn = Fraction(int(plan.freq[i]) % (1 << 64), 1 << 64)
+            # half a unit of 2^-64 turn (of the slowest pair here, 2e-13 of it), and the double's own error
+            want = theta ** (-2.0 * i / 128)
+            assert abs(float(turn) * 2 * math.pi - want) <= 2 * math.pi * 2.0 ** -65 + 1e-14 * want
+    assert int(P.rope_plan(16, device="cpu").freq[0]) == round(Fraction(1 << 64) / Fraction("6.283185307179586476925286766559"))
+
+
+def test_plain_forms_on_hand_worked_numbers():
+    # pages: a segment of 3 entries that gets 4 (pages of 2): one page more, from the head of the ring
+    table, ring = np.array([[[5, 7, -1]]]), np.array([9, 1, 2, 3])
+    st, lens, t, r, state = R.resize(np.array([[3]]), np.array([[5]]), table, ring, np.array([3, 2]), 2)
+    assert (st, lens.tolist(), t.tolist(), state.tolist()) == (0, [[5]], [[[5, 7, 3]]], [0, 1])
+    st, lens, t, r, state = R.resize(lens, np.array([[1]]), t, r, state, 2)
+    assert (st, r.tolist(), state.tolist()) == (0, [9, 7, 3, 3], [0, 3])
+    st, lens, t, state, slots = R.append(np.array([[1]]), np.array([1, 4]), 5, t, r, state, 2)
+    assert (st, slots.tolist(), state.tolist()) == (0, [[-1, 11, 18, 19, -1]], [1, 2])
+    # a quarter turn
+    y = R.rope(np.array([[[[1.0, 2.0, 3.0]]]]), np.array([[1]]), [0], math.pi / 2, 2, False)
+    np.testing.assert_allclose(y[0, 0, 0], [math.cos(1) - 2 * math.sin(1), 2 * math.cos(1) + math.sin(1), 3.0])
+    # attention: equal scores give the mean of what is seen; what is not seen may be anything
+    k, v = np.zeros((3, 2)), np.array([[1.0, 0], [3.0, 4], [np.nan, np.inf]])
+    out, mag, lse = R.attend(np.zeros((3, 2)), k, v, 1.0, -1)
+    assert out[:2].tolist() == [[0, 0], [1, 0]] and out[2].tolist() == [2, 2] and lse[2] == math.log(2)
