@@ -176,7 +176,9 @@ def test_rope_plan():
             # half a unit of 2^-64 turn (of the slowest pair here, 2e-13 of it), and the double's own error
             want = theta ** (-2.0 * i / 128)
             assert abs(float(turn) * 2 * math.pi - want) <= 2 * math.pi * 2.0 ** -65 + 1e-14 * want
-    assert int(P.rope_plan(16, device="cpu").freq[0]) == round(Fraction(1 << 64) / Fraction("6.283185307179586476925286766559"))
+    # pi, the power and the quotient are rounded to 64 bits each, a quarter of a unit at this size, then to whole units: one unit
+    exact = Fraction(1 << 64) / Fraction("6.283185307179586476925286766559")
+    assert abs(int(P.rope_plan(16, device="cpu").freq[0]) - exact) <= 1.25
 
 
 def test_plain_forms_on_hand_worked_numbers():
