@@ -308,9 +308,9 @@ def prepare(c, seed):
             import paper_2412_03409_amd as pkv
             st["plan"] = pkv.rope_plan(c["rot"], sections, theta=st["theta"], interleaved=c["inter"], device=DEV)
             if c["store"]:
-                t = torch.zeros((1, L, 1), dtype=torch.int32, device=DEV)
-                st["cache"] = pkv.PagedCache(kp=st["kp"], vp=st["vp"], table=t, lens=t[:, :, 0].contiguous(), ring=t.flatten(),
-                                             state=_i32([0, 0]))
+                t = torch.zeros((1, L, 1), dtype=torch.int32, device=DEV)      # a store goes by the slots alone
+                st["cache"] = pkv.PagedCache(kp=st["kp"], vp=st["vp"], table=t, lens=t[:, :, 0].contiguous(),
+                                             ring=torch.zeros(pages, dtype=torch.int32, device=DEV), state=_i32([0, 0]))
         return st
     if k == "compact":
         B, L, Hkv, N = c["B"], c["L"], c["Hkv"], c["N"]
