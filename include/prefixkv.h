@@ -429,7 +429,8 @@ int prefixkv_prefill_attn_packed(const pkv_packed *shape, const void *q, pkv_str
  *       has more are left as they are.  It chooses the kernel: with few rows the cache is read by wavefronts
  *       that share its entries out evenly.
  *   ws [dev]: prefixkv_attn_workspace_bytes(shape, max_rows) bytes, 16-byte aligned (NULL if that is 0).
- *       Calls on different streams need workspaces of their own. */
+ *       Calls on different streams need workspaces of their own.
+ * S * L * Hkv * max_pages * page_size < 2^36 (PKV_ERR_UNSUPPORTED otherwise: fewer layers a call). */
 int prefixkv_chunk_attn(const pkv_packed *shape, const void *q, pkv_strides qs, const int32_t *row_off,
                         const pkv_paging *paging, int l0, const void *kp, const void *vp,
                         const int32_t *table, const int32_t *lens, const float *scale, int max_rows,

@@ -376,6 +376,7 @@ int prefixkv_prefill_attn_packed(const pkv_packed* s, const void* q, pkv_strides
     if (!row_strides_ok(qs, 2) || !row_strides_ok(ks, 2) || !row_strides_ok(vs, 2) || !row_strides_ok(os, 2) || !aligned16(q) ||
         !aligned16(k) || !aligned16(v) || !aligned16(out))
         return PKV_ERR_STRIDE;
+    if (!packed_attn_fits(*s, nullptr)) return PKV_ERR_UNSUPPORTED;
     const size_t need = packed_attn_ws_bytes(*s, 0);
     if (need > 0 && (!ws || ws_bytes < need || !aligned16(ws))) return PKV_ERR_WORKSPACE;
     PackedAttn a{};
@@ -395,6 +396,7 @@ int prefixkv_chunk_attn(const pkv_packed* s, const void* q, pkv_strides qs, cons
     if (!row_strides_ok(qs, esize) || !row_strides_ok(os, esize) || !aligned16(q) || !aligned16(kp) || !aligned16(vp) ||
         !aligned16(out))
         return PKV_ERR_STRIDE;
+    if (!packed_attn_fits(*s, g)) return PKV_ERR_UNSUPPORTED;
     const size_t need = packed_attn_ws_bytes(*s, max_rows);
     if (need > 0 && (!ws || ws_bytes < need || !aligned16(ws))) return PKV_ERR_WORKSPACE;
     PackedAttn a{};

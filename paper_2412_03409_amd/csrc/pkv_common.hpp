@@ -124,6 +124,7 @@ struct PackedAttn {
     int l0, max_rows;     // max_rows 0: packed prompts
     void* ws;
 };
+bool packed_attn_fits(const pkv_packed& s, const pkv_paging* g);
 size_t packed_attn_ws_bytes(const pkv_packed& s, int max_rows);
 hipError_t launch_packed_attn(const pkv_packed& s, const PackedAttn& a, hipStream_t st);
 
