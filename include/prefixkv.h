@@ -408,7 +408,7 @@ int prefixkv_compact_paged(const pkv_shape *shape, const void *k, pkv_strides ks
 
 /* ---- Causal attention of packed prompts: prefixkv_prefill_attn for sequences of different lengths.
  * Row m of a sequence attends to rows 0 ... m of the same sequence.  bf16 storage only.
- *   q, out [L,H,T,D] strides qs, os;  k, v [L,Hkv,T,D] strides ks, vs;  scale [dev] fp32 [L]
+ *   q, out [L,H,T,D] strides qs, os;  k, v [L,Hkv,T,D] strides ks, vs (n below 2^26);  scale [dev] fp32 [L]
  *   lse [dev] fp32 [L*H*T]: natural log; those of sequence s lie together as [L][H][n_s] from element
  *       L*H*row_off[s] on, so that prefixkv_importance with B = 1 and N = n_s takes them, and the rows of q
  *       and k, as they are.

@@ -593,7 +593,9 @@ def prefixkv_decode_attn_evict(cache: CompactResult, base_lens: torch.Tensor, q:
 
 
 # ---- packed prompts and paged caches -----------------------------------------------------------------------
-@dataclass
+# These calls come once per layer and step, and the small ones take the GPU less time than a look at ten tensors takes here:
+# what follows from shapes, strides and types alone (the checks and the argument structs) is worked out once per combination.
+@dataclass(frozen=True, eq=False)
 class PagedCache:
     kp: torch.Tensor      # [num_pages,Hkv,page_size,D] storage dtype
     vp: torch.Tensor
@@ -612,7 +614,10 @@ class PagedCache:
                 or self.state.shape != (2,)):
             raise ValueError("table must be [S,layers,max_pages], lens [S,layers], ring [num_pages], state [2]")
         P, Hkv, ps, D = self.kp.shape
-        self._paging = _Paging(P, ps, self.table.shape[2], self.table.shape[1])
+        pool = (Hkv, D, self.kp.dtype) if self.kp.is_contiguous() and self.vp.is_contiguous() else None
+        for name, x in (("_paging", C.byref(_Paging(P, ps, self.table.shape[2], self.table.shape[1]))), ("_pool", pool),
+                        ("_S", self.table.shape[0]), ("_layers", self.table.shape[1])):
+            object.__setattr__(self, name, x)
 
 
 def paged_cache(S: int, layers: int, Hkv: int, D: int, page_size: int, num_pages: int, max_pages: int,
@@ -626,8 +631,19 @@ def paged_cache(S: int, layers: int, Hkv: int, D: int, page_size: int, num_pages
                       state=torch.tensor([0, num_pages], dtype=torch.int32, device=device))
 
 
+def _here(*ts) -> int:
+    """The current stream's handle; every tensor has to be on the current GPU."""
+    if not ts[0].is_cuda:
+        raise ValueError("all tensors must be on the GPU")
+    d = torch.cuda.current_device()
+    for t in ts:
+        if t is not None and t.get_device() != d:
+            raise ValueError("all tensors must be on the current GPU")
+    return _raw_stream(d) if _raw_stream is not None else torch.cuda.current_stream(d).cuda_stream
+
+
 def _i32_like(t: torch.Tensor, shape, what: str) -> torch.Tensor:
-    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous i32 {list(shape)}")
     return t
 
@@ -638,12 +654,11 @@ def page_workspace_bytes(S: int, layers: int) -> int:
 
 
 def _page_out(cache: PagedCache, status, lens_out, state_out, ws):
-    _need_cuda(cache.table, cache.lens, cache.ring, cache.state, status, lens_out, state_out, ws)
-    S, layers = cache.lens.shape
-    status = torch.empty(1, dtype=torch.int32, device=cache.lens.device) if status is None else _i32_like(status, (1,), "status")
-    lens_out = cache.lens if lens_out is None else _i32_like(lens_out, (S, layers), "lens_out")
+    lens = cache.lens
+    status = torch.empty(1, dtype=torch.int32, device=lens.device) if status is None else _i32_like(status, (1,), "status")
+    lens_out = lens if lens_out is None else _i32_like(lens_out, lens.shape, "lens_out")
     state_out = cache.state if state_out is None else _i32_like(state_out, (2,), "state_out")
-    return status, lens_out, state_out, _ws(page_workspace_bytes(S, layers), cache.lens.device, ws)
+    return status, lens_out, state_out, _ws(page_workspace_bytes(cache._S, cache._layers), lens.device, ws)
 
 
 def prefixkv_page_resize(cache: PagedCache, target: torch.Tensor, status: Optional[torch.Tensor] = None,
@@ -651,12 +666,13 @@ def prefixkv_page_resize(cache: PagedCache, target: torch.Tensor, status: Option
                          ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gives every segment the length target [S,layers] i32: pages come from the ring or go back to it; the cache's lens and
     state are updated (or lens_out, state_out written in their place).  -> status [1] i32, 0 if it was done."""
-    _need_cuda(target)
-    _i32_like(target, cache.lens.shape, "target")
+    lens, table, ring, state = cache.lens, cache.table, cache.ring, cache.state
+    stream = _here(target, lens, table, ring, state, status, lens_out, state_out, ws)
+    _i32_like(target, lens.shape, "target")
     status, lens_out, state_out, w = _page_out(cache, status, lens_out, state_out, ws)
-    rc = load().prefixkv_page_resize(cache.lens.shape[0], C.byref(cache._paging), _ptr(target), _ptr(cache.lens),
-                                     _ptr(cache.table), _ptr(cache.ring), _ptr(cache.state), _ptr(lens_out), _ptr(state_out),
-                                     _ptr(status), _ptr(w), w.numel() * w.element_size(), _stream())
+    rc = load().prefixkv_page_resize(cache._S, cache._paging, target.data_ptr(), lens.data_ptr(), table.data_ptr(),
+                                     ring.data_ptr(), state.data_ptr(), lens_out.data_ptr(), state_out.data_ptr(),
+                                     status.data_ptr(), w.data_ptr(), w.numel() * w.element_size(), stream)
     if rc != 0:
         raise PrefixKVError(rc, "prefixkv_page_resize")
     return status
@@ -667,23 +683,24 @@ def prefixkv_page_append(cache: PagedCache, row_off: torch.Tensor, T: int, slots
                          state_out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
     """Room for the new rows of every sequence, in every layer: row_off [S+1] i32, T packed rows
     -> (slots [layers,T] i64, status [1] i32)."""
-    S, layers = cache.lens.shape
-    _need_cuda(row_off, slots)
-    _i32_like(row_off, (S + 1,), "row_off")
+    lens, table, ring, state = cache.lens, cache.table, cache.ring, cache.state
+    stream = _here(row_off, lens, table, ring, state, slots, status, lens_out, state_out, ws)
+    T = index(T)
+    _i32_like(row_off, (cache._S + 1,), "row_off")
     if slots is None:
-        slots = torch.empty((layers, T), dtype=torch.int64, device=cache.lens.device)
-    elif slots.dtype != torch.int64 or tuple(slots.shape) != (layers, T) or not slots.is_contiguous():
+        slots = torch.empty((cache._layers, T), dtype=torch.int64, device=lens.device)
+    elif slots.dtype is not torch.int64 or slots.shape != (cache._layers, T) or not slots.is_contiguous():
         raise ValueError("slots must be contiguous i64 [layers,T]")
     status, lens_out, state_out, w = _page_out(cache, status, lens_out, state_out, ws)
-    rc = load().prefixkv_page_append(S, int(T), C.byref(cache._paging), _ptr(row_off), _ptr(cache.lens), _ptr(cache.table),
-                                     _ptr(cache.ring), _ptr(cache.state), _ptr(lens_out), _ptr(state_out), _ptr(slots),
-                                     _ptr(status), _ptr(w), w.numel() * w.element_size(), _stream())
+    rc = load().prefixkv_page_append(cache._S, T, cache._paging, row_off.data_ptr(), lens.data_ptr(), table.data_ptr(),
+                                     ring.data_ptr(), state.data_ptr(), lens_out.data_ptr(), state_out.data_ptr(),
+                                     slots.data_ptr(), status.data_ptr(), w.data_ptr(), w.numel() * w.element_size(), stream)
     if rc != 0:
         raise PrefixKVError(rc, "prefixkv_page_append")
     return slots, status
 
 
-@dataclass
+@dataclass(frozen=True, eq=False)
 class RopePlan:
     freq: torch.Tensor    # [rot_dim/2] i64 holding the u64 fractions of a turn
     axis: torch.Tensor    # [rot_dim/2] i32
@@ -694,7 +711,8 @@ class RopePlan:
         if self.freq.dtype != torch.int64 or self.freq.dim() != 1 or not self.freq.is_contiguous():
             raise ValueError("freq must be contiguous i64 [rot_dim/2]")
         _i32_like(self.axis, self.freq.shape, "axis")
-        self._struct = _Rope(_ptr(self.freq), _ptr(self.axis), 2 * self.freq.shape[0], self.axes, int(self.interleaved))
+        object.__setattr__(self, "_args", C.byref(_Rope(self.freq.data_ptr(), self.axis.data_ptr(), 2 * self.freq.shape[0],
+                                                        self.axes, int(self.interleaved))))
 
 
 def rope_plan(rot_dim: int, sections=None, theta: float = 10000.0, interleaved: bool = False, cycled: bool = False,
@@ -723,46 +741,51 @@ def rope_plan(rot_dim: int, sections=None, theta: float = 10000.0, interleaved: 
                     axis=torch.tensor(axis, dtype=torch.int32, device=device), axes=len(sections), interleaved=bool(interleaved))
 
 
-def _strides4(t: torch.Tensor) -> _Strides:
+def _row_strides(shape, stride, dtype) -> _Strides:
     """Strides of [L,heads,T,D] rows.  (A dimension of one element may have any stride: its own is not looked at.)"""
-    if t.stride(3) != 1:
-        raise ValueError("the head dimension must be contiguous")
-    a = 16 // t.element_size()
-    st = [a if n == 1 else x for x, n in zip(t.stride(), t.shape)]
+    if len(shape) != 4 or stride[3] != 1:
+        raise ValueError("row tensors must be [L,heads,T,D] with D contiguous")
+    a = 4 if dtype is torch.float32 else 8
+    st = [a if n == 1 else x for x, n in zip(stride, shape)]
     return _Strides(0, st[0], st[1], st[2])
 
 
-@lru_cache(maxsize=256, typed=True)
-def _packed_of(S, L, H, Hkv, T, D, dtype) -> _Packed:
-    return _Packed(S, L, H, Hkv, T, D, dtype)
+_CODES = {torch.float32: PKV_F32, torch.bfloat16: PKV_BF16}
 
 
-def _rows(*ts: torch.Tensor):
-    L, _, T, D = ts[0].shape
-    for t in ts:
-        if t.dim() != 4 or t.shape[0] != L or t.shape[2] != T or t.shape[3] != D or t.dtype != ts[0].dtype:
-            raise ValueError("row tensors must be [L,heads,T,D] of one dtype")
+def _packed(S, Hkv, qsh, dtype) -> _Packed:
+    if dtype not in _CODES:
+        raise TypeError(f"unsupported storage dtype {dtype}")
+    return _Packed(S, qsh[0], qsh[1], Hkv, qsh[2], qsh[3], _CODES[dtype])
 
 
-def _rope_args(q, k, positions, plan):
-    if positions.dtype != torch.int32 or positions.shape != (plan.axes, q.shape[2]) or not positions.is_contiguous():
+@lru_cache(maxsize=512)
+def _rope_args(qsh, qst, qdt, ksh, kst, kdt, osh, ost, odt, xsh, xst, xdt, psh, pst, pdt, axes, cache):
+    """Argument structs of a rotation: x is k_out, or v if the keys go into a cache (its heads, head dimension and dtype)."""
+    strides = [_row_strides(*a) for a in ((qsh, qst, qdt), (ksh, kst, kdt), (xsh, xst, xdt), (osh, ost, odt))]
+    if not (qdt == kdt == odt == xdt) or (ksh[0], ksh[2], ksh[3]) != (qsh[0], qsh[2], qsh[3]):
+        raise ValueError("row tensors must be [L,heads,T,D] of one dtype")
+    if osh != qsh or xsh != ksh:
+        raise ValueError("q_out must have the shape of q, k_out or v that of k")
+    if pdt != torch.int32 or psh != (axes, qsh[2]) or any(x != s for x, s, n in zip(pst, (qsh[2], 1), psh) if n > 1):
         raise ValueError("positions must be contiguous i32 [axes,T]")
-    return _packed_of(1, q.shape[0], q.shape[1], k.shape[1], q.shape[2], q.shape[3], _dtype_code(q))
+    if cache is not None and cache != (ksh[1], ksh[3], kdt):
+        raise ValueError("the cache must have k's heads, head dimension and dtype, and contiguous pools")
+    return (C.byref(_packed(1, ksh[1], qsh, qdt)), *strides)
 
 
 def prefixkv_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, plan: RopePlan,
                   q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
     """q [L,H,T,D], k [L,Hkv,T,D] (bf16 or f32, any strides with D contiguous), positions [axes,T] i32
     -> (q_out, k_out), rotated; q_out = q and k_out = k rotate in place."""
-    _need_cuda(q, k, positions, plan.freq, plan.axis, q_out, k_out)
+    stream = _here(q, k, positions, plan.freq, plan.axis, q_out, k_out)
     q_out = torch.empty_like(q) if q_out is None else q_out
     k_out = torch.empty_like(k) if k_out is None else k_out
-    _rows(q, k, q_out, k_out)
-    if q_out.shape != q.shape or k_out.shape != k.shape:
-        raise ValueError("outputs must have the shapes of q and k")
-    s = _rope_args(q, k, positions, plan)
-    rc = load().prefixkv_rope(C.byref(s), C.byref(plan._struct), _ptr(positions), _ptr(q), _strides4(q), _ptr(k), _strides4(k),
-                              _ptr(q_out), _strides4(q_out), _ptr(k_out), _strides4(k_out), _stream())
+    s, qs, ks, kos, qos = _rope_args(q.shape, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, q_out.shape, q_out.stride(),
+                                     q_out.dtype, k_out.shape, k_out.stride(), k_out.dtype, positions.shape, positions.stride(),
+                                     positions.dtype, plan.axes, None)
+    rc = load().prefixkv_rope(s, plan._args, positions.data_ptr(), q.data_ptr(), qs, k.data_ptr(), ks, q_out.data_ptr(), qos,
+                              k_out.data_ptr(), kos, stream)
     if rc != 0:
         raise PrefixKVError(rc, "prefixkv_rope")
     return q_out, k_out
@@ -771,20 +794,16 @@ def prefixkv_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, pla
 def prefixkv_rope_store(cache: PagedCache, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor,
                         plan: RopePlan, slots: torch.Tensor, q_out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Rotates q [L,H,T,D] and k [L,Hkv,T,D] and stores k and v into the cache's pages at slots [L,T] i64 -> q_out."""
-    _need_cuda(q, k, v, positions, plan.freq, plan.axis, slots, q_out, cache.kp, cache.vp)
+    kp, vp = cache.kp, cache.vp
+    stream = _here(q, k, v, positions, plan.freq, plan.axis, slots, q_out, kp, vp)
     q_out = torch.empty_like(q) if q_out is None else q_out
-    _rows(q, k, v, q_out)
-    if q_out.shape != q.shape or v.shape != k.shape:
-        raise ValueError("q_out must have the shape of q, v that of k")
-    if slots.dtype != torch.int64 or slots.shape != (q.shape[0], q.shape[2]) or not slots.is_contiguous():
+    s, qs, ks, vs, qos = _rope_args(q.shape, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, q_out.shape, q_out.stride(),
+                                    q_out.dtype, v.shape, v.stride(), v.dtype, positions.shape, positions.stride(),
+                                    positions.dtype, plan.axes, cache._pool or ())
+    if slots.dtype is not torch.int64 or slots.shape != q.shape[::2] or not slots.is_contiguous():
         raise ValueError("slots must be contiguous i64 [L,T]")
-    if (cache.kp.dtype != q.dtype or cache.kp.shape[1] != k.shape[1] or cache.kp.shape[3] != q.shape[3]
-            or not cache.kp.is_contiguous() or not cache.vp.is_contiguous()):
-        raise ValueError("the cache must have k's heads, head dimension and dtype, and contiguous pools")
-    s = _rope_args(q, k, positions, plan)
-    rc = load().prefixkv_rope_store(C.byref(s), C.byref(plan._struct), _ptr(positions), _ptr(q), _strides4(q), _ptr(k),
-                                    _strides4(k), _ptr(v), _strides4(v), _ptr(q_out), _strides4(q_out), _ptr(slots),
-                                    C.byref(cache._paging), _ptr(cache.kp), _ptr(cache.vp), _stream())
+    rc = load().prefixkv_rope_store(s, plan._args, positions.data_ptr(), q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
+                                    q_out.data_ptr(), qos, slots.data_ptr(), cache._paging, kp.data_ptr(), vp.data_ptr(), stream)
     if rc != 0:
         raise PrefixKVError(rc, "prefixkv_rope_store")
     return q_out
@@ -794,7 +813,7 @@ def prefixkv_compact_paged(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, 
                            kept_pos: Optional[torch.Tensor] = None, l0: int = 0) -> PagedCache:
     """prefixkv_compact into the cache's pages: k,v [B,L,Hkv,N,D], order [B,L,N] i32, lengths [B,L] i32; sequence b of the
     batch is sequence b of the cache, layer l its layer l0 + l.  kept_pos [B,L,N] i32, optional output."""
-    _need_cuda(k, v, order, lengths, kept_pos, cache.kp, cache.vp, cache.table)
+    stream = _here(k, v, order, lengths, kept_pos, cache.kp, cache.vp, cache.table)
     B, L, Hkv, N, D = k.shape
     if v.shape != k.shape or v.dtype != k.dtype:
         raise ValueError("v must match k")
@@ -802,32 +821,36 @@ def prefixkv_compact_paged(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, 
     _i32_like(lengths, (B, L), "lengths")
     if kept_pos is not None:
         _i32_like(kept_pos, (B, L, N), "kept_pos")
-    if (cache.kp.dtype != k.dtype or cache.kp.shape[1] != Hkv or cache.kp.shape[3] != D or cache.table.shape[0] < B
-            or not cache.kp.is_contiguous() or not cache.vp.is_contiguous()):
+    if cache._pool != (Hkv, D, k.dtype) or cache._S < B:
         raise ValueError("the cache must have k's heads, head dimension and dtype, B sequences and contiguous pools")
     s = _shape_of(B, L, Hkv, Hkv, N, D, _dtype_code(k))
-    rc = load().prefixkv_compact_paged(C.byref(s), _ptr(k), _strides5(k), _ptr(v), _strides5(v), _ptr(order), _ptr(lengths),
-                                       C.byref(cache._paging), int(l0), _ptr(cache.table), _ptr(cache.kp), _ptr(cache.vp),
-                                       _ptr(kept_pos), _stream())
+    rc = load().prefixkv_compact_paged(C.byref(s), k.data_ptr(), _strides5(k), v.data_ptr(), _strides5(v), order.data_ptr(),
+                                       lengths.data_ptr(), cache._paging, int(l0), cache.table.data_ptr(), cache.kp.data_ptr(),
+                                       cache.vp.data_ptr(), _ptr(kept_pos), stream)
     if rc != 0:
         raise PrefixKVError(rc, "prefixkv_compact_paged")
     return cache
 
 
-@lru_cache(maxsize=256, typed=True)
-def _attn_ws_bytes_of(S, L, H, Hkv, T, D, dtype, max_rows) -> int:
-    s = _packed_of(S, L, H, Hkv, T, D, dtype)
-    return int(load().prefixkv_attn_workspace_bytes(C.byref(s), max_rows))
-
-
 def attn_workspace_bytes(S: int, L: int, H: int, Hkv: int, T: int, D: int, dtype: torch.dtype, max_rows: int = 0) -> int:
     """Workspace of prefixkv_chunk_attn, or (max_rows = 0) of prefixkv_prefill_attn_packed."""
-    return _attn_ws_bytes_of(S, L, H, Hkv, T, D, PKV_F32 if dtype == torch.float32 else PKV_BF16, max_rows)
+    return int(load().prefixkv_attn_workspace_bytes(C.byref(_packed(S, Hkv, (L, H, T, D), dtype)), int(max_rows)))
 
 
-def _scale_of(scale: torch.Tensor, L: int):
-    if scale.dtype != torch.float32 or scale.shape != (L,) or not scale.is_contiguous():
-        raise ValueError("scale must be contiguous f32 [L]")
+@lru_cache(maxsize=512)
+def _attn_args(qsh, qst, qdt, osh, ost, odt, S, Hkv, max_rows):
+    """Argument structs of rows q and out, and the call's workspace."""
+    qs, os_ = _row_strides(qsh, qst, qdt), _row_strides(osh, ost, odt)
+    if osh != qsh or odt != qdt:
+        raise ValueError("out must have the shape and dtype of q")
+    return C.byref(_packed(S, Hkv, qsh, qdt)), qs, os_, attn_workspace_bytes(S, qsh[0], qsh[1], Hkv, qsh[2], qsh[3], qdt, max_rows)
+
+
+@lru_cache(maxsize=512)
+def _key_args(ksh, kst, kdt, vsh, vst, vdt, qsh, qdt):
+    if vsh != ksh or not (kdt == vdt == qdt) or len(ksh) != 4 or (ksh[0], ksh[2], ksh[3]) != (qsh[0], qsh[2], qsh[3]):
+        raise ValueError("k, v must be [L,Hkv,T,D] with q's dtype")
+    return _row_strides(ksh, kst, kdt), _row_strides(vsh, vst, vdt)
 
 
 def prefixkv_prefill_attn_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_off: torch.Tensor, scale: torch.Tensor,
@@ -836,23 +859,23 @@ def prefixkv_prefill_attn_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tens
     """Causal attention of packed prompts: q [L,H,T,D], k/v [L,Hkv,T,D] (bf16), row_off [S+1] i32, scale [L] f32
     -> (out [L,H,T,D], lse [L*H*T] f32: [L,H,n] of each sequence one behind the other).  Rows that belong to no sequence are
     left as they are."""
-    _need_cuda(q, k, v, row_off, scale, out, lse, ws)
+    stream = _here(q, k, v, row_off, scale, out, lse, ws)
     out = torch.empty_like(q) if out is None else out
-    _rows(q, k, v, out)
-    L, H, T, D = q.shape
-    if k.shape != v.shape or out.shape != q.shape:
-        raise ValueError("v must have the shape of k, out that of q")
-    _i32_like(row_off, (row_off.numel(),), "row_off")
-    _scale_of(scale, L)
+    S = row_off.numel() - 1
+    s, qs, os_, need = _attn_args(q.shape, q.stride(), q.dtype, out.shape, out.stride(), out.dtype, S, k.shape[1], 0)
+    ks, vs = _key_args(k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype, q.shape, q.dtype)
+    L, H, T, _ = q.shape
+    _i32_like(row_off, (S + 1,), "row_off")
+    if scale.dtype is not torch.float32 or scale.shape != (L,) or not scale.is_contiguous():
+        raise ValueError("scale must be contiguous f32 [L]")
     if lse is None:
         lse = torch.empty(L * H * T, dtype=torch.float32, device=q.device)
-    elif lse.dtype != torch.float32 or lse.numel() != L * H * T or not lse.is_contiguous():
+    elif lse.dtype is not torch.float32 or lse.numel() != L * H * T or not lse.is_contiguous():
         raise ValueError("lse must be contiguous f32 [L*H*T]")
-    dims = (row_off.numel() - 1, L, H, k.shape[1], T, D, _dtype_code(q))
-    w = _ws(_attn_ws_bytes_of(*dims, 0), q.device, ws)
-    rc = load().prefixkv_prefill_attn_packed(C.byref(_packed_of(*dims)), _ptr(q), _strides4(q), _ptr(k), _strides4(k), _ptr(v),
-                                             _strides4(v), _ptr(row_off), _ptr(scale), _ptr(out), _strides4(out), _ptr(lse),
-                                             _ptr(w), w.numel() * w.element_size(), _stream())
+    w = _ws(need, q.device, ws)
+    rc = load().prefixkv_prefill_attn_packed(s, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, row_off.data_ptr(),
+                                             scale.data_ptr(), out.data_ptr(), os_, lse.data_ptr(), w.data_ptr(),
+                                             w.numel() * w.element_size(), stream)
     if rc != 0:
         raise PrefixKVError(rc, "prefixkv_prefill_attn_packed")
     return out, lse
@@ -862,22 +885,21 @@ def prefixkv_chunk_attn(cache: PagedCache, q: torch.Tensor, row_off: torch.Tenso
                         l0: int = 0, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of new rows q [L,H,T,D] over the cache's layers l0 ... l0+L-1, which hold their keys and values already:
     row_off [S+1] i32, scale [L] f32, max_rows = the most rows of a sequence -> out [L,H,T,D]."""
-    _need_cuda(q, row_off, scale, out, ws, cache.kp, cache.vp, cache.table, cache.lens)
+    kp, vp, table, lens = cache.kp, cache.vp, cache.table, cache.lens
+    stream = _here(q, row_off, scale, out, ws, kp, vp, table, lens)
     out = torch.empty_like(q) if out is None else out
-    _rows(q, out)
-    L, H, T, D = q.shape
-    S = cache.lens.shape[0]
-    if out.shape != q.shape:
-        raise ValueError("out must have the shape of q")
-    _i32_like(row_off, (S + 1,), "row_off")
-    _scale_of(scale, L)
-    if (cache.kp.dtype != q.dtype or cache.kp.shape[3] != D or not cache.kp.is_contiguous() or not cache.vp.is_contiguous()):
+    pool, max_rows = cache._pool, index(max_rows)
+    qsh = q.shape
+    if pool is None or pool[1:] != (qsh[3], q.dtype):
         raise ValueError("the cache must have q's head dimension and dtype, and contiguous pools")
-    dims = (S, L, H, cache.kp.shape[1], T, D, _dtype_code(q))
-    w = _ws(_attn_ws_bytes_of(*dims, int(max_rows)), q.device, ws)
-    rc = load().prefixkv_chunk_attn(C.byref(_packed_of(*dims)), _ptr(q), _strides4(q), _ptr(row_off), C.byref(cache._paging),
-                                    int(l0), _ptr(cache.kp), _ptr(cache.vp), _ptr(cache.table), _ptr(cache.lens), _ptr(scale),
-                                    int(max_rows), _ptr(out), _strides4(out), _ptr(w), w.numel() * w.element_size(), _stream())
+    s, qs, os_, need = _attn_args(qsh, q.stride(), q.dtype, out.shape, out.stride(), out.dtype, cache._S, pool[0], max_rows)
+    _i32_like(row_off, (cache._S + 1,), "row_off")
+    if scale.dtype is not torch.float32 or scale.shape != (qsh[0],) or not scale.is_contiguous():
+        raise ValueError("scale must be contiguous f32 [L]")
+    w = _ws(need, q.device, ws)
+    rc = load().prefixkv_chunk_attn(s, q.data_ptr(), qs, row_off.data_ptr(), cache._paging, int(l0), kp.data_ptr(),
+                                    vp.data_ptr(), table.data_ptr(), lens.data_ptr(), scale.data_ptr(), max_rows,
+                                    out.data_ptr(), os_, w.data_ptr(), w.numel() * w.element_size(), stream)
     if rc != 0:
         raise PrefixKVError(rc, "prefixkv_chunk_attn")
     return out

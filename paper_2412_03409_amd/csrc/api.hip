@@ -376,7 +376,8 @@ int prefixkv_prefill_attn_packed(const pkv_packed* s, const void* q, pkv_strides
     if (!row_strides_ok(qs, 2) || !row_strides_ok(ks, 2) || !row_strides_ok(vs, 2) || !row_strides_ok(os, 2) || !aligned16(q) ||
         !aligned16(k) || !aligned16(v) || !aligned16(out))
         return PKV_ERR_STRIDE;
-    if (!packed_attn_fits(*s, nullptr)) return PKV_ERR_UNSUPPORTED;
+    // the copies address 16 rows with 32-bit byte offsets
+    if (!packed_attn_fits(*s, nullptr) || ks.n >= (1ll << 26) || vs.n >= (1ll << 26)) return PKV_ERR_UNSUPPORTED;
     const size_t need = packed_attn_ws_bytes(*s, 0);
     if (need > 0 && (!ws || ws_bytes < need || !aligned16(ws))) return PKV_ERR_WORKSPACE;
     PackedAttn a{};

@@ -148,6 +148,24 @@ __device__ __forceinline__ int swz(int r) {
     else return ((r & 1) << 2) | ((r >> 1) & 3);
 }
 
+// Where a lane copies from when 16 rows go to LDS, 1 KB at a time: lane i of copy x writes 16 bytes at 1024 x + 16 i, that is
+// chunk i % CPR of row x * 64 / CPR + i / CPR, which holds the row's chunk that the swizzle moves there.
+template <int D>
+struct CopyLane {
+    static constexpr int CPR = D / 8, RPC = kWave / CPR, kCopies = 16 / RPC;
+    uint32_t row, col;                        // of copy 0; column in bytes
+    __device__ __forceinline__ explicit CopyLane(int lane) {
+        row = (uint32_t)(lane / CPR);
+        col = 16u * (uint32_t)((lane % CPR) ^ swz<CPR>(lane / CPR));
+        asm volatile("" : "+v"(row), "+v"(col));
+    }
+    // byte offset of copy x; rows from `last` on are read like row `last`
+    __device__ __forceinline__ uint32_t at(int x, uint32_t last, uint32_t row_bytes) const {
+        const uint32_t r = min(row + (uint32_t)(x * RPC), last);
+        return r * row_bytes + (CPR == 16 ? col ^ (16u * (uint32_t)x) : col);      // (rows a multiple of 8 apart are swizzled alike if CPR is 8)
+    }
+};
+
 __device__ __forceinline__ void copy_to_lds(const unsigned char* src, unsigned char* dst) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
 }
@@ -222,10 +240,15 @@ struct RowTile {
 #pragma unroll
             for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const bool see = 32 * kt + 8 * (r >> 2) + (r & 3) <= mine && !((bad >> (2 * kt + (r >> 3))) & 1u);
-                    s[kt][r] = see ? s[kt][r] : -INFINITY;
-                }
+                for (int r = 0; r < 16; ++r) s[kt][r] = 32 * kt + 8 * (r >> 2) + (r & 3) <= mine ? s[kt][r] : -INFINITY;
+            if (bad != 0) {
+#pragma unroll
+                for (int x = 0; x < 2 * NKT; ++x)
+                    if ((bad >> x) & 1u) {
+#pragma unroll
+                        for (int r = 0; r < 8; ++r) s[x / 2][8 * (x % 2) + r] = -INFINITY;
+                    }
+            }
         }
         float mx[NKT];
 #pragma unroll
@@ -373,8 +396,6 @@ __device__ __forceinline__ float score_scale(float sc) {
     return a < 1e-30f ? 1e-30f : a;
 }
 
-struct Sequence { int first, n, rows; };    // first packed row, rows, rows of this call (times the heads of a KV head)
-
 // What a row of a tile or unit is: row = token * grp + head of the KV head
 struct RowAt { int token, head; };
 __device__ __forceinline__ RowAt row_at(int row, FastDiv grp) {
@@ -382,262 +403,467 @@ __device__ __forceinline__ RowAt row_at(int row, FastDiv grp) {
     return {x.q, x.r};
 }
 
-struct TileParams {
+// What both kernels share out: segments (sequence, layer of the call), the KV heads of each one after the other.
+struct Work {
     PackedParams a;
-    FastDiv grp, by_heads, by_hkv, by_tail, by_tiles, by_parts;
-    int heads, tiles, parts;       // L * Hkv; tiles of all sequences at most; parts of a tile's keys at most
-    int heads_per_xcd;             // 0: the heads do not divide up
-    float* part_o;                 // [heads][tiles][parts][128][D]
-    float2* part_ms;
+    FastDiv grp, by_layers;
+    int segs;                       // S * L
 };
-constexpr int kPartStages = 6;     // stages of a part at least
+struct Segment { int s, l, first, n, rows, len, before, end; };   // rows: of this call, times the heads of a KV head; keys; keys in front
+                                                                  // of the first new row (below 0: the first rows see nothing); keys that some row sees
 
-// Tile tt: sequence by sequence, the last tile of a sequence first (its rows see the most).  false: there are fewer.
-__device__ __forceinline__ bool find_tile(const PackedParams& p, int grp, int tt, int lane, Sequence& sq, int& s, int& tile) {
-    int base = 0;
-    for (int c = 0; c < p.S; c += kWave) {
-        const int i = c + lane;
-        int first = 0, n = 0;
-        if (i < p.S) {
-            const int last = p.row_off[i + 1];
-            first = p.row_off[i];
-            n = first >= 0 && last <= p.T ? max(0, last - first) : 0;
-        }
-        const int rows = (p.max_rows > 0 ? min(n, p.max_rows) : n) * grp, tiles = (rows + kTileRows - 1) / kTileRows;
-        int incl = tiles;
+template <bool PAGED>
+__device__ __forceinline__ Segment segment(const Work& p, int i) {
+    Segment x;
+    const DivMod sl = div_mod(i, p.by_layers);
+    x.s = sl.q; x.l = sl.r;
+    const int last = p.a.row_off[x.s + 1];
+    x.first = p.a.row_off[x.s];
+    x.n = x.first >= 0 && last <= p.a.T ? max(0, last - x.first) : 0;
+    x.len = PAGED ? entries(p.a, x.s, x.l) : x.n;
+    const int rows = PAGED ? min(x.n, p.a.max_rows) : x.n;
+    x.rows = rows * p.a.grp;
+    x.before = x.len - x.n;
+    x.end = max(0, min(x.len, x.before + rows));
+    return x;
+}
+template <bool PAGED>
+__device__ __forceinline__ Segment uniform_segment(const Work& p, int i) {
+    Segment x = segment<PAGED>(p, i);
+    x.s = __builtin_amdgcn_readfirstlane(x.s); x.l = __builtin_amdgcn_readfirstlane(x.l);
+    x.first = __builtin_amdgcn_readfirstlane(x.first); x.n = __builtin_amdgcn_readfirstlane(x.n);
+    x.rows = __builtin_amdgcn_readfirstlane(x.rows); x.len = __builtin_amdgcn_readfirstlane(x.len);
+    x.before = __builtin_amdgcn_readfirstlane(x.before); x.end = __builtin_amdgcn_readfirstlane(x.end);
+    return x;
+}
+__device__ __forceinline__ int64_t shfl_up64(int64_t x, int d) {
+    const int lo = __shfl_up((int)(uint32_t)x, d, kWave), hi = __shfl_up((int)(x >> 32), d, kWave);
+    return (int64_t)(((uint64_t)(uint32_t)hi << 32) | (uint32_t)lo);
+}
+__device__ __forceinline__ int64_t lane64(int64_t x, int j) {
+    return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), j) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, j));
+}
+
+// The segment that holds place x of a launch, and the place in it: segment i has cost(i) places.
+template <class F>
+__device__ __forceinline__ int find_segment(int segs, int lane, int64_t x, int64_t& in, F cost) {
+    int64_t base = 0;
+    for (int c = 0; c < segs; c += kWave) {
+        const int64_t mine = c + lane < segs ? cost(c + lane) : 0;
+        int64_t incl = mine;
 #pragma unroll
         for (int d = 1; d < kWave; d <<= 1) {
-            const int up = __shfl_up(incl, d, kWave);
+            const int64_t up = shfl_up64(incl, d);
             if (lane >= d) incl += up;
         }
-        const unsigned long long at = __builtin_amdgcn_ballot_w64(base + incl > tt);
+        const unsigned long long at = __builtin_amdgcn_ballot_w64(base + incl > x);
         if (at != 0) {
             const int j = __builtin_ctzll(at);
-            s = c + j;
-            sq = {__builtin_amdgcn_readlane(first, j), __builtin_amdgcn_readlane(n, j), __builtin_amdgcn_readlane(rows, j)};
-            tile = base + __builtin_amdgcn_readlane(incl, j) - 1 - tt;
-            return true;
+            in = x - base - lane64(incl, j) + lane64(mine, j);
+            return c + j;
         }
-        base += __builtin_amdgcn_readlane(incl, kWave - 1);
+        base += lane64(incl, kWave - 1);
     }
-    return false;
+    in = 0;
+    return segs;
+}
+template <class F>
+__device__ __forceinline__ int64_t all_segments(int segs, int lane, F cost) {
+    int64_t sum = 0;
+    for (int i = lane; i < segs; i += kWave) sum += cost(i);
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        const int64_t up = shfl_up64(sum, d);
+        if (lane >= d) sum += up;
+    }
+    return lane64(sum, kWave - 1);
 }
 
-template <bool PAGED>
-struct TileKeys { int len, before, end, nst, parts; };   // keys; keys in front of the first new row; keys that the tile sees; stages; parts
+// ---- many rows -----------------------------------------------------------------------------------------
+struct TileParams : Work {
+    int workgroups;                // that share the launch out; 0: a workgroup per tile
+    FastDiv by_hkv, by_heads, by_tiles, by_tail;
+    int heads_per_xcd;             // of the call's L * Hkv heads; 0: they do not divide up
+    int4* cut;                     // workspace [workgroups]: {segment, head, tile, stage} where a workgroup begins; stage 0: with a whole tile
+    float* part_o;                 // [2 * workgroups][128][D]
+    float2* part_ms;
+};
+constexpr int kStartKeys = 192;     // what the start and the end of a tile cost, in keys
+constexpr int kJoinStages = 3;      // what a cut costs: two parts written and read again, and a second start
 
+// Every workgroup takes the same share of a launch, wherever that begins and ends: tiles differ in length by two orders of
+// magnitude (a prompt's first and last one, caches of other layers), and a launch of one workgroup per tile ended with a few long
+// ones on an empty chip.  (Two prompts of 6001 and 4000 ... rows, H32/8: 690 us; 600 rows over 6000 keys among shorter sequences,
+// tiles cut in halves: 137.)
+// A tile's cost is the keys that it sees, if it were full, and kStartKeys, in units of one key and row of grp; that has a closed sum.
 template <bool PAGED>
-__device__ __forceinline__ TileKeys<PAGED> tile_keys(const TileParams& p, const Sequence& sq, int s, int l, int tile) {
-    TileKeys<PAGED> k;
-    k.len = PAGED ? entries(p.a, s, l) : sq.n;
-    k.before = k.len - sq.n;                                    // below 0: the first rows see nothing
-    const int last = __builtin_amdgcn_readfirstlane(row_at(min(sq.rows, (tile + 1) * kTileRows) - 1, p.grp).token);
-    k.end = max(0, min(k.len, k.before + last + 1));
-    k.nst = (k.end + kStage - 1) / kStage;
-    k.parts = max(1, min(p.parts, k.nst / kPartStages));
-    return k;
+struct TileCost {
+    int64_t first;                  // of tile 0, without its rows
+    int tiles;
+    __device__ __forceinline__ TileCost(const Work& p, const Segment& x)
+        : first((int64_t)p.a.grp * (max(x.before, 0) + kStartKeys)), tiles((x.rows + kTileRows - 1) / kTileRows) {}
+    __device__ __forceinline__ int64_t up_to(int i) const { return i * first + (int64_t)(kTileRows / 2) * i * (i + 1); }   // tiles 0 ... i-1
+    __device__ __forceinline__ int64_t of(int i) const { return first + (int64_t)kTileRows * (i + 1); }
+};
+// stages of tile i
+__device__ __forceinline__ int tile_end(const Work& p, const Segment& x, int i) {       // keys that its rows see
+    const int last = __builtin_amdgcn_readfirstlane(row_at(min(x.rows, (i + 1) * kTileRows) - 1, p.grp).token);
+    return max(0, min(x.len, x.before + last + 1));
 }
 
-struct TileAt { int head, tt, part; };
-// Which tile a workgroup has.  With heads in eighths every head stays on one XCD: the tiles of a head run next to each other and
-// share its keys through that XCD's L2; the last heads of an XCD are taken together, so that the launch does not end on the long
-// tiles of a single one.  Else, and where tiles come in parts, heads alternate and the tiles go from long to short.
-__device__ __forceinline__ TileAt tile_at(const TileParams& p, int bid) {
-    if (p.parts == 1 && p.heads_per_xcd > 0) {
-        const int xcd = bid % kXcds, j = bid / kXcds, lead = p.heads_per_xcd - (int)p.by_tail.d;
-        if (j < lead * p.tiles) {
-            const DivMod x = uniform_div_mod(j, p.by_tiles);
-            return {xcd * p.heads_per_xcd + x.q, x.r, 0};
+struct Cut { int seg, head, tile, stage; };
+
+// What the workgroups share out.  Up to 64 segments (a layer of 64 sequences) are looked at once, a lane each; beyond, they are read
+// again where they are needed.
+template <bool PAGED>
+struct Shares {
+    const TileParams& p;
+    int lane;
+    Segment mine;                   // segment `lane`
+    int64_t upto, all, share;       // places of the segments up to `lane`; of all; of a workgroup
+    int tol;                        // stages
+
+    __device__ __forceinline__ int64_t cost(const Segment& x) const {
+        const TileCost<PAGED> t(p, x);
+        return t.up_to(t.tiles) * p.a.Hkv;
+    }
+    __device__ __forceinline__ Shares(const TileParams& params, int ln) : p(params), lane(ln) {
+        mine = segment<PAGED>(p, min(lane, p.segs - 1));
+        int longest = mine.end;
+        if (p.segs <= kWave) {
+            upto = lane < p.segs ? cost(mine) : 0;
+#pragma unroll
+            for (int d = 1; d < kWave; d <<= 1) {
+                const int64_t up = shfl_up64(upto, d);
+                if (lane >= d) upto += up;
+            }
+            all = lane64(upto, kWave - 1);
+        } else {
+            all = all_segments(p.segs, lane, [&](int i) { return cost(segment<PAGED>(p, i)); });
+            for (int i = lane + kWave; i < p.segs; i += kWave) longest = max(longest, segment<PAGED>(p, i).end);
         }
-        const DivMod x = uniform_div_mod(j - lead * p.tiles, p.by_tail);
-        return {xcd * p.heads_per_xcd + lead + x.r, x.q, 0};
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) longest = max(longest, __shfl_xor(longest, d, kWave));
+        // A cut costs what kJoinStages stages do.  Where the tiles are short none is made closer to an end of a tile, and where a
+        // launch is small a long tile is cut into pieces that are no shorter.
+        const int64_t stage = (int64_t)kStage * p.a.grp;
+        const int least = min(8, __builtin_amdgcn_readfirstlane(longest) / (2 * kStage) + 1);
+        share = max((int64_t)least * stage, (int64_t)((double)all / (double)p.workgroups) + 1);
+        tol = kJoinStages;
     }
-    const DivMod x = uniform_div_mod(bid, p.by_heads), y = uniform_div_mod(x.q, p.by_parts);
-    return {x.r, y.q, y.r};
+    __device__ __forceinline__ int find(int64_t x, int64_t& in, Segment& sg) const {
+        if (p.segs <= kWave) {
+            const int j = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > x));
+            in = x - (j == 0 ? 0 : lane64(upto, j - 1));
+            sg.s = __builtin_amdgcn_readlane(mine.s, j); sg.l = __builtin_amdgcn_readlane(mine.l, j);
+            sg.first = __builtin_amdgcn_readlane(mine.first, j); sg.n = __builtin_amdgcn_readlane(mine.n, j);
+            sg.rows = __builtin_amdgcn_readlane(mine.rows, j); sg.len = __builtin_amdgcn_readlane(mine.len, j);
+            sg.before = __builtin_amdgcn_readlane(mine.before, j); sg.end = __builtin_amdgcn_readlane(mine.end, j);
+            return j;
+        }
+        const int j = find_segment(p.segs, lane, x, in, [&](int i) { return cost(segment<PAGED>(p, i)); });
+        sg = uniform_segment<PAGED>(p, j);
+        return j;
+    }
+    // Where workgroup w begins.  A cut close to an end of a tile moves there.
+    __device__ __forceinline__ Cut cut(int w) const {
+        const int64_t x = w * share;
+        if (x >= all) return {p.segs, 0, 0, 0};
+        int64_t in;
+        Cut c;
+        Segment sg;
+        c.seg = find(x, in, sg);
+        const TileCost<PAGED> t(p, sg);
+        const int64_t head = t.up_to(t.tiles);
+        c.head = min(p.a.Hkv - 1, (int)((double)in / (double)head));       // (a quotient that is rounded up is corrected)
+        in -= c.head * head;
+        if (in < 0) { --c.head; in += head; }
+        int lo = 0, hi = t.tiles;                           // up_to(lo) <= in < up_to(hi)
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (t.up_to(mid) <= in) lo = mid; else hi = mid;
+        }
+        c.tile = lo;
+        const int nst = (tile_end(p, sg, lo) + kStage - 1) / kStage;
+        c.stage = min(nst, (int)((float)(in - t.up_to(lo)) / (float)t.of(lo) * (float)nst));
+        if (c.stage <= tol && 2 * c.stage <= nst) c.stage = 0;
+        else if (nst - c.stage <= tol) {                    // the next tile
+            c.stage = 0;
+            if (++c.tile == t.tiles) {
+                c.tile = 0;
+                if (++c.head == p.a.Hkv) { c.head = 0; ++c.seg; }      // (a segment without tiles is passed over)
+            }
+        }
+        return c;
+    }
+};
+// (the compiler does not see that all lanes agree)
+__device__ __forceinline__ Cut uniform(const Cut& c) {
+    return {__builtin_amdgcn_readfirstlane(c.seg), __builtin_amdgcn_readfirstlane(c.head), __builtin_amdgcn_readfirstlane(c.tile),
+            __builtin_amdgcn_readfirstlane(c.stage)};
 }
 
-template <int D, bool PAGED>
+// A workgroup per tile, where there are many: which one it has.  With heads in eighths every head stays on one XCD: the tiles of a
+// head run next to each other and read its keys at about the same time through that XCD's L2; the last heads of an XCD are taken
+// together, so that the launch does not end on the long tiles of a single one.  Else heads alternate.  Within a head: sequence by
+// sequence, the last tile first, whose rows see the most.
+template <bool PAGED>
+__device__ __forceinline__ Cut tile_of(const TileParams& p, int lane, int bid) {
+    int head, tt;
+    if (p.heads_per_xcd > 0) {
+        const int xcd = bid % kXcds, j = bid / kXcds, hx = p.heads_per_xcd, lead = hx - (int)p.by_tail.d, tiles = (int)p.by_tiles.d;
+        const bool front = j < lead * tiles;
+        const DivMod x = front ? uniform_div_mod(j, p.by_tiles) : uniform_div_mod(j - lead * tiles, p.by_tail);
+        head = xcd * hx + (front ? x.q : lead + x.r);
+        tt = front ? x.r : x.q;
+    } else {
+        const DivMod x = uniform_div_mod(bid, p.by_heads);
+        head = x.r; tt = x.q;
+    }
+    const DivMod lg = uniform_div_mod(head, p.by_hkv);
+    auto tiles = [&](int s) { return (int64_t)((segment<PAGED>(p, s * p.a.L + lg.q).rows + kTileRows - 1) / kTileRows); };
+    int64_t in;
+    const int s = find_segment(p.a.S, lane, tt, in, tiles);
+    if (s >= p.a.S) return {p.segs, 0, 0, 0};
+    return {s * p.a.L + lg.q, lg.r, (int)in, 0};
+}
+
+template <int D, bool PAGED, bool WHOLE>
 __global__ void __launch_bounds__(256, 2)
 attn_tiles_kernel(TileParams p) {
-    constexpr int ROWB = D * 2, CPR = D / 8, kInst = kStage * ROWB / 1024 / 4;    // copies per wavefront, stage and tensor: 16 rows
+    constexpr int ROWB = D * 2, kInst = CopyLane<D>::kCopies;               // copies per wavefront, stage and tensor: 16 rows
     __shared__ __attribute__((aligned(1024))) unsigned char sKa[kStage * ROWB];
     __shared__ __attribute__((aligned(1024))) unsigned char sVa[kStage * ROWB];
     __shared__ __attribute__((aligned(1024))) unsigned char sKb[kStage * ROWB];
     __shared__ __attribute__((aligned(1024))) unsigned char sVb[kStage * ROWB];
     const PackedParams& a = p.a;
     const int lane = threadIdx.x & (kWave - 1), wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const TileAt at = tile_at(p, (int)blockIdx.x);
-    Sequence sq;
-    int s, tile;
-    if (!find_tile(a, a.grp, at.tt, lane, sq, s, tile)) return;
-    const DivMod lh = uniform_div_mod(at.head, p.by_hkv);
-    const int l = lh.q, g = lh.r;
-    const TileKeys<PAGED> keys = tile_keys<PAGED>(p, sq, s, l, tile);
-    if (at.part >= keys.parts) return;
-    const int st0 = keys.nst * at.part / keys.parts, st1 = keys.nst * (at.part + 1) / keys.parts;
-
-    // this wavefront's rows
-    const int r0 = tile * kTileRows + wv * 32, ln = lane & 31, hf = lane >> 5, row = r0 + ln;
-    const bool mine = r0 < sq.rows, real = row < sq.rows;
-    const RowAt ra = row_at(real ? row : mine ? r0 : 0, p.grp);               // (rows that do not exist repeat one that does)
-    const int lim = keys.before + ra.token;                                   // the last key that the row sees
-    const int lim_first = keys.before + __builtin_amdgcn_readfirstlane(row_at(mine ? r0 : 0, p.grp).token);
-    const int lim_last = keys.before + __builtin_amdgcn_readfirstlane(row_at(min(sq.rows, r0 + 32) - 1, p.grp).token);
-    const int h = g * a.grp + ra.head;
-    const int64_t t = sq.first + ra.token;
-
-    // Keys and values of a stage: a wavefront copies 16 rows of each, which lie in one page.
-    const unsigned char *kb, *vb;
-    const int32_t* pages = nullptr;
-    if constexpr (PAGED) {
-        pages = a.table + ((int64_t)s * a.layers + a.l0 + l) * a.max_pages;
-        kb = a.k; vb = a.v;
+    const int ln = lane & 31, hf = lane >> 5;
+    int wg = 0;
+    Cut from, to;
+    if constexpr (WHOLE) {
+        from = to = uniform(tile_of<PAGED>(p, lane, (int)blockIdx.x));
     } else {
-        kb = a.k + a.ks.l * l + a.ks.h * g + a.ks.n * sq.first;
-        vb = a.v + a.vs.l * l + a.vs.h * g + a.vs.n * sq.first;
+        // neighbours in the order of the work run on one XCD and share keys through its L2
+        wg = (int)xcd_swizzle(blockIdx.x, (uint32_t)p.workgroups);
+        const Shares<PAGED> sh(p, lane);
+        from = uniform(sh.cut(wg));
+        to = uniform(sh.cut(wg + 1));
+        if (threadIdx.x == 0) p.cut[wg] = make_int4(from.seg, from.head, from.tile, from.stage);
     }
-    int cp_row[kInst], cp_col[kInst];
-#pragma unroll
-    for (int i = 0; i < kInst; ++i) {
-        const int idx = (wv * kInst + i) * 64 + lane, r = idx / CPR;
-        cp_row[i] = r;
-        cp_col[i] = 16 * ((idx % CPR) ^ swz<CPR>(r));
-    }
-    // Page ids ahead of their use: lane i has that of the i-th group of 16 keys from ids0 on, `next` the 64 groups behind them.
-    int ids = 0, next = 0, ids0 = st0 * 4;
-    unsigned long long bad_now = 0, bad_next = 0;
-    auto load_ids = [&](int group) {
-        const int key = min((group + lane) * 16, max(keys.end - 1, 0));
-        return keys.end > 0 ? pages[key >> a.shift] : 0;
-    };
-    auto check_ids = [&](int& x) {
-        const bool out = (uint32_t)x >= (uint32_t)a.num_pages;
-        if (out) x = 0;
-        return __builtin_amdgcn_ballot_w64(out);
-    };
-    if constexpr (PAGED) {
-        ids = load_ids(ids0);
-        next = load_ids(ids0 + kWave);
-        bad_now = check_ids(ids);
-        bad_next = check_ids(next);
-    }
-    auto bad_of = [&](int st) -> uint32_t {
-        if constexpr (!PAGED) return 0u;
-        const int x = st * 4 - ids0;      // a stage behind: its groups may have moved out at the front
-        return x < 0 ? 0u : (uint32_t)((bad_now >> x) & 15u);
-    };
-    auto issue = [&](int st, unsigned char* dK, unsigned char* dV) -> uint32_t {
-        uint32_t bad = 0;
+
+    const CopyLane<D> cp(lane);
+    RowTile<D> tl;
+    tl.offsets(lane);
+    int seg = from.seg, g = from.head, tile = from.tile, stage = from.stage;
+    while (seg < p.segs && seg <= to.seg) {                 // (`to` may be a segment without rows)
+        const Segment sg = uniform_segment<PAGED>(p, seg);
+        const int tiles = (sg.rows + kTileRows - 1) / kTileRows;
+        if (!WHOLE && tile >= tiles) { tile = 0; g = 0; ++seg; continue; }  // a segment without rows
+        if constexpr (WHOLE) tile = tiles - 1 - tile;
+        const bool last = !WHOLE && seg == to.seg && g == to.head && tile == to.tile;
+        if (last && to.stage == 0) break;
+        const int end = tile_end(p, sg, tile), nst = (end + kStage - 1) / kStage;
+        const int st0 = stage, st1 = last ? to.stage : nst;
+
+        // this wavefront's rows
+        const int r0 = tile * kTileRows + wv * 32, row = r0 + ln;
+        const bool mine = r0 < sg.rows, real = row < sg.rows;
+        const RowAt ra = row_at(real ? row : mine ? r0 : 0, p.grp);         // (rows that do not exist repeat one that does)
+        const int lim = sg.before + ra.token;                               // the last key that the row sees
+        const int lim_last = sg.before + __builtin_amdgcn_readfirstlane(row_at(max(min(sg.rows, r0 + 32) - 1, 0), p.grp).token);
+        const int h = g * a.grp + ra.head;
+        const int64_t t = sg.first + ra.token;
+
+        // Keys and values of a stage: a wavefront copies 16 rows of each, which lie in one page.
+        const unsigned char *kb = a.k, *vb = a.v;
+        const int32_t* pages = nullptr;
         if constexpr (PAGED) {
-            if (st * 4 >= ids0 + kWave) {
-                ids = next; bad_now = bad_next; ids0 += kWave;
-                next = load_ids(ids0 + kWave);
-                bad_next = check_ids(next);
-            }
-            bad = bad_of(st);
-            const int64_t id = __builtin_amdgcn_readlane(ids, st * 4 + wv - ids0);
-            const int64_t base = ((id * a.Hkv + g) << a.shift) * ROWB;
-#pragma unroll
-            for (int i = 0; i < kInst; ++i) {
-                const int key = min(st * kStage + cp_row[i], keys.end - 1);
-                const uint32_t off = (uint32_t)((key & ((1 << a.shift) - 1)) * ROWB + cp_col[i]);
-                copy_to_lds(kb + base + off, dK + (wv * kInst + i) * 1024);
-                copy_to_lds(vb + base + off, dV + (wv * kInst + i) * 1024);
-            }
+            pages = a.table + ((int64_t)sg.s * a.layers + a.l0 + sg.l) * a.max_pages;
         } else {
+            kb += a.ks.l * sg.l + a.ks.h * g + a.ks.n * sg.first;
+            vb += a.vs.l * sg.l + a.vs.h * g + a.vs.n * sg.first;
+        }
+        // Page ids ahead of their use: lane i has that of the i-th group of 16 keys from ids0 on, `next` the 64 groups behind them.
+        // Ids outside the pool are read as page 0; a tile that has one is worked on with masks throughout.
+        int ids = 0, next = 0, ids0 = st0 * 4;
+        unsigned long long bad_now = 0, bad_next = 0;
+        bool hidden = false;
+        auto load_ids = [&](int group) {
+            const int key = min((group + lane) * 16, max(end - 1, 0));
+            return end > 0 ? pages[key >> a.shift] : 0;
+        };
+        auto check_ids = [&](int& x) {
+            const bool out = (uint32_t)x >= (uint32_t)a.num_pages;
+            if (out) x = 0;
+            return __builtin_amdgcn_ballot_w64(out);
+        };
+        if constexpr (PAGED) {
+            ids = load_ids(ids0);
+            next = load_ids(ids0 + kWave);
+            const int to_page = (min(st1 * kStage, end) - 1) >> a.shift;
+            for (int i = ((st0 * kStage) >> a.shift) + lane; i <= to_page; i += kWave) hidden = hidden || (uint32_t)pages[i] >= (uint32_t)a.num_pages;
+            hidden = __builtin_amdgcn_ballot_w64(hidden) != 0;
+            bad_now = check_ids(ids);
+            bad_next = check_ids(next);
+        }
+        auto issue = [&](int st, unsigned char* dK, unsigned char* dV) -> uint32_t {
+            uint32_t bad = 0;
+            const int key = min(st * kStage + wv * 16, end - 1);            // the group's first key, or the last one there is
+            const uint32_t rest = (uint32_t)(end - 1 - key);
+            if constexpr (PAGED) {
+                if (st * 4 >= ids0 + kWave) {
+                    ids = next; bad_now = bad_next; ids0 += kWave;
+                    next = load_ids(ids0 + kWave);
+                    bad_next = check_ids(next);
+                }
+                bad = (uint32_t)((bad_now >> (st * 4 - ids0)) & 15u);
+                const int64_t id = __builtin_amdgcn_readlane(ids, st * 4 + wv - ids0);
+                const int64_t base = (((id * a.Hkv + g) << a.shift) + (key & ((1 << a.shift) - 1))) * ROWB;
 #pragma unroll
-            for (int i = 0; i < kInst; ++i) {
-                const int64_t key = min(st * kStage + cp_row[i], keys.end - 1);
-                copy_to_lds(kb + a.ks.n * key + cp_col[i], dK + (wv * kInst + i) * 1024);
-                copy_to_lds(vb + a.vs.n * key + cp_col[i], dV + (wv * kInst + i) * 1024);
+                for (int i = 0; i < kInst; ++i) {
+                    const uint32_t off = cp.at(i, rest, ROWB);
+                    copy_to_lds(kb + base + off, dK + (wv * kInst + i) * 1024);
+                    copy_to_lds(vb + base + off, dV + (wv * kInst + i) * 1024);
+                }
+            } else {
+                const unsigned char *ka = kb + a.ks.n * (int64_t)key, *va = vb + a.vs.n * (int64_t)key;
+#pragma unroll
+                for (int i = 0; i < kInst; ++i) {
+                    copy_to_lds(ka + cp.at(i, rest, (uint32_t)a.ks.n), dK + (wv * kInst + i) * 1024);
+                    copy_to_lds(va + cp.at(i, rest, (uint32_t)a.vs.n), dV + (wv * kInst + i) * 1024);
+                }
+            }
+            return bad;
+        };
+        uint32_t bad_a = 0, bad_b = 0;
+        const int seen = sg.before + __builtin_amdgcn_readfirstlane(row_at(tile * kTileRows, p.grp).token) + 1;
+        const int plain = hidden ? 0 : max(0, min(st1, seen / kStage) - st0);
+        if (st0 < st1) {
+            if (plain & 1) issue(st0, sKb, sVb);
+            else bad_a = issue(st0, sKa, sVa);
+        }
+
+        const float sc = a.scale[sg.l], qs = score_scale(sc);
+        tl.load_q(a.q + a.qs.l * sg.l + a.qs.h * h + a.qs.n * t, hf, sc < 0.f);
+        tl.clear();
+
+        auto sync = [&]() {
+            __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0): this wavefront's part of the stage has landed
+            __syncthreads();                                     // ... and everybody's; the other pair is free again
+        };
+        // Stages whose keys every row of the tile sees, two at a time, without a branch between them: a masked stage in the same
+        // loop made the compiler move the output between two sets of registers (four prompts of 8192 rows 3160 us, so 2870).  A
+        // wavefront without rows works along on rows that are not stored.
+        int st = st0;
+        if (plain & 1) {                                         // (the first stage of an odd number is in the other pair)
+            sync();
+            if (st + 1 < st1) bad_a = issue(st + 1, sKa, sVa);
+            tl.template attend<2, false>(sKb, sVb, qs, lane, 0, 0u, 2);
+            ++st;
+        }
+        for (; st < st0 + plain; st += 2) {
+            sync();
+            issue(st + 1, sKb, sVb);
+            tl.template attend<2, false>(sKa, sVa, qs, lane, 0, 0u, 2);
+            sync();
+            if (st + 2 < st1) bad_a = issue(st + 2, sKa, sVa);
+            tl.template attend<2, false>(sKb, sVb, qs, lane, 0, 0u, 2);
+        }
+        auto attend = [&](int st, const unsigned char* sK, const unsigned char* sV, uint32_t bad) {
+            const int key0 = st * kStage;
+            if (mine && key0 <= lim_last) tl.template attend<2, true>(sK, sV, qs, lane, lim - key0, bad, key0 + 32 <= lim_last ? 2 : 1);
+        };
+        for (; st < st1; st += 2) {
+            sync();
+            if (st + 1 < st1) bad_b = issue(st + 1, sKb, sVb);
+            attend(st, sKa, sVa, bad_a);
+            if (st + 1 >= st1) break;
+            sync();
+            if (st + 2 < st1) bad_a = issue(st + 2, sKa, sVa);
+            attend(st + 1, sKb, sVb, bad_b);
+        }
+        if (mine) {
+            const float sum = tl.total();
+            if (WHOLE || (st0 == 0 && st1 == nst)) {
+                tl.store(a.out + a.os.l * sg.l + a.os.h * h + a.os.n * t, hf, sum == 0.f ? 0.f : 1.f / sum, real);
+                if (!PAGED && real && hf == 0)
+                    a.lse[(int64_t)a.L * a.H * sg.first + (int64_t)(sg.l * a.H + h) * sg.n + ra.token] = kLn2 * (tl.m + __builtin_amdgcn_logf(sum));
+            } else {
+                // a workgroup has at most two parts of tiles that others share: of one that began before it, and of one that goes on
+                const int64_t slot = (int64_t)(2 * wg + (st0 > 0 ? 0 : 1)) * kTileRows + wv * 32 + ln;
+                if (real) tl.store_part(p.part_o + slot * D, p.part_ms + slot, hf, sum);
             }
         }
-        return bad;
-    };
-    uint32_t bad_a = 0, bad_b = 0;
-    if (st0 < st1) bad_a = issue(st0, sKa, sVa);
-
-    const float sc = a.scale[l], qs = score_scale(sc);
-    RowTile<D> tl;
-    tl.load_q(a.q + a.qs.l * l + a.qs.h * h + a.qs.n * t, hf, sc < 0.f);
-    tl.clear();
-    tl.offsets(lane);
-
-    auto sync = [&]() {
-        __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0): this wavefront's part of the stage has landed
-        __syncthreads();                                     // ... and everybody's; the other pair is free again
-    };
-    auto attend = [&](int st, const unsigned char* sK, const unsigned char* sV, uint32_t bad) {
-        const int key0 = st * kStage;
-        if (!mine) return;
-        if (key0 + kStage - 1 <= lim_first && bad == 0) tl.template attend<2, false>(sK, sV, qs, lane, 0, 0u, 2);
-        else if (key0 <= lim_last) tl.template attend<2, true>(sK, sV, qs, lane, lim - key0, bad, key0 + 32 <= lim_last ? 2 : 1);
-    };
-    for (int st = st0; st < st1; st += 2) {
-        sync();
-        if (st + 1 < st1) bad_b = issue(st + 1, sKb, sVb);
-        attend(st, sKa, sVa, bad_a);
-        if (st + 1 >= st1) break;
-        sync();
-        if (st + 2 < st1) bad_a = issue(st + 2, sKa, sVa);
-        attend(st + 1, sKb, sVb, bad_b);
+        if (WHOLE || last) break;
+        stage = 0;
+        if (++tile == tiles) {
+            tile = 0;
+            if (++g == a.Hkv) { g = 0; ++seg; }
+        }
+        __syncthreads();                                         // the buffers are free
     }
-    if (!mine) return;
-    const float all = tl.total();
-    if (keys.parts > 1) {
-        const int64_t slot = (((int64_t)at.head * p.tiles + at.tt) * p.parts + at.part) * kTileRows + wv * 32 + ln;
-        if (real) tl.store_part(p.part_o + slot * D, p.part_ms + slot, hf, all);
-        return;
-    }
-    tl.store(a.out + a.os.l * l + a.os.h * h + a.os.n * t, hf, all == 0.f ? 0.f : 1.f / all, real);
-    if (!PAGED && real && hf == 0)
-        a.lse[(int64_t)a.L * a.H * sq.first + (int64_t)(l * a.H + h) * sq.n + ra.token] = kLn2 * (tl.m + __builtin_amdgcn_logf(all));
 }
 
-// Joins the parts of a tile's rows: a wavefront takes 4 columns per lane of 256 / D rows at a time.
+// Joins the parts of the tiles that were cut: the first cut of a tile has all of its parts.  D / 4 lanes per row.
+constexpr int kMergeRows = 32;      // rows of a workgroup
 template <int D, bool PAGED>
 __global__ void __launch_bounds__(256)
 attn_merge_tiles_kernel(TileParams p) {
     constexpr int LPR = D / 4, RPB = 256 / LPR;
     const PackedParams& a = p.a;
-    const int lane = threadIdx.x & (kWave - 1);
-    const DivMod x = uniform_div_mod((int)blockIdx.x, p.by_heads);
-    Sequence sq;
-    int s, tile;
-    if (!find_tile(a, a.grp, x.q, lane, sq, s, tile)) return;
-    const DivMod lh = uniform_div_mod(x.r, p.by_hkv);
-    const TileKeys<PAGED> keys = tile_keys<PAGED>(p, sq, s, lh.q, tile);
-    if (keys.parts == 1) return;
-    const int in_tile = (int)blockIdx.y * RPB + threadIdx.x / LPR, row = tile * kTileRows + in_tile, c = 4 * (threadIdx.x % LPR);
-    if (row >= sq.rows) return;
-    const int64_t slot0 = ((int64_t)x.r * p.tiles + x.q) * p.parts * kTileRows + in_tile;
-    float m = -INFINITY;
-    for (int i = 0; i < keys.parts; ++i) m = fmaxf(m, p.part_ms[slot0 + i * kTileRows].x);
-    const float ref = m == -INFINITY ? 0.f : m;
-    float sum = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = 0; i < keys.parts; ++i) {
-        const int64_t slot = slot0 + i * kTileRows;
-        const float2 ms = p.part_ms[slot];
-        const float4 y = *(const float4*)(p.part_o + slot * D + c);
-        const float w = __builtin_amdgcn_exp2f(ms.x - ref);
-        sum = fmaf(w, ms.y, sum);
-        o.x = fmaf(w, y.x, o.x); o.y = fmaf(w, y.y, o.y); o.z = fmaf(w, y.z, o.z); o.w = fmaf(w, y.w, o.w);
+    const int w0 = (int)blockIdx.x + 1, lane = threadIdx.x & (kWave - 1);
+    // the cuts from the one before this on: those inside the same tile follow each other
+    int w1 = w0;
+    int4 c;
+    for (int base = w0 - 1;; base += kWave) {
+        const int4 x = p.cut[min(base + lane, p.workgroups - 1)];
+        if (base == w0 - 1) {
+            c = make_int4(__builtin_amdgcn_readlane(x.x, 1), __builtin_amdgcn_readlane(x.y, 1), __builtin_amdgcn_readlane(x.z, 1),
+                          __builtin_amdgcn_readlane(x.w, 1));
+            if (c.w == 0) return;
+        }
+        const bool same = base + lane < p.workgroups && x.w != 0 && x.x == c.x && x.y == c.y && x.z == c.z;
+        unsigned long long m = __builtin_amdgcn_ballot_w64(same);
+        if (base == w0 - 1) {
+            if (m & 1ull) return;                                // a later cut of its tile
+            m |= 1ull;
+        }
+        const int run = ~m == 0ull ? kWave : __builtin_ctzll(~m);
+        w1 = base + run - 1;
+        if (run < kWave) break;
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    const RowAt ra = row_at(row, p.grp);
-    const int h = lh.r * a.grp + ra.head;
-    *(uint2*)(a.out + a.os.l * lh.q + a.os.h * h + a.os.n * (int64_t)(sq.first + ra.token) + 2 * c) =
-        make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-    if (!PAGED && c == 0)
-        a.lse[(int64_t)a.L * a.H * sq.first + (int64_t)(lh.q * a.H + h) * sq.n + ra.token] = kLn2 * (m + __builtin_amdgcn_logf(sum));
+    const Segment sg = uniform_segment<PAGED>(p, c.x);
+    const int col = 4 * (threadIdx.x % LPR);
+    for (int in_tile = (int)blockIdx.y * kMergeRows + threadIdx.x / LPR; in_tile < ((int)blockIdx.y + 1) * kMergeRows; in_tile += RPB) {
+        const int row = c.z * kTileRows + in_tile;
+        if (row >= sg.rows) return;
+        float m = -INFINITY, sum = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int w = w0 - 1; w <= w1; ++w) {                     // a running maximum: every part is read once
+            const int64_t slot = (int64_t)(2 * w + (w < w0 ? 1 : 0)) * kTileRows + in_tile;
+            const float2 ms = p.part_ms[slot];
+            const float4 y = *(const float4*)(p.part_o + slot * D + col);
+            const float mx = fmaxf(m, ms.x), ref = mx == -INFINITY ? 0.f : mx;
+            const float c0 = __builtin_amdgcn_exp2f(m - ref), c1 = __builtin_amdgcn_exp2f(ms.x - ref);
+            sum = fmaf(sum, c0, ms.y * c1);
+            o.x = fmaf(o.x, c0, y.x * c1); o.y = fmaf(o.y, c0, y.y * c1); o.z = fmaf(o.z, c0, y.z * c1); o.w = fmaf(o.w, c0, y.w * c1);
+            m = mx;
+        }
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const RowAt ra = row_at(row, p.grp);
+        const int h = c.y * a.grp + ra.head;
+        *(uint2*)(a.out + a.os.l * sg.l + a.os.h * h + a.os.n * (int64_t)(sg.first + ra.token) + 2 * col) =
+            make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+        if (!PAGED && col == 0)
+            a.lse[(int64_t)a.L * a.H * sg.first + (int64_t)(sg.l * a.H + h) * sg.n + ra.token] = kLn2 * (m + __builtin_amdgcn_logf(sum));
+    }
 }
 
 // ---- few rows: the keys of a launch shared out evenly over the wavefronts ---------------------------------
-struct StreamParams {
-    PackedParams a;
-    FastDiv grp, by_layers;         // by_layers: layers of the call
-    int segs, waves;                // S * L
+struct StreamParams : Work {
+    int waves;
     int* share;                     // workspace: blocks of a wavefront
     int* start;                     // [segs]: first block of a segment (segments that have blocks)
     float* part_o;                  // [2 * waves][32][D]
@@ -645,35 +871,12 @@ struct StreamParams {
 };
 constexpr int kLeastBlocks = 2;     // of a wavefront
 
-struct Segment { int s, l, first, n, rows, len, end, blocks; };   // rows: of this call, times the heads; end: keys that some row sees
-
-__device__ __forceinline__ Segment segment(const StreamParams& p, int i) {
-    Segment x;
-    const DivMod sl = div_mod(i, p.by_layers);
-    x.s = sl.q; x.l = sl.r;
-    const int last = p.a.row_off[x.s + 1];
-    x.first = p.a.row_off[x.s];
-    x.n = x.first >= 0 && last <= p.a.T ? max(0, last - x.first) : 0;
-    x.len = entries(p.a, x.s, x.l);
-    const int rows = min(x.n, p.a.max_rows);
-    x.rows = rows * p.a.grp;
-    x.end = x.n > 0 ? max(0, min(x.len, x.len - x.n + rows)) : 0;
-    x.blocks = (x.end + kBlockKeys - 1) / kBlockKeys;
-    return x;
-}
-__device__ __forceinline__ Segment uniform_segment(const StreamParams& p, int i) {
-    Segment x = segment(p, i);
-    x.s = __builtin_amdgcn_readfirstlane(x.s); x.l = __builtin_amdgcn_readfirstlane(x.l);
-    x.first = __builtin_amdgcn_readfirstlane(x.first); x.n = __builtin_amdgcn_readfirstlane(x.n);
-    x.rows = __builtin_amdgcn_readfirstlane(x.rows); x.len = __builtin_amdgcn_readfirstlane(x.len);
-    x.end = __builtin_amdgcn_readfirstlane(x.end); x.blocks = __builtin_amdgcn_readfirstlane(x.blocks);
-    return x;
-}
+__device__ __forceinline__ int blocks_of(const Segment& x) { return (x.end + kBlockKeys - 1) / kBlockKeys; }
 
 template <int D>
 __global__ void __launch_bounds__(128, 128 / D)
 attn_stream_kernel(StreamParams p) {
-    constexpr int ROWB = D * 2, CPR = D / 8, kBytes = kBlockKeys * ROWB, kInst = 16 * ROWB / 1024;   // copies per 16 keys and tensor
+    constexpr int ROWB = D * 2, kBytes = kBlockKeys * ROWB, kInst = CopyLane<D>::kCopies;            // copies per 16 keys and tensor
     __shared__ __attribute__((aligned(1024))) unsigned char sKa[2][kBytes];
     __shared__ __attribute__((aligned(1024))) unsigned char sVa[2][kBytes];
     __shared__ __attribute__((aligned(1024))) unsigned char sKb[2][kBytes];
@@ -683,55 +886,32 @@ attn_stream_kernel(StreamParams p) {
     const int wave = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 2 + wv), ln = lane & 31, hf = lane >> 5;
 
     // the launch's blocks, and this wavefront's: segment by segment, KV head by KV head
-    int sum = 0;
-    for (int i = lane; i < p.segs; i += kWave) sum += segment(p, i).blocks;
-    const int all_blocks = __builtin_amdgcn_readfirstlane(wave_sum(sum)) * a.Hkv;
+    auto blocks = [&](int i) { return (int64_t)blocks_of(segment<true>(p, i)) * a.Hkv; };
+    const int all_blocks = (int)all_segments(p.segs, lane, blocks);        // (below 2^31: the call is refused otherwise)
     const int share = max(kLeastBlocks, (all_blocks + p.waves - 1) / p.waves);
     if (wave == 0 && lane == 0) *p.share = share;
     const int b0 = (int)min((int64_t)wave * share, (int64_t)all_blocks), b1 = (int)min((int64_t)b0 + share, (int64_t)all_blocks);
     if (b0 >= b1) return;
-    int seg = 0, before = 0;                                   // segment of block b0, blocks in front of it
-    for (int c = 0; c < p.segs; c += kWave) {
-        const int mine = c + lane < p.segs ? segment(p, c + lane).blocks : 0;
-        int incl = mine;
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) {
-            const int up = __shfl_up(incl, d, kWave);
-            if (lane >= d) incl += up;
-        }
-        const unsigned long long at = __builtin_amdgcn_ballot_w64((before + incl) * a.Hkv > b0);
-        if (at != 0) {
-            const int j = __builtin_ctzll(at);
-            seg = c + j;
-            before += __builtin_amdgcn_readlane(incl, j) - __builtin_amdgcn_readlane(mine, j);
-            break;
-        }
-        before += __builtin_amdgcn_readlane(incl, kWave - 1);
-    }
+    int64_t in_seg;
+    const int seg = find_segment(p.segs, lane, b0, in_seg, blocks);
 
     // where copies are asked for (`in`), and where the work is (`sg`): both walk the same blocks
     struct Cursor { int seg, g, blk; };
-    Segment sg = uniform_segment(p, seg), in = sg;
-    Cursor cw = {seg, 0, b0 - before * a.Hkv};
-    cw.g = cw.blk / sg.blocks;
-    cw.blk -= cw.g * sg.blocks;
-    int seg_start = before * a.Hkv;                             // first block of the segment worked on
+    Segment sg = uniform_segment<true>(p, seg), in = sg;
+    Cursor cw = {seg, 0, (int)in_seg};
+    cw.g = cw.blk / blocks_of(sg);
+    cw.blk -= cw.g * blocks_of(sg);
+    int seg_start = b0 - (int)in_seg;                           // first block of the segment worked on
     Cursor ci = cw;
     auto step = [&](Cursor& c, Segment& x) -> bool {            // true: another segment
-        if (++c.blk < x.blocks) return false;
+        if (++c.blk < blocks_of(x)) return false;
         c.blk = 0;
         if (++c.g < a.Hkv) return false;
         c.g = 0;
-        do { ++c.seg; x = uniform_segment(p, c.seg); } while (x.blocks == 0);    // (a block is left, so a segment is)
+        do { ++c.seg; x = uniform_segment<true>(p, c.seg); } while (x.end == 0);    // (a block is left, so a segment is)
         return true;
     };
-    int cp_row[kInst], cp_col[kInst];                           // of 16 keys
-#pragma unroll
-    for (int i = 0; i < kInst; ++i) {
-        const int idx = i * 64 + lane, r = idx / CPR;
-        cp_row[i] = r;
-        cp_col[i] = idx % CPR;
-    }
+    const CopyLane<D> cp(lane);
     // lane i has the page of the i-th group of 16 keys from ids0 on
     int ids = 0, ids0 = 0;
     unsigned long long bad_ids = 0;
@@ -749,12 +929,12 @@ attn_stream_kernel(StreamParams p) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             const int64_t id = __builtin_amdgcn_readlane(ids, 2 * ci.blk + x - ids0);
-            const int64_t base = ((id * a.Hkv + ci.g) << a.shift) * ROWB;
+            const int key = min(ci.blk * kBlockKeys + 16 * x, in.end - 1);
+            const int64_t base = (((id * a.Hkv + ci.g) << a.shift) + (key & ((1 << a.shift) - 1))) * ROWB;
+            const uint32_t last = (uint32_t)(in.end - 1 - key);
 #pragma unroll
             for (int i = 0; i < kInst; ++i) {
-                const int r = 16 * x + cp_row[i];
-                const int key = min(ci.blk * kBlockKeys + r, in.end - 1);
-                const uint32_t off = (uint32_t)((key & ((1 << a.shift) - 1)) * ROWB + 16 * (cp_col[i] ^ swz<CPR>(r)));
+                const uint32_t off = cp.at(i, last, ROWB);
                 copy_to_lds(a.k + base + off, dK + (x * kInst + i) * 1024);
                 copy_to_lds(a.v + base + off, dV + (x * kInst + i) * 1024);
             }
@@ -785,7 +965,7 @@ attn_stream_kernel(StreamParams p) {
         qs = score_scale(sc);
         tl.load_q(a.q + a.qs.l * sg.l + a.qs.h * h + a.qs.n * t, hf, sc < 0.f);
         out = a.out + a.os.l * sg.l + a.os.h * h + a.os.n * t;
-        lim = sg.len - sg.n + ra.token;
+        lim = sg.before + ra.token;
         tl.clear();
         piece = cw.blk;
         if (cw.g == 0 && cw.blk == 0 && lane == 0) p.start[cw.seg] = seg_start;
@@ -800,17 +980,17 @@ attn_stream_kernel(StreamParams p) {
     };
     auto attend = [&](const unsigned char* sK, const unsigned char* sV, uint32_t bad) {
         const int key0 = cw.blk * kBlockKeys;
-        if (key0 + kBlockKeys - 1 <= sg.len - sg.n && bad == 0) tl.template attend<1, false>(sK, sV, qs, lane, 0, 0u, 1);
+        if (key0 + kBlockKeys - 1 <= sg.before && bad == 0) tl.template attend<1, false>(sK, sV, qs, lane, 0, 0u, 1);
         else tl.template attend<1, true>(sK, sV, qs, lane, lim - key0, bad, 1);
     };
     // one block of the work: `more` blocks are in flight behind it
     auto work = [&](int b, const unsigned char* sK, const unsigned char* sV, uint32_t bad) {
         attend(sK, sV, bad);
-        const bool whole = cw.blk + 1 == sg.blocks;
+        const bool whole = cw.blk + 1 == blocks_of(sg);
         if (whole || b + 1 == b1) {
             end(whole);
             if (b + 1 < b1) {
-                const int old = sg.blocks;
+                const int old = blocks_of(sg);
                 if (step(cw, sg)) seg_start += old * a.Hkv;
                 begin();
             }
@@ -854,16 +1034,16 @@ attn_merge_stream_kernel(StreamParams p) {
     __shared__ float4 s_o[PG][LPP];
     const PackedParams& a = p.a;
     const int i = (int)blockIdx.x / a.Hkv, g = (int)blockIdx.x % a.Hkv, row = (int)blockIdx.y;
-    const Segment x = uniform_segment(p, i);
+    const Segment x = uniform_segment<true>(p, i);
     if (row >= x.rows) return;
     const RowAt ra = row_at(row, p.grp);
     const int c = threadIdx.x % LPP, pg = threadIdx.x / LPP, h = g * a.grp + ra.head;
     unsigned char* out = a.out + a.os.l * x.l + a.os.h * h + a.os.n * (int64_t)(x.first + ra.token) + 8 * c;
-    if (x.blocks == 0) {
+    if (x.end == 0) {
         if (pg == 0) *(uint2*)out = make_uint2(0u, 0u);
         return;
     }
-    const int share = *p.share, u0 = p.start[i] + g * x.blocks, w0 = u0 / share, w1 = (u0 + x.blocks - 1) / share;
+    const int share = *p.share, u0 = p.start[i] + g * blocks_of(x), w0 = u0 / share, w1 = (u0 + blocks_of(x) - 1) / share;
     if (w0 == w1) return;                                       // one wavefront has written it
     float m = -INFINITY, sum = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -901,70 +1081,81 @@ attn_merge_stream_kernel(StreamParams p) {
 
 // ---- launches ------------------------------------------------------------------------------------------
 constexpr int kStreamWorkgroups = 2;          // of a compute unit: 64 KB of LDS each at D = 128
-constexpr int kTileSlots = 2;                 // workgroups of attn_tiles_kernel that a compute unit holds
+constexpr int kTileWorkgroups = 2;            // of attn_tiles_kernel: 256 registers
+
 constexpr int kTailTiles = 256;               // workgroups of an XCD at the end of a launch whose heads are taken together
 
 static bool few_rows(const pkv_packed& s, int max_rows) { return max_rows > 0 && (int64_t)max_rows * (s.H / s.Hkv) <= kFewRows; }
 static int stream_waves(const pkv_packed& s) { return compute_units() * kStreamWorkgroups * 2 * (128 / s.D); }
+static int tile_workgroups() { return compute_units() * kTileWorkgroups / kXcds * kXcds; }
+static size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
-// tiles of all sequences at most, and the parts that a tile's keys are split into so that the launch fills the chip once
-struct TileCount { long long tiles, heads; int parts; };
-static TileCount tile_count(const pkv_packed& s) {
-    TileCount c;
-    const long long grp = s.H / s.Hkv;
-    c.heads = (long long)s.L * s.Hkv;
-    c.tiles = ((long long)s.T * grp) / kTileRows + (s.S < s.T ? s.S : s.T);
-    const long long slots = (long long)compute_units() * kTileSlots, items = c.tiles * c.heads;
-    c.parts = (int)(items >= slots ? 1 : slots / items < 16 ? slots / items : 16);
-    return c;
+// tiles of all sequences of a KV head at most
+static long long most_tiles(const pkv_packed& s) { return (long long)s.T * (s.H / s.Hkv) / kTileRows + (s.S < s.T ? s.S : s.T); }
+// Whether tiles are cut.  A launch of a workgroup per tile takes as long as its longest tile (1.33 us a stage with a compute unit of
+// its own) or as the whole work shared out (2.1 us a stage on each of the workgroups), whichever is longer; cutting brings the first down
+// to the second and costs about 30 us (parts, joining them, shares, a phase of its own for every workgroup).  The longest tile and the
+// average are taken from the most that can be: the rows of a prompt, the width of a table row, of which a cache holds three quarters.
+// us, whole / cut: H32/8, 512 rows over 8192 keys 192 / 112, 4 x 128 rows 179 / 101, 16 x 40 over 2000 56 / 60; H32, 8 x 64 over 1000
+// 35 / 50, 64 over 4000 88 / 44; prompts: H32 680 22 / 41, 2048 63 / 83, H8 2048 53 / 47, H12/4 6000 156 / 174.
+static bool cut_tiles(const pkv_packed& s, long long keys, bool paged) {
+    const double stages = (double)((keys + kStage - 1) / kStage), tiles = (double)most_tiles(s) * s.L * s.Hkv;
+    return stages * (1.33 - (paged ? 0.75 : 0.5) * 2.1 * tiles / tile_workgroups()) > 30.0;
 }
 
-// grids and block numbers are 32 bits wide
+// block numbers are 32 bits wide, and so are grids
 bool packed_attn_fits(const pkv_packed& s, const pkv_paging* g) {
-    const TileCount c = tile_count(s);
-    if (c.tiles * c.heads * c.parts > 0x7fffffffll) return false;
+    if ((int64_t)s.S * s.L * s.Hkv > 0x7fffffffll || most_tiles(s) * s.L * s.Hkv > 0x7fffffffll) return false;
     return !g || (double)s.S * s.L * s.Hkv * g->max_pages * g->page_size / kBlockKeys < 2147483648.0;
 }
 
 size_t packed_attn_ws_bytes(const pkv_packed& s, int max_rows) {
     if (s.dtype != PKV_BF16) return 0;
-    if (few_rows(s, max_rows)) {
-        const size_t slots = (size_t)2 * stream_waves(s) * kFewRows;
-        return 256 + ((size_t)s.S * s.L * 4 + 255) / 256 * 256 + slots * (sizeof(float2) + s.D * sizeof(float));
-    }
-    const TileCount c = tile_count(s);
-    return c.parts == 1 ? 0 : (size_t)(c.tiles * c.heads * c.parts) * kTileRows * (sizeof(float2) + s.D * sizeof(float));
+    const size_t row = sizeof(float2) + s.D * sizeof(float);
+    if (few_rows(s, max_rows)) return 256 + up256((size_t)s.S * s.L * 4) + (size_t)2 * stream_waves(s) * kFewRows * row;
+    // (whether tiles are cut goes by the table's width too, which the size does not ask for: where the widest would not be, none is)
+    if (!cut_tiles(s, max_rows > 0 ? kMaxSegmentSlots : s.T, max_rows > 0)) return 0;
+    return up256(tile_workgroups() * sizeof(int4)) + (size_t)2 * tile_workgroups() * kTileRows * row;
+}
+
+static Work work_of(const pkv_packed& s, const PackedParams& a) {
+    Work w;
+    w.a = a;
+    w.grp = fast_div(a.grp); w.by_layers = fast_div(s.L);
+    w.segs = s.S * s.L;
+    return w;
 }
 
 template <int D, bool PAGED>
 static hipError_t launch_tiles(const pkv_packed& s, const PackedParams& a, void* ws, hipStream_t st) {
-    const TileCount c = tile_count(s);
-    const long long items = c.tiles * c.heads;
     TileParams p;
-    p.a = a;
-    p.heads = (int)c.heads; p.tiles = (int)c.tiles; p.parts = c.parts;
-    p.heads_per_xcd = c.heads % kXcds == 0 ? (int)(c.heads / kXcds) : 0;
-    const long long tail = (kTailTiles + c.tiles - 1) / c.tiles;
-    p.grp = fast_div(a.grp); p.by_heads = fast_div(c.heads); p.by_hkv = fast_div(s.Hkv); p.by_tiles = fast_div(c.tiles);
-    p.by_tail = fast_div(p.heads_per_xcd > 0 && tail < p.heads_per_xcd ? tail : p.heads_per_xcd > 0 ? p.heads_per_xcd : 1);
-    p.by_parts = fast_div(c.parts);
-    p.part_o = (float*)ws;
-    p.part_ms = (float2*)(p.part_o + (size_t)(items * c.parts) * kTileRows * D);
-    hipLaunchKernelGGL((attn_tiles_kernel<D, PAGED>), dim3((unsigned)(items * c.parts)), dim3(256), 0, st, p);
-    if (c.parts > 1)
-        hipLaunchKernelGGL((attn_merge_tiles_kernel<D, PAGED>), dim3((unsigned)items, kTileRows * (D / 4) / 256), dim3(256), 0, st, p);
+    (Work&)p = work_of(s, a);
+    const long long tiles = most_tiles(s), heads = (long long)s.L * s.Hkv;
+    p.by_hkv = fast_div(s.Hkv); p.by_heads = fast_div(heads); p.by_tiles = fast_div(tiles);
+    p.heads_per_xcd = heads % kXcds == 0 ? (int)(heads / kXcds) : 0;
+    const long long tail = (kTailTiles + tiles - 1) / tiles;
+    p.by_tail = fast_div(tail < p.heads_per_xcd ? tail : p.heads_per_xcd > 0 ? p.heads_per_xcd : 1);
+    p.cut = (int4*)ws;
+    p.workgroups = tile_workgroups();
+    p.part_o = (float*)((char*)ws + up256(p.workgroups * sizeof(int4)));
+    p.part_ms = (float2*)(p.part_o + (size_t)2 * p.workgroups * kTileRows * D);
+    if (!cut_tiles(s, PAGED ? (long long)a.max_pages << a.shift : s.T, PAGED)) {
+        hipLaunchKernelGGL((attn_tiles_kernel<D, PAGED, true>), dim3((unsigned)(tiles * heads)), dim3(256), 0, st, p);
+    } else {
+        hipLaunchKernelGGL((attn_tiles_kernel<D, PAGED, false>), dim3((unsigned)p.workgroups), dim3(256), 0, st, p);
+        hipLaunchKernelGGL((attn_merge_tiles_kernel<D, PAGED>), dim3((unsigned)p.workgroups - 1, kTileRows / kMergeRows), dim3(256), 0, st, p);
+    }
     return hipGetLastError();
 }
 
 template <int D>
 static hipError_t launch_stream(const pkv_packed& s, const PackedParams& a, void* ws, hipStream_t st) {
     StreamParams p;
-    p.a = a;
-    p.grp = fast_div(a.grp); p.by_layers = fast_div(s.L);
-    p.segs = s.S * s.L; p.waves = stream_waves(s);
+    (Work&)p = work_of(s, a);
+    p.waves = stream_waves(s);
     p.share = (int*)ws;
     p.start = (int*)((char*)ws + 256);
-    p.part_o = (float*)((char*)ws + 256 + ((size_t)p.segs * 4 + 255) / 256 * 256);
+    p.part_o = (float*)((char*)ws + 256 + up256((size_t)p.segs * 4));
     p.part_ms = (float2*)(p.part_o + (size_t)2 * p.waves * kFewRows * D);
     hipLaunchKernelGGL(attn_stream_kernel<D>, dim3((unsigned)(p.waves / 2)), dim3(128), 0, st, p);
     hipLaunchKernelGGL(attn_merge_stream_kernel<D>, dim3((unsigned)(p.segs * s.Hkv), (unsigned)(a.max_rows * a.grp)), dim3(256), 0, st, p);
