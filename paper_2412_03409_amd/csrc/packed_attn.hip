@@ -10,8 +10,10 @@
 //                     LDS of its own.  All keys of a launch are one sequence of blocks that the wavefronts share out evenly,
 //                     wherever the units begin and end.  Bound: HBM.
 //  attn_merge_*       join the parts of a tile or unit that several workgroups or wavefronts worked on.
-//  attn_rows_kernel   fp32: a wavefront per (row, head, layer).  The keys stream past one row: LPR lanes hold a key
-//                     row, scores meet by shuffles, softmax online (running maximum and sum, everything fp32).
+//  attn_rows_kernel   fp32: a workgroup per (row, head, layer).  The keys stream past one row: LPR lanes hold a key
+//                     row, scores meet by shuffles, softmax online (running maximum and sum, everything fp32); the four
+//                     wavefronts take every fourth group of keys and join through LDS.  Bound: latency at the sizes of the fp32
+//                     validation shape.
 //
 // The two bf16 kernels work as the prompt attention of rectangular batches does: S^T[32 keys x 32 rows] = K Q^T and
 // O^T[32 columns x 32 rows] += V^T P^T with v_mfma_f32_32x32x16_bf16.  A lane holds one row's scores, so the softmax state is a
@@ -54,8 +56,7 @@ __global__ void __launch_bounds__(256)
 attn_rows_kernel(PackedParams p) {
     constexpr int LPR = D / 4, RG = kWave / LPR, U = 4, kRow = D * 4;
     const int lane = threadIdx.x & (kWave - 1), wv = threadIdx.x / kWave, sub = lane % LPR, rg = lane / LPR;
-    const int t = blockIdx.x, h = blockIdx.y * 4 + wv, l = blockIdx.z;
-    if (h >= p.H) return;
+    const int t = blockIdx.x, h = blockIdx.y, l = blockIdx.z;
     // the sequence of row t: how many end at t or before it
     int s = 0;
     for (int i = lane; i < p.S; i += kWave) s += p.row_off[i + 1] <= t;
@@ -71,7 +72,7 @@ attn_rows_kernel(PackedParams p) {
     float m = -INFINITY, sum = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     auto weigh = [](float4& x, float c) { x.x *= c; x.y *= c; x.z *= c; x.w *= c; };
-    for (int j0 = 0; j0 < count; j0 += RG * U) {
+    for (int j0 = wv * RG * U; j0 < count; j0 += 4 * RG * U) {
         float4 kr[U], vr[U];
         bool real[U];
 #pragma unroll
@@ -119,7 +120,26 @@ attn_rows_kernel(PackedParams p) {
         o.x += __shfl_xor(o.x, x, kWave); o.y += __shfl_xor(o.y, x, kWave);
         o.z += __shfl_xor(o.z, x, kWave); o.w += __shfl_xor(o.w, x, kWave);
     }
-    if (rg != 0) return;
+    __shared__ float2 s_ms[4];
+    __shared__ float4 s_o[4][LPR];
+    if (lane == 0) s_ms[wv] = make_float2(all, sum);
+    if (rg == 0) s_o[wv][sub] = o;
+    __syncthreads();
+    if (wv != 0 || rg != 0) return;
+    float top = all;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) top = fmaxf(top, s_ms[w].x);
+    const float base = top == -INFINITY ? 0.f : top, mine = __builtin_amdgcn_exp2f(all - base);
+    sum *= mine;
+    weigh(o, mine);
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+        const float2 ms = s_ms[w];
+        const float4 y = s_o[w][sub];
+        const float c = __builtin_amdgcn_exp2f(ms.x - base);
+        sum = fmaf(ms.y, c, sum);
+        o.x = fmaf(y.x, c, o.x); o.y = fmaf(y.y, c, o.y); o.z = fmaf(y.z, c, o.z); o.w = fmaf(y.w, c, o.w);
+    }
     weigh(o, sum == 0.f ? 0.f : 1.f / sum);                     // nothing seen: zeros
     *(float4*)(p.out + p.os.l * l + p.os.h * h + p.os.n * t + sub * 16) = o;
 }
@@ -467,17 +487,44 @@ __device__ __forceinline__ int find_segment(int segs, int lane, int64_t x, int64
     in = 0;
     return segs;
 }
-template <class F>
-__device__ __forceinline__ int64_t all_segments(int segs, int lane, F cost) {
-    int64_t sum = 0;
-    for (int i = lane; i < segs; i += kWave) sum += cost(i);
+
+// All segments and their places.  Up to 64 of them (a layer of 64 sequences) are read once, a lane each; beyond, they are read again
+// where they are asked for.
+template <bool PAGED, class F>
+struct Looked {
+    const Work& p;
+    int lane;
+    F cost;                         // places of a segment
+    Segment mine;                   // segment `lane`
+    int64_t upto, all;              // places of the segments up to `lane`; of all
+
+    __device__ __forceinline__ Looked(const Work& work, int ln, F f) : p(work), lane(ln), cost(f) {
+        mine = segment<PAGED>(p, min(lane, p.segs - 1));
+        upto = lane < p.segs ? cost(mine) : 0;
+        for (int i = lane + kWave; i < p.segs; i += kWave) upto += cost(segment<PAGED>(p, i));
 #pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        const int64_t up = shfl_up64(sum, d);
-        if (lane >= d) sum += up;
+        for (int d = 1; d < kWave; d <<= 1) {
+            const int64_t up = shfl_up64(upto, d);
+            if (lane >= d) upto += up;
+        }
+        all = lane64(upto, kWave - 1);
     }
-    return lane64(sum, kWave - 1);
-}
+    // the segment that holds place x, the place in it, and what the segment is
+    __device__ __forceinline__ int find(int64_t x, int64_t& in, Segment& sg) const {
+        if (p.segs <= kWave) {
+            const int j = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > x));
+            in = x - (j == 0 ? 0 : lane64(upto, j - 1));
+            sg.s = __builtin_amdgcn_readlane(mine.s, j); sg.l = __builtin_amdgcn_readlane(mine.l, j);
+            sg.first = __builtin_amdgcn_readlane(mine.first, j); sg.n = __builtin_amdgcn_readlane(mine.n, j);
+            sg.rows = __builtin_amdgcn_readlane(mine.rows, j); sg.len = __builtin_amdgcn_readlane(mine.len, j);
+            sg.before = __builtin_amdgcn_readlane(mine.before, j); sg.end = __builtin_amdgcn_readlane(mine.end, j);
+            return j;
+        }
+        const int j = find_segment(p.segs, lane, x, in, [&](int i) { return cost(segment<PAGED>(p, i)); });
+        sg = uniform_segment<PAGED>(p, j);
+        return j;
+    }
+};
 
 // ---- many rows -----------------------------------------------------------------------------------------
 struct TileParams : Work {
@@ -513,66 +560,30 @@ __device__ __forceinline__ int tile_end(const Work& p, const Segment& x, int i) 
 
 struct Cut { int seg, head, tile, stage; };
 
-// What the workgroups share out.  Up to 64 segments (a layer of 64 sequences) are looked at once, a lane each; beyond, they are read
-// again where they are needed.
-template <bool PAGED>
+// What the workgroups share out.
+template <bool PAGED, class L>
 struct Shares {
     const TileParams& p;
-    int lane;
-    Segment mine;                   // segment `lane`
-    int64_t upto, all, share;       // places of the segments up to `lane`; of all; of a workgroup
-    int tol;                        // stages
+    const L& segs;
+    int64_t share;                  // places of a workgroup
 
-    __device__ __forceinline__ int64_t cost(const Segment& x) const {
-        const TileCost<PAGED> t(p, x);
-        return t.up_to(t.tiles) * p.a.Hkv;
-    }
-    __device__ __forceinline__ Shares(const TileParams& params, int ln) : p(params), lane(ln) {
-        mine = segment<PAGED>(p, min(lane, p.segs - 1));
-        int longest = mine.end;
-        if (p.segs <= kWave) {
-            upto = lane < p.segs ? cost(mine) : 0;
-#pragma unroll
-            for (int d = 1; d < kWave; d <<= 1) {
-                const int64_t up = shfl_up64(upto, d);
-                if (lane >= d) upto += up;
-            }
-            all = lane64(upto, kWave - 1);
-        } else {
-            all = all_segments(p.segs, lane, [&](int i) { return cost(segment<PAGED>(p, i)); });
-            for (int i = lane + kWave; i < p.segs; i += kWave) longest = max(longest, segment<PAGED>(p, i).end);
-        }
+    __device__ __forceinline__ Shares(const TileParams& params, const L& looked) : p(params), segs(looked) {
+        int longest = segs.mine.end;
+        for (int i = segs.lane + kWave; i < p.segs; i += kWave) longest = max(longest, segment<PAGED>(p, i).end);
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) longest = max(longest, __shfl_xor(longest, d, kWave));
-        // A cut costs what kJoinStages stages do.  Where the tiles are short none is made closer to an end of a tile, and where a
-        // launch is small a long tile is cut into pieces that are no shorter.
-        const int64_t stage = (int64_t)kStage * p.a.grp;
+        // where a launch is small a long tile is cut into pieces of eight stages at least
         const int least = min(8, __builtin_amdgcn_readfirstlane(longest) / (2 * kStage) + 1);
-        share = max((int64_t)least * stage, (int64_t)((double)all / (double)p.workgroups) + 1);
-        tol = kJoinStages;
-    }
-    __device__ __forceinline__ int find(int64_t x, int64_t& in, Segment& sg) const {
-        if (p.segs <= kWave) {
-            const int j = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > x));
-            in = x - (j == 0 ? 0 : lane64(upto, j - 1));
-            sg.s = __builtin_amdgcn_readlane(mine.s, j); sg.l = __builtin_amdgcn_readlane(mine.l, j);
-            sg.first = __builtin_amdgcn_readlane(mine.first, j); sg.n = __builtin_amdgcn_readlane(mine.n, j);
-            sg.rows = __builtin_amdgcn_readlane(mine.rows, j); sg.len = __builtin_amdgcn_readlane(mine.len, j);
-            sg.before = __builtin_amdgcn_readlane(mine.before, j); sg.end = __builtin_amdgcn_readlane(mine.end, j);
-            return j;
-        }
-        const int j = find_segment(p.segs, lane, x, in, [&](int i) { return cost(segment<PAGED>(p, i)); });
-        sg = uniform_segment<PAGED>(p, j);
-        return j;
+        share = max((int64_t)least * kStage * p.a.grp, (int64_t)((double)segs.all / (double)p.workgroups) + 1);
     }
     // Where workgroup w begins.  A cut close to an end of a tile moves there.
     __device__ __forceinline__ Cut cut(int w) const {
         const int64_t x = w * share;
-        if (x >= all) return {p.segs, 0, 0, 0};
+        if (x >= segs.all) return {p.segs, 0, 0, 0};
         int64_t in;
         Cut c;
         Segment sg;
-        c.seg = find(x, in, sg);
+        c.seg = segs.find(x, in, sg);
         const TileCost<PAGED> t(p, sg);
         const int64_t head = t.up_to(t.tiles);
         c.head = min(p.a.Hkv - 1, (int)((double)in / (double)head));       // (a quotient that is rounded up is corrected)
@@ -586,8 +597,8 @@ struct Shares {
         c.tile = lo;
         const int nst = (tile_end(p, sg, lo) + kStage - 1) / kStage;
         c.stage = min(nst, (int)((float)(in - t.up_to(lo)) / (float)t.of(lo) * (float)nst));
-        if (c.stage <= tol && 2 * c.stage <= nst) c.stage = 0;
-        else if (nst - c.stage <= tol) {                    // the next tile
+        if (c.stage <= kJoinStages && 2 * c.stage <= nst) c.stage = 0;
+        else if (nst - c.stage <= kJoinStages) {                    // the next tile
             c.stage = 0;
             if (++c.tile == t.tiles) {
                 c.tile = 0;
@@ -646,7 +657,12 @@ attn_tiles_kernel(TileParams p) {
     } else {
         // neighbours in the order of the work run on one XCD and share keys through its L2
         wg = (int)xcd_swizzle(blockIdx.x, (uint32_t)p.workgroups);
-        const Shares<PAGED> sh(p, lane);
+        auto cost = [&](const Segment& x) {
+            const TileCost<PAGED> t(p, x);
+            return t.up_to(t.tiles) * a.Hkv;
+        };
+        const Looked<PAGED, decltype(cost)> looked(p, lane, cost);
+        const Shares<PAGED, decltype(looked)> sh(p, looked);
         from = uniform(sh.cut(wg));
         to = uniform(sh.cut(wg + 1));
         if (threadIdx.x == 0) p.cut[wg] = make_int4(from.seg, from.head, from.tile, from.stage);
@@ -864,6 +880,7 @@ attn_merge_tiles_kernel(TileParams p) {
 // ---- few rows: the keys of a launch shared out evenly over the wavefronts ---------------------------------
 struct StreamParams : Work {
     int waves;
+    int join_rows;                  // rows of a workgroup that joins: 1, or all of its groups of lanes
     int* share;                     // workspace: blocks of a wavefront
     int* start;                     // [segs]: first block of a segment (segments that have blocks)
     float* part_o;                  // [2 * waves][32][D]
@@ -886,18 +903,20 @@ attn_stream_kernel(StreamParams p) {
     const int wave = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 2 + wv), ln = lane & 31, hf = lane >> 5;
 
     // the launch's blocks, and this wavefront's: segment by segment, KV head by KV head
-    auto blocks = [&](int i) { return (int64_t)blocks_of(segment<true>(p, i)) * a.Hkv; };
-    const int all_blocks = (int)all_segments(p.segs, lane, blocks);        // (below 2^31: the call is refused otherwise)
+    auto blocks = [&](const Segment& x) { return (int64_t)blocks_of(x) * a.Hkv; };
+    const Looked<true, decltype(blocks)> looked(p, lane, blocks);
+    const int all_blocks = (int)looked.all;                                // (below 2^31: the call is refused otherwise)
     const int share = max(kLeastBlocks, (all_blocks + p.waves - 1) / p.waves);
     if (wave == 0 && lane == 0) *p.share = share;
     const int b0 = (int)min((int64_t)wave * share, (int64_t)all_blocks), b1 = (int)min((int64_t)b0 + share, (int64_t)all_blocks);
     if (b0 >= b1) return;
     int64_t in_seg;
-    const int seg = find_segment(p.segs, lane, b0, in_seg, blocks);
+    Segment sg;
+    const int seg = looked.find(b0, in_seg, sg);
 
     // where copies are asked for (`in`), and where the work is (`sg`): both walk the same blocks
     struct Cursor { int seg, g, blk; };
-    Segment sg = uniform_segment<true>(p, seg), in = sg;
+    Segment in = sg;
     Cursor cw = {seg, 0, (int)in_seg};
     cw.g = cw.blk / blocks_of(sg);
     cw.blk -= cw.g * blocks_of(sg);
@@ -1024,59 +1043,67 @@ attn_stream_kernel(StreamParams p) {
     }
 }
 
-// Joins the pieces of a unit's row; rows of units without a block get zeros.  One workgroup per (unit, row): D / 4 lanes per
-// piece, the pieces dealt out over the groups of lanes.
+// Joins the pieces of a unit's rows; rows of units without a block get zeros.  D / 4 lanes have a row.  Units of up to eight rows get a
+// workgroup per row, whose groups of lanes share the row's pieces (one sequence of 8192 keys, H32/8: 128 pieces per unit); with more
+// rows there are few pieces, and a group has a row (a workgroup per row took 42 us for 1600 units of 20 rows that nobody shared).
+constexpr int kJoinThreads = 256;
 template <int D>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kJoinThreads)
 attn_merge_stream_kernel(StreamParams p) {
-    constexpr int LPP = D / 4, PG = 256 / LPP;
-    __shared__ float s_m[PG], s_sum[PG];
-    __shared__ float4 s_o[PG][LPP];
+    constexpr int LPP = D / 4, GROUPS = kJoinThreads / LPP;
+    __shared__ float2 s_ms[GROUPS];
+    __shared__ float4 s_o[GROUPS][LPP];
     const PackedParams& a = p.a;
-    const int i = (int)blockIdx.x / a.Hkv, g = (int)blockIdx.x % a.Hkv, row = (int)blockIdx.y;
+    const int i = (int)blockIdx.x / a.Hkv, g = (int)blockIdx.x % a.Hkv;
     const Segment x = uniform_segment<true>(p, i);
-    if (row >= x.rows) return;
-    const RowAt ra = row_at(row, p.grp);
-    const int c = threadIdx.x % LPP, pg = threadIdx.x / LPP, h = g * a.grp + ra.head;
-    unsigned char* out = a.out + a.os.l * x.l + a.os.h * h + a.os.n * (int64_t)(x.first + ra.token) + 8 * c;
-    if (x.end == 0) {
-        if (pg == 0) *(uint2*)out = make_uint2(0u, 0u);
-        return;
-    }
-    const int share = *p.share, u0 = p.start[i] + g * blocks_of(x), w0 = u0 / share, w1 = (u0 + blocks_of(x) - 1) / share;
-    if (w0 == w1) return;                                       // one wavefront has written it
+    if ((int)blockIdx.y * p.join_rows >= x.rows) return;
+    const int share = *p.share, u0 = x.end == 0 ? 0 : p.start[i] + g * blocks_of(x);
+    const int w0 = u0 / share, w1 = (u0 + blocks_of(x) - 1) / share;
+    if (x.end > 0 && w0 == w1) return;                          // one wavefront has written it
+    const int c = threadIdx.x % LPP, group = threadIdx.x / LPP;
+    const int rows = p.join_rows, pieces = GROUPS / rows, mine = group / rows;      // rows here, groups of a row, and which this is
+    const int row = (int)blockIdx.y * rows + group % rows;
     float m = -INFINITY, sum = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    // a running maximum, so that every piece is read once
-    for (int w = w0 + pg; w <= w1; w += PG) {
-        const int64_t slot = (int64_t)(2 * w + (w == w0 ? 1 : 0)) * kFewRows + row;
-        const float2 ms = p.part_ms[slot];
-        const float4 y = *(const float4*)(p.part_o + slot * D + 4 * c);
-        const float mx = fmaxf(m, ms.x), ref = mx == -INFINITY ? 0.f : mx;
-        const float c0 = __builtin_amdgcn_exp2f(m - ref), c1 = __builtin_amdgcn_exp2f(ms.x - ref);
-        sum = fmaf(sum, c0, ms.y * c1);
-        o.x = fmaf(o.x, c0, y.x * c1); o.y = fmaf(o.y, c0, y.y * c1); o.z = fmaf(o.z, c0, y.z * c1); o.w = fmaf(o.w, c0, y.w * c1);
-        m = mx;
+    if (row < x.rows && x.end > 0) {
+#pragma unroll 4
+        for (int w = w0 + mine; w <= w1; w += pieces) {     // a running maximum: every piece is read once
+            const int64_t slot = (int64_t)(2 * w + (w == w0 ? 1 : 0)) * kFewRows + row;
+            const float2 ms = p.part_ms[slot];
+            const float4 y = *(const float4*)(p.part_o + slot * D + 4 * c);
+            const float mx = fmaxf(m, ms.x), ref = mx == -INFINITY ? 0.f : mx;
+            const float c0 = __builtin_amdgcn_exp2f(m - ref), c1 = __builtin_amdgcn_exp2f(ms.x - ref);
+            sum = fmaf(sum, c0, ms.y * c1);
+            o.x = fmaf(o.x, c0, y.x * c1); o.y = fmaf(o.y, c0, y.y * c1); o.z = fmaf(o.z, c0, y.z * c1); o.w = fmaf(o.w, c0, y.w * c1);
+            m = mx;
+        }
     }
-    if (c == 0) { s_m[pg] = m; s_sum[pg] = sum; }
-    s_o[pg][c] = o;
-    __syncthreads();
-    if (pg != 0) return;
-    float all = -INFINITY;
-#pragma unroll
-    for (int k = 0; k < PG; ++k) all = fmaxf(all, s_m[k]);
-    const float ref = all == -INFINITY ? 0.f : all;
-    sum = 0.f;
-    o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int k = 0; k < PG; ++k) {
-        const float w = __builtin_amdgcn_exp2f(s_m[k] - ref);
-        const float4 y = s_o[k][c];
-        sum = fmaf(w, s_sum[k], sum);
-        o.x = fmaf(w, y.x, o.x); o.y = fmaf(w, y.y, o.y); o.z = fmaf(w, y.z, o.z); o.w = fmaf(w, y.w, o.w);
+    if (pieces > 1) {
+        if (c == 0) s_ms[group] = make_float2(m, sum);
+        s_o[group][c] = o;
+        __syncthreads();
+        if (mine == 0) {
+            float top = m;
+            for (int k = 1; k < pieces; ++k) top = fmaxf(top, s_ms[group + k * rows].x);
+            const float ref = top == -INFINITY ? 0.f : top, c0 = __builtin_amdgcn_exp2f(m - ref);
+            sum *= c0;
+            o.x *= c0; o.y *= c0; o.z *= c0; o.w *= c0;
+            for (int k = 1; k < pieces; ++k) {
+                const float2 ms = s_ms[group + k * rows];
+                const float4 y = s_o[group + k * rows][c];
+                const float c1 = __builtin_amdgcn_exp2f(ms.x - ref);
+                sum = fmaf(ms.y, c1, sum);
+                o.x = fmaf(y.x, c1, o.x); o.y = fmaf(y.y, c1, o.y); o.z = fmaf(y.z, c1, o.z); o.w = fmaf(y.w, c1, o.w);
+            }
+        }
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    *(uint2*)out = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+    if (mine == 0 && row < x.rows) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const RowAt ra = row_at(row, p.grp);
+        const int h = g * a.grp + ra.head;
+        *(uint2*)(a.out + a.os.l * x.l + a.os.h * h + a.os.n * (int64_t)(x.first + ra.token) + 8 * c) =
+            make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+    }
 }
 
 // ---- launches ------------------------------------------------------------------------------------------
@@ -1157,8 +1184,11 @@ static hipError_t launch_stream(const pkv_packed& s, const PackedParams& a, void
     p.start = (int*)((char*)ws + 256);
     p.part_o = (float*)((char*)ws + 256 + up256((size_t)p.segs * 4));
     p.part_ms = (float2*)(p.part_o + (size_t)2 * p.waves * kFewRows * D);
+    const int rows = a.max_rows * a.grp;
+    p.join_rows = rows <= 8 ? 1 : kJoinThreads / (D / 4);
     hipLaunchKernelGGL(attn_stream_kernel<D>, dim3((unsigned)(p.waves / 2)), dim3(128), 0, st, p);
-    hipLaunchKernelGGL(attn_merge_stream_kernel<D>, dim3((unsigned)(p.segs * s.Hkv), (unsigned)(a.max_rows * a.grp)), dim3(256), 0, st, p);
+    hipLaunchKernelGGL(attn_merge_stream_kernel<D>, dim3((unsigned)(p.segs * s.Hkv), (unsigned)((rows + p.join_rows - 1) / p.join_rows)),
+                       dim3(kJoinThreads), 0, st, p);
     return hipGetLastError();
 }
 
@@ -1178,7 +1208,7 @@ hipError_t launch_packed_attn(const pkv_packed& s, const PackedAttn& a, hipStrea
         if (paged) return s.D == 128 ? launch_tiles<128, true>(s, p, a.ws, st) : launch_tiles<64, true>(s, p, a.ws, st);
         return s.D == 128 ? launch_tiles<128, false>(s, p, a.ws, st) : launch_tiles<64, false>(s, p, a.ws, st);
     }
-    const dim3 grid((unsigned)s.T, (unsigned)((s.H + 3) / 4), (unsigned)s.L);
+    const dim3 grid((unsigned)s.T, (unsigned)s.H, (unsigned)s.L);
     if (s.D == 128) hipLaunchKernelGGL(attn_rows_kernel<128>, grid, dim3(256), 0, st, p);
     else hipLaunchKernelGGL(attn_rows_kernel<64>, grid, dim3(256), 0, st, p);
     return hipGetLastError();

@@ -20,13 +20,13 @@ namespace pkv {
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / kWave;
 constexpr int kSmallSegs = 4096;        // segments whose records fit the planning workgroup's LDS
-constexpr int kSmallSlots = 16384;      // slots that the planning workgroup gives out itself
+constexpr int kSmallSlots = 16384;      // slots, or places of the table, that the planning workgroup looks after itself
 constexpr int kSlotThreads = 256;
 
 struct PageParams {
     int S, T, layers, n;                // n = S * layers segments
     int num_pages, max_pages, shift;    // shift: log2 of the page size
-    FastDiv by_layers, by_t;
+    FastDiv by_layers, by_t, by_width;
     const int32_t *target, *row_off, *lens;
     int32_t *table, *ring;
     const int32_t* state;
@@ -66,14 +66,7 @@ __device__ __forceinline__ int64_t give_slot(const PageParams& p, const int4& hd
     return ((int64_t)id << p.shift) + row;
 }
 
-// lane `lane` of `w` moves the pages of one segment
-__device__ __forceinline__ void move_pages(const PageParams& p, const int4& hd, const int2& r, int len_new, int seg, int lane, int w) {
-    const int held = pages_of(p, r.x), want = pages_of(p, len_new);
-    int32_t* row = p.table + (int64_t)seg * p.max_pages;
-    for (int j = held + lane; j < want; j += w) row[j] = p.ring[ring_at(p, (uint32_t)hd.y + (uint32_t)r.y + (uint32_t)(j - held))];
-    for (int j = want + lane; j < held; j += w)
-        p.ring[ring_at(p, (uint32_t)hd.y + (uint32_t)hd.z + (uint32_t)r.y + (uint32_t)(j - want))] = row[j];
-}
+constexpr int kPer = 4;                 // segments of a thread: 4096 in a round
 
 template <bool APPEND, bool SMALL>
 __global__ void __launch_bounds__(kPlanThreads)
@@ -82,56 +75,70 @@ page_plan_kernel(PageParams p) {
     __shared__ int s_bad;
     __shared__ int2 s_rec[SMALL ? kSmallSegs : 1];
     __shared__ int s_off[APPEND && SMALL ? kMaxS + 1 : 1];
+    __shared__ int s_len[!APPEND && SMALL ? kSmallSegs : 1];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = tid / kWave;
     const int limit = p.max_pages << p.shift;
     if (tid == 0) s_bad = 0;
     if constexpr (APPEND && SMALL)
         for (int i = tid; i <= p.S; i += kPlanThreads) s_off[i] = p.row_off[i];
-    __syncthreads();
-    int head = p.state[0], count = p.state[1];
+    const int head = p.state[0], count = p.state[1];
     int2 carry = make_int2(0, 0);
     bool bad = false;
-    // rounds of 1024 segments; two rounds' sums alternate in LDS, so that one barrier per round is enough
-    for (int base = 0, turn = 0; base < p.n; base += kPlanThreads, turn ^= 1) {
-        const int i = base + tid;
-        int old = 0, want_len = 0;
-        bool wrong = false;
-        if (i < p.n) {
-            old = p.lens[i];
-            if constexpr (APPEND) {
-                const int s = div_mod(i, p.by_layers).q;
-                const int a = p.row_off[s], b = p.row_off[s + 1];
-                wrong = a < 0 || b < a || b > p.T;
-                want_len = wrong ? old : old + (b - a);    // lengths stay below 2^20 + 2^22
-            } else {
-                want_len = p.target[i];
+    int len[kPer];                      // new lengths (SMALL: there is one round)
+    // Two rounds' sums alternate in LDS, so that one barrier per round is enough.
+    for (int base = 0, turn = 0; base < p.n; base += kPlanThreads * kPer, turn ^= 1) {
+        const int i0 = base + tid * kPer;
+        int old[kPer];
+        int2 mine[kPer], sum = make_int2(0, 0);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            const int i = i0 + e;
+            old[e] = len[e] = 0;
+            bool wrong = false;
+            if (i < p.n) {
+                old[e] = p.lens[i];
+                if constexpr (APPEND) {
+                    const int s = div_mod(i, p.by_layers).q;
+                    const int a = p.row_off[s], b = p.row_off[s + 1];
+                    wrong = a < 0 || b < a || b > p.T;
+                    len[e] = wrong ? old[e] : old[e] + (b - a);    // lengths stay below 2^20 + 2^22
+                } else {
+                    len[e] = p.target[i];
+                }
+                wrong = wrong || old[e] < 0 || old[e] > limit || len[e] < 0 || len[e] > limit;
             }
-            wrong = wrong || old < 0 || old > limit || want_len < 0 || want_len > limit;
+            bad = bad || wrong;
+            const int diff = wrong ? 0 : pages_of(p, len[e]) - pages_of(p, old[e]);
+            mine[e] = make_int2(max(diff, 0), max(-diff, 0));
+            sum.x += mine[e].x; sum.y += mine[e].y;
         }
-        bad = bad || wrong;
-        const int diff = wrong ? 0 : pages_of(p, want_len) - pages_of(p, old);
-        const int2 mine = make_int2(max(diff, 0), max(-diff, 0));
-        int2 incl = mine;
+        int2 incl = sum;
 #pragma unroll
         for (int d = 1; d < kWave; d <<= 1) {
             const int ux = __shfl_up(incl.x, d, kWave), uy = __shfl_up(incl.y, d, kWave);
             if (lane >= d) { incl.x += ux; incl.y += uy; }
         }
         if (lane == kWave - 1) s_sum[turn][wv] = incl;
+        if (turn == 0 && base == 0) __syncthreads();               // s_bad is cleared
+        if (bad) s_bad = 1;
         __syncthreads();
-        int2 before = carry;
+        int2 before = make_int2(carry.x + incl.x - sum.x, carry.y + incl.y - sum.y);
 #pragma unroll
         for (int w = 0; w < kPlanWaves; ++w) {
             const int2 x = s_sum[turn][w];
             if (w < wv) { before.x += x.x; before.y += x.y; }
             carry.x += x.x; carry.y += x.y;
         }
-        if (i < p.n) {
-            const int2 r = make_int2(old, diff >= 0 ? before.x + incl.x - mine.x : before.y + incl.y - mine.y);
-            if constexpr (SMALL) s_rec[i] = r; else p.rec[i] = r;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            if (i0 + e < p.n) {
+                const int2 r = make_int2(old[e], mine[e].x > 0 ? before.x : before.y);
+                if constexpr (SMALL) s_rec[i0 + e] = r; else p.rec[i0 + e] = r;
+                if constexpr (SMALL && !APPEND) s_len[i0 + e] = len[e];
+            }
+            before.x += mine[e].x; before.y += mine[e].y;
         }
     }
-    if (bad) s_bad = 1;
     __syncthreads();
     const bool range = s_bad != 0 || head < 0 || head >= p.num_pages || count < 0 || count > p.num_pages ||
                        (int64_t)count - carry.x + carry.y > p.num_pages;
@@ -139,18 +146,25 @@ page_plan_kernel(PageParams p) {
     const bool ok = !range && !few;
     const int4 hd = make_int4(ok ? 1 : 0, head, count, 0);
     // (every thread has read what it needs of lens and state in front of the barrier: lens_out and state_out may be the same)
-    for (int i = tid; i < p.n; i += kPlanThreads) {
-        int len = SMALL ? s_rec[i].x : p.rec[i].x;
-        if (ok) {
-            if constexpr (APPEND) {
-                const int s = div_mod(i, p.by_layers).q;
-                len += p.row_off[s + 1] - p.row_off[s];
-            } else {
-                len = p.target[i];
-            }
+    if constexpr (SMALL) {
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            const int i = tid * kPer + e;
+            if (i < p.n) p.lens_out[i] = ok ? len[e] : s_rec[i].x;
         }
-        p.lens_out[i] = len;
-        if constexpr (SMALL && !APPEND) { if (ok) move_pages(p, hd, s_rec[i], len, i, 0, 1); }
+    } else {
+        for (int i = tid; i < p.n; i += kPlanThreads) {
+            int n = p.rec[i].x;
+            if (ok) {
+                if constexpr (APPEND) {
+                    const int s = div_mod(i, p.by_layers).q;
+                    n += p.row_off[s + 1] - p.row_off[s];
+                } else {
+                    n = p.target[i];
+                }
+            }
+            p.lens_out[i] = n;
+        }
     }
     if (tid == 0) {
         p.state_out[0] = ok ? ring_at(p, (uint32_t)head + (uint32_t)carry.x) : head;
@@ -158,8 +172,21 @@ page_plan_kernel(PageParams p) {
         *p.status = range ? PKV_PAGES_RANGE : few ? PKV_PAGES_SHORT : 0;
         if constexpr (!SMALL) *p.head = hd;
     }
+    if constexpr (!APPEND && SMALL) {
+        if (!ok) return;
+        // a thread per place of the table
+        for (int x = tid; x < p.n * p.max_pages; x += kPlanThreads) {
+            const DivMod sj = div_mod(x, p.by_width);
+            const int2 r = s_rec[sj.q];
+            const int held = pages_of(p, r.x), want = pages_of(p, s_len[sj.q]), j = sj.r;
+            if (j >= held && j < want) p.table[x] = p.ring[ring_at(p, (uint32_t)hd.y + (uint32_t)r.y + (uint32_t)(j - held))];
+            if (j >= want && j < held)
+                p.ring[ring_at(p, (uint32_t)hd.y + (uint32_t)hd.z + (uint32_t)r.y + (uint32_t)(j - want))] = p.table[x];
+        }
+    }
     if constexpr (APPEND && SMALL) {
         const int total = p.layers * p.T;
+#pragma unroll 2
         for (int x = tid; x < total; x += kPlanThreads) {
             const DivMod lt = div_mod(x, p.by_t);      // layer, row
             int64_t slot = -1;
@@ -197,7 +224,15 @@ page_move_kernel(PageParams p) {
     const int seg = blockIdx.x * (kSlotThreads / kWave) + threadIdx.x / kWave;
     if (seg >= p.n) return;
     const int4 hd = *p.head;
-    if (hd.x != 0) move_pages(p, hd, p.rec[seg], p.target[seg], seg, threadIdx.x & (kWave - 1), kWave);
+    if (hd.x == 0) return;
+    const int2 r = p.rec[seg];
+    const int held = pages_of(p, r.x), want = pages_of(p, p.target[seg]), lane = threadIdx.x & (kWave - 1);
+    int32_t* row = p.table + (int64_t)seg * p.max_pages;
+#pragma unroll 4
+    for (int j = held + lane; j < want; j += kWave) row[j] = p.ring[ring_at(p, (uint32_t)hd.y + (uint32_t)r.y + (uint32_t)(j - held))];
+#pragma unroll 4
+    for (int j = want + lane; j < held; j += kWave)
+        p.ring[ring_at(p, (uint32_t)hd.y + (uint32_t)hd.z + (uint32_t)r.y + (uint32_t)(j - want))] = row[j];
 }
 
 size_t page_ws_bytes(int S, int layers) { return 256 + (size_t)S * layers * sizeof(int2); }
@@ -208,7 +243,7 @@ hipError_t launch_pages(int S, int T, const pkv_paging& g, const int32_t* target
     PageParams p;
     p.S = S; p.T = T; p.layers = g.layers; p.n = S * g.layers;
     p.num_pages = g.num_pages; p.max_pages = g.max_pages; p.shift = __builtin_ctz((unsigned)g.page_size);
-    p.by_layers = fast_div(g.layers); p.by_t = fast_div(T > 0 ? T : 1);
+    p.by_layers = fast_div(g.layers); p.by_t = fast_div(T > 0 ? T : 1); p.by_width = fast_div(g.max_pages);
     p.target = target; p.row_off = row_off; p.lens = lens; p.table = table; p.ring = ring; p.state = state;
     p.lens_out = lens_out; p.state_out = state_out; p.slots = slots; p.status = status;
     p.head = (int4*)ws; p.rec = (int2*)((char*)ws + 256);
