@@ -190,6 +190,23 @@ __device__ __forceinline__ void copy_to_lds(const unsigned char* src, unsigned c
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
 }
 
+// 32 columns of 32 finished rows: register r is column 8 (r / 4) + 4 (lane / 32) + r % 4.  16 bytes per lane and 8 columns: the
+// halves of a row swap their pieces.
+__device__ __forceinline__ void store_columns(const f32x16_t& o, unsigned char* row, int hf, float inv, bool real) {
+#pragma unroll
+    for (int g = 0; g < 4; g += 2) {
+        uint32_t w[2][2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            w[x][0] = pack_bf16(o[4 * (g + x)] * inv, o[4 * (g + x) + 1] * inv);
+            w[x][1] = pack_bf16(o[4 * (g + x) + 2] * inv, o[4 * (g + x) + 3] * inv);
+        }
+        const auto s0 = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
+        const auto s1 = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+        if (real) *(uint4*)(row + 2 * (8 * (g + hf))) = make_uint4(s0[0], s1[0], s0[1], s1[1]);
+    }
+}
+
 // Softmax state and output of the 32 rows of a wavefront: row lane % 32; register r of o[dt] is column
 // 32 dt + 8 (r / 4) + 4 (lane / 32) + r % 4.
 template <int D>
@@ -382,22 +399,19 @@ struct RowTile {
     // the whole row sum, in both halves
     __device__ __forceinline__ float total() const { return sum + __shfl_xor(sum, 32, kWave); }
 
-    // the finished row (16 bytes per lane and 8 columns: the halves of a row swap their pieces)
+    // the finished row
     __device__ __forceinline__ void store(unsigned char* row, int hf, float inv, bool real) const {
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) store_columns(o[dt], row + 64 * dt, hf, inv, real);
+    }
+    // the 32 rows unfinished, as the registers are: numerators, and {maximum, sum} of the halves' rows
+    __device__ __forceinline__ void store_tile(float* to, float2* ms, int lane, float all) const {
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-            for (int g = 0; g < 4; g += 2) {
-                uint32_t w[2][2];
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    w[x][0] = pack_bf16(o[dt][4 * (g + x)] * inv, o[dt][4 * (g + x) + 1] * inv);
-                    w[x][1] = pack_bf16(o[dt][4 * (g + x) + 2] * inv, o[dt][4 * (g + x) + 3] * inv);
-                }
-                const auto s0 = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
-                const auto s1 = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
-                if (real) *(uint4*)(row + 2 * (32 * dt + 8 * (g + hf))) = make_uint4(s0[0], s1[0], s0[1], s1[1]);
-            }
+            for (int c = 0; c < 4; ++c)
+                *(float4*)(to + ((dt * 4 + c) * kWave + lane) * 4) = make_float4(o[dt][4 * c], o[dt][4 * c + 1], o[dt][4 * c + 2], o[dt][4 * c + 3]);
+        ms[lane] = make_float2(m, all);
     }
     // the unfinished row: numerators, and {maximum, sum}
     __device__ __forceinline__ void store_part(float* row, float2* ms, int hf, float all) const {
@@ -532,8 +546,8 @@ struct TileParams : Work {
     FastDiv by_hkv, by_heads, by_tiles, by_tail;
     int heads_per_xcd;             // of the call's L * Hkv heads; 0: they do not divide up
     int4* cut;                     // workspace [workgroups]: {segment, head, tile, stage} where a workgroup begins; stage 0: with a whole tile
-    float* part_o;                 // [2 * workgroups][128][D]
-    float2* part_ms;
+    float* part_o;                 // [2 * workgroups][4 wavefronts][32 * D], as registers are
+    float2* part_ms;               // [2 * workgroups][4 wavefronts][64]
 };
 constexpr int kStartKeys = 192;     // what the start and the end of a tile cost, in keys
 constexpr int kJoinStages = 3;      // what a cut costs: two parts written and read again, and a second start
@@ -807,8 +821,8 @@ attn_tiles_kernel(TileParams p) {
                     a.lse[(int64_t)a.L * a.H * sg.first + (int64_t)(sg.l * a.H + h) * sg.n + ra.token] = kLn2 * (tl.m + __builtin_amdgcn_logf(sum));
             } else {
                 // a workgroup has at most two parts of tiles that others share: of one that began before it, and of one that goes on
-                const int64_t slot = (int64_t)(2 * wg + (st0 > 0 ? 0 : 1)) * kTileRows + wv * 32 + ln;
-                if (real) tl.store_part(p.part_o + slot * D, p.part_ms + slot, hf, sum);
+                const int64_t slot = (int64_t)(2 * wg + (st0 > 0 ? 0 : 1)) * 4 + wv;
+                tl.store_tile(p.part_o + slot * 32 * D, p.part_ms + slot * kWave, lane, sum);
             }
         }
         if (WHOLE || last) break;
@@ -821,14 +835,14 @@ attn_tiles_kernel(TileParams p) {
     }
 }
 
-// Joins the parts of the tiles that were cut: the first cut of a tile has all of its parts.  D / 4 lanes per row.
-constexpr int kMergeRows = 32;      // rows of a workgroup
+// Joins the parts of the tiles that were cut: the first cut of a tile has all of its parts.  A wavefront has 32 columns of 32 rows, in
+// the registers' order, in which the parts were written.
 template <int D, bool PAGED>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kWave)
 attn_merge_tiles_kernel(TileParams p) {
-    constexpr int LPR = D / 4, RPB = 256 / LPR;
     const PackedParams& a = p.a;
-    const int w0 = (int)blockIdx.x + 1, lane = threadIdx.x & (kWave - 1);
+    const int w0 = (int)blockIdx.x + 1, lane = threadIdx.x, wv = (int)blockIdx.y / (D / 32), dt = (int)blockIdx.y % (D / 32);
+    const int ln = lane & 31, hf = lane >> 5;
     // the cuts from the one before this on: those inside the same tile follow each other
     int w1 = w0;
     int4 c;
@@ -850,31 +864,34 @@ attn_merge_tiles_kernel(TileParams p) {
         if (run < kWave) break;
     }
     const Segment sg = uniform_segment<PAGED>(p, c.x);
-    const int col = 4 * (threadIdx.x % LPR);
-    for (int in_tile = (int)blockIdx.y * kMergeRows + threadIdx.x / LPR; in_tile < ((int)blockIdx.y + 1) * kMergeRows; in_tile += RPB) {
-        const int row = c.z * kTileRows + in_tile;
-        if (row >= sg.rows) return;
-        float m = -INFINITY, sum = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int r0 = c.z * kTileRows + wv * 32, row = r0 + ln;
+    if (r0 >= sg.rows) return;
+    float m = -INFINITY, sum = 0.f;
+    f32x16_t o;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[r] = 0.f;
 #pragma unroll 4
-        for (int w = w0 - 1; w <= w1; ++w) {                     // a running maximum: every part is read once
-            const int64_t slot = (int64_t)(2 * w + (w < w0 ? 1 : 0)) * kTileRows + in_tile;
-            const float2 ms = p.part_ms[slot];
-            const float4 y = *(const float4*)(p.part_o + slot * D + col);
-            const float mx = fmaxf(m, ms.x), ref = mx == -INFINITY ? 0.f : mx;
-            const float c0 = __builtin_amdgcn_exp2f(m - ref), c1 = __builtin_amdgcn_exp2f(ms.x - ref);
-            sum = fmaf(sum, c0, ms.y * c1);
-            o.x = fmaf(o.x, c0, y.x * c1); o.y = fmaf(o.y, c0, y.y * c1); o.z = fmaf(o.z, c0, y.z * c1); o.w = fmaf(o.w, c0, y.w * c1);
-            m = mx;
+    for (int w = w0 - 1; w <= w1; ++w) {                         // a running maximum: every part is read once
+        const int64_t slot = (int64_t)(2 * w + (w < w0 ? 1 : 0)) * 4 + wv;
+        const float2 x = p.part_ms[slot * kWave + lane];
+        const float4* from = (const float4*)(p.part_o + slot * 32 * D) + dt * 4 * kWave + lane;
+        const float4 y[4] = {from[0], from[kWave], from[2 * kWave], from[3 * kWave]};
+        const float mx = fmaxf(m, x.x), ref = mx == -INFINITY ? 0.f : mx;
+        const float c0 = __builtin_amdgcn_exp2f(m - ref), c1 = __builtin_amdgcn_exp2f(x.x - ref);
+        sum = fmaf(sum, c0, x.y * c1);
+        m = mx;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            o[4 * i] = fmaf(o[4 * i], c0, y[i].x * c1); o[4 * i + 1] = fmaf(o[4 * i + 1], c0, y[i].y * c1);
+            o[4 * i + 2] = fmaf(o[4 * i + 2], c0, y[i].z * c1); o[4 * i + 3] = fmaf(o[4 * i + 3], c0, y[i].w * c1);
         }
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        const RowAt ra = row_at(row, p.grp);
-        const int h = c.y * a.grp + ra.head;
-        *(uint2*)(a.out + a.os.l * sg.l + a.os.h * h + a.os.n * (int64_t)(sg.first + ra.token) + 2 * col) =
-            make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-        if (!PAGED && col == 0)
-            a.lse[(int64_t)a.L * a.H * sg.first + (int64_t)(sg.l * a.H + h) * sg.n + ra.token] = kLn2 * (m + __builtin_amdgcn_logf(sum));
     }
+    const bool real = row < sg.rows;
+    const RowAt ra = row_at(real ? row : r0, p.grp);
+    const int h = c.y * a.grp + ra.head;
+    store_columns(o, a.out + a.os.l * sg.l + a.os.h * h + a.os.n * (int64_t)(sg.first + ra.token) + 64 * dt, hf, sum == 0.f ? 0.f : 1.f / sum, real);
+    if (!PAGED && real && hf == 0 && dt == 0)
+        a.lse[(int64_t)a.L * a.H * sg.first + (int64_t)(sg.l * a.H + h) * sg.n + ra.token] = kLn2 * (m + __builtin_amdgcn_logf(sum));
 }
 
 // ---- few rows: the keys of a launch shared out evenly over the wavefronts ---------------------------------
@@ -1055,9 +1072,10 @@ attn_merge_stream_kernel(StreamParams p) {
     __shared__ float4 s_o[GROUPS][LPP];
     const PackedParams& a = p.a;
     const int i = (int)blockIdx.x / a.Hkv, g = (int)blockIdx.x % a.Hkv;
+    const int share = max(1, *p.share), start = p.start[i];     // (asked for with the segment; `start` is looked at if it has blocks)
     const Segment x = uniform_segment<true>(p, i);
     if ((int)blockIdx.y * p.join_rows >= x.rows) return;
-    const int share = *p.share, u0 = x.end == 0 ? 0 : p.start[i] + g * blocks_of(x);
+    const int u0 = x.end == 0 ? 0 : start + g * blocks_of(x);
     const int w0 = u0 / share, w1 = (u0 + blocks_of(x) - 1) / share;
     if (x.end > 0 && w0 == w1) return;                          // one wavefront has written it
     const int c = threadIdx.x % LPP, group = threadIdx.x / LPP;
@@ -1138,11 +1156,11 @@ bool packed_attn_fits(const pkv_packed& s, const pkv_paging* g) {
 
 size_t packed_attn_ws_bytes(const pkv_packed& s, int max_rows) {
     if (s.dtype != PKV_BF16) return 0;
-    const size_t row = sizeof(float2) + s.D * sizeof(float);
+    const size_t row = sizeof(float2) + s.D * sizeof(float);                    // (a part of a tile has two of the first per row)
     if (few_rows(s, max_rows)) return 256 + up256((size_t)s.S * s.L * 4) + (size_t)2 * stream_waves(s) * kFewRows * row;
     // (whether tiles are cut goes by the table's width too, which the size does not ask for: where the widest would not be, none is)
     if (!cut_tiles(s, max_rows > 0 ? kMaxSegmentSlots : s.T, max_rows > 0)) return 0;
-    return up256(tile_workgroups() * sizeof(int4)) + (size_t)2 * tile_workgroups() * kTileRows * row;
+    return up256(tile_workgroups() * sizeof(int4)) + (size_t)2 * tile_workgroups() * kTileRows * (row + sizeof(float2));
 }
 
 static Work work_of(const pkv_packed& s, const PackedParams& a) {
@@ -1170,7 +1188,8 @@ static hipError_t launch_tiles(const pkv_packed& s, const PackedParams& a, void*
         hipLaunchKernelGGL((attn_tiles_kernel<D, PAGED, true>), dim3((unsigned)(tiles * heads)), dim3(256), 0, st, p);
     } else {
         hipLaunchKernelGGL((attn_tiles_kernel<D, PAGED, false>), dim3((unsigned)p.workgroups), dim3(256), 0, st, p);
-        hipLaunchKernelGGL((attn_merge_tiles_kernel<D, PAGED>), dim3((unsigned)p.workgroups - 1, kTileRows / kMergeRows), dim3(256), 0, st, p);
+        hipLaunchKernelGGL((attn_merge_tiles_kernel<D, PAGED>), dim3((unsigned)p.workgroups - 1, kTileRows / 32 * (D / 32)), dim3(kWave), 0,
+                           st, p);
     }
     return hipGetLastError();
 }

@@ -1,6 +1,11 @@
-"""Pre-allocated driver of the whole hot path for one workload shape: importance -> select ->
-compact -> T decode steps.  Only buffer management and call sequencing; every step runs in the
-HIP library.  Used by the benchmark, the smoke check and the end-to-end tests."""
+"""Drivers of the hot path.  Only buffer management and call sequencing; every step runs in the HIP
+library.
+
+HotPath    one rectangular batch on pre-allocated buffers: importance -> select -> compact -> T
+           decode steps.  Used by the benchmark, the smoke check and the end-to-end tests.
+PagedPath  sequences of different lengths that come, ask again and go: packed prompts -> rotation ->
+           attention -> importance and search per sequence -> pages -> further rows over the pages.
+"""
 from __future__ import annotations
 
 from typing import Optional
@@ -107,3 +112,70 @@ class HotPath:
 
     def replay_decode_loop(self):
         self._graph.replay()
+
+
+class PagedPath:
+    """S places for sequences over one pool of pages.  All layers of the model are called at once, as the queries, keys and
+    values [L,heads,T,D] of the packed rows of all layers are given (bf16).  Nothing is read back: `status` [1] tells whether
+    the last call that needed pages got them."""
+
+    def __init__(self, S: int, L: int, H: int, Hkv: int, D: int, scale: torch.Tensor, plan: B_.RopePlan, num_pages: int,
+                 max_pages: int, page_size: int = 64, device="cuda"):
+        self.S, self.L, self.H, self.Hkv, self.D = S, L, H, Hkv, D
+        self.scale, self.plan, self.device = scale, plan, torch.device(device)
+        self.cache = B_.paged_cache(S, L, Hkv, D, page_size, num_pages, max_pages, torch.bfloat16, device)
+        self.target = torch.zeros((S, L), dtype=torch.int32, device=device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
+        self.page_ws = torch.empty(B_.page_workspace_bytes(S, L), dtype=torch.uint8, device=device)
+
+    def _offsets(self, lengths) -> torch.Tensor:
+        off = [0]
+        for n in lengths:
+            off.append(off[-1] + int(n))
+        return torch.tensor(off, dtype=torch.int32).to(self.device, non_blocking=True)
+
+    def prefill(self, places, lengths, q, k, v, positions, budgets, kept_pos=None):
+        """Prompts of these lengths, packed, for sequences that begin at `places`; budgets[i] of the L * lengths[i] entries are
+        kept.  q, k are rotated in place.  -> attention output [L,H,T,D].  kept_pos: a list that receives the kept positions."""
+        off = self._offsets(lengths)
+        B_.prefixkv_rope(q, k, positions, self.plan, q_out=q, k_out=k)
+        out, lse = B_.prefixkv_prefill_attn_packed(q, k, v, off, self.scale)
+        rank, a = [], 0
+        self.target.copy_(self.cache.lens)
+        for place, n, budget in zip(places, lengths, budgets):
+            n = int(n)
+            rows = slice(a, a + n)
+            imp = B_.prefixkv_importance(q[None, :, :, rows], k[None, :, :, rows], self.scale,
+                                         lse=lse[self.L * self.H * a:self.L * self.H * (a + n)].view(1, self.L, self.H, n))
+            sel = B_.prefixkv_select(imp, int(budget), want_prefix=False)
+            self.target[place].copy_(sel.lengths[0])
+            rank.append((place, rows, sel))
+            a += n
+        B_.prefixkv_page_resize(self.cache, self.target, status=self.status, ws=self.page_ws)
+        for place, rows, sel in rank:
+            # (after a refused call lens is what it was: nothing is stored then)
+            lengths_now = torch.minimum(sel.lengths, self.cache.lens[place:place + 1])
+            pos = None if kept_pos is None else torch.full_like(sel.order, -1)
+            B_.prefixkv_compact_paged(self._at(place), k[None, :, :, rows], v[None, :, :, rows], sel.order, lengths_now, kept_pos=pos)
+            if kept_pos is not None:
+                kept_pos.append(pos[0])
+        return out
+
+    def _at(self, place: int) -> B_.PagedCache:
+        c = self.cache
+        return B_.PagedCache(kp=c.kp, vp=c.vp, table=c.table[place:place + 1], lens=c.lens[place:place + 1], ring=c.ring,
+                             state=c.state)
+
+    def extend(self, lengths, q, k, v, positions):
+        """Further rows of every sequence (lengths[s] of place s, 0 for one that waits): they are stored, and attend to what the
+        cache holds and to each other.  One row each is a decode step.  -> attention output [L,H,T,D]."""
+        off, T = self._offsets(lengths), q.shape[2]
+        slots, _ = B_.prefixkv_page_append(self.cache, off, T, status=self.status, ws=self.page_ws)
+        turned = B_.prefixkv_rope_store(self.cache, q, k, v, positions, self.plan, slots)
+        return B_.prefixkv_chunk_attn(self.cache, turned, off, self.scale, max(1, max(int(n) for n in lengths)))
+
+    def end(self, places):
+        """The sequences at these places are over: their pages are free again."""
+        self.target.copy_(self.cache.lens)
+        self.target[list(places)] = 0
+        B_.prefixkv_page_resize(self.cache, self.target, status=self.status, ws=self.page_ws)

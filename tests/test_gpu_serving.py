@@ -301,6 +301,7 @@ PROMPTS = [
     (3, 12, 4, 64, [200, 17], 0, 0),
     (1, 16, 2, 128, [90, 1, 40], 0, 0),
     (1, 1, 1, 128, [1200], 0, 0),
+    (1, 2, 1, 64, [2500, 1, 200], 0, 1),                         # few long tiles: cut and joined
 ]
 
 
@@ -398,6 +399,9 @@ CHUNKS = [
     (1, 16, 16, 128, 16, [2000], [1], 0, 0, 0),
     (1, 64, 1, 128, 16, [900, 33], [1, 2], 0, 0, 0),
     (1, 3, 1, 128, 32, [2100], [260], 0, 0, 0),
+    (1, 4, 4, 64, 16, [50, 0, 150], [150, 140, 10], 1, 1, 0),               # whole tiles that see nothing
+    (1, 8, 2, 128, 64, [5000, 70, 640], [100, 2, 64], 0, 0, 0),             # few long tiles: cut and joined
+    (2, 2, 1, 64, 16, [4100, 3000], [130, 128], 0, 0, 1),
 ]
 
 
@@ -459,3 +463,148 @@ def test_chunk_attn_lowest_values_and_infinities(dtype, n):
     want, mag = R.chunk(f64(q), off, f64(c.kp), f64(c.vp), table, lens, np.ones(1))
     close(out, want, mag, dtype)
     assert bool((out[:, :, off[1]:] == 0).all())
+
+
+def test_chunk_attn_more_segments_than_lanes():
+    """70 sequences: single tokens, and one of 40 rows over a long cache among them (tiles that are cut)."""
+    H, Hkv, D, ps = 2, 1, 64, 16
+    for n, sizes in (([1] * 70, [(37 * i) % 300 + 1 for i in range(70)]),
+                     ([1] * 33 + [40] + [0] + [1] * 35, [20] * 33 + [2500] + [0] * 2 + [60] * 34)):
+        lens = np.array(sizes)[:, None]
+        c, table = chunk_state(11, 70, 1, Hkv, D, ps, lens, BF16, width=800)
+        off = offsets(n)
+        q, _, _ = projected(gen(12), 1, H, Hkv, int(off[-1]), D, BF16)
+        scale = torch.full((1,), 0.15, device=DEV)
+        out = P.prefixkv_chunk_attn(c, q, i32(off), scale, max(n))
+        want, mag = R.chunk(f64(q), off, f64(c.kp), f64(c.vp), table, lens, scale.double().cpu().numpy())
+        close(out, want, mag, BF16)
+
+
+@pytest.mark.parametrize("n,sizes", [([1, 1, 1], [700, 33, 2000]), ([9, 150, 30], [90, 700, 31]), ([100, 2], [6000, 300])])
+def test_chunk_attn_is_repeatable_and_replays_from_a_graph(n, sizes):
+    """The same bits from every call, from another stream, and from a captured graph that is replayed with eager work between."""
+    H, Hkv, D, ps = 8, 2, 128, 32
+    lens = np.array(sizes)[:, None]
+    c, _ = chunk_state(3, len(n), 1, Hkv, D, ps, lens, BF16)
+    off = i32(offsets(n))
+    q, _, _ = projected(gen(5), 1, H, Hkv, sum(n), D, BF16)
+    scale = torch.full((1,), 0.1, device=DEV)
+    ws = torch.empty(P.attn_workspace_bytes(len(n), 1, H, Hkv, sum(n), D, BF16, max_rows=max(n)), dtype=torch.uint8, device=DEV)
+    want = P.prefixkv_chunk_attn(c, q, off, scale, max(n), ws=ws).clone()
+    out = torch.empty_like(q)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        P.prefixkv_chunk_attn(c, q, off, scale, max(n), out=out)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        P.prefixkv_chunk_attn(c, q, off, scale, max(n), out=out, ws=ws)
+    for i in range(4):
+        out.zero_()
+        ws.fill_(255 * (i % 2))            # nothing is carried in it
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        torch.cuda.synchronize()
+        assert torch.equal(P.prefixkv_chunk_attn(c, q, off, scale, max(n)), want)
+
+
+def test_page_calls_replay_from_a_graph():
+    """A captured append: every replay gives the next tokens their slots."""
+    S, layers, ps, width = 6, 4, 16, 8
+    lens, table, ring, state = page_state(2, S, layers, ps, width, 200, 40)
+    c = as_cache(lens, table, ring, state, ps)
+    off = offsets([1] * S)
+    slots = torch.empty((layers, S), dtype=torch.int64, device=DEV)
+    status = torch.empty(1, dtype=torch.int32, device=DEV)
+    ws = torch.empty(P.page_workspace_bytes(S, layers), dtype=torch.uint8, device=DEV)
+    offd = i32(off)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        P.prefixkv_page_append(c, offd, S, slots=slots, status=status, ws=ws)
+    for _ in range(40):
+        g.replay()
+        torch.cuda.synchronize()
+        st, lens, table, state, want = R.append(lens, off, S, table, ring, state, ps)
+        assert int(status) == st
+        for a, b in zip((c.lens, c.table, c.state, slots), (lens, table, state, want)):
+            np.testing.assert_array_equal(a.cpu().numpy(), b)
+
+
+# ---- together ------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("H,Hkv,D,ps", [(4, 2, 64, 16), (7, 1, 128, 64)])
+def test_sequences_come_ask_again_and_go(H, Hkv, D, ps):
+    """Packed prompts, what the search keeps of them in pages, a second question, decode steps, an end, a new prompt in the
+    freed pages: every output against the definitions in 64 bits on the positions that were kept."""
+    from paper_2412_03409_amd.pipeline import PagedPath
+    L, S = 2, 4
+    g = gen(H)
+    scale = torch.tensor([0.15, 0.3])
+    plan = P.rope_plan(D, [D // 2 - 2 * (D // 6), D // 6, D // 6], device=DEV)
+    axis = plan.axis.cpu().numpy()
+    path = PagedPath(S, L, H, Hkv, D, scale.to(DEV), plan, num_pages=52 if ps == 64 else 150, max_pages=400 // ps + 1, page_size=ps, device=DEV)
+    keys = [[None] * L for _ in range(S)]      # rotated keys and values [Hkv,len,D] of every segment, as the cache must hold them
+
+    def rows(T):
+        x = projected(g, L, H, Hkv, T, D, BF16)
+        pos = torch.randint(0, 3000, (3, T), generator=g).to(torch.int32).to(DEV)
+        return (*x, pos)
+
+    def rotated(x, pos):       # as the storage type holds it
+        return torch.from_numpy(R.rope(f64(x), pos.cpu().numpy(), axis, 10000.0, D, False)).to(BF16).double().numpy()
+
+    def prefill(places, lengths, budgets):
+        q, k, v, pos = rows(sum(lengths))
+        qr, kr, vr = rotated(q, pos), rotated(k, pos), f64(v)
+        kept = []
+        out = path.prefill(places, lengths, q, k, v, pos, budgets, kept_pos=kept)
+        assert int(path.status) == 0
+        off = offsets(lengths)
+        want, mag, _ = R.prompt(qr, kr, vr, off, scale.double().numpy())
+        close(out, want, mag, BF16)
+        for i, (s, b) in enumerate(zip(places, budgets)):
+            total = 0
+            for l in range(L):
+                pos_l = kept[i][l].cpu().numpy()
+                pos_l = pos_l[pos_l >= 0]
+                assert len(pos_l) == int(path.cache.lens[s, l])
+                total += len(pos_l)
+                keys[s][l] = [x[l][:, off[i] + pos_l] for x in (kr, vr)]
+            assert total == b
+    def extend(lengths, pad=0):
+        T = sum(lengths) + pad
+        q, k, v, pos = rows(T)
+        qr, kr, vr = rotated(q, pos), rotated(k, pos), f64(v)
+        out = path.extend(lengths, q, k, v, pos)
+        assert int(path.status) == 0
+        off = offsets(lengths)
+        for s in range(S):
+            t = slice(off[s], off[s + 1])
+            for l in range(L):
+                if lengths[s] == 0:
+                    continue
+                keys[s][l] = [np.concatenate([old, x[l][:, t]], axis=1) for old, x in zip(keys[s][l], (kr, vr))]
+                kk, vv = keys[s][l]
+                assert kk.shape[1] == int(path.cache.lens[s, l])
+                for h in range(H):
+                    o, m, _ = R.attend(qr[l, h, t], kk[h // (H // Hkv)], vv[h // (H // Hkv)], float(scale[l]), kk.shape[1] - lengths[s])
+                    close(out[l:l + 1, h:h + 1, t], o[None, None], m[None, None], BF16)
+
+    prefill([0, 2, 3], [70, 1, 130], [56, 2, 100])
+    extend([5, 0, 1, 40], pad=3)
+    for _ in range(3):
+        extend([1, 0, 1, 1])
+    free = int(path.cache.state[1])
+    path.end([0])
+    assert int(path.cache.state[1]) > free and path.cache.lens[0].tolist() == [0, 0]
+    prefill([0, 1], [200, 33], [200, 20])
+    extend([1, 2, 33, 60])
+    extend([1, 1, 1, 1])
+    # more than the pool has: nothing changes
+    before = [x.clone() for x in (path.cache.lens, path.cache.table, path.cache.ring, path.cache.state)]
+    P.prefixkv_page_resize(path.cache, torch.full_like(path.cache.lens, 399), status=path.status)
+    assert int(path.status) == 1
+    for a, b in zip((path.cache.lens, path.cache.table, path.cache.ring, path.cache.state), before):
+        assert torch.equal(a, b)
