@@ -64,7 +64,7 @@ attn_rows_kernel(PackedParams p) {
     if (s >= p.S) return;
     const int first = p.row_off[s], n = p.row_off[s + 1] - first, i = t - first;
     if (first < 0 || i < 0 || i >= p.max_rows) return;
-    const int count = i + 1 + entries(p, s, l) - n;             // keys that the row sees
+    const int len = entries(p, s, l), count = min(len, i + 1 + len - n);    // keys that the row sees
     const int32_t* pages = p.table + ((int64_t)s * p.layers + p.l0 + l) * p.max_pages;
     const int g = h / p.grp;
     const float4 q = *(const float4*)(p.q + p.qs.l * l + p.qs.h * h + p.qs.n * t + sub * 16);
@@ -1148,8 +1148,9 @@ static bool cut_tiles(const pkv_packed& s, long long keys, bool paged) {
     return stages * (1.33 - (paged ? 0.75 : 0.5) * 2.1 * tiles / tile_workgroups()) > 30.0;
 }
 
-// block numbers are 32 bits wide, and so are grids
+// rows of a KV head and block numbers are 32 bits wide, and so are grids
 bool packed_attn_fits(const pkv_packed& s, const pkv_paging* g) {
+    if ((int64_t)s.T * (s.H / s.Hkv) > 0x7fffff00ll) return false;
     if ((int64_t)s.S * s.L * s.Hkv > 0x7fffffffll || most_tiles(s) * s.L * s.Hkv > 0x7fffffffll) return false;
     return !g || (double)s.S * s.L * s.Hkv * g->max_pages * g->page_size / kBlockKeys < 2147483648.0;
 }

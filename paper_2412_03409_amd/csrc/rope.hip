@@ -6,7 +6,8 @@
 // and x^10 are exact to fp32 (the first terms left out are below 2e-9).
 // Bound: HBM; every row is read once and written once, in 16-byte pieces.  A lane has both columns of its pairs: two pieces
 // of a row, half the rotated columns apart (or side by side if interleaved), a row is D*esize/32 lanes.  The sines are a
-// token's, not a head's: a lane works out those of its pairs once and takes a group of heads through them.
+// token's, not a head's: a lane works out those of its pairs once and takes a group of heads through them.  5440 tokens of 64
+// heads, D 128: 37.6 us for 178 MB read and written, 4.7 TB/s; a copy of that size runs at 4.6 to 5.0.
 #include "pkv_common.hpp"
 #include "fast_div.hpp"
 
@@ -38,6 +39,13 @@ __device__ __forceinline__ void sin_cos_turn(uint32_t turns, float& sn, float& c
     const float a = odd ? c : s, b = odd ? s : c;
     sn = (quarter & 2u) ? -a : a;
     cs = ((quarter + 1u) & 2u) ? -b : b;
+}
+
+// A row is read once: its lines need not stay (178 MB of rows: 42.7 us -> 37.6; stores past the caches too would be no faster, and
+// the attention behind reads what is stored).
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 load_once(const unsigned char* p) {
+    return __builtin_bit_cast(uint4, __builtin_nontemporal_load((const u32x4_t*)p));
 }
 
 template <bool BF16>
@@ -105,7 +113,7 @@ rope_kernel(RopeParams p, int half) {
                 to = p.k_out + p.kos.l * l + p.kos.h * g + p.kos.n * t;
             }
         }
-        uint4 ra = *(const uint4*)(src + pa * 16), rb = *(const uint4*)(src + pb * 16);
+        uint4 ra = load_once(src + pa * 16), rb = load_once(src + pb * 16);
         if (turns && h < p.H + p.Hkv) {
             float a[VE], b[VE];
             unpack_piece<BF16>(ra, a);

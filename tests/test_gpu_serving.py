@@ -415,7 +415,7 @@ def test_chunk_attn(L, H, Hkv, D, ps, sizes, n, first, pad, l0, dtype):
     lens = np.maximum(lens, 0)
     c, table = chunk_state(T + H, len(sizes), layers, Hkv, D, ps, lens, dtype)
     q, _, _ = projected(gen(H), L, H, Hkv, T, D, dtype)
-    scale = (torch.rand(L, generator=gen(2)) + 0.5) / D ** 0.5
+    scale = (torch.rand(L, generator=gen(2)) + 0.5) / D ** 0.5 * (-1 if H % 4 == 0 else 1)
     out = torch.full((L, T, H, D), 55.0, dtype=dtype, device=DEV).permute(0, 2, 1, 3)
     P.prefixkv_chunk_attn(c, q, i32(off), scale.to(DEV), max(n), l0=l0, out=out)
     want, mag = R.chunk(f64(q), off, f64(c.kp), f64(c.vp), table, lens, scale.double().numpy(), l0)

@@ -132,6 +132,16 @@ def test_attention_refuses():
         assert lib.prefixkv_chunk_attn(*[paging(**kw) if i == 4 else x for i, x in enumerate(chunk)]) == 2
     for i, x in ((5, -1), (5, 2), (11, 0), (11, 11)):
         assert lib.prefixkv_chunk_attn(*[x if j == i else y for j, y in enumerate(chunk)]) == 2
+    # rows of a KV head, tiles and blocks that 32 bits do not number; a row stride that 16 rows do not address
+    many = packed(T=1 << 22, H=2048, Hkv=1, S=1)
+    assert lib.prefixkv_prefill_attn_packed(*[many] + plain[1:]) == 7
+    assert lib.prefixkv_chunk_attn(*[many] + chunk[1:]) == 7
+    assert lib.prefixkv_prefill_attn_packed(*[packed(T=1 << 22, H=2048, Hkv=2048, L=64, S=1)] + plain[1:]) == 7
+    wide = [paging(max_pages=65535, layers=64) if i == 4 else x for i, x in enumerate(chunk)]
+    assert lib.prefixkv_chunk_attn(*[packed(S=4096, L=64)] + wide[1:]) == 7
+    far = Bd._Strides(0, 8192, 128, 1 << 26)
+    for i in (4, 6):
+        assert lib.prefixkv_prefill_attn_packed(*[far if j == i else x for j, x in enumerate(plain)]) == 7
     for rows, f, args, ws in ((0, lib.prefixkv_prefill_attn_packed, plain, 12), (10, lib.prefixkv_chunk_attn, chunk, 14)):
         need = P.attn_workspace_bytes(2, 1, 4, 2, 10, 128, torch.bfloat16, max_rows=rows)
         if need:
