@@ -615,8 +615,12 @@ class PagedCache:
             raise ValueError("table must be [S,layers,max_pages], lens [S,layers], ring [num_pages], state [2]")
         P, Hkv, ps, D = self.kp.shape
         pool = (Hkv, D, self.kp.dtype) if self.kp.is_contiguous() and self.vp.is_contiguous() else None
+        device = {t.device for t in (self.kp, self.vp, self.table, self.lens, self.ring, self.state)}
+        if len(device) > 1:
+            raise ValueError("the parts of a cache must be on one device")
         for name, x in (("_paging", C.byref(_Paging(P, ps, self.table.shape[2], self.table.shape[1]))), ("_pool", pool),
-                        ("_S", self.table.shape[0]), ("_layers", self.table.shape[1])):
+                        ("_S", self.table.shape[0]), ("_layers", self.table.shape[1]), ("_seg", self.lens.shape),
+                        ("_offs", (self.table.shape[0] + 1,)), ("_device", self.kp.get_device())):
             object.__setattr__(self, name, x)
 
 
@@ -631,11 +635,12 @@ def paged_cache(S: int, layers: int, Hkv: int, D: int, page_size: int, num_pages
                       state=torch.tensor([0, num_pages], dtype=torch.int32, device=device))
 
 
-def _here(*ts) -> int:
-    """The current stream's handle; every tensor has to be on the current GPU."""
-    if not ts[0].is_cuda:
+def _here(d: int, *ts) -> int:
+    """The current stream's handle; d (a tensor's or a cache's GPU) has to be the current one, and every tensor on it."""
+    if d < 0:
         raise ValueError("all tensors must be on the GPU")
-    d = torch.cuda.current_device()
+    if d != torch.cuda.current_device():
+        raise ValueError("all tensors must be on the current GPU")
     for t in ts:
         if t is not None and t.get_device() != d:
             raise ValueError("all tensors must be on the current GPU")
@@ -656,7 +661,7 @@ def page_workspace_bytes(S: int, layers: int) -> int:
 def _page_out(cache: PagedCache, status, lens_out, state_out, ws):
     lens = cache.lens
     status = torch.empty(1, dtype=torch.int32, device=lens.device) if status is None else _i32_like(status, (1,), "status")
-    lens_out = lens if lens_out is None else _i32_like(lens_out, lens.shape, "lens_out")
+    lens_out = lens if lens_out is None else _i32_like(lens_out, cache._seg, "lens_out")
     state_out = cache.state if state_out is None else _i32_like(state_out, (2,), "state_out")
     return status, lens_out, state_out, _ws(page_workspace_bytes(cache._S, cache._layers), lens.device, ws)
 
@@ -667,8 +672,8 @@ def prefixkv_page_resize(cache: PagedCache, target: torch.Tensor, status: Option
     """Gives every segment the length target [S,layers] i32: pages come from the ring or go back to it; the cache's lens and
     state are updated (or lens_out, state_out written in their place).  -> status [1] i32, 0 if it was done."""
     lens, table, ring, state = cache.lens, cache.table, cache.ring, cache.state
-    stream = _here(target, lens, table, ring, state, status, lens_out, state_out, ws)
-    _i32_like(target, lens.shape, "target")
+    stream = _here(cache._device, target, status, lens_out, state_out, ws)
+    _i32_like(target, cache._seg, "target")
     status, lens_out, state_out, w = _page_out(cache, status, lens_out, state_out, ws)
     rc = load().prefixkv_page_resize(cache._S, cache._paging, target.data_ptr(), lens.data_ptr(), table.data_ptr(),
                                      ring.data_ptr(), state.data_ptr(), lens_out.data_ptr(), state_out.data_ptr(),
@@ -684,9 +689,9 @@ def prefixkv_page_append(cache: PagedCache, row_off: torch.Tensor, T: int, slots
     """Room for the new rows of every sequence, in every layer: row_off [S+1] i32, T packed rows
     -> (slots [layers,T] i64, status [1] i32)."""
     lens, table, ring, state = cache.lens, cache.table, cache.ring, cache.state
-    stream = _here(row_off, lens, table, ring, state, slots, status, lens_out, state_out, ws)
+    stream = _here(cache._device, row_off, slots, status, lens_out, state_out, ws)
     T = index(T)
-    _i32_like(row_off, (cache._S + 1,), "row_off")
+    _i32_like(row_off, cache._offs, "row_off")
     if slots is None:
         slots = torch.empty((cache._layers, T), dtype=torch.int64, device=lens.device)
     elif slots.dtype is not torch.int64 or slots.shape != (cache._layers, T) or not slots.is_contiguous():
@@ -711,6 +716,9 @@ class RopePlan:
         if self.freq.dtype != torch.int64 or self.freq.dim() != 1 or not self.freq.is_contiguous():
             raise ValueError("freq must be contiguous i64 [rot_dim/2]")
         _i32_like(self.axis, self.freq.shape, "axis")
+        if self.axis.device != self.freq.device:
+            raise ValueError("freq and axis must be on one device")
+        object.__setattr__(self, "_device", self.freq.get_device())
         object.__setattr__(self, "_args", C.byref(_Rope(self.freq.data_ptr(), self.axis.data_ptr(), 2 * self.freq.shape[0],
                                                         self.axes, int(self.interleaved))))
 
@@ -778,7 +786,7 @@ def prefixkv_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, pla
                   q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
     """q [L,H,T,D], k [L,Hkv,T,D] (bf16 or f32, any strides with D contiguous), positions [axes,T] i32
     -> (q_out, k_out), rotated; q_out = q and k_out = k rotate in place."""
-    stream = _here(q, k, positions, plan.freq, plan.axis, q_out, k_out)
+    stream = _here(plan._device, q, k, positions, q_out, k_out)
     q_out = torch.empty_like(q) if q_out is None else q_out
     k_out = torch.empty_like(k) if k_out is None else k_out
     s, qs, ks, kos, qos = _rope_args(q.shape, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, q_out.shape, q_out.stride(),
@@ -795,7 +803,7 @@ def prefixkv_rope_store(cache: PagedCache, q: torch.Tensor, k: torch.Tensor, v: 
                         plan: RopePlan, slots: torch.Tensor, q_out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Rotates q [L,H,T,D] and k [L,Hkv,T,D] and stores k and v into the cache's pages at slots [L,T] i64 -> q_out."""
     kp, vp = cache.kp, cache.vp
-    stream = _here(q, k, v, positions, plan.freq, plan.axis, slots, q_out, kp, vp)
+    stream = _here(plan._device, q, k, v, positions, slots, q_out, kp)
     q_out = torch.empty_like(q) if q_out is None else q_out
     s, qs, ks, vs, qos = _rope_args(q.shape, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, q_out.shape, q_out.stride(),
                                     q_out.dtype, v.shape, v.stride(), v.dtype, positions.shape, positions.stride(),
@@ -813,7 +821,7 @@ def prefixkv_compact_paged(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, 
                            kept_pos: Optional[torch.Tensor] = None, l0: int = 0) -> PagedCache:
     """prefixkv_compact into the cache's pages: k,v [B,L,Hkv,N,D], order [B,L,N] i32, lengths [B,L] i32; sequence b of the
     batch is sequence b of the cache, layer l its layer l0 + l.  kept_pos [B,L,N] i32, optional output."""
-    stream = _here(k, v, order, lengths, kept_pos, cache.kp, cache.vp, cache.table)
+    stream = _here(cache._device, k, v, order, lengths, kept_pos)
     B, L, Hkv, N, D = k.shape
     if v.shape != k.shape or v.dtype != k.dtype:
         raise ValueError("v must match k")
@@ -859,7 +867,7 @@ def prefixkv_prefill_attn_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tens
     """Causal attention of packed prompts: q [L,H,T,D], k/v [L,Hkv,T,D] (bf16), row_off [S+1] i32, scale [L] f32
     -> (out [L,H,T,D], lse [L*H*T] f32: [L,H,n] of each sequence one behind the other).  Rows that belong to no sequence are
     left as they are."""
-    stream = _here(q, k, v, row_off, scale, out, lse, ws)
+    stream = _here(q.get_device(), k, v, row_off, scale, out, lse, ws)
     out = torch.empty_like(q) if out is None else out
     S = row_off.numel() - 1
     s, qs, os_, need = _attn_args(q.shape, q.stride(), q.dtype, out.shape, out.stride(), out.dtype, S, k.shape[1], 0)
@@ -886,15 +894,15 @@ def prefixkv_chunk_attn(cache: PagedCache, q: torch.Tensor, row_off: torch.Tenso
     """Attention of new rows q [L,H,T,D] over the cache's layers l0 ... l0+L-1, which hold their keys and values already:
     row_off [S+1] i32, scale [L] f32, max_rows = the most rows of a sequence -> out [L,H,T,D]."""
     kp, vp, table, lens = cache.kp, cache.vp, cache.table, cache.lens
-    stream = _here(q, row_off, scale, out, ws, kp, vp, table, lens)
+    stream = _here(cache._device, q, row_off, scale, out, ws)
     out = torch.empty_like(q) if out is None else out
     pool, max_rows = cache._pool, index(max_rows)
     qsh = q.shape
     if pool is None or pool[1:] != (qsh[3], q.dtype):
         raise ValueError("the cache must have q's head dimension and dtype, and contiguous pools")
     s, qs, os_, need = _attn_args(qsh, q.stride(), q.dtype, out.shape, out.stride(), out.dtype, cache._S, pool[0], max_rows)
-    _i32_like(row_off, (cache._S + 1,), "row_off")
-    if scale.dtype is not torch.float32 or scale.shape != (qsh[0],) or not scale.is_contiguous():
+    _i32_like(row_off, cache._offs, "row_off")
+    if scale.dtype is not torch.float32 or scale.shape != qsh[:1] or not scale.is_contiguous():
         raise ValueError("scale must be contiguous f32 [L]")
     w = _ws(need, q.device, ws)
     rc = load().prefixkv_chunk_attn(s, q.data_ptr(), qs, row_off.data_ptr(), cache._paging, int(l0), kp.data_ptr(),

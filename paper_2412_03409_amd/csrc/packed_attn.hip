@@ -502,20 +502,21 @@ __device__ __forceinline__ int find_segment(int segs, int lane, int64_t x, int64
     return segs;
 }
 
-// All segments and their places.  Up to 64 of them (a layer of 64 sequences) are read once, a lane each; beyond, they are read again
-// where they are asked for.
+// `count` segments, first + i * step, and their places.  Up to 64 of them (a layer of 64 sequences) are read once, a lane each; beyond,
+// they are read again where they are asked for.
 template <bool PAGED, class F>
 struct Looked {
     const Work& p;
-    int lane;
+    int lane, count, first, step;
     F cost;                         // places of a segment
-    Segment mine;                   // segment `lane`
-    int64_t upto, all;              // places of the segments up to `lane`; of all
+    Segment mine;                   // the segment of this lane
+    int64_t upto, all;              // places of the segments up to that one; of all
 
-    __device__ __forceinline__ Looked(const Work& work, int ln, F f) : p(work), lane(ln), cost(f) {
-        mine = segment<PAGED>(p, min(lane, p.segs - 1));
-        upto = lane < p.segs ? cost(mine) : 0;
-        for (int i = lane + kWave; i < p.segs; i += kWave) upto += cost(segment<PAGED>(p, i));
+    __device__ __forceinline__ Looked(const Work& work, int ln, int n, int from, int by, F f)
+        : p(work), lane(ln), count(n), first(from), step(by), cost(f) {
+        mine = segment<PAGED>(p, first + min(lane, count - 1) * step);
+        upto = lane < count ? cost(mine) : 0;
+        for (int i = lane + kWave; i < count; i += kWave) upto += cost(segment<PAGED>(p, first + i * step));
 #pragma unroll
         for (int d = 1; d < kWave; d <<= 1) {
             const int64_t up = shfl_up64(upto, d);
@@ -523,9 +524,9 @@ struct Looked {
         }
         all = lane64(upto, kWave - 1);
     }
-    // the segment that holds place x, the place in it, and what the segment is
+    // which of them holds place x, the place in it, and what it is
     __device__ __forceinline__ int find(int64_t x, int64_t& in, Segment& sg) const {
-        if (p.segs <= kWave) {
+        if (count <= kWave) {
             const int j = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > x));
             in = x - (j == 0 ? 0 : lane64(upto, j - 1));
             sg.s = __builtin_amdgcn_readlane(mine.s, j); sg.l = __builtin_amdgcn_readlane(mine.l, j);
@@ -534,8 +535,8 @@ struct Looked {
             sg.before = __builtin_amdgcn_readlane(mine.before, j); sg.end = __builtin_amdgcn_readlane(mine.end, j);
             return j;
         }
-        const int j = find_segment(p.segs, lane, x, in, [&](int i) { return cost(segment<PAGED>(p, i)); });
-        sg = uniform_segment<PAGED>(p, j);
+        const int j = find_segment(count, lane, x, in, [&](int i) { return cost(segment<PAGED>(p, first + i * step)); });
+        sg = uniform_segment<PAGED>(p, first + j * step);
         return j;
     }
 };
@@ -633,7 +634,7 @@ __device__ __forceinline__ Cut uniform(const Cut& c) {
 // together, so that the launch does not end on the long tiles of a single one.  Else heads alternate.  Within a head: sequence by
 // sequence, the last tile first, whose rows see the most.
 template <bool PAGED>
-__device__ __forceinline__ Cut tile_of(const TileParams& p, int lane, int bid) {
+__device__ __forceinline__ Cut tile_of(const TileParams& p, int lane, int bid, Segment& sg) {
     int head, tt;
     if (p.heads_per_xcd > 0) {
         const int xcd = bid % kXcds, j = bid / kXcds, hx = p.heads_per_xcd, lead = hx - (int)p.by_tail.d, tiles = (int)p.by_tiles.d;
@@ -646,10 +647,11 @@ __device__ __forceinline__ Cut tile_of(const TileParams& p, int lane, int bid) {
         head = x.r; tt = x.q;
     }
     const DivMod lg = uniform_div_mod(head, p.by_hkv);
-    auto tiles = [&](int s) { return (int64_t)((segment<PAGED>(p, s * p.a.L + lg.q).rows + kTileRows - 1) / kTileRows); };
+    auto tiles = [&](const Segment& x) { return (int64_t)((x.rows + kTileRows - 1) / kTileRows); };
+    const Looked<PAGED, decltype(tiles)> looked(p, lane, p.a.S, lg.q, p.a.L, tiles);      // the layer's sequences
+    if (tt >= looked.all) return {p.segs, 0, 0, 0};
     int64_t in;
-    const int s = find_segment(p.a.S, lane, tt, in, tiles);
-    if (s >= p.a.S) return {p.segs, 0, 0, 0};
+    const int s = looked.find(tt, in, sg);
     return {s * p.a.L + lg.q, lg.r, (int)in, 0};
 }
 
@@ -666,8 +668,9 @@ attn_tiles_kernel(TileParams p) {
     const int ln = lane & 31, hf = lane >> 5;
     int wg = 0;
     Cut from, to;
+    Segment sg;
     if constexpr (WHOLE) {
-        from = to = uniform(tile_of<PAGED>(p, lane, (int)blockIdx.x));
+        from = to = uniform(tile_of<PAGED>(p, lane, (int)blockIdx.x, sg));
     } else {
         // neighbours in the order of the work run on one XCD and share keys through its L2
         wg = (int)xcd_swizzle(blockIdx.x, (uint32_t)p.workgroups);
@@ -675,7 +678,7 @@ attn_tiles_kernel(TileParams p) {
             const TileCost<PAGED> t(p, x);
             return t.up_to(t.tiles) * a.Hkv;
         };
-        const Looked<PAGED, decltype(cost)> looked(p, lane, cost);
+        const Looked<PAGED, decltype(cost)> looked(p, lane, p.segs, 0, 1, cost);
         const Shares<PAGED, decltype(looked)> sh(p, looked);
         from = uniform(sh.cut(wg));
         to = uniform(sh.cut(wg + 1));
@@ -687,7 +690,7 @@ attn_tiles_kernel(TileParams p) {
     tl.offsets(lane);
     int seg = from.seg, g = from.head, tile = from.tile, stage = from.stage;
     while (seg < p.segs && seg <= to.seg) {                 // (`to` may be a segment without rows)
-        const Segment sg = uniform_segment<PAGED>(p, seg);
+        if constexpr (!WHOLE) sg = uniform_segment<PAGED>(p, seg);
         const int tiles = (sg.rows + kTileRows - 1) / kTileRows;
         if (!WHOLE && tile >= tiles) { tile = 0; g = 0; ++seg; continue; }  // a segment without rows
         if constexpr (WHOLE) tile = tiles - 1 - tile;
@@ -921,7 +924,7 @@ attn_stream_kernel(StreamParams p) {
 
     // the launch's blocks, and this wavefront's: segment by segment, KV head by KV head
     auto blocks = [&](const Segment& x) { return (int64_t)blocks_of(x) * a.Hkv; };
-    const Looked<true, decltype(blocks)> looked(p, lane, blocks);
+    const Looked<true, decltype(blocks)> looked(p, lane, p.segs, 0, 1, blocks);
     const int all_blocks = (int)looked.all;                                // (below 2^31: the call is refused otherwise)
     const int share = max(kLeastBlocks, (all_blocks + p.waves - 1) / p.waves);
     if (wave == 0 && lane == 0) *p.share = share;
