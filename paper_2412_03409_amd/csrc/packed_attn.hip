@@ -207,6 +207,20 @@ __device__ __forceinline__ void store_columns(const f32x16_t& o, unsigned char* 
     }
 }
 
+// Whether `count` KB of staged values, at 1 KB a read of the wavefront, hold one that is infinite or NaN.
+template <int COUNT>
+__device__ __forceinline__ bool wild_values(const unsigned char* sV, int lane) {
+    v2u16_t big = {0, 0};
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        const uint4 w = *(const uint4*)(sV + i * 1024 + lane * 16);
+        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) big = __builtin_elementwise_max(big, __builtin_bit_cast(v2u16_t, x[e] & 0x7fff7fffu));
+    }
+    return __builtin_amdgcn_ballot_w64(big.x >= 0x7f80 || big.y >= 0x7f80) != 0;
+}
+
 // Softmax state and output of the 32 rows of a wavefront: row lane % 32; register r of o[dt] is column
 // 32 dt + 8 (r / 4) + 4 (lane / 32) + r % 4.
 template <int D>
@@ -254,11 +268,12 @@ struct RowTile {
     }
 
     // NKT tiles of 32 staged keys.  MASKED: the row sees the keys up to `lim` (of the stage), bit x of `bad` hides keys
-    // 16x ... 16x+15, and tiles from `tiles` on are seen by no row of the wavefront.  Each tile has its own reference, the maximum up
+    // 16x ... 16x+15, tiles from `tiles` on are seen by no row of the wavefront, those in front of `full` by all of them.  Each tile has
+    // its own reference, the maximum up
     // to its end: the probabilities are rounded against it.
     template <int NKT, bool MASKED>
     __device__ __forceinline__ void attend(const unsigned char* sK, const unsigned char* sV, float qs, int lane, int lim, uint32_t bad,
-                                           int tiles) {
+                                           int tiles, int full) {
         constexpr int ROWB = D * 2, NJ = D / 16, NDT = D / 32, CPR = D / 8;
         const int hf = lane >> 5;
         f32x16_t s[NKT];
@@ -344,19 +359,10 @@ struct RowTile {
             }
             if constexpr (MASKED) {
                 // An infinite or NaN value that some rows must not see would reach them as 0 * value: such a tile is added up row by
-                // row, over the keys that each of them sees.  (The look costs a masked stage 2 NDT x 8 packed maxima.)
-                v2u16_t big = {0, 0};
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-#pragma unroll
-                    for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            const uint2 w = __builtin_bit_cast(uint2, lds_read_tr(sV + (32 * kt + 16 * x) * ROWB + voff[dt][y]));
-                            big = __builtin_elementwise_max(big, __builtin_bit_cast(v2u16_t, w.x & 0x7fff7fffu));
-                            big = __builtin_elementwise_max(big, __builtin_bit_cast(v2u16_t, w.y & 0x7fff7fffu));
-                        }
-                if (__builtin_amdgcn_ballot_w64(big.x >= 0x7f80 || big.y >= 0x7f80)) {
+                // row, over the keys that each of them sees.  (Looked for where a row may not see a key.  It takes 1.5 us
+                // of a prompt of 680 rows, H32, 21.6 us; a look at the copies in front of the barrier, a quarter each, took 2.5, and
+                // working a tile over again whose output is not finite more than that in spilled registers.)
+                if (kt >= full && wild_values<32 * ROWB / 1024>(sV + 32 * kt * ROWB, lane)) {
                     const int ln = lane & 31;
 #pragma unroll 1
                     for (int r = 0; r < 16; ++r) {
@@ -478,64 +484,61 @@ __device__ __forceinline__ int64_t lane64(int64_t x, int j) {
     return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), j) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, j));
 }
 
-// The segment that holds place x of a launch, and the place in it: segment i has cost(i) places.
-template <class F>
-__device__ __forceinline__ int find_segment(int segs, int lane, int64_t x, int64_t& in, F cost) {
-    int64_t base = 0;
-    for (int c = 0; c < segs; c += kWave) {
-        const int64_t mine = c + lane < segs ? cost(c + lane) : 0;
-        int64_t incl = mine;
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) {
-            const int64_t up = shfl_up64(incl, d);
-            if (lane >= d) incl += up;
-        }
-        const unsigned long long at = __builtin_amdgcn_ballot_w64(base + incl > x);
-        if (at != 0) {
-            const int j = __builtin_ctzll(at);
-            in = x - base - lane64(incl, j) + lane64(mine, j);
-            return c + j;
-        }
-        base += lane64(incl, kWave - 1);
-    }
-    in = 0;
-    return segs;
-}
+__device__ __forceinline__ int up(int x, int d) { return __shfl_up(x, d, kWave); }
+__device__ __forceinline__ int64_t up(int64_t x, int d) { return shfl_up64(x, d); }
+__device__ __forceinline__ int of_lane(int x, int j) { return __builtin_amdgcn_readlane(x, j); }
+__device__ __forceinline__ int64_t of_lane(int64_t x, int j) { return lane64(x, j); }
 
-// `count` segments, first + i * step, and their places.  Up to 64 of them (a layer of 64 sequences) are read once, a lane each; beyond,
-// they are read again where they are asked for.
-template <bool PAGED, class F>
+// `count` segments, first + i * step, and their places (of type N).  Up to 64 of them (a layer of 64 sequences) are read once, a lane
+// each; beyond, they are read again where they are asked for.
+template <bool PAGED, class N, class F>
 struct Looked {
     const Work& p;
     int lane, count, first, step;
     F cost;                         // places of a segment
     Segment mine;                   // the segment of this lane
-    int64_t upto, all;              // places of the segments up to that one; of all
+    N upto, all;                    // places of the segments up to that one (of the first 64); of all
 
     __device__ __forceinline__ Looked(const Work& work, int ln, int n, int from, int by, F f)
         : p(work), lane(ln), count(n), first(from), step(by), cost(f) {
         mine = segment<PAGED>(p, first + min(lane, count - 1) * step);
-        upto = lane < count ? cost(mine) : 0;
+        upto = lane < count ? cost(mine) : (N)0;
         for (int i = lane + kWave; i < count; i += kWave) upto += cost(segment<PAGED>(p, first + i * step));
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) {
-            const int64_t up = shfl_up64(upto, d);
-            if (lane >= d) upto += up;
+        for (int d = 1; d < min(count, kWave); d <<= 1) {
+            const N before = up(upto, d);
+            if (lane >= d) upto += before;
         }
-        all = lane64(upto, kWave - 1);
+        all = of_lane(upto, min(count, kWave) - 1);
     }
     // which of them holds place x, the place in it, and what it is
-    __device__ __forceinline__ int find(int64_t x, int64_t& in, Segment& sg) const {
+    __device__ __forceinline__ int find(N x, N& in, Segment& sg) const {
         if (count <= kWave) {
             const int j = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > x));
-            in = x - (j == 0 ? 0 : lane64(upto, j - 1));
+            in = x - (j == 0 ? (N)0 : of_lane(upto, j - 1));
             sg.s = __builtin_amdgcn_readlane(mine.s, j); sg.l = __builtin_amdgcn_readlane(mine.l, j);
             sg.first = __builtin_amdgcn_readlane(mine.first, j); sg.n = __builtin_amdgcn_readlane(mine.n, j);
             sg.rows = __builtin_amdgcn_readlane(mine.rows, j); sg.len = __builtin_amdgcn_readlane(mine.len, j);
             sg.before = __builtin_amdgcn_readlane(mine.before, j); sg.end = __builtin_amdgcn_readlane(mine.end, j);
             return j;
         }
-        const int j = find_segment(count, lane, x, in, [&](int i) { return cost(segment<PAGED>(p, first + i * step)); });
+        int j = 0;
+        N base = 0;
+        for (int c = 0; c < count; c += kWave) {
+            const N here = c + lane < count ? cost(segment<PAGED>(p, first + (c + lane) * step)) : (N)0;
+            N incl = here;
+#pragma unroll
+            for (int d = 1; d < kWave; d <<= 1) {
+                const N before = up(incl, d);
+                if (lane >= d) incl += before;
+            }
+            const unsigned long long at = __builtin_amdgcn_ballot_w64(base + incl > x);
+            if (at != 0) {
+                j = c + __builtin_ctzll(at);
+                in = x - base - of_lane(incl, j - c) + of_lane(here, j - c);
+                break;
+            }
+            base += of_lane(incl, kWave - 1);
+        }
         sg = uniform_segment<PAGED>(p, first + j * step);
         return j;
     }
@@ -647,12 +650,12 @@ __device__ __forceinline__ Cut tile_of(const TileParams& p, int lane, int bid, S
         head = x.r; tt = x.q;
     }
     const DivMod lg = uniform_div_mod(head, p.by_hkv);
-    auto tiles = [&](const Segment& x) { return (int64_t)((x.rows + kTileRows - 1) / kTileRows); };
-    const Looked<PAGED, decltype(tiles)> looked(p, lane, p.a.S, lg.q, p.a.L, tiles);      // the layer's sequences
+    auto tiles = [&](const Segment& x) { return (x.rows + kTileRows - 1) / kTileRows; };
+    const Looked<PAGED, int, decltype(tiles)> looked(p, lane, p.a.S, lg.q, p.a.L, tiles);      // the layer's sequences
     if (tt >= looked.all) return {p.segs, 0, 0, 0};
-    int64_t in;
+    int in;
     const int s = looked.find(tt, in, sg);
-    return {s * p.a.L + lg.q, lg.r, (int)in, 0};
+    return {s * p.a.L + lg.q, lg.r, in, 0};
 }
 
 template <int D, bool PAGED, bool WHOLE>
@@ -678,7 +681,7 @@ attn_tiles_kernel(TileParams p) {
             const TileCost<PAGED> t(p, x);
             return t.up_to(t.tiles) * a.Hkv;
         };
-        const Looked<PAGED, decltype(cost)> looked(p, lane, p.segs, 0, 1, cost);
+        const Looked<PAGED, int64_t, decltype(cost)> looked(p, lane, p.segs, 0, 1, cost);
         const Shares<PAGED, decltype(looked)> sh(p, looked);
         from = uniform(sh.cut(wg));
         to = uniform(sh.cut(wg + 1));
@@ -704,6 +707,7 @@ attn_tiles_kernel(TileParams p) {
         const bool mine = r0 < sg.rows, real = row < sg.rows;
         const RowAt ra = row_at(real ? row : mine ? r0 : 0, p.grp);         // (rows that do not exist repeat one that does)
         const int lim = sg.before + ra.token;                               // the last key that the row sees
+        const int lim_first = sg.before + __builtin_amdgcn_readfirstlane(row_at(mine ? r0 : 0, p.grp).token);
         const int lim_last = sg.before + __builtin_amdgcn_readfirstlane(row_at(max(min(sg.rows, r0 + 32) - 1, 0), p.grp).token);
         const int h = g * a.grp + ra.head;
         const int64_t t = sg.first + ra.token;
@@ -792,20 +796,22 @@ attn_tiles_kernel(TileParams p) {
         if (plain & 1) {                                         // (the first stage of an odd number is in the other pair)
             sync();
             if (st + 1 < st1) bad_a = issue(st + 1, sKa, sVa);
-            tl.template attend<2, false>(sKb, sVb, qs, lane, 0, 0u, 2);
+            tl.template attend<2, false>(sKb, sVb, qs, lane, 0, 0u, 2, 2);
             ++st;
         }
         for (; st < st0 + plain; st += 2) {
             sync();
             issue(st + 1, sKb, sVb);
-            tl.template attend<2, false>(sKa, sVa, qs, lane, 0, 0u, 2);
+            tl.template attend<2, false>(sKa, sVa, qs, lane, 0, 0u, 2, 2);
             sync();
             if (st + 2 < st1) bad_a = issue(st + 2, sKa, sVa);
-            tl.template attend<2, false>(sKb, sVb, qs, lane, 0, 0u, 2);
+            tl.template attend<2, false>(sKb, sVb, qs, lane, 0, 0u, 2, 2);
         }
         auto attend = [&](int st, const unsigned char* sK, const unsigned char* sV, uint32_t bad) {
             const int key0 = st * kStage;
-            if (mine && key0 <= lim_last) tl.template attend<2, true>(sK, sV, qs, lane, lim - key0, bad, key0 + 32 <= lim_last ? 2 : 1);
+            if (mine && key0 <= lim_last)
+                tl.template attend<2, true>(sK, sV, qs, lane, lim - key0, bad, key0 + 32 <= lim_last ? 2 : 1,
+                                            bad != 0 ? 0 : (max(lim_first - key0, -1) + 1) / 32);
         };
         for (; st < st1; st += 2) {
             sync();
@@ -924,7 +930,7 @@ attn_stream_kernel(StreamParams p) {
 
     // the launch's blocks, and this wavefront's: segment by segment, KV head by KV head
     auto blocks = [&](const Segment& x) { return (int64_t)blocks_of(x) * a.Hkv; };
-    const Looked<true, decltype(blocks)> looked(p, lane, p.segs, 0, 1, blocks);
+    const Looked<true, int64_t, decltype(blocks)> looked(p, lane, p.segs, 0, 1, blocks);
     const int all_blocks = (int)looked.all;                                // (below 2^31: the call is refused otherwise)
     const int share = max(kLeastBlocks, (all_blocks + p.waves - 1) / p.waves);
     if (wave == 0 && lane == 0) *p.share = share;
@@ -1019,8 +1025,8 @@ attn_stream_kernel(StreamParams p) {
     };
     auto attend = [&](const unsigned char* sK, const unsigned char* sV, uint32_t bad) {
         const int key0 = cw.blk * kBlockKeys;
-        if (key0 + kBlockKeys - 1 <= sg.before && bad == 0) tl.template attend<1, false>(sK, sV, qs, lane, 0, 0u, 1);
-        else tl.template attend<1, true>(sK, sV, qs, lane, lim - key0, bad, 1);
+        if (key0 + kBlockKeys - 1 <= sg.before && bad == 0) tl.template attend<1, false>(sK, sV, qs, lane, 0, 0u, 1, 1);
+        else tl.template attend<1, true>(sK, sV, qs, lane, lim - key0, bad, 1, 0);
     };
     // one block of the work: `more` blocks are in flight behind it
     auto work = [&](int b, const unsigned char* sK, const unsigned char* sV, uint32_t bad) {
