@@ -431,8 +431,8 @@ int prefixkv_prefill_attn_packed(const pkv_packed *shape, const void *q, pkv_str
  *   ws [dev]: prefixkv_attn_workspace_bytes(shape, max_rows) bytes, 16-byte aligned (NULL if that is 0).
  *       Calls on different streams need workspaces of their own.
  * S * L * Hkv * max_pages * page_size < 2^36 (PKV_ERR_UNSUPPORTED otherwise: fewer layers a call).
- * For both attention calls T * H / Hkv and the tiles of 128 such rows over all layers and KV heads stay below
- * 2^31 (PKV_ERR_UNSUPPORTED otherwise). */
+ * For both attention calls T * H / Hkv stays below 2^31 - 256, and S * L * Hkv and the tiles of 128 such rows
+ * over all sequences, layers and KV heads below 2^24 (PKV_ERR_UNSUPPORTED otherwise: fewer layers a call). */
 int prefixkv_chunk_attn(const pkv_packed *shape, const void *q, pkv_strides qs, const int32_t *row_off,
                         const pkv_paging *paging, int l0, const void *kp, const void *vp,
                         const int32_t *table, const int32_t *lens, const float *scale, int max_rows,

@@ -1157,10 +1157,10 @@ static bool cut_tiles(const pkv_packed& s, long long keys, bool paged) {
     return stages * (1.33 - (paged ? 0.75 : 0.5) * 2.1 * tiles / tile_workgroups()) > 30.0;
 }
 
-// rows of a KV head and block numbers are 32 bits wide, and so are grids
+// rows of a KV head and block numbers are 32 bits wide, and so are the threads of a grid (256 of a workgroup)
 bool packed_attn_fits(const pkv_packed& s, const pkv_paging* g) {
     if ((int64_t)s.T * (s.H / s.Hkv) > 0x7fffff00ll) return false;
-    if ((int64_t)s.S * s.L * s.Hkv > 0x7fffffffll || most_tiles(s) * s.L * s.Hkv > 0x7fffffffll) return false;
+    if ((int64_t)s.S * s.L * s.Hkv >= 1 << 24 || most_tiles(s) * s.L * s.Hkv >= 1 << 24) return false;
     return !g || (double)s.S * s.L * s.Hkv * g->max_pages * g->page_size / kBlockKeys < 2147483648.0;
 }
 

@@ -8,6 +8,7 @@ PagedPath  sequences of different lengths that come, ask again and go: packed pr
 """
 from __future__ import annotations
 
+from operator import index
 from typing import Optional
 
 import torch
@@ -136,14 +137,19 @@ class PagedPath:
 
     def prefill(self, places, lengths, q, k, v, positions, budgets, kept_pos=None):
         """Prompts of these lengths, packed, for sequences that begin at `places`; budgets[i] of the L * lengths[i] entries are
-        kept.  q, k are rotated in place.  -> attention output [L,H,T,D].  kept_pos: a list that receives the kept positions."""
+        kept.  q, k are rotated in place.  A place that still has a sequence is given to the new one.  -> attention output
+        [L,H,T,D] (whatever `status`).  kept_pos: a list that receives the kept positions, ascending, -1 behind them."""
+        places, lengths = [index(s) for s in places], [index(n) for n in lengths]
+        if len(set(places)) != len(places) or any(not 0 <= s < self.S for s in places):
+            raise ValueError(f"places must be different numbers in 0 ... {self.S - 1}")
+        if not len(places) == len(lengths) == len(budgets) or any(n < 1 for n in lengths) or sum(lengths) > q.shape[2]:
+            raise ValueError("a length and a budget per place, rows for all of them")
         off = self._offsets(lengths)
         B_.prefixkv_rope(q, k, positions, self.plan, q_out=q, k_out=k)
         out, lse = B_.prefixkv_prefill_attn_packed(q, k, v, off, self.scale)
         rank, a = [], 0
         self.target.copy_(self.cache.lens)
         for place, n, budget in zip(places, lengths, budgets):
-            n = int(n)
             rows = slice(a, a + n)
             imp = B_.prefixkv_importance(q[None, :, :, rows], k[None, :, :, rows], self.scale,
                                          lse=lse[self.L * self.H * a:self.L * self.H * (a + n)].view(1, self.L, self.H, n))
@@ -153,8 +159,7 @@ class PagedPath:
             a += n
         B_.prefixkv_page_resize(self.cache, self.target, status=self.status, ws=self.page_ws)
         for place, rows, sel in rank:
-            # (after a refused call lens is what it was: nothing is stored then)
-            lengths_now = torch.minimum(sel.lengths, self.cache.lens[place:place + 1])
+            lengths_now = sel.lengths * (self.status == 0)      # nothing is stored after a refused call
             pos = None if kept_pos is None else torch.full_like(sel.order, -1)
             B_.prefixkv_compact_paged(self._at(place), k[None, :, :, rows], v[None, :, :, rows], sel.order, lengths_now, kept_pos=pos)
             if kept_pos is not None:
@@ -169,6 +174,8 @@ class PagedPath:
     def extend(self, lengths, q, k, v, positions):
         """Further rows of every sequence (lengths[s] of place s, 0 for one that waits): they are stored, and attend to what the
         cache holds and to each other.  One row each is a decode step.  -> attention output [L,H,T,D]."""
+        if len(lengths) != self.S or any(n < 0 for n in lengths) or sum(lengths) > q.shape[2]:
+            raise ValueError("a length per place, rows for all of them")
         off, T = self._offsets(lengths), q.shape[2]
         slots, _ = B_.prefixkv_page_append(self.cache, off, T, status=self.status, ws=self.page_ws)
         turned = B_.prefixkv_rope_store(self.cache, q, k, v, positions, self.plan, slots)
@@ -176,6 +183,8 @@ class PagedPath:
 
     def end(self, places):
         """The sequences at these places are over: their pages are free again."""
+        if any(not 0 <= s < self.S for s in places):
+            raise ValueError(f"places must be in 0 ... {self.S - 1}")
         self.target.copy_(self.cache.lens)
         self.target[list(places)] = 0
         B_.prefixkv_page_resize(self.cache, self.target, status=self.status, ws=self.page_ws)

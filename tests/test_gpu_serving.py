@@ -608,3 +608,28 @@ def test_sequences_come_ask_again_and_go(H, Hkv, D, ps):
     assert int(path.status) == 1
     for a, b in zip((path.cache.lens, path.cache.table, path.cache.ring, path.cache.state), before):
         assert torch.equal(a, b)
+
+
+def test_a_prompt_without_pages_leaves_the_path_as_it_was():
+    """A prompt for a place that still has a sequence, refused for want of pages: every page, table row and length stays."""
+    from paper_2412_03409_amd.pipeline import PagedPath
+    L, H, Hkv, D = 2, 4, 2, 64
+    g = gen(11)
+    path = PagedPath(2, L, H, Hkv, D, torch.tensor([0.2, 0.3], device=DEV), P.rope_plan(D, device=DEV), num_pages=6, max_pages=8,
+                     page_size=16, device=DEV)
+    path.cache.kp.zero_(), path.cache.vp.zero_()
+
+    def prefill(place, n, budget, kept):
+        pos = torch.arange(n, dtype=torch.int32, device=DEV)[None]
+        return path.prefill([place], [n], *projected(g, L, H, Hkv, n, D, BF16), pos, [budget], kept_pos=kept)
+
+    kept = []
+    prefill(0, 40, 60, kept)
+    assert int(path.status) == 0 and int((kept[0] >= 0).sum()) == 60
+    c = path.cache
+    before = [x.clone() for x in (c.kp, c.vp, c.lens, c.table, c.ring, c.state)]
+    kept = []
+    prefill(0, 100, 200, kept)
+    assert int(path.status) == 1 and int((kept[0] >= 0).sum()) == 0
+    for a, b in zip((c.kp, c.vp, c.lens, c.table, c.ring, c.state), before):
+        assert torch.equal(a, b)

@@ -175,6 +175,35 @@ def test_binding_refuses():
         P.rope_plan(64, theta=0.5, device="cpu")
 
 
+def test_paths_refuse():
+    from paper_2412_03409_amd.pipeline import PagedPath
+    path = PagedPath(3, 1, 2, 1, 64, torch.ones(1), P.rope_plan(64, device="cpu"), num_pages=4, max_pages=2, device="cpu")
+    q, k = torch.zeros((1, 2, 6, 64), dtype=torch.bfloat16), torch.zeros((1, 1, 6, 64), dtype=torch.bfloat16)
+    pos = torch.zeros((1, 6), dtype=torch.int32)
+    for places, lengths, budgets in (([0, 0], [3, 3], [3, 3]), ([0, 3], [3, 3], [3, 3]), ([-1], [3], [3]), ([0, 1], [3], [3, 3]),
+                                     ([0], [3], []), ([0, 1], [0, 3], [1, 3]), ([0, 1], [3, 4], [3, 4])):
+        with pytest.raises(ValueError, match="place"):
+            path.prefill(places, lengths, q, k, k, pos, budgets)
+    for lengths in ([3, 3], [3, 4, 0], [-1, 1, 1]):
+        with pytest.raises(ValueError, match="place"):
+            path.extend(lengths, q, k, k, pos)
+    for places in ([3], [0, -1]):
+        with pytest.raises(ValueError, match="places"):
+            path.end(places)
+
+
+def test_grids_that_one_launch_does_not_hold():
+    """2^24 workgroups of 256 threads."""
+    lib = P.load()
+    # T / 128 tiles and one for each sequence, of 64 layers of 8 heads
+    plain = [A, ST, A, ST, A, ST, A, A, A, ST, A, None, 0, None]
+    assert lib.prefixkv_prefill_attn_packed(packed(T=1 << 22, H=8, Hkv=8, L=64, S=1), *plain) == 7
+    # a segment for every KV head; what is missing with one sequence less is the workspace
+    chunk = [A, ST, A, paging(layers=64, max_pages=1), 0, A, A, A, A, A, 1, A, ST, None, 0, None]
+    assert lib.prefixkv_chunk_attn(packed(S=4096, L=64, H=64, Hkv=64), *chunk) == 7
+    assert lib.prefixkv_chunk_attn(packed(S=4095, L=64, H=64, Hkv=64), *chunk) == 5
+
+
 def test_rope_plan():
     plan = P.rope_plan(64, [8, 12, 12], theta=10000.0, device="cpu")
     assert plan.axis.tolist() == [0] * 8 + [1] * 12 + [2] * 12
