@@ -1,7 +1,7 @@
 // C ABI of libprefixkv: argument validation and dispatch.  No allocation, no synchronisation; every
 // launch goes to the caller's stream.  The only state kept between calls is looked up once per device:
 // the compute-unit count, and the address of the built-in scratch array of prefixkv_select_static.
-#include "pkv_common.hpp"
+#include "packed.hpp"
 
 #include <math.h>
 

@@ -6,7 +6,7 @@
 //                         exclusive scan -> scatter) and streams its whole rows (16 B per lane) from K/V into
 //                         the segment.  Pure HBM traffic.
 //  merge_position_kernel  the positional-distance merge of Sec. 4.3 on top of a compacted cache.
-#include "pkv_common.hpp"
+#include "packed.hpp"
 
 namespace pkv {
 

@@ -21,7 +21,7 @@
 // O^T[32 columns x 32 rows] += V^T P^T with v_mfma_f32_32x32x16_bf16.  A lane holds one row's scores, so the softmax state is a
 // scalar per lane, and the probabilities, rounded to bf16 against the running maximum, are the second product's operand where
 // they are.  V^T comes from row-major V by the transposing LDS read.
-#include "pkv_common.hpp"
+#include "packed.hpp"
 #include "fast_div.hpp"
 
 namespace pkv {

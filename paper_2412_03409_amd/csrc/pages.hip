@@ -14,7 +14,7 @@
 // workgroup moves it (SMALL: one launch), else a second launch spreads it over the chip.  64 sequences of 32 layers, a row each:
 // 7.2 us, of which 3 go to the scattered table entries that one compute unit reads (all of them asked for next to the sums: 8.7).
 // 64 sequences of 40 layers resized: 4.2 + 4.2.
-#include "pkv_common.hpp"
+#include "packed.hpp"
 #include "fast_div.hpp"
 
 namespace pkv {

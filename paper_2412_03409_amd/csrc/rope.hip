@@ -8,7 +8,7 @@
 // of a row, half the rotated columns apart (or side by side if interleaved), a row is D*esize/32 lanes.  The sines are a
 // token's, not a head's: a lane works out those of its pairs once and takes a group of heads through them.  5440 tokens of 64
 // heads, D 128: 37.6 us for 178 MB read and written, 4.7 TB/s; a copy of that size runs at 4.6 to 5.0.
-#include "pkv_common.hpp"
+#include "packed.hpp"
 #include "fast_div.hpp"
 
 namespace pkv {
