@@ -633,3 +633,58 @@ def test_a_prompt_without_pages_leaves_the_path_as_it_was():
     assert int(path.status) == 1 and int((kept[0] >= 0).sum()) == 0
     for a, b in zip((c.kp, c.vp, c.lens, c.table, c.ring, c.state), before):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_pages_behind_the_first_four_gigabytes(dtype):
+    """The same sequences in the last pages of a pool of more than 2^32 bytes and in a small one: rotation with the store, paged
+    compaction and attention give the same bits."""
+    S, H, Hkv, D, ps, n = 2, 8, 4, 128, 256, [40, 3]
+    page = Hkv * ps * D * torch.finfo(dtype).bits // 8
+    high = (1 << 32) // page + 9
+    off, T = i32(offsets(n)), sum(n)
+    scale = torch.full((1,), 0.1, device=DEV)
+    plan = P.rope_plan(D, device=DEV)
+    pos = torch.arange(T, dtype=torch.int32, device=DEV)[None]
+    outs = []
+    for pages in (12, high):
+        g = gen(21)
+        q, k, v = projected(g, 1, H, Hkv, T, D, dtype)
+        kk, vv = torch.randn((2, S, 1, Hkv, 700, D), generator=g).to(dtype).to(DEV)
+        order = torch.stack([torch.randperm(700, generator=g) for _ in range(S)]).to(torch.int32).to(DEV)[:, None].contiguous()
+        lengths = i32([[600], [350]])
+        c = P.paged_cache(S, 1, Hkv, D, ps, pages, 4, dtype, DEV)
+        c.state.copy_(i32([pages - 8, 8]))                 # only the last eight pages are free
+        assert int(P.prefixkv_page_resize(c, lengths)) == 0
+        P.prefixkv_compact_paged(c, kk, vv, order, lengths)
+        slots, status = P.prefixkv_page_append(c, off, T)
+        assert int(status) == 0 and int(slots.min()) >= (pages - 8) * ps
+        q = P.prefixkv_rope_store(c, q, k, v, pos, plan, slots)
+        outs.append([P.prefixkv_chunk_attn(c, q, off, scale, 40)] +
+                    [x[c.table[s, 0, :-(-int(c.lens[s, 0]) // ps)].long()].reshape(-1, Hkv, ps, D) for s in range(S) for x in (c.kp, c.vp)])
+    for s in range(S):         # the entries (what is behind them in a page is nobody's)
+        held = lengths[s, 0] + n[s]
+        for i in (1 + 2 * s, 2 + 2 * s):
+            a, b = (o[i].permute(0, 2, 1, 3).reshape(-1, Hkv, D)[:int(held)] for o in outs)
+            assert torch.equal(a, b)
+    assert torch.equal(outs[0][0], outs[1][0])
+
+
+def test_packed_rows_far_apart():
+    """Rows of 2^25 elements: 70 of them pass 2^32 bytes."""
+    H, Hkv, D, n = 2, 1, 64, [3, 67]
+    q, k, v = projected(gen(31), 1, H, Hkv, sum(n), D, BF16)
+    off, scale = i32(offsets(n)), torch.full((1,), 0.2, device=DEV)
+    want, want_lse = P.prefixkv_prefill_attn_packed(q, k, v, off, scale)
+    room = torch.empty(sum(n) << 25, dtype=BF16, device=DEV).view(sum(n), 1 << 25)
+    far = []
+    for x, at in ((q, 0), (k, 1024), (v, 2048), (torch.empty_like(q), 4096)):
+        y = room[:, at:at + x.shape[1] * D].view(sum(n), x.shape[1], D).permute(1, 0, 2)[None]
+        y.copy_(x)
+        far.append(y)
+    _, lse = P.prefixkv_prefill_attn_packed(*far[:3], off, scale, out=far[3])
+    assert torch.equal(far[3], want) and torch.equal(lse, want_lse)
+    rq, rk = P.prefixkv_rope(q, k, torch.arange(sum(n), dtype=torch.int32, device=DEV)[None], P.rope_plan(D, device=DEV))
+    P.prefixkv_rope(far[0], far[1], torch.arange(sum(n), dtype=torch.int32, device=DEV)[None], P.rope_plan(D, device=DEV),
+                    q_out=far[0], k_out=far[1])
+    assert torch.equal(far[0], rq) and torch.equal(far[1], rk)
