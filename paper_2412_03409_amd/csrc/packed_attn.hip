@@ -280,15 +280,25 @@ struct RowTile {
         const int hf = lane >> 5;
         f32x16_t s[NKT];
 #pragma unroll
-        for (int kt = 0; kt < NKT; ++kt) {
+        for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[kt][r] = 0.f;
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) {
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int kt = 0; kt < NKT; ++kt) {
                 const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *(const uint4*)(sK + kt * 32 * ROWB + koff[j]));
                 s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[j], s[kt], 0, 0, 0);
             }
+        // left to itself the compiler reads a fragment, waits for it and multiplies
+        constexpr int kFrags = NKT * NJ, kEarly = kFrags < 8 ? kFrags : 8;
+        __builtin_amdgcn_sched_group_barrier(0x100, kEarly, 0);
+#pragma unroll
+        for (int i = 0; i < kFrags - kEarly; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
+        __builtin_amdgcn_sched_group_barrier(0x008, kEarly, 0);
         if constexpr (MASKED) {
             const int mine = lim - 4 * hf;                    // register r holds key 8 (r/4) + r%4 + 4 hf
 #pragma unroll
@@ -312,31 +322,25 @@ struct RowTile {
             for (int r = 1; r + 1 < 16; r += 2) mx[kt] = fmaxf(fmaxf(mx[kt], s[kt][r]), s[kt][r + 1]);
             mx[kt] = fmaxf(mx[kt], s[kt][15]);
         }
-        float mref[NKT], corr[NKT], top = mx[0];
-        bool later = false;                                  // the second tile moves the maximum
+        float top = mx[0], corr = 1.f;
 #pragma unroll
-        for (int kt = 0; kt < NKT; ++kt) { mref[kt] = m; corr[kt] = 1.f; top = fmaxf(top, mx[kt]); }
+        for (int kt = 1; kt < NKT; ++kt) top = fmaxf(top, mx[kt]);
         // most stages of a long prompt move no row's maximum: one look, before the two halves of a row exchange theirs
         if (__builtin_amdgcn_ballot_w64(top * qs > m)) {
+            const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+            const float next = fmaxf(m, fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * qs);
+            corr = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - next);
+            m = next;
 #pragma unroll
-            for (int kt = 0; kt < NKT; ++kt) {
-                const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx[kt]), __float_as_uint(mx[kt]), false, false);
-                mref[kt] = fmaxf(m, fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * qs);
-                corr[kt] = mref[kt] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mref[kt]);
-                if (kt == 1) later = __builtin_amdgcn_ballot_w64(mref[kt] > m) != 0;
-                m = mref[kt];
-            }
-            if (__builtin_amdgcn_ballot_w64(corr[0] != 1.f)) {
+            for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
-                for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[dt][r] *= corr[0];
-            }
+                for (int r = 0; r < 16; ++r) o[dt][r] *= corr;
         }
+        const float ref = m == -INFINITY ? 0.f : m;          // no score so far
+        sum *= corr;
 #pragma unroll
         for (int kt = 0; kt < NKT; ++kt) {
             if (MASKED && kt >= tiles) break;
-            const float ref = mref[kt] == -INFINITY ? 0.f : mref[kt];      // no score so far
             bf16x8_t pf[2];
             float psum = 0.f;
 #pragma unroll
@@ -352,13 +356,7 @@ struct RowTile {
                 }
                 pf[sl] = __builtin_bit_cast(bf16x8_t, make_uint4(pk[0], pk[1], pk[2], pk[3]));
             }
-            sum = fmaf(sum, corr[kt], psum);
-            if (kt == 1 && later) {
-#pragma unroll
-                for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[dt][r] *= corr[kt];
-            }
+            sum += psum;
             if constexpr (MASKED) {
                 // An infinite or NaN value that some rows must not see would reach them as 0 * value: such a tile is added up row by
                 // row, over the keys that each of them sees.  (Looked for where a row may not see a key.  It takes 1.5 us
