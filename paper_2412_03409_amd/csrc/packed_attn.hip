@@ -399,6 +399,15 @@ struct RowTile {
                     const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
                     o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[sl], o[dt], 0, 0, 0);
                 }
+            if constexpr (MASKED) {          // (nothing else is left to hide the reads' way: 29.3 us -> 28.9 for six short prompts)
+                __builtin_amdgcn_sched_group_barrier(0x100, 2 * NDT, 0);
+#pragma unroll
+                for (int i = 0; i < NDT; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x008, NDT, 0);
+            }
         }
     }
 
