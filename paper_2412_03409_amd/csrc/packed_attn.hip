@@ -5,8 +5,8 @@
 //
 //  attn_tiles_kernel  bf16, many rows.  A workgroup has 128 rows of one (sequence, KV head), a wavefront 32 of them.  Keys and
 //                     values stream through LDS 64 at a time (asynchronous copies, two buffer pairs).  Bound: the matrix cores
-//                     and the softmax next to them; four prompts of 8192 rows, H32/8, D128: 2.2 ms, 995 TFLOP/s.  Short prompts: the
-//                     longest tile, 1.33 us a stage and about 8 us to begin and end (680 rows of 32 heads 21.8 us).
+//                     and the softmax next to them; four prompts of 8192 rows, H32/8, D128: 2.1 to 2.2 ms, 1 PFLOP/s.  Short prompts:
+//                     the longest tile, 1.27 us a stage and about 6 us to begin and end (680 rows of 32 heads 19 to 20 us).
 //  attn_stream_kernel bf16, at most 32 rows per (sequence, KV head): decode steps.  A wavefront streams 32 keys at a time through
 //                     LDS of its own.  All keys of a launch are one sequence of blocks that the wavefronts share out evenly,
 //                     wherever the units begin and end.  Bound: HBM; 467 MB of keys and values of 32 sequences in 88 us, 5.3 TB/s
@@ -270,9 +270,9 @@ struct RowTile {
     }
 
     // NKT tiles of 32 staged keys.  MASKED: the row sees the keys up to `lim` (of the stage), bit x of `bad` hides keys
-    // 16x ... 16x+15, tiles from `tiles` on are seen by no row of the wavefront, those in front of `full` by all of them.  Each tile has
-    // its own reference, the maximum up to its end: the probabilities are rounded to bf16 against it (the product's operand; their
-    // sum is of the unrounded ones, in fp32).
+    // 16x ... 16x+15, tiles from `tiles` on are seen by no row of the wavefront, those in front of `full` by all of them.  The
+    // probabilities are rounded to bf16 (the product's operand) against the maximum up to the end of these tiles; their sum is of the
+    // unrounded ones, in fp32.
     template <int NKT, bool MASKED>
     __device__ __forceinline__ void attend(const unsigned char* sK, const unsigned char* sV, float qs, int lane, int lim, uint32_t bad,
                                            int tiles, int full) {
@@ -290,7 +290,9 @@ struct RowTile {
                 const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *(const uint4*)(sK + kt * 32 * ROWB + koff[j]));
                 s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[j], s[kt], 0, 0, 0);
             }
-        // left to itself the compiler reads a fragment, waits for it and multiplies
+        // Eight fragments ahead; left to itself the compiler reads one, waits for it and multiplies.  (Two tiles' products in turn have no
+        // wait for each other either.  680 rows, H32: 21.6 us -> 19.9.  The exponentials of one tile spread between the products of the
+        // other by the same means, in this order or a tile at a time, gave nothing or cost 4 %.)
         constexpr int kFrags = NKT * NJ, kEarly = kFrags < 8 ? kFrags : 8;
         __builtin_amdgcn_sched_group_barrier(0x100, kEarly, 0);
 #pragma unroll
@@ -360,7 +362,7 @@ struct RowTile {
             if constexpr (MASKED) {
                 // An infinite or NaN value that some rows must not see would reach them as 0 * value: such a tile is added up row by
                 // row, over the keys that each of them sees.  (Looked for where a row may not see a key.  It takes 1.5 us
-                // of a prompt of 680 rows, H32, 21.6 us; a look at the copies in front of the barrier, a quarter each, took 2.5, and
+                // of a prompt of 680 rows, H32, 20 us; a look at the copies in front of the barrier, a quarter each, took 2.5, and
                 // working a tile over again whose output is not finite more than that in spilled registers.)
                 if (kt >= full && wild_values<32 * ROWB / 1024>(sV + 32 * kt * ROWB, lane)) {
                     const int ln = lane & 31;
@@ -567,8 +569,8 @@ constexpr int kJoinStages = 3;      // what a cut costs: two parts written and r
 
 // Where tiles are cut, every workgroup takes the same share of the launch, wherever that begins and ends: tiles differ in length by two
 // orders of magnitude (a prompt's first and last one, caches of other layers), and a launch of a workgroup per tile ends with a few
-// long ones on an empty chip.  (600 rows over 6000 keys among shorter sequences, H32/8: 137 us with the long tiles cut in halves, 108
-// so, of which 10 join the parts.)
+// long ones on an empty chip.  (600 rows over 6000 keys among shorter sequences, H32/8: 135 us so, 108 in
+// equal shares, of which 10 join the parts.)
 // A tile's cost is the keys that it sees, if it were full, and kStartKeys, in units of one key and row of grp; that has a closed sum.
 template <bool PAGED>
 struct TileCost {
@@ -799,7 +801,7 @@ attn_tiles_kernel(TileParams p) {
             __syncthreads();                                     // ... and everybody's; the other pair is free again
         };
         // Stages whose keys every row of the tile sees, two at a time, without a branch between them: a masked stage in the same
-        // loop made the compiler move the output between two sets of registers (four prompts of 8192 rows 3160 us, so 2870).  A
+        // loop made the compiler move the output between two sets of registers (four prompts of 8192 rows then 3160 us, so 2870).  A
         // wavefront without rows works along on rows that are not stored.
         int st = st0;
         if (plain & 1) {                                         // (the first stage of an odd number is in the other pair)
@@ -1156,15 +1158,15 @@ static size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 // tiles of all sequences of a KV head at most
 static long long most_tiles(const pkv_packed& s) { return (long long)s.T * (s.H / s.Hkv) / kTileRows + (s.S < s.T ? s.S : s.T); }
-// Whether tiles are cut.  A launch of a workgroup per tile takes as long as its longest tile (1.33 us a stage with a compute unit of
-// its own) or as the whole work shared out (2.1 us a stage on each of the workgroups), whichever is longer; cutting brings the first down
+// Whether tiles are cut.  A launch of a workgroup per tile takes as long as its longest tile (1.27 us a stage with a compute unit of
+// its own) or as the whole work shared out (2.0 us a stage on each of the workgroups), whichever is longer; cutting brings the first down
 // to the second and costs about 30 us (parts, joining them, shares, a phase of its own for every workgroup).  The longest tile and the
 // average are taken from the most that can be: the rows of a prompt, the width of a table row, of which a cache holds three quarters.
-// us, whole / cut: H32/8, 512 rows over 8192 keys 192 / 112, 4 x 128 rows 179 / 101, 16 x 40 over 2000 56 / 60; H32, 8 x 64 over 1000
-// 35 / 50, 64 over 4000 88 / 44; prompts: H32 680 22 / 41, 2048 63 / 83, H8 2048 53 / 47, H12/4 6000 156 / 174.
+// us, whole / cut: H32/8, 512 rows over 8192 keys 178 / 108, 4 x 128 rows 168 / 104, 16 x 40 over 2000 50 / 59; H32, 8 x 64 over 1000
+// 31 / 46, 64 over 4000 80 / 40; prompts: H32 680 19 / 37, 2048 52 / 69, H8 2048 43 / 38, H12/4 6000 140 / 149.
 static bool cut_tiles(const pkv_packed& s, long long keys, bool paged) {
     const double stages = (double)((keys + kStage - 1) / kStage), tiles = (double)most_tiles(s) * s.L * s.Hkv;
-    return stages * (1.33 - (paged ? 0.75 : 0.5) * 2.1 * tiles / tile_workgroups()) > 30.0;
+    return stages * (1.27 - (paged ? 0.75 : 0.5) * 2.0 * tiles / tile_workgroups()) > 30.0;
 }
 
 // rows of a KV head and block numbers are 32 bits wide, and so are the threads of a grid (256 of a workgroup)
