@@ -290,10 +290,10 @@ struct RowTile {
                 const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *(const uint4*)(sK + kt * 32 * ROWB + koff[j]));
                 s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[j], s[kt], 0, 0, 0);
             }
-        // Eight fragments ahead; left to itself the compiler reads one, waits for it and multiplies.  (Two tiles' products in turn have no
-        // wait for each other either.  680 rows, H32: 21.6 us -> 19.9.  The exponentials of one tile spread between the products of the
-        // other by the same means, in this order or a tile at a time, gave nothing or cost 4 %.)
-        constexpr int kFrags = NKT * NJ, kEarly = kFrags < 8 ? kFrags : 8;
+        // Six fragments ahead (4, 8 and 11: up to 1 % slower); left to itself the compiler reads one, waits for it and multiplies.  (Two
+        // tiles' products in turn have no wait for each other either.  680 rows, H32: 21.6 us -> 19.9.  The exponentials of one tile
+        // spread between the products of the other by the same means, in this order or a tile at a time, gave nothing or cost 4 %.)
+        constexpr int kFrags = NKT * NJ, kEarly = kFrags < 6 ? kFrags : 6;
         __builtin_amdgcn_sched_group_barrier(0x100, kEarly, 0);
 #pragma unroll
         for (int i = 0; i < kFrags - kEarly; ++i) {
