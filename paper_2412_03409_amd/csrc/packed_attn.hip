@@ -23,6 +23,7 @@
 // they are.  V^T comes from row-major V by the transposing LDS read.
 #include "packed.hpp"
 #include "fast_div.hpp"
+#include "packed_rules.hpp"
 
 namespace pkv {
 
@@ -461,7 +462,7 @@ struct Work {
     int segs;                       // S * L
 };
 struct Segment { int s, l, first, n, rows, len, before, end; };   // rows: of this call, times the heads of a KV head; keys; keys in front
-                                                                  // of the first new row (below 0: the first rows see nothing); keys that some row sees
+                                                                  // of the first new row (below 0: the first rows see nothing); keys that some row sees (none without rows)
 
 template <bool PAGED>
 __device__ __forceinline__ Segment segment(const Work& p, int i) {
@@ -470,12 +471,12 @@ __device__ __forceinline__ Segment segment(const Work& p, int i) {
     x.s = sl.q; x.l = sl.r;
     const int last = p.a.row_off[x.s + 1];
     x.first = p.a.row_off[x.s];
-    x.n = x.first >= 0 && last <= p.a.T ? max(0, last - x.first) : 0;
+    x.n = new_rows(x.first, last, p.a.T);
     x.len = PAGED ? entries(p.a, x.s, x.l) : x.n;
     const int rows = PAGED ? min(x.n, p.a.max_rows) : x.n;
     x.rows = rows * p.a.grp;
     x.before = x.len - x.n;
-    x.end = max(0, min(x.len, x.before + rows));
+    x.end = keys_seen(rows, x.n, x.len);
     return x;
 }
 template <bool PAGED>
