@@ -8,7 +8,8 @@
 //   slot of a new row = page * ps + row in the page
 //
 // Free pages wait in a ring and not on a stack: what a call takes (at the head) and what it gives back (behind the end) are
-// disjoint places, so that all entries move at once, in any order, with the same result.
+// disjoint places, so that all entries move at once, in any order, with the same result.  (Ends of the ring without room for what
+// comes back, which no sequence of calls leads to, are refused.)
 // Bound: latency.  The sums need every length before the first entry can move; one workgroup of 1024 threads forms them (a
 // sum of two counts by wavefront shuffles, the wavefronts' totals through LDS).  While what has to move is little the same
 // workgroup moves it (SMALL: one launch), else a second launch spreads it over the chip.  64 sequences of 32 layers, a row each:
@@ -16,6 +17,7 @@
 // 64 sequences of 40 layers resized: 4.2 + 4.2.
 #include "packed.hpp"
 #include "fast_div.hpp"
+#include "packed_rules.hpp"
 
 namespace pkv {
 
@@ -40,9 +42,7 @@ struct PageParams {
 };
 
 __device__ __forceinline__ int pages_of(const PageParams& p, int len) { return (len + (1 << p.shift) - 1) >> p.shift; }
-__device__ __forceinline__ int ring_at(const PageParams& p, uint32_t at) {     // at < 2 * num_pages
-    return (int)(at >= (uint32_t)p.num_pages ? at - (uint32_t)p.num_pages : at);
-}
+__device__ __forceinline__ int ring_at(const PageParams& p, uint32_t at) { return ring_place(at, p.num_pages); }
 
 // the sequence of row t: the last one that begins at t or before it (sequences without rows are passed over)
 __device__ __forceinline__ int sequence_of(const int* off, int S, int t) {
@@ -142,10 +142,8 @@ page_plan_kernel(PageParams p) {
         }
     }
     __syncthreads();
-    const bool range = s_bad != 0 || head < 0 || head >= p.num_pages || count < 0 || count > p.num_pages ||
-                       (int64_t)count - carry.x + carry.y > p.num_pages;
-    const bool few = carry.x > count;
-    const bool ok = !range && !few;
+    const int verdict = s_bad != 0 ? (int)PKV_PAGES_RANGE : ring_verdict(head, count, carry.x, carry.y, p.num_pages);
+    const bool ok = verdict == 0;
     const int4 hd = make_int4(ok ? 1 : 0, head, count, 0);
     // (every thread has read what it needs of lens and state in front of the barrier: lens_out and state_out may be the same)
     if constexpr (SMALL) {
@@ -171,7 +169,7 @@ page_plan_kernel(PageParams p) {
     if (tid == 0) {
         p.state_out[0] = ok ? ring_at(p, (uint32_t)head + (uint32_t)carry.x) : head;
         p.state_out[1] = ok ? count - carry.x + carry.y : count;
-        *p.status = range ? PKV_PAGES_RANGE : few ? PKV_PAGES_SHORT : 0;
+        *p.status = verdict;
         if constexpr (!SMALL) *p.head = hd;
     }
     if constexpr (!APPEND && SMALL) {

@@ -1,12 +1,12 @@
-"""Packed prompts and paged caches at the places where a serving program's state is unusual: sequences that wait beside others.
-Every output against its plain form in 64 bits, with the bars of test_gpu_serving.py."""
+"""Packed prompts and paged caches where a serving program's state is unusual: sequences that wait beside others, a ring of free
+pages whose ends cannot be.  Every output against its plain form in 64 bits, with the bars of test_gpu_serving.py."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2412_03409_amd as P
 import serving_reference as R
-from test_gpu_serving import BF16, DEV, F32, chunk_state, close, f64, gen, i32, offsets, projected
+from test_gpu_serving import BF16, DEV, F32, as_cache, chunk_state, close, f64, gen, i32, offsets, page_state, projected
 
 pytestmark = pytest.mark.gpu
 
@@ -32,3 +32,29 @@ def test_chunk_attn_beside_sequences_that_wait(H, Hkv, D, ps, rows, waits, dtype
     want, mag = R.chunk(f64(q), off, f64(c.kp), f64(c.vp), table, lens, scale.double().cpu().numpy())
     close(out, want, mag, dtype)
     assert bool((out[torch.from_numpy(np.isnan(want)).to(DEV)] == 55).all())
+
+
+# ---- the ring of free pages ----------------------------------------------------------------------------
+@pytest.mark.parametrize("S,layers,width", [(3, 2, 8), (130, 40, 8), (40, 60, 16)])      # one launch; more segments, more places than one holds
+@pytest.mark.parametrize("moved", [1, 3])
+def test_pages_that_come_back_need_room_before_the_call(S, layers, width, moved):
+    """A ring that is full although segments hold pages: what one segment gives back has no place, also when another takes as many."""
+    ps = 16
+    lens, table, ring, state = page_state(7, S, layers, ps, width, 20, 3 * ps)
+    lens[0, 0], lens[1, 1] = 4 * ps, 0
+    table[0, 0, :4], table[1, 1, :4] = [0, 1, 2, 3], -1
+    ring[:] = np.arange(len(ring))
+    state[:] = len(ring) - 1, len(ring)
+    target = lens.copy()
+    target[0, 0], target[1, 1] = (4 - moved) * ps, moved * ps
+    c = as_cache(lens, table, ring, state, ps)
+    assert int(P.prefixkv_page_resize(c, i32(target))) == 2
+    for a, b in zip((c.lens, c.table, c.ring, c.state), (lens, table, ring, state)):
+        np.testing.assert_array_equal(a.cpu().numpy(), b)
+    # with room for them the same call is done, and the ring's ends come round
+    state[:] = len(ring) - 1, len(ring) - moved
+    c.state.copy_(i32(state))
+    status, *want = R.resize(lens, target, table, ring, state, ps)
+    assert status == 0 and int(P.prefixkv_page_resize(c, i32(target))) == 0
+    for a, b in zip((c.lens, c.table, c.ring, c.state), want):
+        np.testing.assert_array_equal(a.cpu().numpy(), b)

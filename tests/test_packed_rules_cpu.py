@@ -1,4 +1,5 @@
-"""csrc/packed_rules.hpp, compiled for the host: which rows and keys a call over packed rows or a paged cache works on."""
+"""csrc/packed_rules.hpp, compiled for the host: which rows and keys a call over packed rows or a paged cache works on; what the
+ring of free pages gives and takes."""
 import ctypes as C
 import os
 import subprocess
@@ -13,6 +14,8 @@ SHIM = """
 #include "packed_rules.hpp"
 extern "C" int new_rows(int first, int last, int T) { return pkv::new_rows(first, last, T); }
 extern "C" int keys_seen(int rows, int n, int len) { return pkv::keys_seen(rows, n, len); }
+extern "C" int ring_verdict(int head, int count, int taken, int given, int P) { return pkv::ring_verdict(head, count, taken, given, P); }
+extern "C" int ring_place(unsigned at, int P) { return pkv::ring_place(at, P); }
 """
 
 
@@ -44,3 +47,24 @@ def test_keys_of_a_segment(rules):
                 seen = [max(0, min(length, length - n + i + 1)) for i in range(rows)]
                 assert rules.keys_seen(rows, n, length) == max(seen, default=0), (rows, n, length)
     assert rules.keys_seen(0, 0, 1 << 20) == 0
+
+
+def test_ring_of_free_pages(rules):
+    """Every place that an accepted call touches is in the ring, and none is both read and written, whatever the ends are."""
+    short, wrong = 1, 2
+    for P in range(1, 8):
+        for head in range(-1, P + 2):
+            for count in range(-1, P + 2):
+                for taken in range(0, P + 3):
+                    for given in range(0, P + 3):
+                        v = rules.ring_verdict(head, count, taken, given, P)
+                        real = 0 <= head < P and 0 <= count <= P and count + given <= P
+                        assert v == (wrong if not real else short if taken > count else 0), (P, head, count, taken, given)
+                        if v == 0:
+                            places = [rules.ring_place(head + i, P) for i in range(taken)]
+                            places += [rules.ring_place(head + count + i, P) for i in range(given)]
+                            assert len(set(places)) == taken + given and all(0 <= x < P for x in places)
+                            assert places == [(head + i) % P for i in range(taken)] + [(head + count + i) % P for i in range(given)]
+    top = (1 << 31) - 1
+    assert rules.ring_verdict(top - 1, top, top, 0, top) == 0 and rules.ring_verdict(top - 1, top, 1, 1, top) == wrong
+    assert rules.ring_verdict(0, 0, 0, top, top) == 0 and rules.ring_place(2 * top - 1, top) == top - 1
