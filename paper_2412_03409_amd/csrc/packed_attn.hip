@@ -41,6 +41,17 @@ struct PackedParams {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+// The logit scale's size; its sign goes into the queries (exact), so that maxima can be taken on the products.  Above 0, so that a masked
+// -inf stays one: the smallest number there is, times the largest score, is still below 2^-20 (NaN stays NaN).
+__device__ __forceinline__ float scale_size(float sc) {
+    const float a = fabsf(sc);
+    return a < 1.401298464e-45f ? 1.401298464e-45f : a;
+}
+// The same in units of log2: a weight is 2^((score - maximum) * this).  Scores are scaled behind their difference, because the largest
+// finite ones leave the range when they are scaled, and lose whole units in the rounding: rows whose keys all score the type's lowest
+// value weigh them equally.
+__device__ __forceinline__ float score_scale(float sc) { return scale_size(sc) * kLog2e; }
+
 __device__ __forceinline__ int wave_sum(int x) {
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d, kWave);
@@ -70,8 +81,9 @@ attn_rows_kernel(PackedParams p) {
     const int len = entries(p, s, l), count = min(len, i + 1 + len - n);    // keys that the row sees
     const int32_t* pages = p.table + ((int64_t)s * p.layers + p.l0 + l) * p.max_pages;
     const int g = h / p.grp;
-    const float4 q = *(const float4*)(p.q + p.qs.l * l + p.qs.h * h + p.qs.n * t + sub * 16);
-    const float scale = p.scale[l] * kLog2e;
+    float4 q = *(const float4*)(p.q + p.qs.l * l + p.qs.h * h + p.qs.n * t + sub * 16);
+    const float sc0 = p.scale[l], scale = score_scale(sc0);
+    if (sc0 < 0.f) q = make_float4(-q.x, -q.y, -q.z, -q.w);
     float m = -INFINITY, sum = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     auto weigh = [](float4& x, float c) { x.x *= c; x.y *= c; x.z *= c; x.w *= c; };
@@ -96,16 +108,16 @@ attn_rows_kernel(PackedParams p) {
             float d = fmaf(q.x, kr[u].x, fmaf(q.y, kr[u].y, fmaf(q.z, kr[u].z, q.w * kr[u].w)));
 #pragma unroll
             for (int x = 1; x < LPR; x <<= 1) d += __shfl_xor(d, x, kWave);
-            sc[u] = real[u] ? d * scale : -INFINITY;
+            sc[u] = real[u] ? d : -INFINITY;
             mx = fmaxf(mx, sc[u]);
         }
-        const float ref = mx == -INFINITY ? 0.f : mx, corr = __builtin_amdgcn_exp2f(m - ref);
+        const float ref = mx == -INFINITY ? 0.f : mx, corr = __builtin_amdgcn_exp2f((m - ref) * scale);
         m = mx;
         sum *= corr;
         weigh(o, corr);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const float w = __builtin_amdgcn_exp2f(sc[u] - ref);
+            const float w = __builtin_amdgcn_exp2f((sc[u] - ref) * scale);
             sum += w;
             o.x = fmaf(w, vr[u].x, o.x); o.y = fmaf(w, vr[u].y, o.y); o.z = fmaf(w, vr[u].z, o.z); o.w = fmaf(w, vr[u].w, o.w);
         }
@@ -114,7 +126,7 @@ attn_rows_kernel(PackedParams p) {
     float all = m;
 #pragma unroll
     for (int x = LPR; x < kWave; x <<= 1) all = fmaxf(all, __shfl_xor(all, x, kWave));
-    const float ref = all == -INFINITY ? 0.f : all, corr = __builtin_amdgcn_exp2f(m - ref);
+    const float ref = all == -INFINITY ? 0.f : all, corr = __builtin_amdgcn_exp2f((m - ref) * scale);
     sum *= corr;
     weigh(o, corr);
 #pragma unroll
@@ -132,14 +144,14 @@ attn_rows_kernel(PackedParams p) {
     float top = all;
 #pragma unroll
     for (int w = 1; w < 4; ++w) top = fmaxf(top, s_ms[w].x);
-    const float base = top == -INFINITY ? 0.f : top, mine = __builtin_amdgcn_exp2f(all - base);
+    const float base = top == -INFINITY ? 0.f : top, mine = __builtin_amdgcn_exp2f((all - base) * scale);
     sum *= mine;
     weigh(o, mine);
 #pragma unroll
     for (int w = 1; w < 4; ++w) {
         const float2 ms = s_ms[w];
         const float4 y = s_o[w][sub];
-        const float c = __builtin_amdgcn_exp2f(ms.x - base);
+        const float c = __builtin_amdgcn_exp2f((ms.x - base) * scale);
         sum = fmaf(ms.y, c, sum);
         o.x = fmaf(y.x, c, o.x); o.y = fmaf(y.y, c, o.y); o.z = fmaf(y.z, c, o.z); o.w = fmaf(y.w, c, o.w);
     }
@@ -158,6 +170,7 @@ constexpr int kTileRows = 128;      // rows of a workgroup
 constexpr int kStage = 64;          // keys that a workgroup stages at a time
 constexpr int kBlockKeys = 32;      // keys that a wavefront of the stream kernel takes at a time
 constexpr int kFewRows = 32;        // rows of a unit of the stream kernel
+constexpr float kWide = 4096.f;     // scaled scores beyond are scaled behind their difference
 
 // 4 keys of one column of row-major V (lane i of a group of 16 receives column i of the 4 keys that the group points at)
 __device__ __forceinline__ v4i16_t lds_read_tr(const unsigned char* p) {
@@ -230,12 +243,15 @@ template <int D>
 struct RowTile {
     bf16x8_t q[D / 16];
     f32x16_t o[D / 32];
-    float m, sum;             // running maximum of score * qs, and this half's part of the sum
+    float m, sum;             // running maximum of the products, and this half's part of the sum
+    float ref;                // the maximum, scaled; 0 before a score, and where some row's is past kWide:
+    bool wide;                // there the scores' differences from the maximum are scaled
     uint32_t koff[D / 16], voff[D / 32][2];   // byte offsets of the lane's fragment reads in a staged 32-key tile
 
     __device__ __forceinline__ void clear() {
         m = -INFINITY;
-        sum = 0.f;
+        sum = ref = 0.f;
+        wide = false;
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -329,17 +345,27 @@ struct RowTile {
 #pragma unroll
         for (int kt = 1; kt < NKT; ++kt) top = fmaxf(top, mx[kt]);
         // most stages of a long prompt move no row's maximum: one look, before the two halves of a row exchange theirs
-        if (__builtin_amdgcn_ballot_w64(top * qs > m)) {
+        if (__builtin_amdgcn_ballot_w64(top > m)) {
             const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-            const float next = fmaxf(m, fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * qs);
-            corr = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - next);
+            const float next = fmaxf(m, fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])));
+            corr = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - next) * qs);
             m = next;
+            ref = m == -INFINITY ? 0.f : m * qs;
+            wide = __builtin_amdgcn_ballot_w64(fabsf(ref) > kWide) != 0;
+            ref = wide ? 0.f : ref;
 #pragma unroll
             for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[dt][r] *= corr;
         }
-        const float ref = m == -INFINITY ? 0.f : m;          // no score so far
+        // One fma scales a score and takes the maximum from it; up to kWide its half step is below 2^-13 and the same for a whole row.
+        if (__builtin_expect(wide, 0)) {
+            const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+            for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[kt][r] -= base;
+        }
         sum *= corr;
 #pragma unroll
         for (int kt = 0; kt < NKT; ++kt) {
@@ -441,12 +467,6 @@ struct RowTile {
         if (hf == 0) *ms = make_float2(m, all);
     }
 };
-
-// scale in units of log2, above 0 so that a masked -inf stays one (NaN stays NaN)
-__device__ __forceinline__ float score_scale(float sc) {
-    const float a = fabsf(sc) * kLog2e;
-    return a < 1e-30f ? 1e-30f : a;
-}
 
 // What a row of a tile or unit is: row = token * grp + head of the KV head
 struct RowAt { int token, head; };
@@ -793,7 +813,7 @@ attn_tiles_kernel(TileParams p) {
             else bad_a = issue(st0, sKa, sVa);
         }
 
-        const float sc = a.scale[sg.l], qs = score_scale(sc);
+        const float sc = a.scale[sg.l], qs = score_scale(sc), size = scale_size(sc);
         tl.load_q(a.q + a.qs.l * sg.l + a.qs.h * h + a.qs.n * t, hf, sc < 0.f);
         tl.clear();
 
@@ -839,7 +859,7 @@ attn_tiles_kernel(TileParams p) {
             if (WHOLE || (st0 == 0 && st1 == nst)) {
                 tl.store(a.out + a.os.l * sg.l + a.os.h * h + a.os.n * t, hf, sum == 0.f ? 0.f : 1.f / sum, real);
                 if (!PAGED && real && hf == 0)
-                    a.lse[(int64_t)a.L * a.H * sg.first + (int64_t)(sg.l * a.H + h) * sg.n + ra.token] = kLn2 * (tl.m + __builtin_amdgcn_logf(sum));
+                    a.lse[(int64_t)a.L * a.H * sg.first + (int64_t)(sg.l * a.H + h) * sg.n + ra.token] = fmaf(tl.m, size, kLn2 * __builtin_amdgcn_logf(sum));
             } else {
                 // a workgroup has at most two parts of tiles that others share: of one that began before it, and of one that goes on
                 const int64_t slot = (int64_t)(2 * wg + (st0 > 0 ? 0 : 1)) * 4 + wv;
@@ -888,6 +908,7 @@ attn_merge_tiles_kernel(TileParams p) {
     const Segment sg = uniform_segment<PAGED>(p, c.x);
     const int r0 = c.z * kTileRows + wv * 32, row = r0 + ln;
     if (r0 >= sg.rows) return;
+    const float size = scale_size(a.scale[sg.l]), qs = size * kLog2e;
     float m = -INFINITY, sum = 0.f;
     f32x16_t o;
 #pragma unroll
@@ -899,7 +920,7 @@ attn_merge_tiles_kernel(TileParams p) {
         const float4* from = (const float4*)(p.part_o + slot * 32 * D) + dt * 4 * kWave + lane;
         const float4 y[4] = {from[0], from[kWave], from[2 * kWave], from[3 * kWave]};
         const float mx = fmaxf(m, x.x), ref = mx == -INFINITY ? 0.f : mx;
-        const float c0 = __builtin_amdgcn_exp2f(m - ref), c1 = __builtin_amdgcn_exp2f(x.x - ref);
+        const float c0 = __builtin_amdgcn_exp2f((m - ref) * qs), c1 = __builtin_amdgcn_exp2f((x.x - ref) * qs);
         sum = fmaf(sum, c0, x.y * c1);
         m = mx;
 #pragma unroll
@@ -913,7 +934,7 @@ attn_merge_tiles_kernel(TileParams p) {
     const int h = c.y * a.grp + ra.head;
     store_columns(o, a.out + a.os.l * sg.l + a.os.h * h + a.os.n * (int64_t)(sg.first + ra.token) + 64 * dt, hf, sum == 0.f ? 0.f : 1.f / sum, real);
     if (!PAGED && real && hf == 0 && dt == 0)
-        a.lse[(int64_t)a.L * a.H * sg.first + (int64_t)(sg.l * a.H + h) * sg.n + ra.token] = kLn2 * (m + __builtin_amdgcn_logf(sum));
+        a.lse[(int64_t)a.L * a.H * sg.first + (int64_t)(sg.l * a.H + h) * sg.n + ra.token] = fmaf(m, size, kLn2 * __builtin_amdgcn_logf(sum));
 }
 
 // ---- few rows: the keys of a launch shared out evenly over the wavefronts ---------------------------------
@@ -1103,6 +1124,7 @@ attn_merge_stream_kernel(StreamParams p) {
     const int c = threadIdx.x % LPP, group = threadIdx.x / LPP;
     const int rows = p.join_rows, pieces = GROUPS / rows, mine = group / rows;      // rows here, groups of a row, and which this is
     const int row = (int)blockIdx.y * rows + group % rows;
+    const float qs = score_scale(a.scale[x.l]);
     float m = -INFINITY, sum = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     if (row < x.rows && x.end > 0) {
@@ -1112,7 +1134,7 @@ attn_merge_stream_kernel(StreamParams p) {
             const float2 ms = p.part_ms[slot];
             const float4 y = *(const float4*)(p.part_o + slot * D + 4 * c);
             const float mx = fmaxf(m, ms.x), ref = mx == -INFINITY ? 0.f : mx;
-            const float c0 = __builtin_amdgcn_exp2f(m - ref), c1 = __builtin_amdgcn_exp2f(ms.x - ref);
+            const float c0 = __builtin_amdgcn_exp2f((m - ref) * qs), c1 = __builtin_amdgcn_exp2f((ms.x - ref) * qs);
             sum = fmaf(sum, c0, ms.y * c1);
             o.x = fmaf(o.x, c0, y.x * c1); o.y = fmaf(o.y, c0, y.y * c1); o.z = fmaf(o.z, c0, y.z * c1); o.w = fmaf(o.w, c0, y.w * c1);
             m = mx;
@@ -1125,13 +1147,13 @@ attn_merge_stream_kernel(StreamParams p) {
         if (mine == 0) {
             float top = m;
             for (int k = 1; k < pieces; ++k) top = fmaxf(top, s_ms[group + k * rows].x);
-            const float ref = top == -INFINITY ? 0.f : top, c0 = __builtin_amdgcn_exp2f(m - ref);
+            const float ref = top == -INFINITY ? 0.f : top, c0 = __builtin_amdgcn_exp2f((m - ref) * qs);
             sum *= c0;
             o.x *= c0; o.y *= c0; o.z *= c0; o.w *= c0;
             for (int k = 1; k < pieces; ++k) {
                 const float2 ms = s_ms[group + k * rows];
                 const float4 y = s_o[group + k * rows][c];
-                const float c1 = __builtin_amdgcn_exp2f(ms.x - ref);
+                const float c1 = __builtin_amdgcn_exp2f((ms.x - ref) * qs);
                 sum = fmaf(ms.y, c1, sum);
                 o.x = fmaf(y.x, c1, o.x); o.y = fmaf(y.y, c1, o.y); o.z = fmaf(y.z, c1, o.z); o.w = fmaf(y.w, c1, o.w);
             }

@@ -1,5 +1,5 @@
 """Packed prompts and paged caches where a serving program's state is unusual: sequences that wait beside others, a ring of free
-pages whose ends cannot be.  Every output against its plain form in 64 bits, with the bars of test_gpu_serving.py."""
+pages whose ends cannot be, scores as large as the type holds.  Every output against its plain form in 64 bits, with the bars of test_gpu_serving.py."""
 import numpy as np
 import pytest
 import torch
@@ -58,3 +58,88 @@ def test_pages_that_come_back_need_room_before_the_call(S, layers, width, moved)
     assert status == 0 and int(P.prefixkv_page_resize(c, i32(target))) == 0
     for a, b in zip((c.lens, c.table, c.ring, c.state), want):
         np.testing.assert_array_equal(a.cpu().numpy(), b)
+
+
+# ---- scores of any size ----------------------------------------------------------------------------------
+# Queries have ones in two columns and zeros elsewhere, so a score is k[0] + k[1], exact in fp32; the 64-bit form gets the same.
+SIZES = [("decode", [1, 1], [300, 90]), ("few", [4, 2], [2500, 90]), ("tiles", [70, 40], [400, 90]), ("cut", [100, 90], [6000, 90])]
+
+
+def lowest_and_highest(dtype):
+    top = torch.finfo(dtype).max
+    return [("lowest", -top, 1.0), ("lowest, scaled", -top, 0.125), ("highest", top, 1.0), ("lowest, above one", -top, 40.0),
+            ("highest, negative", top, -3.0), ("lowest, by nothing", -top, 0.0)]
+
+
+def one_hot_state(seed, n, sizes, dtype, H=2, Hkv=1, D=64, ps=16):
+    lens = np.array(sizes)[:, None]
+    c, table = chunk_state(seed, len(n), 1, Hkv, D, ps, lens, dtype)
+    off = offsets(n)
+    q = torch.zeros((1, H, int(off[-1]), D), dtype=dtype, device=DEV)
+    q[..., 0] = q[..., 1] = 1.0
+    c.kp.zero_()
+    return c, table, lens, off, q
+
+
+def place(c, table, s, x, column, ps=16):
+    """Column `column` of the keys of sequence s, entry by entry."""
+    for j0 in range(0, len(x), ps):
+        m = min(ps, len(x) - j0)
+        c.kp[int(table[s, 0, j0 // ps]), :, :m, column] = x[j0:j0 + m].to(c.kp.dtype).to(DEV)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("what,n,sizes", SIZES)
+@pytest.mark.parametrize("case", range(6))
+def test_chunk_attn_where_every_score_is_the_lowest_or_the_highest(dtype, what, n, sizes, case):
+    """Every visible key of a sequence has one score, the type's lowest or highest finite value: the mean of the values."""
+    _, value, scale = lowest_and_highest(dtype)[case]
+    c, table, lens, off, q = one_hot_state(21, n, sizes, dtype)
+    place(c, table, 0, torch.full((sizes[0],), value), 0)
+    place(c, table, 1, torch.randn(sizes[1], generator=gen(3)), 0)
+    sc = torch.tensor([scale], device=DEV)
+    out = P.prefixkv_chunk_attn(c, q, i32(off), sc, max(n))
+    want, mag = R.chunk(f64(q), off, f64(c.kp), f64(c.vp), table, lens, sc.double().cpu().numpy())
+    close(out, want, mag, dtype)
+    assert bool((out[:, :, 0].float().abs() > 0).any())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("what,n,sizes", SIZES)
+@pytest.mark.parametrize("big", [2.0 ** 11, 2.0 ** 16, -2.0 ** 16])
+@pytest.mark.parametrize("scale", [1.0, -0.5])
+def test_chunk_attn_scores_far_from_zero(dtype, what, n, sizes, big, scale):
+    """Scores that differ by a little and are large, from some key on or throughout; lowest and ordinary ones among them."""
+    c, table, lens, off, q = one_hot_state(22, n, sizes, dtype)
+    g = gen(7)
+    for s, length in enumerate(sizes):
+        x = torch.full((length,), big)
+        if s == 0:
+            x[:length // 3] = 0                          # ordinary ones first: the maximum moves by a long way
+        else:
+            x[5:9] = torch.finfo(dtype).min if scale > 0 else torch.finfo(dtype).max
+        place(c, table, s, x, 0)
+        place(c, table, s, torch.randint(-12, 13, (length,), generator=g) / 4, 1)
+    sc = torch.tensor([scale], device=DEV)
+    out = P.prefixkv_chunk_attn(c, q, i32(off), sc, max(n))
+    want, mag = R.chunk(f64(q), off, f64(c.kp), f64(c.vp), table, lens, sc.double().cpu().numpy())
+    close(out, want, mag, dtype)
+
+
+@pytest.mark.parametrize("n", [[3, 70], [300, 1], [2500, 40]])        # (the last one is cut)
+@pytest.mark.parametrize("case", range(4))
+def test_prefill_attn_packed_where_every_score_is_the_lowest_or_the_highest(n, case):
+    """The mean of the values that a row sees, and a finite log-sum-exp where the scaled score is one."""
+    _, value, scale = lowest_and_highest(BF16)[case]
+    H, Hkv, D, off = 2, 1, 64, offsets(n)
+    _, _, v = projected(gen(5), 1, H, Hkv, int(off[-1]), D, BF16)
+    q = torch.zeros((1, H, int(off[-1]), D), dtype=BF16, device=DEV)
+    q[..., 0] = 1.0
+    k = torch.zeros((1, Hkv, int(off[-1]), D), dtype=BF16, device=DEV)
+    k[..., 0] = value
+    sc = torch.tensor([scale], device=DEV)
+    out, lse = P.prefixkv_prefill_attn_packed(q, k, v, i32(off), sc)
+    want, mag, wlse = R.prompt(f64(q), f64(k), f64(v), off, sc.double().cpu().numpy())
+    close(out, want, mag, BF16)
+    if abs(value * scale) <= torch.finfo(F32).max:
+        assert np.all(np.abs(f64(lse) - wlse) <= 1e-4 * np.abs(wlse))
