@@ -400,7 +400,8 @@ int prefixkv_rope_store(const pkv_packed *shape, const pkv_rope *rope, const int
  * prefixkv_page_resize with target = lengths.  A length is taken as at most N and at most
  * max_pages*page_size.
  *   table [dev] i32 [B, layers, max_pages];  l0 + L <= layers
- *   kept_pos [dev] i32 [B,L,N] or NULL: the kept positions, ascending, in the first lengths[b,l] places */
+ *   kept_pos [dev] i32 [B,L,N] or NULL: the kept positions, ascending, in the first lengths[b,l] places
+ * B * L * Hkv times the chunks of 64 positions (17 at most, an odd number) stays below 2^24 (PKV_ERR_UNSUPPORTED otherwise). */
 int prefixkv_compact_paged(const pkv_shape *shape, const void *k, pkv_strides ks, const void *v,
                            pkv_strides vs, const int32_t *order, const int32_t *lengths,
                            const pkv_paging *paging, int l0, const int32_t *table, void *kp, void *vp,

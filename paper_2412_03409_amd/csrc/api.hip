@@ -2,6 +2,7 @@
 // launch goes to the caller's stream.  The only state kept between calls is looked up once per device:
 // the compute-unit count, and the address of the built-in scratch array of prefixkv_select_static.
 #include "packed.hpp"
+#include "packed_rules.hpp"
 
 #include <math.h>
 
@@ -355,7 +356,7 @@ int prefixkv_compact_paged(const pkv_shape* s, const void* k, pkv_strides ks, co
     const int esize = s->dtype == PKV_F32 ? 4 : 2;
     if (!strides_ok(ks, esize) || !strides_ok(vs, esize) || !aligned16(k) || !aligned16(v) || !aligned16(kp) || !aligned16(vp))
         return PKV_ERR_STRIDE;
-    if ((size_t)((s->N + 63) / 64) * s->Hkv * s->B * s->L >= 1u << 24) return PKV_ERR_UNSUPPORTED;     // workgroups of 256 threads
+    if (!gather_fits(s->N, s->Hkv, (long long)s->B * s->L)) return PKV_ERR_UNSUPPORTED;
     const hipError_t e = launch_compact_paged(*s, k, to_strides(ks), v, to_strides(vs), order, lengths, *g, l0, table, kp, vp,
                                               kept_pos, (hipStream_t)stream);
     return e == hipSuccess ? PKV_OK : PKV_ERR_HIP;

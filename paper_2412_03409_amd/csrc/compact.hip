@@ -7,6 +7,7 @@
 //                         the segment.  Pure HBM traffic.
 //  merge_position_kernel  the positional-distance merge of Sec. 4.3 on top of a compacted cache.
 #include "packed.hpp"
+#include "packed_rules.hpp"
 
 namespace pkv {
 
@@ -306,16 +307,6 @@ hipError_t launch_merge_position(const pkv_shape& s, const void* k, Strides ks, 
     return hipGetLastError();
 }
 
-// Workgroups per (segment, kv head): one per 64-row chunk up to 16 chunks (1024 rows), made odd.  The hardware
-// deals consecutive workgroups out to the eight XCDs in turn; with an even count -- 16 above all -- chunk c of
-// every (segment, head) lands on the same XCD, and since most segments keep few rows the XCDs of the high
-// chunk indices see hardly any work (measured with 16: 2.3 instead of 4.3 TB/s from N = 1000 on).
-static int gather_chunks(int N) {
-    const int all_chunks = (N + 63) / 64;
-    const int nchunk = all_chunks < 16 ? all_chunks : 16;
-    return nchunk | 1;
-}
-
 hipError_t launch_compact(const pkv_shape& s, const void* k, Strides ks, const void* v, Strides vs,
                           const int32_t* order, const int32_t* lengths, int decode_capacity,
                           int64_t* seg_off, int32_t* caps, void* kc, void* vc, int32_t* kept_pos,
@@ -354,7 +345,7 @@ hipError_t launch_compact_paged(const pkv_shape& s, const void* k, Strides ks, c
     const int row_bytes = s.D * esize;
     const int lpr = row_bytes / 16;
     const int nchunk = gather_chunks(s.N);
-    dim3 grid((uint32_t)((size_t)nchunk * s.Hkv * nseg));
+    dim3 grid((uint32_t)gather_workgroups(s.N, s.Hkv, nseg));
     const size_t lds = (size_t)s.N * 4 + (size_t)((s.N + 3) / 4) * 4;
     const bool ntl = 2 * (size_t)nseg * s.Hkv * s.N * row_bytes >= ((size_t)1 << 31);   // as in launch_compact
     const PagedDst pg{table, g.num_pages, g.max_pages, g.layers, l0, __builtin_ctz((unsigned)g.page_size)};

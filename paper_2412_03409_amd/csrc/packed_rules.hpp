@@ -1,5 +1,5 @@
-// Which rows and keys of a paged or packed cache a call works on, and what the ring of free pages can give and take.  Plain integer
-// rules, apart from the kernels so that they can be compiled and enumerated on the host.
+// Which rows and keys of a paged or packed cache a call works on, what the ring of free pages can give and take, and how many
+// workgroups a compaction has.  Plain integer rules, apart from the kernels so that they can be compiled and enumerated on the host.
 #pragma once
 
 #include <stdint.h>
@@ -29,5 +29,19 @@ __host__ __device__ __forceinline__ int ring_verdict(int head, int count, int ta
 __host__ __device__ __forceinline__ int ring_place(uint32_t at, int num_pages) {
     return (int)(at >= (uint32_t)num_pages ? at - (uint32_t)num_pages : at);
 }
+
+// Workgroups per (segment, kv head): one per 64-row chunk up to 16 chunks (1024 rows), made odd.  The hardware
+// deals consecutive workgroups out to the eight XCDs in turn; with an even count -- 16 above all -- chunk c of
+// every (segment, head) lands on the same XCD, and since most segments keep few rows the XCDs of the high
+// chunk indices see hardly any work (measured with 16: 2.3 instead of 4.3 TB/s from N = 1000 on).
+inline int gather_chunks(int N) {
+    const int all_chunks = (N + 63) / 64;
+    const int nchunk = all_chunks < 16 ? all_chunks : 16;
+    return nchunk | 1;
+}
+
+// Workgroups of a launch: below 2^24, as a grid's threads (256 of a workgroup) are counted in 32 bits.
+inline long long gather_workgroups(int N, int Hkv, long long segments) { return gather_chunks(N) * (long long)Hkv * segments; }
+inline bool gather_fits(int N, int Hkv, long long segments) { return gather_workgroups(N, Hkv, segments) < 1ll << 24; }
 
 }  // namespace pkv

@@ -1,10 +1,13 @@
 """csrc/packed_rules.hpp, compiled for the host: which rows and keys a call over packed rows or a paged cache works on; what the
-ring of free pages gives and takes."""
+ring of free pages gives and takes; how many workgroups a compaction has."""
 import ctypes as C
 import os
 import subprocess
 
 import pytest
+
+import paper_2412_03409_amd as P
+from paper_2412_03409_amd import binding as Bd
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2412_03409_amd", "csrc")
 SHIM = """
@@ -16,6 +19,8 @@ extern "C" int new_rows(int first, int last, int T) { return pkv::new_rows(first
 extern "C" int keys_seen(int rows, int n, int len) { return pkv::keys_seen(rows, n, len); }
 extern "C" int ring_verdict(int head, int count, int taken, int given, int P) { return pkv::ring_verdict(head, count, taken, given, P); }
 extern "C" int ring_place(unsigned at, int P) { return pkv::ring_place(at, P); }
+extern "C" int gather_chunks(int N) { return pkv::gather_chunks(N); }
+extern "C" int gather_fits(int N, int Hkv, long long segments) { return pkv::gather_fits(N, Hkv, segments); }
 """
 
 
@@ -68,3 +73,19 @@ def test_ring_of_free_pages(rules):
     top = (1 << 31) - 1
     assert rules.ring_verdict(top - 1, top, top, 0, top) == 0 and rules.ring_verdict(top - 1, top, 1, 1, top) == wrong
     assert rules.ring_verdict(0, 0, 0, top, top) == 0 and rules.ring_place(2 * top - 1, top) == top - 1
+
+
+def test_workgroups_of_a_compaction(rules):
+    """What is checked is what is launched: an odd number of chunks, 17 at most, and fewer than 2^24 workgroups of 256 threads."""
+    for N in range(1, 8193):
+        n = min((N + 63) // 64, 16)
+        assert rules.gather_chunks(N) == n + (n % 2 == 0)
+    A, st = C.c_void_p(4096), Bd._Strides(0, 8192, 128, 64)
+    for N in (1, 64, 65, 128, 129, 1024, 1025, 8192):
+        chunks, L, Hkv = rules.gather_chunks(N), 64, 3
+        most = ((1 << 24) - 1) // (chunks * L * Hkv)          # sequences
+        assert rules.gather_fits(N, Hkv, C.c_longlong(most * L)) and not rules.gather_fits(N, Hkv, C.c_longlong((most + 1) * L))
+        assert (most * L * Hkv * chunks) * 256 < 1 << 32 <= ((most + 1) * L * Hkv * chunks) * 256
+        shape = C.byref(Bd._Shape(most + 1, L, Hkv, Hkv, N, 64, P.PKV_BF16))
+        paging = C.byref(Bd._Paging(8, 16, 4, 64))
+        assert P.load().prefixkv_compact_paged(shape, A, st, A, st, A, A, paging, 0, A, A, A, A, None) == 7, N
