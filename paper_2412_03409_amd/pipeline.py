@@ -173,13 +173,16 @@ class PagedPath:
 
     def extend(self, lengths, q, k, v, positions):
         """Further rows of every sequence (lengths[s] of place s, 0 for one that waits): they are stored, and attend to what the
-        cache holds and to each other.  One row each is a decode step.  -> attention output [L,H,T,D]."""
+        cache holds and to each other.  One row each is a decode step.  -> attention output [L,H,T,D]; zeros if `status` says that
+        the rows got no pages, and then nothing is stored and every length stays."""
         if len(lengths) != self.S or any(n < 0 for n in lengths) or sum(lengths) > q.shape[2]:
             raise ValueError("a length per place, rows for all of them")
         off, T = self._offsets(lengths), q.shape[2]
         slots, _ = B_.prefixkv_page_append(self.cache, off, T, status=self.status, ws=self.page_ws)
         turned = B_.prefixkv_rope_store(self.cache, q, k, v, positions, self.plan, slots)
-        return B_.prefixkv_chunk_attn(self.cache, turned, off, self.scale, max(1, max(int(n) for n in lengths)))
+        out = B_.prefixkv_chunk_attn(self.cache, turned, off, self.scale, max(1, max(int(n) for n in lengths)))
+        # (after a refused call the lengths do not count the rows: they would see the last entries of the cache as their own)
+        return out.masked_fill_(self.status != 0, 0)
 
     def end(self, places):
         """The sequences at these places are over: their pages are free again."""

@@ -143,3 +143,35 @@ def test_prefill_attn_packed_where_every_score_is_the_lowest_or_the_highest(n, c
     close(out, want, mag, BF16)
     if abs(value * scale) <= torch.finfo(F32).max:
         assert np.all(np.abs(f64(lse) - wlse) <= 1e-4 * np.abs(wlse))
+
+
+# ---- the path --------------------------------------------------------------------------------------------
+def small_path(S=2, L=2, H=4, Hkv=2, D=64, num_pages=6, **kw):
+    from paper_2412_03409_amd.pipeline import PagedPath
+    path = PagedPath(S, L, H, Hkv, D, torch.tensor([0.2, 0.3], device=DEV)[:L], P.rope_plan(D, device=DEV), num_pages=num_pages,
+                     max_pages=8, page_size=16, device=DEV, **kw)
+    path.cache.kp.zero_(), path.cache.vp.zero_()
+    return path
+
+
+def path_state(path):
+    c = path.cache
+    return [x.clone() for x in (c.kp, c.vp, c.lens, c.table, c.ring, c.state)]
+
+
+def path_rows(path, g, T):
+    return (*projected(g, path.L, path.H, path.Hkv, T, path.D, BF16), torch.arange(T, dtype=torch.int32, device=DEV)[None])
+
+
+def test_rows_without_pages_leave_the_path_as_it_was_and_answer_zeros():
+    g, path = gen(13), small_path(num_pages=12)
+    path.prefill([0, 1], [40, 9], *path_rows(path, g, 49), [60, 10])
+    assert int(path.status) == 0
+    before = path_state(path)
+    out = path.extend([1, 70], *path_rows(path, g, 71))
+    assert int(path.status) == 1 and not bool(out.any())
+    for a, b in zip(path_state(path), before):
+        assert torch.equal(a, b)
+    out = path.extend([1, 2], *path_rows(path, g, 3))          # what has room goes on
+    assert int(path.status) == 0 and bool(out.any())
+    assert torch.equal(path.cache.lens - before[2], i32([[1, 1], [2, 2]]))
