@@ -118,7 +118,8 @@ class HotPath:
 class PagedPath:
     """S places for sequences over one pool of pages.  All layers of the model are called at once, as the queries, keys and
     values [L,heads,T,D] of the packed rows of all layers are given (bf16).  Nothing is read back: `status` [1] tells whether
-    the last call that needed pages got them."""
+    the last call that needed pages got them, `search` [S] what the search said (its status bits, 0 if nothing) of the last
+    prompt of every place: a prompt that it could not rank, with NaN in a query for instance, keeps no entries."""
 
     def __init__(self, S: int, L: int, H: int, Hkv: int, D: int, scale: torch.Tensor, plan: B_.RopePlan, num_pages: int,
                  max_pages: int, page_size: int = 64, device="cuda"):
@@ -127,6 +128,7 @@ class PagedPath:
         self.cache = B_.paged_cache(S, L, Hkv, D, page_size, num_pages, max_pages, torch.bfloat16, device)
         self.target = torch.zeros((S, L), dtype=torch.int32, device=device)
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
+        self.search = torch.zeros(S, dtype=torch.int32, device=device)
         self.page_ws = torch.empty(B_.page_workspace_bytes(S, L), dtype=torch.uint8, device=device)
 
     def _offsets(self, lengths) -> torch.Tensor:
@@ -155,6 +157,7 @@ class PagedPath:
                                          lse=lse[self.L * self.H * a:self.L * self.H * (a + n)].view(1, self.L, self.H, n))
             sel = B_.prefixkv_select(imp, int(budget), want_prefix=False)
             self.target[place].copy_(sel.lengths[0])
+            self.search[place:place + 1].copy_(sel.status)
             rank.append((place, rows, sel))
             a += n
         B_.prefixkv_page_resize(self.cache, self.target, status=self.status, ws=self.page_ws)

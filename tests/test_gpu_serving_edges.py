@@ -175,3 +175,15 @@ def test_rows_without_pages_leave_the_path_as_it_was_and_answer_zeros():
     out = path.extend([1, 2], *path_rows(path, g, 3))          # what has room goes on
     assert int(path.status) == 0 and bool(out.any())
     assert torch.equal(path.cache.lens - before[2], i32([[1, 1], [2, 2]]))
+
+
+def test_a_prompt_that_the_search_cannot_rank_is_told():
+    """NaN in a query of one prompt of three: no entries for it, the search's verdict at its place, the others as they are."""
+    g, path = gen(14), small_path(S=4, num_pages=40)
+    q, k, v, pos = path_rows(path, g, 90)
+    q[1, 2, 45, 3] = float("nan")
+    path.prefill([3, 0, 2], [30, 30, 30], q, k, v, pos, [20, 20, 20])
+    assert int(path.status) == 0
+    assert path.search.tolist() == [1, 0, 0, 0] and path.cache.lens.sum(1).tolist() == [0, 0, 20, 20]
+    path.prefill([0], [30], *path_rows(path, g, 30), [20])
+    assert path.search.tolist() == [0, 0, 0, 0] and path.cache.lens.sum(1).tolist() == [20, 0, 20, 20]
