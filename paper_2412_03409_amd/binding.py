@@ -718,9 +718,16 @@ class RopePlan:
         _i32_like(self.axis, self.freq.shape, "axis")
         if self.axis.device != self.freq.device:
             raise ValueError("freq and axis must be on one device")
-        object.__setattr__(self, "_device", self.freq.get_device())
-        object.__setattr__(self, "_args", C.byref(_Rope(self.freq.data_ptr(), self.axis.data_ptr(), 2 * self.freq.shape[0],
-                                                        self.axes, int(self.interleaved))))
+        at = self.freq.data_ptr(), self.axis.data_ptr()
+        for name, x in (("_device", self.freq.get_device()), ("_at", at),
+                        ("_struct", C.byref(_Rope(*at, 2 * self.freq.shape[0], self.axes, int(self.interleaved))))):
+            object.__setattr__(self, name, x)
+
+    def _args(self):
+        """The argument struct, of where the tensors are now: a program may give them other storage."""
+        if (self.freq.data_ptr(), self.axis.data_ptr()) != self._at:
+            self.__post_init__()
+        return self._struct
 
 
 def rope_plan(rot_dim: int, sections=None, theta: float = 10000.0, interleaved: bool = False, cycled: bool = False,
@@ -786,13 +793,14 @@ def prefixkv_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, pla
                   q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
     """q [L,H,T,D], k [L,Hkv,T,D] (bf16 or f32, any strides with D contiguous), positions [axes,T] i32
     -> (q_out, k_out), rotated; q_out = q and k_out = k rotate in place."""
+    rope = plan._args()
     stream = _here(plan._device, q, k, positions, q_out, k_out)
     q_out = torch.empty_like(q) if q_out is None else q_out
     k_out = torch.empty_like(k) if k_out is None else k_out
     s, qs, ks, kos, qos = _rope_args(q.shape, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, q_out.shape, q_out.stride(),
                                      q_out.dtype, k_out.shape, k_out.stride(), k_out.dtype, positions.shape, positions.stride(),
                                      positions.dtype, plan.axes, None)
-    rc = load().prefixkv_rope(s, plan._args, positions.data_ptr(), q.data_ptr(), qs, k.data_ptr(), ks, q_out.data_ptr(), qos,
+    rc = load().prefixkv_rope(s, rope, positions.data_ptr(), q.data_ptr(), qs, k.data_ptr(), ks, q_out.data_ptr(), qos,
                               k_out.data_ptr(), kos, stream)
     if rc != 0:
         raise PrefixKVError(rc, "prefixkv_rope")
@@ -803,6 +811,7 @@ def prefixkv_rope_store(cache: PagedCache, q: torch.Tensor, k: torch.Tensor, v: 
                         plan: RopePlan, slots: torch.Tensor, q_out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Rotates q [L,H,T,D] and k [L,Hkv,T,D] and stores k and v into the cache's pages at slots [L,T] i64 -> q_out."""
     kp, vp = cache.kp, cache.vp
+    rope = plan._args()
     stream = _here(plan._device, q, k, v, positions, slots, q_out, kp)
     q_out = torch.empty_like(q) if q_out is None else q_out
     s, qs, ks, vs, qos = _rope_args(q.shape, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, q_out.shape, q_out.stride(),
@@ -810,7 +819,7 @@ def prefixkv_rope_store(cache: PagedCache, q: torch.Tensor, k: torch.Tensor, v: 
                                     positions.dtype, plan.axes, cache._pool or ())
     if slots.dtype is not torch.int64 or slots.shape != q.shape[::2] or not slots.is_contiguous():
         raise ValueError("slots must be contiguous i64 [L,T]")
-    rc = load().prefixkv_rope_store(s, plan._args, positions.data_ptr(), q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
+    rc = load().prefixkv_rope_store(s, rope, positions.data_ptr(), q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
                                     q_out.data_ptr(), qos, slots.data_ptr(), cache._paging, kp.data_ptr(), vp.data_ptr(), stream)
     if rc != 0:
         raise PrefixKVError(rc, "prefixkv_rope_store")
