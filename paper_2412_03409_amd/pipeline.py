@@ -189,8 +189,9 @@ class PagedPath:
 
     def end(self, places):
         """The sequences at these places are over: their pages are free again."""
+        places = [index(s) for s in places]
         if any(not 0 <= s < self.S for s in places):
             raise ValueError(f"places must be in 0 ... {self.S - 1}")
         self.target.copy_(self.cache.lens)
-        self.target[list(places)] = 0
+        self.target[places] = 0
         B_.prefixkv_page_resize(self.cache, self.target, status=self.status, ws=self.page_ws)

@@ -187,3 +187,14 @@ def test_a_prompt_that_the_search_cannot_rank_is_told():
     assert path.search.tolist() == [1, 0, 0, 0] and path.cache.lens.sum(1).tolist() == [0, 0, 20, 20]
     path.prefill([0], [30], *path_rows(path, g, 30), [20])
     assert path.search.tolist() == [0, 0, 0, 0] and path.cache.lens.sum(1).tolist() == [20, 0, 20, 20]
+
+
+def test_sequences_that_any_iterable_names_end():
+    g, path = gen(15), small_path(S=3, num_pages=30)
+    path.prefill([0, 1, 2], [20, 20, 20], *path_rows(path, g, 60), [10, 10, 10])
+    path.end(s for s in (0, 2))
+    assert path.cache.lens.sum(1).tolist() == [0, 10, 0]
+    path.end(np.array([1, 1]))
+    assert int(path.cache.lens.sum()) == 0 and int(path.cache.state[1]) == 30
+    path.end([])
+    assert int(path.status) == 0

@@ -1,5 +1,22 @@
 """Packed prompts and paged caches: what the host side does with a program's tensors and numbers, without a GPU."""
+import pytest
+import torch
+
 import paper_2412_03409_amd as P
+from paper_2412_03409_amd.pipeline import PagedPath
+
+
+def a_path(S=3, L=2, H=4, Hkv=2, D=64):
+    return PagedPath(S, L, H, Hkv, D, torch.ones(L), P.rope_plan(D, device="cpu"), num_pages=4, max_pages=2, device="cpu")
+
+
+def test_the_places_that_end_are_those_of_any_iterable():
+    path = a_path()
+    path.cache.lens.fill_(5)
+    for places in ([0, 2], (s for s in (0, 2)), iter([2, 0])):
+        with pytest.raises(ValueError, match="GPU"):        # (the call itself; what it asks for is there)
+            path.end(places)
+        assert path.target.tolist() == [[0, 0], [5, 5], [0, 0]]
 
 
 def test_a_rotation_goes_by_where_the_plan_s_tensors_are():
