@@ -115,6 +115,9 @@ class HotPath:
         self._graph.replay()
 
 
+_LONGEST = 8192      # positions of a prompt that the importance and the search take
+
+
 class PagedPath:
     """S places for sequences over one pool of pages.  All layers of the model are called at once, as the queries, keys and
     values [L,heads,T,D] of the packed rows of all layers are given (bf16).  Nothing is read back: `status` [1] tells whether
@@ -134,8 +137,19 @@ class PagedPath:
     def _offsets(self, lengths) -> torch.Tensor:
         off = [0]
         for n in lengths:
-            off.append(off[-1] + int(n))
+            off.append(off[-1] + n)
         return torch.tensor(off, dtype=torch.int32).to(self.device, non_blocking=True)
+
+    def _look_at(self, q, k, v, positions):
+        """What a later step would refuse is refused before the first: no prompt is left rotated, no length counts rows that were
+        not stored."""
+        T = q.shape[2] if q.dim() == 4 else 0
+        for x, heads in ((q, self.H), (k, self.Hkv), (v, self.Hkv)):
+            if (x.shape != (self.L, heads, T, self.D) or x.dtype != torch.bfloat16 or x.stride(3) != 1 or x.data_ptr() % 16
+                    or any(st % 8 for st, n in zip(x.stride()[:3], x.shape) if n > 1) or (T > 1 and x.stride(2) == 0)):
+                raise ValueError("queries, keys and values must be bf16 [L,heads,T,D], with rows that begin at multiples of 16 bytes")
+        if positions.dtype != torch.int32 or positions.shape != (self.plan.axes, T) or not positions.is_contiguous():
+            raise ValueError("positions must be contiguous i32 [axes,T]")
 
     def prefill(self, places, lengths, q, k, v, positions, budgets, kept_pos=None):
         """Prompts of these lengths, packed, for sequences that begin at `places`; budgets[i] of the L * lengths[i] entries are
@@ -144,8 +158,12 @@ class PagedPath:
         places, lengths = [index(s) for s in places], [index(n) for n in lengths]
         if len(set(places)) != len(places) or any(not 0 <= s < self.S for s in places):
             raise ValueError(f"places must be different numbers in 0 ... {self.S - 1}")
-        if not len(places) == len(lengths) == len(budgets) or any(n < 1 for n in lengths) or sum(lengths) > q.shape[2]:
+        if not 0 < len(places) == len(lengths) == len(budgets) or any(n < 1 for n in lengths) or sum(lengths) > q.shape[2]:
             raise ValueError("a length and a budget per place, rows for all of them")
+        budgets = [int(b) for b in budgets]
+        if any(n > _LONGEST for n in lengths) or any(not 1 <= b < 1 << 63 for b in budgets):
+            raise ValueError(f"prompts of at most {_LONGEST} positions, budgets of at least 1")
+        self._look_at(q, k, v, positions)
         off = self._offsets(lengths)
         B_.prefixkv_rope(q, k, positions, self.plan, q_out=q, k_out=k)
         out, lse = B_.prefixkv_prefill_attn_packed(q, k, v, off, self.scale)
@@ -155,7 +173,7 @@ class PagedPath:
             rows = slice(a, a + n)
             imp = B_.prefixkv_importance(q[None, :, :, rows], k[None, :, :, rows], self.scale,
                                          lse=lse[self.L * self.H * a:self.L * self.H * (a + n)].view(1, self.L, self.H, n))
-            sel = B_.prefixkv_select(imp, int(budget), want_prefix=False)
+            sel = B_.prefixkv_select(imp, budget, want_prefix=False)
             self.target[place].copy_(sel.lengths[0])
             self.search[place:place + 1].copy_(sel.status)
             rank.append((place, rows, sel))
@@ -178,12 +196,14 @@ class PagedPath:
         """Further rows of every sequence (lengths[s] of place s, 0 for one that waits): they are stored, and attend to what the
         cache holds and to each other.  One row each is a decode step.  -> attention output [L,H,T,D]; zeros if `status` says that
         the rows got no pages, and then nothing is stored and every length stays."""
+        lengths = [int(n) for n in lengths]
         if len(lengths) != self.S or any(n < 0 for n in lengths) or sum(lengths) > q.shape[2]:
             raise ValueError("a length per place, rows for all of them")
+        self._look_at(q, k, v, positions)
         off, T = self._offsets(lengths), q.shape[2]
         slots, _ = B_.prefixkv_page_append(self.cache, off, T, status=self.status, ws=self.page_ws)
         turned = B_.prefixkv_rope_store(self.cache, q, k, v, positions, self.plan, slots)
-        out = B_.prefixkv_chunk_attn(self.cache, turned, off, self.scale, max(1, max(int(n) for n in lengths)))
+        out = B_.prefixkv_chunk_attn(self.cache, turned, off, self.scale, max(1, max(lengths)))
         # (after a refused call the lengths do not count the rows: they would see the last entries of the cache as their own)
         return out.masked_fill_(self.status != 0, 0)
 

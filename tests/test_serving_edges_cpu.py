@@ -19,6 +19,30 @@ def test_the_places_that_end_are_those_of_any_iterable():
         assert path.target.tolist() == [[0, 0], [5, 5], [0, 0]]
 
 
+def test_a_path_refuses_rows_before_its_first_step(monkeypatch):
+    """What the attention, the search or the store would refuse: nothing has been rotated, and no page given, by then."""
+    import paper_2412_03409_amd.pipeline as pipeline
+    path = a_path()
+    for name in ("prefixkv_rope", "prefixkv_page_append"):
+        monkeypatch.setattr(pipeline.B_, name, lambda *a, **kw: pytest.fail("a step was made"))
+    T, bf = 9000, torch.bfloat16
+    rows = lambda h, dtype=bf, D=64: torch.zeros((2, h, T, D), dtype=dtype)
+    q, k, pos = rows(4), rows(2), torch.zeros((1, T), dtype=torch.int32)
+    wrong = [(q, k, rows(4), pos), (q, rows(4), k, pos), (rows(2), k, k, pos), (q, k, k.float(), pos), (q.float(), k.float(), k.float(), pos),
+             (q, k, k[:, :, 1:], pos), (q, k, rows(2, D=128), pos), (q, k[:1], k[:1], pos), (q[0], k, k, pos),
+             (q, k, rows(2, D=128)[..., ::2], pos), (q, k, rows(2, D=68)[..., :64], pos), (q, k, rows(2, D=72)[..., 4:68], pos),
+             (q, k, k[:, :, :1].expand(-1, -1, T, -1), pos), (q, k, k, pos[:, 1:]), (q, k, k, pos.long()),
+             (q, k, k, pos.expand(2, -1)), (q, k, k, torch.zeros((1, 2 * T), dtype=torch.int32)[:, ::2])]
+    for x in wrong:
+        with pytest.raises(ValueError):
+            path.prefill([0], [100], *x, [10])
+        with pytest.raises(ValueError):
+            path.extend([1, 0, 2], *x)
+    for places, lengths, budgets in (([0], [8193], [10]), ([0, 1], [5, 6], [5, 0]), ([0], [5], [-1]), ([0], [5], [1 << 63]), ([], [], [])):
+        with pytest.raises(ValueError):
+            path.prefill(places, lengths, q, k, k, pos, budgets)
+
+
 def test_a_rotation_goes_by_where_the_plan_s_tensors_are():
     """Tensors whose storage is replaced: the old one may belong to somebody else by the next call."""
     plan, other = P.rope_plan(64, [16, 16], device="cpu"), P.rope_plan(32, [8, 8], theta=500.0, device="cpu")
