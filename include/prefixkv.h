@@ -317,7 +317,8 @@ int prefixkv_decode_attn_evict(const pkv_shape *shape, int l0, int l1, const voi
  * row_off[s] ... row_off[s+1]-1 (none is a sequence without rows), rows in front of row_off[0] and from
  * row_off[S] on belong to nobody and are left as they are.  Row tensors are [L, heads, T, D] with
  * element strides l, h and n (b is not looked at, n may be any multiple of 16 bytes), so that a
- * projection's token-major [T, heads, D] output is passed as it is.
+ * projection's token-major [T, heads, D] output is passed as it is.  Inputs may repeat a layer or head (a stride of 0); the rows of
+ * an output are its own (PKV_ERR_STRIDE).
  *
  * The cache of a (sequence, layer) is a list of pages, because every layer keeps another number of
  * positions.  A page holds page_size entries of one (sequence, layer), all KV heads: kp and vp are

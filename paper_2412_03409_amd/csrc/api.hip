@@ -38,6 +38,10 @@ bool row_strides_ok(pkv_strides t, int esize) {
     t.b = 0;
     return strides_ok(t, esize);
 }
+// An output's: a layer or head stride of 0 would have several rows written (rotated in place: turned) over each other.
+bool out_strides_ok(const pkv_strides& t, int esize, int L, int heads) {
+    return row_strides_ok(t, esize) && (L == 1 || t.l > 0) && (heads == 1 || t.h > 0);
+}
 bool paging_ok(const pkv_paging* g) {
     return g->num_pages >= 1 && g->page_size >= 16 && g->page_size <= 256 && (g->page_size & (g->page_size - 1)) == 0 &&
            g->max_pages >= 1 && (int64_t)g->max_pages * g->page_size < kMaxSegmentSlots && g->layers >= 1 && g->layers <= kMaxL;
@@ -318,7 +322,7 @@ static int rope_checks(const pkv_packed* s, const pkv_rope* r, const int32_t* po
     if (!packed_ok(s) || !rope_ok(r, s->D)) return PKV_ERR_DIM;
     if (s->dtype != PKV_F32 && s->dtype != PKV_BF16) return PKV_ERR_DTYPE;
     const int e = s->dtype == PKV_F32 ? 4 : 2;
-    if (!row_strides_ok(qs, e) || !row_strides_ok(ks, e) || !row_strides_ok(qos, e) || !aligned16(q) || !aligned16(k) ||
+    if (!row_strides_ok(qs, e) || !row_strides_ok(ks, e) || !out_strides_ok(qos, e, s->L, s->H) || !aligned16(q) || !aligned16(k) ||
         !aligned16(q_out))
         return PKV_ERR_STRIDE;
     return PKV_OK;
@@ -328,7 +332,7 @@ int prefixkv_rope(const pkv_packed* s, const pkv_rope* r, const int32_t* pos, co
                   pkv_strides ks, void* q_out, pkv_strides qos, void* k_out, pkv_strides kos, pkv_stream stream) {
     if (const int rc = rope_checks(s, r, pos, q, qs, k, ks, q_out, qos)) return rc;
     if (!k_out) return PKV_ERR_NULL;
-    if (!row_strides_ok(kos, s->dtype == PKV_F32 ? 4 : 2) || !aligned16(k_out)) return PKV_ERR_STRIDE;
+    if (!out_strides_ok(kos, s->dtype == PKV_F32 ? 4 : 2, s->L, s->Hkv) || !aligned16(k_out)) return PKV_ERR_STRIDE;
     const hipError_t e = launch_rope(*s, *r, pos, q, to_strides(qs), k, to_strides(ks), nullptr, Strides{}, q_out,
                                      to_strides(qos), k_out, to_strides(kos), nullptr, nullptr, nullptr, nullptr,
                                      (hipStream_t)stream);
@@ -374,7 +378,7 @@ int prefixkv_prefill_attn_packed(const pkv_packed* s, const void* q, pkv_strides
     if (!packed_ok(s)) return PKV_ERR_DIM;
     if (s->dtype != PKV_F32 && s->dtype != PKV_BF16) return PKV_ERR_DTYPE;
     if (s->dtype != PKV_BF16) return PKV_ERR_UNSUPPORTED;
-    if (!row_strides_ok(qs, 2) || !row_strides_ok(ks, 2) || !row_strides_ok(vs, 2) || !row_strides_ok(os, 2) || !aligned16(q) ||
+    if (!row_strides_ok(qs, 2) || !row_strides_ok(ks, 2) || !row_strides_ok(vs, 2) || !out_strides_ok(os, 2, s->L, s->H) || !aligned16(q) ||
         !aligned16(k) || !aligned16(v) || !aligned16(out))
         return PKV_ERR_STRIDE;
     // the copies address 16 rows with 32-bit byte offsets
@@ -395,7 +399,7 @@ int prefixkv_chunk_attn(const pkv_packed* s, const void* q, pkv_strides qs, cons
     if (!packed_ok(s) || !paging_ok(g) || l0 < 0 || l0 > g->layers - s->L || max_rows < 1 || max_rows > s->T) return PKV_ERR_DIM;
     if (s->dtype != PKV_F32 && s->dtype != PKV_BF16) return PKV_ERR_DTYPE;
     const int esize = s->dtype == PKV_F32 ? 4 : 2;
-    if (!row_strides_ok(qs, esize) || !row_strides_ok(os, esize) || !aligned16(q) || !aligned16(kp) || !aligned16(vp) ||
+    if (!row_strides_ok(qs, esize) || !out_strides_ok(os, esize, s->L, s->H) || !aligned16(q) || !aligned16(kp) || !aligned16(vp) ||
         !aligned16(out))
         return PKV_ERR_STRIDE;
     if (!packed_attn_fits(*s, g)) return PKV_ERR_UNSUPPORTED;

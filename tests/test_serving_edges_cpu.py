@@ -1,8 +1,11 @@
 """Packed prompts and paged caches: what the host side does with a program's tensors and numbers, without a GPU."""
+import ctypes as C
+
 import pytest
 import torch
 
 import paper_2412_03409_amd as P
+from paper_2412_03409_amd import binding as Bd
 from paper_2412_03409_amd.pipeline import PagedPath
 
 
@@ -52,3 +55,31 @@ def test_a_rotation_goes_by_where_the_plan_s_tensors_are():
     now = plan._args()._obj
     assert (now.freq, now.axis) == (plan.freq.data_ptr(), plan.axis.data_ptr())
     assert now.rot_dim == 32 and now.axes == 2
+
+
+def test_rows_of_an_output_are_its_own():
+    """A layer or head stride of 0 repeats an input; as an output, or rotated in place, it is refused.  (A
+    workspace off by four bytes, which is looked at behind the strides, tells that an input was not.)"""
+    A, odd, dims = C.c_void_p(4096), C.c_void_p(4100), dict(S=1, L=2, H=4, Hkv=2, T=10, D=64)
+    ST, lib = Bd._Strides(0, 8192, 128, 4096), P.load()
+    shape = C.byref(Bd._Packed(*dims.values(), P.PKV_BF16))
+    rope = C.byref(Bd._Rope(4096, 4096, 64, 1, 0))
+    paging = C.byref(Bd._Paging(8, 16, 4, 2))
+    calls = [  # the call, its output strides, and where its keys' strides are
+        (lib.prefixkv_rope, [shape, rope, A, A, ST, A, ST, A, ST, A, ST, None], (8, 10)),
+        (lib.prefixkv_rope_store, [shape, rope, A, A, ST, A, ST, A, ST, A, ST, A, paging, A, A, None], (10,)),
+        (lib.prefixkv_prefill_attn_packed, [shape, A, ST, A, ST, A, ST, A, A, A, ST, A, A, 1 << 30, None], (10,)),
+        (lib.prefixkv_chunk_attn, [shape, A, ST, A, paging, 0, A, A, A, A, A, 10, A, ST, A, 1 << 30, None], (13,))]
+    for f, args, outs in calls:
+        for i in outs:
+            for st in (Bd._Strides(0, 0, 128, 4096), Bd._Strides(0, 8192, 0, 4096)):
+                assert f(*[st if j == i else x for j, x in enumerate(args)]) == 4
+        ins = [i for i, x in enumerate(args) if x is ST and i not in outs]
+        for i in ins:
+            for st in (Bd._Strides(0, 0, 128, 4096), Bd._Strides(0, 8192, 0, 4096)):
+                bad = [st if j == i else x for j, x in enumerate(args)]
+                if f is lib.prefixkv_prefill_attn_packed or f is lib.prefixkv_chunk_attn:
+                    bad[-3] = odd                                   # the workspace, which is looked at behind the strides
+                    need = P.attn_workspace_bytes(**dims, dtype=torch.bfloat16, max_rows=10 if f is lib.prefixkv_chunk_attn else 0)
+                    if need:
+                        assert f(*bad) == 5
