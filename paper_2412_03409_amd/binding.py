@@ -647,6 +647,13 @@ def _here(d: int, *ts) -> int:
     return _raw_stream(d) if _raw_stream is not None else torch.cuda.current_stream(d).cuda_stream
 
 
+def _c_int(x: int, what: str) -> int:
+    """A number for an int argument: ctypes would take it modulo 2^32."""
+    if not -(1 << 31) <= x < 1 << 31:
+        raise ValueError(f"{what} does not fit 32 bits")
+    return x
+
+
 def _i32_like(t: torch.Tensor, shape, what: str) -> torch.Tensor:
     if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous i32 {list(shape)}")
@@ -690,7 +697,7 @@ def prefixkv_page_append(cache: PagedCache, row_off: torch.Tensor, T: int, slots
     -> (slots [layers,T] i64, status [1] i32)."""
     lens, table, ring, state = cache.lens, cache.table, cache.ring, cache.state
     stream = _here(cache._device, row_off, slots, status, lens_out, state_out, ws)
-    T = index(T)
+    T = _c_int(index(T), "T")
     _i32_like(row_off, cache._offs, "row_off")
     if slots is None:
         slots = torch.empty((cache._layers, T), dtype=torch.int64, device=lens.device)
@@ -842,7 +849,7 @@ def prefixkv_compact_paged(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, 
         raise ValueError("the cache must have k's heads, head dimension and dtype, B sequences and contiguous pools")
     s = _shape_of(B, L, Hkv, Hkv, N, D, _dtype_code(k))
     rc = load().prefixkv_compact_paged(C.byref(s), k.data_ptr(), _strides5(k), v.data_ptr(), _strides5(v), order.data_ptr(),
-                                       lengths.data_ptr(), cache._paging, int(l0), cache.table.data_ptr(), cache.kp.data_ptr(),
+                                       lengths.data_ptr(), cache._paging, _c_int(int(l0), "l0"), cache.table.data_ptr(), cache.kp.data_ptr(),
                                        cache.vp.data_ptr(), _ptr(kept_pos), stream)
     if rc != 0:
         raise PrefixKVError(rc, "prefixkv_compact_paged")
@@ -851,7 +858,7 @@ def prefixkv_compact_paged(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, 
 
 def attn_workspace_bytes(S: int, L: int, H: int, Hkv: int, T: int, D: int, dtype: torch.dtype, max_rows: int = 0) -> int:
     """Workspace of prefixkv_chunk_attn, or (max_rows = 0) of prefixkv_prefill_attn_packed."""
-    return int(load().prefixkv_attn_workspace_bytes(C.byref(_packed(S, Hkv, (L, H, T, D), dtype)), int(max_rows)))
+    return int(load().prefixkv_attn_workspace_bytes(C.byref(_packed(S, Hkv, (L, H, T, D), dtype)), _c_int(int(max_rows), "max_rows")))
 
 
 @lru_cache(maxsize=512)
@@ -905,7 +912,7 @@ def prefixkv_chunk_attn(cache: PagedCache, q: torch.Tensor, row_off: torch.Tenso
     kp, vp, table, lens = cache.kp, cache.vp, cache.table, cache.lens
     stream = _here(cache._device, q, row_off, scale, out, ws)
     out = torch.empty_like(q) if out is None else out
-    pool, max_rows = cache._pool, index(max_rows)
+    pool, max_rows = cache._pool, _c_int(index(max_rows), "max_rows")
     qsh = q.shape
     if pool is None or pool[1:] != (qsh[3], q.dtype):
         raise ValueError("the cache must have q's head dimension and dtype, and contiguous pools")
@@ -914,7 +921,7 @@ def prefixkv_chunk_attn(cache: PagedCache, q: torch.Tensor, row_off: torch.Tenso
     if scale.dtype is not torch.float32 or scale.shape != qsh[:1] or not scale.is_contiguous():
         raise ValueError("scale must be contiguous f32 [L]")
     w = _ws(need, q.device, ws)
-    rc = load().prefixkv_chunk_attn(s, q.data_ptr(), qs, row_off.data_ptr(), cache._paging, int(l0), kp.data_ptr(),
+    rc = load().prefixkv_chunk_attn(s, q.data_ptr(), qs, row_off.data_ptr(), cache._paging, _c_int(int(l0), "l0"), kp.data_ptr(),
                                     vp.data_ptr(), table.data_ptr(), lens.data_ptr(), scale.data_ptr(), max_rows,
                                     out.data_ptr(), os_, w.data_ptr(), w.numel() * w.element_size(), stream)
     if rc != 0:

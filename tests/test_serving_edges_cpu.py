@@ -83,3 +83,30 @@ def test_rows_of_an_output_are_its_own():
                     need = P.attn_workspace_bytes(**dims, dtype=torch.bfloat16, max_rows=10 if f is lib.prefixkv_chunk_attn else 0)
                     if need:
                         assert f(*bad) == 5
+
+
+def test_numbers_that_an_int_does_not_hold_are_refused(monkeypatch):
+    """Not taken modulo 2^32: rows or layers of another number would be worked on."""
+    class Library:
+        prefixkv_attn_workspace_bytes = P.load().prefixkv_attn_workspace_bytes
+        prefixkv_page_workspace_bytes = P.load().prefixkv_page_workspace_bytes
+
+        def __getattr__(self, name):
+            return lambda *a: pytest.fail(f"{name} was called")
+    monkeypatch.setattr(Bd, "_here", lambda *a: 0)
+    monkeypatch.setattr(Bd, "load", Library)
+    cache = P.paged_cache(1, 2, 2, 64, 16, 4, 4, device="cpu")
+    off, scale = torch.tensor([0, 3], dtype=torch.int32), torch.ones(1)
+    q, kv = torch.zeros((1, 4, 3, 64), dtype=torch.bfloat16), torch.zeros((1, 1, 2, 3, 64), dtype=torch.bfloat16)
+    order, lengths = torch.zeros((1, 1, 3), dtype=torch.int32), torch.zeros((1, 1), dtype=torch.int32)
+    for x in ((1 << 32) + 1, 1 << 31, -(1 << 32)):
+        with pytest.raises(ValueError, match="max_rows"):
+            P.prefixkv_chunk_attn(cache, q, off, scale, x)
+        with pytest.raises(ValueError, match="l0"):
+            P.prefixkv_chunk_attn(cache, q, off, scale, 3, l0=x)
+        with pytest.raises(ValueError, match="l0"):
+            P.prefixkv_compact_paged(cache, kv, kv, order, lengths, l0=x)
+        with pytest.raises(ValueError, match="T"):
+            P.prefixkv_page_append(cache, off, x)
+        with pytest.raises(ValueError, match="max_rows"):
+            P.attn_workspace_bytes(1, 1, 4, 2, 3, 64, torch.bfloat16, max_rows=x)
