@@ -19,8 +19,8 @@
 //
 // The two bf16 kernels work as the prompt attention of rectangular batches does: S^T[32 keys x 32 rows] = K Q^T and
 // O^T[32 columns x 32 rows] += V^T P^T with v_mfma_f32_32x32x16_bf16.  A lane holds one row's scores, so the softmax state is a
-// scalar per lane, and the probabilities, rounded to bf16 against the running maximum, are the second product's operand where
-// they are.  V^T comes from row-major V by the transposing LDS read.
+// scalar per lane, and the probabilities, as bf16 against the running maximum (the stream kernel: as two bf16 numbers each), are the
+// second product's operand where they are.  V^T comes from row-major V by the transposing LDS read.
 #include "packed.hpp"
 #include "fast_div.hpp"
 #include "packed_rules.hpp"
@@ -288,9 +288,10 @@ struct RowTile {
 
     // NKT tiles of 32 staged keys.  MASKED: the row sees the keys up to `lim` (of the stage), bit x of `bad` hides keys
     // 16x ... 16x+15, tiles from `tiles` on are seen by no row of the wavefront, those in front of `full` by all of them.  The
-    // probabilities are rounded to bf16 (the product's operand) against the maximum up to the end of these tiles; their sum is of the
-    // unrounded ones, in fp32.
-    template <int NKT, bool MASKED>
+    // probabilities are rounded to bf16 (the product's operand) against the maximum up to the end of these tiles, as in the prompt
+    // attention of rectangular batches; their sum is of the unrounded ones, in fp32.  SPLIT: each is the sum of two bf16 numbers, 16 bits
+    // in all, for twice the second products, which a stream of keys that HBM bounds hides.
+    template <int NKT, bool MASKED, bool SPLIT = false>
     __device__ __forceinline__ void attend(const unsigned char* sK, const unsigned char* sV, float qs, int lane, int lim, uint32_t bad,
                                            int tiles, int full) {
         constexpr int ROWB = D * 2, NJ = D / 16, NDT = D / 32, CPR = D / 8;
@@ -370,20 +371,30 @@ struct RowTile {
 #pragma unroll
         for (int kt = 0; kt < NKT; ++kt) {
             if (MASKED && kt >= tiles) break;
-            bf16x8_t pf[2];
+            bf16x8_t pf[2], rest[2];
             float psum = 0.f;
 #pragma unroll
             for (int sl = 0; sl < 2; ++sl) {
-                uint32_t pk[4];
+                uint32_t pk[4], rk[4];
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
                     const float p0 = __builtin_amdgcn_exp2f(fmaf(s[kt][8 * sl + e], qs, -ref));
                     const float p1 = __builtin_amdgcn_exp2f(fmaf(s[kt][8 * sl + e + 1], qs, -ref));
                     psum += p0 + p1;
-                    pk[e / 2] = pack_bf16(p0, p1);
+                    if constexpr (SPLIT) {
+                        // The upper part is the bf16 number below p and not the nearest, the rest above 0: an infinite value, times
+                        // both, stays one.  (0 has two zeros: a key that is not seen adds nothing.)
+                        const uint32_t u0 = __builtin_elementwise_sub_sat(__float_as_uint(p0), 1u) & 0xffff0000u;
+                        const uint32_t u1 = __builtin_elementwise_sub_sat(__float_as_uint(p1), 1u) & 0xffff0000u;
+                        pk[e / 2] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);
+                        rk[e / 2] = pack_bf16(p0 - __uint_as_float(u0), p1 - __uint_as_float(u1));
+                    } else {
+                        pk[e / 2] = pack_bf16(p0, p1);
+                    }
                     if constexpr (MASKED) { s[kt][8 * sl + e] = p0; s[kt][8 * sl + e + 1] = p1; }
                 }
                 pf[sl] = __builtin_bit_cast(bf16x8_t, make_uint4(pk[0], pk[1], pk[2], pk[3]));
+                if constexpr (SPLIT) rest[sl] = __builtin_bit_cast(bf16x8_t, make_uint4(rk[0], rk[1], rk[2], rk[3]));
             }
             sum += psum;
             if constexpr (MASKED) {
@@ -427,8 +438,9 @@ struct RowTile {
                     const v4i16_t a0 = lds_read_tr(sVs + voff[dt][0]), a1 = lds_read_tr(sVs + voff[dt][1]);
                     const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
                     o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[sl], o[dt], 0, 0, 0);
+                    if constexpr (SPLIT) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, rest[sl], o[dt], 0, 0, 0);
                 }
-            if constexpr (MASKED) {          // (nothing else is left to hide the reads' way: 29.3 us -> 28.9 for six short prompts)
+            if constexpr (MASKED && !SPLIT) {          // (nothing else is left to hide the reads' way: 29.3 us -> 28.9 for six short prompts)
                 __builtin_amdgcn_sched_group_barrier(0x100, 2 * NDT, 0);
 #pragma unroll
                 for (int i = 0; i < NDT; ++i) {
@@ -1059,8 +1071,8 @@ attn_stream_kernel(StreamParams p) {
     };
     auto attend = [&](const unsigned char* sK, const unsigned char* sV, uint32_t bad) {
         const int key0 = cw.blk * kBlockKeys;
-        if (key0 + kBlockKeys - 1 <= sg.before && bad == 0) tl.template attend<1, false>(sK, sV, qs, lane, 0, 0u, 1, 1);
-        else tl.template attend<1, true>(sK, sV, qs, lane, lim - key0, bad, 1, 0);
+        if (key0 + kBlockKeys - 1 <= sg.before && bad == 0) tl.template attend<1, false, true>(sK, sV, qs, lane, 0, 0u, 1, 1);
+        else tl.template attend<1, true, true>(sK, sV, qs, lane, lim - key0, bad, 1, 0);
     };
     // one block of the work: `more` blocks are in flight behind it
     auto work = [&](int b, const unsigned char* sK, const unsigned char* sV, uint32_t bad) {

@@ -198,3 +198,41 @@ def test_sequences_that_any_iterable_names_end():
     assert int(path.cache.lens.sum()) == 0 and int(path.cache.state[1]) == 30
     path.end([])
     assert int(path.status) == 0
+
+
+# ---- single tokens keep their probabilities ----------------------------------------------------------------
+@pytest.mark.parametrize("H,Hkv,D,ps,n,sizes", [(16, 2, 128, 16, [1, 1, 1], [5, 64, 2100]), (6, 3, 64, 32, [4, 16, 2], [40, 16, 900]),
+                                                (4, 4, 128, 64, [32, 1], [33, 300]), (32, 1, 128, 16, [1] * 40, [3] * 39 + [700])])
+def test_chunk_attn_of_few_rows_rounds_its_output_only(H, Hkv, D, ps, n, sizes):
+    """Decode steps weigh bf16 values with more than bf16 probabilities, as prefixkv_decode_attn does.  A probability is the sum of two
+    bf16 numbers, the second below 2^-7 of it and rounded by 2^-9 of itself: 2^-16 of sum p|v|, next to the logits' 2e-4."""
+    lens = np.array(sizes)[:, None]
+    c, table = chunk_state(23, len(n), 1, Hkv, D, ps, lens, BF16)
+    off = offsets(n)
+    q, _, _ = projected(gen(24), 1, H, Hkv, int(off[-1]), D, BF16)
+    scale = torch.tensor([0.1], device=DEV)
+    out = P.prefixkv_chunk_attn(c, q, i32(off), scale, max(n))
+    want, mag = R.chunk(f64(q), off, f64(c.kp), f64(c.vp), table, lens, scale.double().cpu().numpy())
+    bar = 2.0 ** -8 * np.abs(want) + (2.0 ** -16 + 2e-4) * mag
+    assert np.all(np.abs(f64(out) - want) <= bar), float(np.max(np.abs(f64(out) - want) / bar))
+
+
+def test_chunk_attn_of_few_rows_infinite_values_stay_infinite():
+    """Values that every row sees: an infinite one makes its column infinite (NaN with one of either sign), and no other column."""
+    H, Hkv, D, ps, n, sizes = 4, 2, 64, 16, [1, 3], [300, 2100]
+    lens = np.array(sizes)[:, None]
+    c, table = chunk_state(25, 2, 1, Hkv, D, ps, lens, BF16)
+    off = offsets(n)
+    q, _, _ = projected(gen(26), 1, H, Hkv, int(off[-1]), D, BF16)
+    q *= 0.05                          # (weights far from underflow)
+    for s, j, column, value in ((0, 7, 3, float("inf")), (0, 250, 9, float("-inf")), (1, 40, 3, float("inf")), (1, 1999, 3, float("-inf")),
+                                (1, 900, 20, float("inf")), (1, 31, 21, torch.finfo(BF16).max)):
+        c.vp[int(table[s, 0, j // ps]), :, j % ps, column] = value
+    out = P.prefixkv_chunk_attn(c, q, i32(off), torch.tensor([0.1], device=DEV), max(n))[0].float()
+    inf = torch.isinf(out) | torch.isnan(out)
+    want = torch.zeros_like(inf)
+    want[:, :1, [3, 9]] = True
+    want[:, 1:, [3, 20]] = True
+    assert torch.equal(inf, want)
+    assert bool((out[:, 0, 3] == float("inf")).all()) and bool((out[:, 0, 9] == float("-inf")).all())
+    assert bool(torch.isnan(out[:, 1:, 3]).all()) and bool((out[:, 1:, 20] == float("inf")).all())
