@@ -1,5 +1,6 @@
 """Packed prompts and paged caches where a serving program's state is unusual: sequences that wait beside others, a ring of free
-pages whose ends cannot be, scores as large as the type holds.  Every output against its plain form in 64 bits, with the bars of test_gpu_serving.py."""
+pages whose ends cannot be, scores as large as the type holds, tiles that several workgroups share.  Every output against its
+plain form in 64 bits, with the bars of test_gpu_serving.py."""
 import numpy as np
 import pytest
 import torch
@@ -7,6 +8,7 @@ import torch
 import paper_2412_03409_amd as P
 import serving_reference as R
 from test_gpu_serving import BF16, DEV, F32, as_cache, chunk_state, close, f64, gen, i32, offsets, page_state, projected
+from tolerances import LSE_ATOL, LSE_RTOL
 
 pytestmark = pytest.mark.gpu
 
@@ -236,3 +238,41 @@ def test_chunk_attn_of_few_rows_infinite_values_stay_infinite():
     assert torch.equal(inf, want)
     assert bool((out[:, 0, 3] == float("inf")).all()) and bool((out[:, 0, 9] == float("-inf")).all())
     assert bool(torch.isnan(out[:, 1:, 3]).all()) and bool((out[:, 1:, 20] == float("inf")).all())
+
+
+# ---- tiles that several workgroups share -------------------------------------------------------------------
+@pytest.mark.parametrize("L,H,Hkv,n,first", [(2, 4, 2, [2500, 1, 200], 0), (1, 8, 8, [2047], 3)])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_cut_prompts(L, H, Hkv, n, first, sign):
+    """Head dimension 128, several layers: outputs and log-sum-exps that the join writes."""
+    D, off = 128, offsets(n, first)
+    T = int(off[-1]) + 1
+    assert P.attn_workspace_bytes(len(n), L, H, Hkv, T, D, BF16) > 0          # (only a launch that cuts tiles has one)
+    q, k, v = projected(gen(27), L, H, Hkv, T, D, BF16)
+    scale = torch.tensor([0.08, 0.13][:L]) * sign
+    out, lse = torch.full_like(q, 77.0), torch.full((L * H * T,), 77.0, device=DEV)
+    P.prefixkv_prefill_attn_packed(q, k, v, i32(off), scale.to(DEV), out=out, lse=lse)
+    want, mag, wlse = R.prompt(f64(q), f64(k), f64(v), off, scale.double().numpy())
+    close(out, want, mag, BF16)
+    assert bool((out[torch.from_numpy(np.isnan(want)).to(DEV)] == 77).all())
+    real, z = ~np.isnan(wlse), f64(lse)
+    assert np.all(z[~real] == 77)
+    assert np.all(np.abs(z - wlse)[real] <= LSE_RTOL * np.abs(wlse[real]) + LSE_ATOL)
+
+
+@pytest.mark.parametrize("H,Hkv,D,ps", [(8, 2, 128, 64), (2, 1, 64, 16)])
+def test_cut_chunks_with_pages_outside_the_pool(H, Hkv, D, ps):
+    """Entries on pages that are not there take no part, in whichever workgroup's share they lie, and whole stages of them."""
+    L, n = 2, [100, 2, 64]
+    lens = np.array([[5000, 4000], [70, 300], [640, 3500]])
+    c, table = chunk_state(28, 3, L, Hkv, D, ps, lens, BF16)
+    for s, l, entry in ((0, 0, 200), (0, 0, 2600), (0, 0, 4999), (0, 1, 0), (1, 1, 299), (2, 0, 64), (2, 1, 3400)):
+        table[s, l, entry // ps] = (-1, c.kp.shape[0], 1 << 30)[entry % 3]
+    table[0, 1, 640 // ps:1280 // ps] = -5
+    c.table.copy_(i32(table))
+    off = offsets(n)
+    q, _, _ = projected(gen(29), L, H, Hkv, int(off[-1]), D, BF16)
+    scale = torch.tensor([0.1, -0.15], device=DEV)
+    out = P.prefixkv_chunk_attn(c, q, i32(off), scale, max(n))
+    want, mag = R.chunk(f64(q), off, f64(c.kp), f64(c.vp), table, lens, scale.double().cpu().numpy())
+    close(out, want, mag, BF16)
