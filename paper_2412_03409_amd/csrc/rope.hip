@@ -15,9 +15,8 @@
 namespace pkv {
 
 struct RopeParams {
-    int T, H, Hkv, D, L;
-    int group;                 // heads that a lane takes one after the other
-    int groups;                // groups of all heads: query heads, key heads, with a store also value heads
+    int T, H, Hkv;
+    int group;                 // heads that a lane takes one after the other: query heads, key heads, with a store also value heads
     int num_pages, shift, axes;
     const uint64_t* freq;
     const int32_t* axis;
@@ -170,7 +169,7 @@ hipError_t launch_rope(const pkv_packed& s, const pkv_rope& r, const int32_t* po
     const int esize = s.dtype == PKV_F32 ? 4 : 2;
     auto bytes = [esize](Strides x) { return Strides{0, x.l * esize, x.h * esize, x.n * esize}; };
     RopeParams p;
-    p.T = s.T; p.H = s.H; p.Hkv = s.Hkv; p.D = s.D; p.L = s.L;
+    p.T = s.T; p.H = s.H; p.Hkv = s.Hkv;
     p.num_pages = g ? g->num_pages : 0; p.shift = g ? __builtin_ctz((unsigned)g->page_size) : 0; p.axes = r.axes;
     p.freq = r.freq; p.axis = r.axis; p.pos = pos;
     p.q = (const unsigned char*)q; p.k = (const unsigned char*)k; p.v = (const unsigned char*)v;
@@ -182,8 +181,8 @@ hipError_t launch_rope(const pkv_packed& s, const pkv_rope& r, const int32_t* po
     // Groups of up to eight heads share a token's sines while that leaves the chip four workgroups per compute unit.
     int group = 8;
     while (group > 1 && rows * s.L * ((all + group - 1) / group) < 4ll * compute_units()) group >>= 1;
-    p.group = group; p.groups = (all + group - 1) / group;
-    const dim3 grid((unsigned)rows, (unsigned)p.groups, (unsigned)s.L);
+    p.group = group;
+    const dim3 grid((unsigned)rows, (unsigned)((all + group - 1) / group), (unsigned)s.L);
     const int half = r.rot_dim / 2 * esize / 16;
     const bool inter = r.interleaved != 0, store = slots != nullptr;
     if (s.dtype == PKV_BF16) {
