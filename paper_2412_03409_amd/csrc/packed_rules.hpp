@@ -18,12 +18,11 @@ __host__ __device__ __forceinline__ int keys_seen(int rows, int n, int len) {
     return rows <= 0 || end <= 0 ? 0 : end < len ? end : len;
 }
 
-// Whether a call may take `taken` pages from the head of the ring and put `given` behind its end: 0, or why not.  The places it puts
-// them into must be free before the call, too: they are disjoint from those it takes from, and none lies a second turn ahead.  (Pages
-// that segments hold are not in the ring, so ends that are possible always have that room.)
-__host__ __device__ __forceinline__ int ring_verdict(int head, int count, int taken, int given, int num_pages) {
-    if (head < 0 || head >= num_pages || count < 0 || count > num_pages || given > num_pages - count) return PKV_PAGES_RANGE;
-    return taken > count ? PKV_PAGES_SHORT : 0;
+// Ends of the ring that cannot be, for a call that gives `given` pages back: the places behind the end that it puts them into must be
+// free before the call, so that they are disjoint from those it takes from at the head, and none lies a second turn ahead.  (Pages that
+// segments hold are not in the ring, so ends that are possible always have that room.)
+__host__ __device__ __forceinline__ bool ring_range(int head, int count, int given, int num_pages) {
+    return head < 0 || head >= num_pages || count < 0 || count > num_pages || (int64_t)count + given > num_pages;
 }
 // The place `at` places behind place 0, for at < 2 num_pages: head + i for i < taken, head + count + i for i < given.
 __host__ __device__ __forceinline__ int ring_place(uint32_t at, int num_pages) {

@@ -142,8 +142,9 @@ page_plan_kernel(PageParams p) {
         }
     }
     __syncthreads();
-    const int verdict = s_bad != 0 ? (int)PKV_PAGES_RANGE : ring_verdict(head, count, carry.x, carry.y, p.num_pages);
-    const bool ok = verdict == 0;
+    const bool range = s_bad != 0 || ring_range(head, count, carry.y, p.num_pages);
+    const bool few = carry.x > count;
+    const bool ok = !range && !few;
     const int4 hd = make_int4(ok ? 1 : 0, head, count, 0);
     // (every thread has read what it needs of lens and state in front of the barrier: lens_out and state_out may be the same)
     if constexpr (SMALL) {
@@ -169,7 +170,7 @@ page_plan_kernel(PageParams p) {
     if (tid == 0) {
         p.state_out[0] = ok ? ring_at(p, (uint32_t)head + (uint32_t)carry.x) : head;
         p.state_out[1] = ok ? count - carry.x + carry.y : count;
-        *p.status = verdict;
+        *p.status = range ? PKV_PAGES_RANGE : few ? PKV_PAGES_SHORT : 0;
         if constexpr (!SMALL) *p.head = hd;
     }
     if constexpr (!APPEND && SMALL) {

@@ -17,7 +17,7 @@ SHIM = """
 #include "packed_rules.hpp"
 extern "C" int new_rows(int first, int last, int T) { return pkv::new_rows(first, last, T); }
 extern "C" int keys_seen(int rows, int n, int len) { return pkv::keys_seen(rows, n, len); }
-extern "C" int ring_verdict(int head, int count, int taken, int given, int P) { return pkv::ring_verdict(head, count, taken, given, P); }
+extern "C" int ring_range(int head, int count, int given, int P) { return pkv::ring_range(head, count, given, P); }
 extern "C" int ring_place(unsigned at, int P) { return pkv::ring_place(at, P); }
 extern "C" int gather_chunks(int N) { return pkv::gather_chunks(N); }
 extern "C" int gather_fits(int N, int Hkv, long long segments) { return pkv::gather_fits(N, Hkv, segments); }
@@ -56,23 +56,20 @@ def test_keys_of_a_segment(rules):
 
 def test_ring_of_free_pages(rules):
     """Every place that an accepted call touches is in the ring, and none is both read and written, whatever the ends are."""
-    short, wrong = 1, 2
     for P in range(1, 8):
         for head in range(-1, P + 2):
             for count in range(-1, P + 2):
-                for taken in range(0, P + 3):
-                    for given in range(0, P + 3):
-                        v = rules.ring_verdict(head, count, taken, given, P)
-                        real = 0 <= head < P and 0 <= count <= P and count + given <= P
-                        assert v == (wrong if not real else short if taken > count else 0), (P, head, count, taken, given)
-                        if v == 0:
-                            places = [rules.ring_place(head + i, P) for i in range(taken)]
-                            places += [rules.ring_place(head + count + i, P) for i in range(given)]
-                            assert len(set(places)) == taken + given and all(0 <= x < P for x in places)
-                            assert places == [(head + i) % P for i in range(taken)] + [(head + count + i) % P for i in range(given)]
+                for given in range(0, P + 3):
+                    wrong = rules.ring_range(head, count, given, P)
+                    assert wrong == (not (0 <= head < P and 0 <= count <= P and count + given <= P)), (P, head, count, given)
+                    for taken in range(0, 0 if wrong else count + 1):
+                        places = [rules.ring_place(head + i, P) for i in range(taken)]
+                        places += [rules.ring_place(head + count + i, P) for i in range(given)]
+                        assert len(set(places)) == taken + given and all(0 <= x < P for x in places)
+                        assert places == [(head + i) % P for i in range(taken)] + [(head + count + i) % P for i in range(given)]
     top = (1 << 31) - 1
-    assert rules.ring_verdict(top - 1, top, top, 0, top) == 0 and rules.ring_verdict(top - 1, top, 1, 1, top) == wrong
-    assert rules.ring_verdict(0, 0, 0, top, top) == 0 and rules.ring_place(2 * top - 1, top) == top - 1
+    assert not rules.ring_range(top - 1, top, 0, top) and rules.ring_range(top - 1, top, 1, top)
+    assert not rules.ring_range(0, 0, top, top) and rules.ring_range(0, 1, top, top) and rules.ring_place(2 * top - 1, top) == top - 1
 
 
 def test_workgroups_of_a_compaction(rules):
