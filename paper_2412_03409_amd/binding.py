@@ -595,6 +595,7 @@ def prefixkv_decode_attn_evict(cache: CompactResult, base_lens: torch.Tensor, q:
 # ---- packed prompts and paged caches -----------------------------------------------------------------------
 # These calls come once per layer and step, and the small ones take the GPU less time than a look at ten tensors takes here:
 # what follows from shapes, strides and types alone (the checks and the argument structs) is worked out once per combination.
+# (Addresses are asked for in every call.  A cache whose tensors get another shape is another PagedCache.)
 @dataclass(frozen=True, eq=False)
 class PagedCache:
     kp: torch.Tensor      # [num_pages,Hkv,page_size,D] storage dtype

@@ -9,7 +9,7 @@
 //                     the longest tile, 1.27 us a stage and about 6 us to begin and end (680 rows of 32 heads 19 to 20 us).
 //  attn_stream_kernel bf16, at most 32 rows per (sequence, KV head): decode steps.  A wavefront streams 32 keys at a time through
 //                     LDS of its own.  All keys of a launch are one sequence of blocks that the wavefronts share out evenly,
-//                     wherever the units begin and end.  Bound: HBM; 467 MB of keys and values of 32 sequences in 88 us, 5.3 TB/s
+//                     wherever the units begin and end.  Bound: HBM; 467 MB of keys and values of 32 sequences in 90 us, 5.2 TB/s
 //                     (a plain read reaches 5.8), and 5 us to join.
 //  attn_merge_*       join the parts of a tile or unit that several workgroups or wavefronts worked on.
 //  attn_rows_kernel   fp32: a workgroup per (row, head, layer).  The keys stream past one row: LPR lanes hold a key
@@ -308,7 +308,7 @@ struct RowTile {
                 const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *(const uint4*)(sK + kt * 32 * ROWB + koff[j]));
                 s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[j], s[kt], 0, 0, 0);
             }
-        // Six fragments ahead (4, 8 and 11: up to 1 % slower); left to itself the compiler reads one, waits for it and multiplies.  (Two
+        // Six fragments ahead (4 to 11 are within the spread of 1 %); left to itself the compiler reads one, waits for it and multiplies.  (Two
         // tiles' products in turn have no wait for each other either.  680 rows, H32: 21.6 us -> 19.9.  The exponentials of one tile
         // spread between the products of the other by the same means, in this order or a tile at a time, gave nothing or cost 4 %.)
         constexpr int kFrags = NKT * NJ, kEarly = kFrags < 6 ? kFrags : 6;
@@ -1203,7 +1203,10 @@ static long long most_tiles(const pkv_packed& s) { return (long long)s.T * (s.H 
 // to the second and costs about 30 us (parts, joining them, shares, a phase of its own for every workgroup).  The longest tile and the
 // average are taken from the most that can be: the rows of a prompt, the width of a table row, of which a cache holds three quarters.
 // us, whole / cut: H32/8, 512 rows over 8192 keys 178 / 108, 4 x 128 rows 168 / 104, 16 x 40 over 2000 50 / 59; H32, 8 x 64 over 1000
-// 31 / 46, 64 over 4000 80 / 40; prompts: H32 680 19 / 37, 2048 52 / 69, H8 2048 43 / 38, H12/4 6000 140 / 149.
+// 31 / 46, 64 over 4000 80 / 40; one prompt: H32 680 19 / 37, 2048 52 / 69, H8 2048 43 / 38, H12/4 6000 140 / 149.
+// What the lengths are is on the device, so the bounds are wide where the rows are several prompts' (T stands for the longest) or the
+// table is wider than its caches, and launches are cut that would be faster whole: prompts of H12/4, 6 x 500 21 / 31, H8/2, 12 x 500
+// 24 / 32, H4, 16 x 1000 41 / 57, H8/1, 64 x 100 13 / 20; H32/8, 8 x 64 rows over 1000 entries of a table of 8192 27 / 43.
 static bool cut_tiles(const pkv_packed& s, long long keys, bool paged) {
     const double stages = (double)((keys + kStage - 1) / kStage), tiles = (double)most_tiles(s) * s.L * s.Hkv;
     return stages * (1.27 - (paged ? 0.75 : 0.5) * 2.0 * tiles / tile_workgroups()) > 30.0;
