@@ -126,6 +126,8 @@ class PagedPath:
 
     def __init__(self, S: int, L: int, H: int, Hkv: int, D: int, scale: torch.Tensor, plan: B_.RopePlan, num_pages: int,
                  max_pages: int, page_size: int = 64, device="cuda"):
+        if scale.dtype != torch.float32 or scale.shape != (L,) or not scale.is_contiguous():
+            raise ValueError("scale must be contiguous f32 [L]")
         self.S, self.L, self.H, self.Hkv, self.D = S, L, H, Hkv, D
         self.scale, self.plan, self.device = scale, plan, torch.device(device)
         self.cache = B_.paged_cache(S, L, Hkv, D, page_size, num_pages, max_pages, torch.bfloat16, device)
@@ -148,6 +150,8 @@ class PagedPath:
             if (x.shape != (self.L, heads, T, self.D) or x.dtype != torch.bfloat16 or x.stride(3) != 1 or x.data_ptr() % 16
                     or any(st % 8 for st, n in zip(x.stride()[:3], x.shape) if n > 1) or (T > 1 and x.stride(2) == 0)):
                 raise ValueError("queries, keys and values must be bf16 [L,heads,T,D], with rows that begin at multiples of 16 bytes")
+        if any(x.get_device() != y.get_device() for x, y in ((q, self.cache.kp), (k, q), (v, q), (positions, q), (self.scale, q))):
+            raise ValueError("all tensors must be on the cache's GPU")
         if positions.dtype != torch.int32 or positions.shape != (self.plan.axes, T) or not positions.is_contiguous():
             raise ValueError("positions must be contiguous i32 [axes,T]")
 

@@ -46,6 +46,28 @@ def test_a_path_refuses_rows_before_its_first_step(monkeypatch):
             path.prefill(places, lengths, q, k, k, pos, budgets)
 
 
+def test_a_path_refuses_a_scale_and_tensors_of_another_device(monkeypatch):
+    for scale in (torch.ones(2).double(), torch.ones(1), torch.ones(2, 1), torch.ones(4)[::2]):
+        with pytest.raises(ValueError, match="scale"):
+            PagedPath(3, 2, 4, 2, 64, scale, P.rope_plan(64, device="cpu"), num_pages=4, max_pages=2, device="cpu")
+    import paper_2412_03409_amd.pipeline as pipeline
+    path = a_path()
+    for name in ("prefixkv_rope", "prefixkv_page_append"):
+        monkeypatch.setattr(pipeline.B_, name, lambda *a, **kw: pytest.fail("a step was made"))
+
+    class Elsewhere(torch.Tensor):
+        def get_device(self):
+            return 3
+    q, k = (torch.zeros((2, h, 9, 64), dtype=torch.bfloat16) for h in (4, 2))
+    pos = torch.zeros((1, 9), dtype=torch.int32)
+    there = lambda x: x.as_subclass(Elsewhere)
+    for x in ((there(q), k, k, pos), (q, there(k), k, pos), (q, k, there(k), pos), (q, k, k, there(pos))):
+        with pytest.raises(ValueError, match="GPU"):
+            path.prefill([0], [5], *x, [10])
+        with pytest.raises(ValueError, match="GPU"):
+            path.extend([1, 0, 2], *x)
+
+
 def test_a_rotation_goes_by_where_the_plan_s_tensors_are():
     """Tensors whose storage is replaced: the old one may belong to somebody else by the next call."""
     plan, other = P.rope_plan(64, [16, 16], device="cpu"), P.rope_plan(32, [8, 8], theta=500.0, device="cpu")
