@@ -440,6 +440,48 @@ int prefixkv_chunk_attn(const pkv_packed *shape, const void *q, pkv_strides qs, 
                         const int32_t *table, const int32_t *lens, const float *scale, int max_rows,
                         void *out, pkv_strides os, void *ws, size_t ws_bytes, pkv_stream stream);
 
+/* ==== Several continuations of a prompt (beam search) ==================================================
+ * W beams of a prompt have W places of the paged cache, one behind the other.  After a step, prefixkv_beam_select names the W best
+ * of all their continuations, and prefixkv_page_reorder makes the places what their new beams continue.
+ *
+ * prefixkv_beam_select: beam w of prompt s by token v has the score
+ *   scores[s,w] + x[v] - log sum_u exp x[u],   x = logits[s,w,:].
+ * An ended beam has one continuation, end_token, of its own score (its logits are not looked at).  The W best of a prompt come in
+ * descending order, equal ones by ascending w * V + v; tokens and parents (the beam that is continued) are -1 and the score
+ * -inf where there are fewer: a forbidden token (a logit of -inf) and the tokens of a beam whose score is -inf are none.  (The first
+ * step of a prompt: scores 0, -inf, -inf, ...)  NaN counts as -inf, +inf as the largest finite number, in logits and scores.
+ *   logits [dev] (dtype) S*W rows of V, row_stride elements apart (any; 0: all rows are the same);  scores [dev] fp32 [S,W]
+ *   ended [dev] u8 [S,W] or NULL (no beam has ended);  end_token: -1: none, then ended and ended_out are NULL
+ *   tokens, parents [dev] i32 [S,W], scores_out [dev] fp32 [S,W], ended_out [dev] u8 [S,W]: the beam had ended or its token is
+ *       end_token.  scores_out may be scores, ended_out may be ended.
+ *   ws [dev]: prefixkv_beam_workspace_bytes(S, W, V, dtype) bytes, any contents, 16-byte aligned
+ * 1 <= S <= 4096, 1 <= W <= 32, 1 <= V <= 2^20.  Sums of exponentials in fp32 by pieces of a row, all else in fp64. */
+size_t prefixkv_beam_workspace_bytes(int S, int W, int V, int dtype);
+int prefixkv_beam_select(int S, int W, int V, int dtype, const void *logits, int64_t row_stride, const float *scores,
+                         const uint8_t *ended, int end_token, int32_t *tokens, int32_t *parents, float *scores_out,
+                         uint8_t *ended_out, void *ws, size_t ws_bytes, pkv_stream stream);
+
+/* prefixkv_page_reorder: in every group of W places, place i becomes what place parents[g,i] was, in all layers; -1: empty.
+ *   parents [dev] i32 [S/W,W], -1 ... W-1
+ * Pages are shared, not copied: the places' rows of the table then name the same pages.  Only the page that a length ends inside of is
+ * copied, as the next entry goes there: the lowest place that continues a beam keeps it, each other takes a page from the ring, in
+ * (place, layer) order, into which the used rows go.  Pages that no place of the group holds any more go back to the ring, in
+ * (place, layer, entry) order, by the lowest place that held them.  All of it is done, or (*status != 0, as of prefixkv_page_resize;
+ * PKV_PAGES_RANGE: also a parent out of range) nothing; as there, a call needs as many free pages before it as it takes.
+ *   table_out may be table: entries that the new lengths reach are written (after a refused call: those of the old lengths).  lens_out
+ *   may be lens, state_out may be state.
+ * From then on the group's pages are shared: its places are ended by parents of -1, not by prefixkv_page_resize, which would give a
+ * page back once for every place that holds it.  prefixkv_page_append, prefixkv_rope_store and prefixkv_chunk_attn work on shared
+ * pages as on any others.  Groups must not share pages with each other.
+ *   ws [dev]: prefixkv_reorder_workspace_bytes(S, layers) bytes, any contents, 16-byte aligned
+ * 1 <= W <= 32, S % W == 0; the table's limits are those of prefixkv_page_resize; S * layers times the workgroups that copy a
+ * segment's rows (32 KB of a page's keys each) stays below 2^24 (PKV_ERR_UNSUPPORTED otherwise). */
+size_t prefixkv_reorder_workspace_bytes(int S, int layers);
+int prefixkv_page_reorder(int S, int W, int Hkv, int D, int dtype, const pkv_paging *paging, const int32_t *parents,
+                          const int32_t *table, const int32_t *lens, int32_t *ring, const int32_t *state, int32_t *table_out,
+                          int32_t *lens_out, int32_t *state_out, void *kp, void *vp, int32_t *status, void *ws, size_t ws_bytes,
+                          pkv_stream stream);
+
 /* Measurement aid, not part of the method: a plain device-to-device copy kernel of a known size
  * (bytes % 16 == 0, 16-byte aligned pointers).  It reads `bytes` and writes `bytes`, which is what
  * hardware byte counters are calibrated against when a kernel's HBM traffic is reported. */

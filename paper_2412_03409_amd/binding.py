@@ -136,6 +136,14 @@ def load(path: Optional[str] = None) -> C.CDLL:
                                                sz, vp]
     L.prefixkv_chunk_attn.restype = C.c_int
     L.prefixkv_chunk_attn.argtypes = [packed, vp, _Strides, vp, paging, i32, vp, vp, vp, vp, vp, i32, vp, _Strides, vp, sz, vp]
+    L.prefixkv_beam_workspace_bytes.restype = sz
+    L.prefixkv_beam_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    L.prefixkv_beam_select.restype = C.c_int
+    L.prefixkv_beam_select.argtypes = [i32, i32, i32, i32, vp, i64, vp, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+    L.prefixkv_reorder_workspace_bytes.restype = sz
+    L.prefixkv_reorder_workspace_bytes.argtypes = [i32, i32]
+    L.prefixkv_page_reorder.restype = C.c_int
+    L.prefixkv_page_reorder.argtypes = [i32, i32, i32, i32, i32, paging, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.prefixkv_calibration_copy.restype = C.c_int
     L.prefixkv_calibration_copy.argtypes = [vp, vp, sz, vp]
     _lib = L
@@ -928,6 +936,99 @@ def prefixkv_chunk_attn(cache: PagedCache, q: torch.Tensor, row_off: torch.Tenso
     if rc != 0:
         raise PrefixKVError(rc, "prefixkv_chunk_attn")
     return out
+
+
+# ---- several continuations of a prompt ---------------------------------------------------------------------
+@lru_cache(maxsize=256)
+def _beam_args(lsh, lst, ldt, ssh, sdt):
+    """Sizes, dtype, row stride and workspace of logits [S,W,V] with these scores."""
+    if len(lsh) != 3 or 0 in lsh or (lsh[2] > 1 and lst[2] != 1) or (lsh[0] > 1 and lsh[1] > 1 and lst[0] != lsh[1] * lst[1]):
+        raise ValueError("logits must be [S,W,V], rows one stride apart, with V contiguous")
+    if ldt not in _CODES:
+        raise TypeError(f"unsupported storage dtype {ldt}")
+    if sdt is not torch.float32 or ssh != lsh[:2]:
+        raise ValueError("scores must be contiguous f32 [S,W]")
+    S, W, V = lsh
+    return S, W, V, _CODES[ldt], lst[1] if W > 1 else lst[0] if S > 1 else V, beam_workspace_bytes(S, W, V, ldt)
+
+
+def beam_workspace_bytes(S: int, W: int, V: int, dtype: torch.dtype) -> int:
+    if dtype not in _CODES:
+        raise TypeError(f"unsupported storage dtype {dtype}")
+    return int(load().prefixkv_beam_workspace_bytes(_c_int(index(S), "S"), _c_int(index(W), "W"), _c_int(index(V), "V"), _CODES[dtype]))
+
+
+def _like(t: Optional[torch.Tensor], shape, dtype, device, what: str) -> torch.Tensor:
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous {dtype} {list(shape)}")
+    return t
+
+
+def prefixkv_beam_select(logits: torch.Tensor, scores: torch.Tensor, ended: Optional[torch.Tensor] = None,
+                         end_token: Optional[int] = None, tokens: Optional[torch.Tensor] = None,
+                         parents: Optional[torch.Tensor] = None, scores_out: Optional[torch.Tensor] = None,
+                         ended_out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """The W best continuations of every prompt: logits [S,W,V] (bf16 or f32), scores [S,W] f32, ended [S,W] bool (with an
+    end_token) -> (tokens [S,W] i32, parents [S,W] i32, scores_out [S,W] f32, ended_out [S,W] bool or None).  -1 where there are
+    fewer; scores_out may be scores, ended_out may be ended."""
+    d = logits.get_device()
+    stream = _here(d, scores, ended, tokens, parents, scores_out, ended_out, ws)
+    S, W, V, code, stride, need = _beam_args(logits.shape, logits.stride(), logits.dtype, scores.shape, scores.dtype)
+    if not scores.is_contiguous():
+        raise ValueError("scores must be contiguous f32 [S,W]")
+    end = -1 if end_token is None else _c_int(index(end_token), "end_token")
+    if end_token is None and (ended is not None or ended_out is not None):
+        raise ValueError("beams end by an end_token")
+    if end_token is not None and not 0 <= end < V:
+        raise ValueError("end_token must be a token")
+    shape, dev = scores.shape, logits.device
+    if ended is not None:
+        _like(ended, shape, torch.bool, dev, "ended")
+    tokens = _like(tokens, shape, torch.int32, dev, "tokens")
+    parents = _like(parents, shape, torch.int32, dev, "parents")
+    scores_out = _like(scores_out, shape, torch.float32, dev, "scores_out")
+    ended_out = None if end < 0 else _like(ended_out, shape, torch.bool, dev, "ended_out")
+    w = _ws(need, dev, ws)
+    rc = load().prefixkv_beam_select(S, W, V, code, logits.data_ptr(), stride, scores.data_ptr(), _ptr(ended), end,
+                                     tokens.data_ptr(), parents.data_ptr(), scores_out.data_ptr(), _ptr(ended_out), w.data_ptr(),
+                                     w.numel() * w.element_size(), stream)
+    if rc != 0:
+        raise PrefixKVError(rc, "prefixkv_beam_select")
+    return tokens, parents, scores_out, ended_out
+
+
+@lru_cache(maxsize=256, typed=True)
+def reorder_workspace_bytes(S: int, layers: int) -> int:
+    return int(load().prefixkv_reorder_workspace_bytes(S, layers))
+
+
+def prefixkv_page_reorder(cache: PagedCache, parents: torch.Tensor, status: Optional[torch.Tensor] = None,
+                          table_out: Optional[torch.Tensor] = None, lens_out: Optional[torch.Tensor] = None,
+                          state_out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Place i of every group of W places becomes what place parents[g,i] was (parents [S/W,W] i32 as prefixkv_beam_select gives
+    them, -1: empty): pages are shared, the last one of a length is copied where it is partly filled.  The cache's table, lens and
+    state are updated (or the tensors given written in their place).  -> status [1] i32, 0 if it was done."""
+    kp, vp, table, lens, ring, state = cache.kp, cache.vp, cache.table, cache.lens, cache.ring, cache.state
+    stream = _here(cache._device, parents, status, table_out, lens_out, state_out, ws)
+    pool = cache._pool
+    if pool is None or pool[2] not in _CODES:
+        raise ValueError("the cache must have contiguous pools of bf16 or f32")
+    if parents.dtype is not torch.int32 or parents.dim() != 2 or parents.numel() != cache._S or not parents.is_contiguous():
+        raise ValueError("parents must be contiguous i32 [S/W,W]")
+    status = torch.empty(1, dtype=torch.int32, device=lens.device) if status is None else _i32_like(status, (1,), "status")
+    table_out = table if table_out is None else _i32_like(table_out, table.shape, "table_out")
+    lens_out = lens if lens_out is None else _i32_like(lens_out, cache._seg, "lens_out")
+    state_out = state if state_out is None else _i32_like(state_out, (2,), "state_out")
+    w = _ws(reorder_workspace_bytes(cache._S, cache._layers), lens.device, ws)
+    rc = load().prefixkv_page_reorder(cache._S, parents.shape[1], pool[0], pool[1], _CODES[pool[2]], cache._paging, parents.data_ptr(),
+                                      table.data_ptr(), lens.data_ptr(), ring.data_ptr(), state.data_ptr(), table_out.data_ptr(),
+                                      lens_out.data_ptr(), state_out.data_ptr(), kp.data_ptr(), vp.data_ptr(), status.data_ptr(),
+                                      w.data_ptr(), w.numel() * w.element_size(), stream)
+    if rc != 0:
+        raise PrefixKVError(rc, "prefixkv_page_reorder")
+    return status
 
 
 def prefixkv_calibration_copy(dst: torch.Tensor, src: torch.Tensor) -> None:

@@ -413,6 +413,49 @@ int prefixkv_chunk_attn(const pkv_packed* s, const void* q, pkv_strides qs, cons
     return e == hipSuccess ? PKV_OK : PKV_ERR_HIP;
 }
 
+size_t prefixkv_reorder_workspace_bytes(int S, int layers) {
+    if (S < 1 || S > kMaxS || layers < 1 || layers > kMaxL) return 0;
+    return reorder_ws_bytes(S, layers);
+}
+
+int prefixkv_page_reorder(int S, int W, int Hkv, int D, int dtype, const pkv_paging* g, const int32_t* parents, const int32_t* table,
+                          const int32_t* lens, int32_t* ring, const int32_t* state, int32_t* table_out, int32_t* lens_out,
+                          int32_t* state_out, void* kp, void* vp, int32_t* status, void* ws, size_t ws_bytes, pkv_stream stream) {
+    if (!g || !parents || !table || !lens || !ring || !state || !table_out || !lens_out || !state_out || !kp || !vp || !status)
+        return PKV_ERR_NULL;
+    if (!page_call_ok(S, g) || W < 1 || W > kMaxBeams || S % W != 0 || Hkv < 1 || Hkv > 2048 || (D != 64 && D != 128)) return PKV_ERR_DIM;
+    if (dtype != PKV_F32 && dtype != PKV_BF16) return PKV_ERR_DTYPE;
+    if (!aligned16(kp) || !aligned16(vp)) return PKV_ERR_STRIDE;
+    const int row_bytes = D * (dtype == PKV_F32 ? 4 : 2);
+    if (!reorder_fits(S, W, Hkv, row_bytes, *g)) return PKV_ERR_UNSUPPORTED;
+    if (!ws || ws_bytes < reorder_ws_bytes(S, g->layers) || !aligned16(ws)) return PKV_ERR_WORKSPACE;
+    const hipError_t e = launch_reorder(S, W, Hkv, row_bytes, *g, parents, table, lens, ring, state, table_out, lens_out, state_out, kp,
+                                        vp, status, ws, (hipStream_t)stream);
+    return e == hipSuccess ? PKV_OK : PKV_ERR_HIP;
+}
+
+static bool beam_ok(int S, int W, int V) { return S >= 1 && S <= kMaxS && W >= 1 && W <= kMaxBeams && V >= 1 && V <= kMaxV; }
+
+size_t prefixkv_beam_workspace_bytes(int S, int W, int V, int dtype) {
+    if (!beam_ok(S, W, V) || (dtype != PKV_F32 && dtype != PKV_BF16)) return 0;
+    return beam_ws_bytes(S, W, V, dtype == PKV_F32 ? 4 : 2);
+}
+
+int prefixkv_beam_select(int S, int W, int V, int dtype, const void* logits, int64_t row_stride, const float* scores,
+                         const uint8_t* ended, int end_token, int32_t* tokens, int32_t* parents, float* scores_out,
+                         uint8_t* ended_out, void* ws, size_t ws_bytes, pkv_stream stream) {
+    if (!logits || !scores || !tokens || !parents || !scores_out || (end_token >= 0 && !ended_out)) return PKV_ERR_NULL;
+    if (!beam_ok(S, W, V) || end_token < -1 || end_token >= V || (end_token < 0 && (ended || ended_out))) return PKV_ERR_DIM;
+    if (dtype != PKV_F32 && dtype != PKV_BF16) return PKV_ERR_DTYPE;
+    const int esize = dtype == PKV_F32 ? 4 : 2;
+    if (row_stride < 0 || ((uintptr_t)logits & (uintptr_t)(esize - 1))) return PKV_ERR_STRIDE;
+    if (!beam_fits(S, W, V, esize)) return PKV_ERR_UNSUPPORTED;
+    if (!ws || ws_bytes < beam_ws_bytes(S, W, V, esize) || !aligned16(ws)) return PKV_ERR_WORKSPACE;
+    const hipError_t e = launch_beam(S, W, V, dtype == PKV_BF16, logits, row_stride, scores, ended, end_token, tokens, parents,
+                                     scores_out, ended_out, ws, (hipStream_t)stream);
+    return e == hipSuccess ? PKV_OK : PKV_ERR_HIP;
+}
+
 int prefixkv_calibration_copy(void* dst, const void* src, size_t bytes, pkv_stream stream) {
     if (!dst || !src) return PKV_ERR_NULL;
     if (bytes == 0 || bytes % 16 != 0) return PKV_ERR_DIM;

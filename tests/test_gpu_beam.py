@@ -1,0 +1,327 @@
+"""Beam search over the paged cache: the choice of continuations and the places that follow them, against their plain forms in 64
+bits and whole numbers.
+
+Bars.  Whole numbers and moved rows: equality.  Choices between beams hang on sums of exponentials in 32 bits: with p the
+probabilities of a row, the exponent of a term is off by three roundings of m - x, in all 3 * 2^-24 sum p (m - x), and that sum is at
+most log V, below 14; the exponential by two steps, a sum by one for each of its up to 32 + 12 additions (a part of a thread's
+terms, then trees): 90 * 2^-24 of the sum, and so of its logarithm.  The inputs' choices have to be further apart than twice that,
+which is looked at, except for exact ties, whose rows have equal sums.  Scores: the same and a rounding to 32 bits."""
+import numpy as np
+import pytest
+import torch
+
+import beam_reference as R
+import paper_2412_03409_amd as P
+import serving_reference as RS
+from test_gpu_serving import BF16, DEV, F32, f64, gen, i32, offsets, page_state
+
+pytestmark = pytest.mark.gpu
+LSE = 90 * 2.0 ** -24
+
+
+def select_inputs(seed, S, W, V, dtype, end=None, spread=2.5):
+    g = gen(seed)
+    x = torch.randn((S, W, V), generator=g) * spread + torch.randn((S, 1, V), generator=g)
+    x[torch.rand((S, W, V), generator=g) < 0.02] = float("-inf")
+    x[torch.rand((S, W, V), generator=g) < 0.01] = float("nan")
+    scores = torch.rand((S, W), generator=g) * -4.0 - 100.0
+    ended = None
+    if end is not None:
+        ended = torch.rand((S, W), generator=g) < 0.25
+    if W > 2:
+        scores[torch.rand((S, W), generator=g) < 0.1] = float("-inf")
+    return x.to(dtype), scores, ended
+
+
+def check_select(x, scores, ended, end, got, ties=False):
+    """x, scores and ended on the host, as the call got them."""
+    want = R.select(x.double().numpy(), scores.double().numpy(), None if ended is None else ended.numpy(), end)
+    assert ties or want[4] > 2 * LSE, "the inputs' choices are too close"
+    for a, b in zip(got[:2], want[:2]):
+        np.testing.assert_array_equal(a.cpu().numpy(), b)
+    s = got[2].cpu().numpy().astype(np.float64)
+    real = np.isfinite(want[2])
+    np.testing.assert_array_equal(np.isneginf(s), np.isneginf(want[2]))
+    assert (np.abs(s[real] - want[2][real]) <= LSE + 2.0 ** -24 * np.abs(want[2][real])).all()
+    if end is None:
+        assert got[3] is None
+    else:
+        np.testing.assert_array_equal(got[3].cpu().numpy(), want[3])
+
+
+SELECT = [(1, 1, 1, F32), (1, 4, 2, BF16), (3, 5, 1003, BF16), (2, 4, 32000, BF16), (1, 32, 5000, F32), (4, 3, 70001, F32), (2, 32, 33, BF16),
+          (1, 2, 1 << 20, BF16), (1, 1, (1 << 20) - 3, F32), (9, 16, 30011, F32), (16, 16, 17001, F32), (20, 16, 30011, F32),
+          (40, 16, 30011, F32), (40, 32, 30011, BF16), (65, 2, 257, BF16)]
+
+
+@pytest.mark.parametrize("S,W,V,dtype", SELECT)
+@pytest.mark.parametrize("end", [None, 0])
+def test_select(S, W, V, dtype, end):
+    x, scores, ended = select_inputs(S + W + V, S, W, V, dtype, end)
+    got = P.prefixkv_beam_select(x.to(DEV), scores.to(DEV), ended=None if ended is None else ended.to(DEV), end_token=end)
+    check_select(x, scores, ended, end, got)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_select_rows_that_begin_anywhere(dtype):
+    """The last step of several, rows of odd length among others; outputs in the inputs' place."""
+    S, W, V, end = 3, 4, 4099, 17
+    x, scores, ended = select_inputs(5, S, W, V, dtype, end)
+    want = P.prefixkv_beam_select(x.to(DEV), scores.to(DEV), ended=ended.to(DEV), end_token=end)
+    for steps, before, behind in ((1, 1, 0), (3, 3, 2), (2, 5, 8)):
+        room = torch.full((S, W, steps, before + V + behind), 1e30, dtype=dtype, device=DEV)
+        y = room[:, :, -1, before:before + V]
+        y.copy_(x)
+        sc, en = scores.to(DEV), ended.to(DEV)
+        got = P.prefixkv_beam_select(y, sc, ended=en, end_token=end, scores_out=sc, ended_out=en)
+        assert got[2] is sc and got[3] is en
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("W,V", [(4, 50), (5, 3001), (32, 9001), (32, 40)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_select_ties_go_to_the_lowest(W, V, dtype):
+    """Equal logits everywhere; a few values only; equal beams."""
+    g = gen(V)
+    flat = torch.zeros((1, W, V))
+    few = torch.randint(0, 3, (1, 1, V), generator=g).float().expand(1, W, V).clone()
+    few[0, :, 0] = -0.0
+    for x in (flat, few):
+        x = x.to(dtype)
+        scores = torch.full((1, W), -3.0)
+        check_select(x, scores, None, None, P.prefixkv_beam_select(x.to(DEV), scores.to(DEV)), ties=True)
+    rising = torch.arange(V).float().expand(1, W, V).to(dtype)             # the best ones side by side at the end
+    scores = torch.arange(W).float()[None] * -0.37
+    check_select(rising, scores, None, None, P.prefixkv_beam_select(rising.to(DEV), scores.to(DEV)), ties=dtype == BF16)
+
+
+def test_select_values_at_the_ends():
+    """Rows without a token, with +inf, with the type's largest values; scores that are NaN or +inf; beams without candidates."""
+    inf, V = float("inf"), 777
+    x, scores, _ = select_inputs(3, 6, 4, V, F32)
+    scores = scores.clamp(min=-200.0)
+    x[0] = -inf                                                            # nothing at all
+    x[1, 1:] = float("nan")
+    x[2, 0, 5] = inf
+    x[2, 1] = 3e38
+    x[3, 0, 9] = -3e38
+    scores[4] = torch.tensor([float("nan"), -inf, -5.0, inf])
+    scores[5] = -inf
+    got = P.prefixkv_beam_select(x.to(DEV), scores.to(DEV))
+    check_select(x[[0, 1, 3, 5]], scores[[0, 1, 3, 5]], None, None, [t[[0, 1, 3, 5]] for t in got[:3]] + [None])
+    # +inf is the largest finite number: all of its beam's weight, scores of the others 3e38 lower
+    assert got[0][2, 0] == 5 and got[1][2, 0] == 0 or bool(scores[2, 0] < scores[2, 1:].max())
+    assert got[1][4, 0] == 3 and not bool(torch.isnan(got[2]).any())
+
+
+def test_select_is_repeatable_and_replays_from_a_graph():
+    S, W, V, end = 5, 4, 20011, 3
+    x, scores, ended = (t.to(DEV) for t in select_inputs(8, S, W, V, BF16, end))
+    want = [t.clone() for t in P.prefixkv_beam_select(x, scores, ended=ended, end_token=end)]
+    ws = torch.empty(P.beam_workspace_bytes(S, W, V, BF16), dtype=torch.uint8, device=DEV)
+    outs = [torch.zeros_like(t) for t in want]
+    kw = dict(ended=ended, end_token=end, tokens=outs[0], parents=outs[1], scores_out=outs[2], ended_out=outs[3])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        P.prefixkv_beam_select(x, scores, **kw)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        P.prefixkv_beam_select(x, scores, ws=ws, **kw)
+    for i in range(4):
+        for t in outs:
+            t.zero_()
+        ws.fill_(255 * (i % 2))
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+        assert all(torch.equal(a, b) for a, b in zip(P.prefixkv_beam_select(x, scores, ended=ended, end_token=end), want))
+
+
+# ---- places -------------------------------------------------------------------------------------------
+def some_parents(r, G, W, empty=0.1):
+    p = np.minimum((r.exponential(size=(G, W)) * W / 2.5).astype(np.int64), W - 1)
+    p[r.random((G, W)) < empty] = -1
+    return p
+
+
+def as_cache(lens, table, ring, state, ps, Hkv, D, dtype, seed):
+    g = gen(seed)
+    kp, vp = (torch.randn((len(ring), Hkv, ps, D), generator=g).to(dtype).to(DEV) for _ in range(2))
+    return P.PagedCache(kp=kp, vp=vp, table=i32(table), lens=i32(lens), ring=i32(ring), state=i32(state))
+
+
+def check_cache(c, table, lens, ring, state, ps, pools=None):
+    np.testing.assert_array_equal(c.lens.cpu().numpy(), lens)
+    np.testing.assert_array_equal(c.state.cpu().numpy(), state)
+    np.testing.assert_array_equal(c.ring.cpu().numpy(), ring)
+    t = c.table.cpu().numpy()
+    reached = np.arange(t.shape[2]) < -(-lens // ps)[..., None]
+    np.testing.assert_array_equal(t[reached], table[reached])
+    for a, b in zip((c.kp, c.vp), pools or ()):
+        np.testing.assert_array_equal(f64(a), b)
+
+
+REORDER = [(1, 1, 2, 16, 1, 64, BF16, 60), (1, 4, 3, 16, 2, 128, BF16, 100), (3, 5, 2, 32, 2, 64, F32, 90), (2, 32, 2, 16, 1, 64, BF16, 50),
+           (5, 3, 4, 64, 3, 128, F32, 300), (2, 2, 1, 256, 8, 128, BF16, 700), (1, 2, 1, 16, 1, 64, BF16, 5000), (35, 2, 60, 16, 1, 64, BF16, 20),
+           (1, 17, 2, 16, 1, 64, BF16, 700)]
+
+
+@pytest.mark.parametrize("G,W,layers,ps,Hkv,D,dtype,ctx", REORDER)
+@pytest.mark.parametrize("in_place", [True, False])
+def test_reorder(G, W, layers, ps, Hkv, D, dtype, ctx, in_place):
+    """Places that share nothing yet, of any lengths, become any of each other."""
+    S = G * W
+    lens, table, ring, state = page_state(S + ctx, S, layers, ps, -(-ctx // ps) + 2, S * layers, ctx)
+    parents = some_parents(np.random.default_rng(W), G, W)
+    c = as_cache(lens, table, ring, state, ps, Hkv, D, dtype, ctx)
+    status, *want = R.reorder(parents, table, lens, ring, state, ps, [f64(c.kp), f64(c.vp)])
+    assert status == 0
+    if in_place:
+        assert int(P.prefixkv_page_reorder(c, i32(parents))) == 0
+        check_cache(c, *want[:4], ps, want[4])
+        return
+    kw = dict(table_out=torch.full_like(c.table, -7), lens_out=torch.empty_like(c.lens), state_out=torch.empty_like(c.state))
+    for _ in range(2):                              # with outputs of its own a call can be made again
+        assert int(P.prefixkv_page_reorder(c, i32(parents), **kw)) == 0
+    assert torch.equal(c.table.cpu(), torch.from_numpy(table).int()) and torch.equal(c.lens.cpu(), torch.from_numpy(lens).int())
+    got = P.PagedCache(kp=c.kp, vp=c.vp, table=kw["table_out"], lens=kw["lens_out"], ring=c.ring, state=kw["state_out"])
+    check_cache(got, *want[:4], ps, want[4])
+    beyond = np.arange(table.shape[2]) >= -(-want[1] // ps)[..., None]
+    assert (kw["table_out"].cpu().numpy()[beyond] == -7).all()
+
+
+@pytest.mark.parametrize("G,W,layers,ps,steps", [(2, 4, 3, 16, 40), (1, 5, 2, 16, 25), (3, 2, 1, 32, 30), (1, 32, 1, 16, 20)])
+def test_a_search_of_many_steps(G, W, layers, ps, steps):
+    """A prompt in the first place of every group, a fork, then tokens and reorderings in turn, an end: tables, lengths, ring and rows
+    after every call, and every page is free again behind the last."""
+    S, r = G * W, np.random.default_rng(W)
+    width = -(-(60 + steps) // ps)
+    n = np.zeros((S, layers), dtype=np.int64)
+    n[::W] = r.integers(1, 60, size=(G, layers))
+    total = int((-(-n // ps)).sum()) + S * layers * (2 + -(-steps // ps)) + 5
+    c = P.paged_cache(S, layers, 1, 64, ps, total, width, BF16, DEV)
+    c.kp.copy_(torch.randn(c.kp.shape, generator=gen(W)))
+    c.vp.copy_(torch.randn(c.kp.shape, generator=gen(W + 1)))
+    assert int(P.prefixkv_page_resize(c, i32(n))) == 0
+    table, lens, ring, state = (x.cpu().numpy().astype(np.int64) for x in (c.table, c.lens, c.ring, c.state))
+    pools = [f64(c.kp), f64(c.vp)]
+    for step in range(steps):
+        parents = np.zeros((G, W), dtype=np.int64) if step == 0 else some_parents(r, G, W, empty=0.03)
+        status, table, lens, ring, state, pools = R.reorder(parents, table, lens, ring, state, ps, pools)
+        assert status == 0 and int(P.prefixkv_page_reorder(c, i32(parents))) == 0
+        check_cache(c, table, lens, ring, state, ps, pools)
+        rows = (lens.max(axis=1) > 0).astype(np.int64)
+        if step % 2 == 0 and rows.sum() > 0:                     # a token for every beam that there is
+            off, T = offsets(rows), int(rows.sum())
+            status, lens, table, state, slots = RS.append(lens, off, T, table, ring, state, ps)
+            got, st = P.prefixkv_page_append(c, i32(off), T)
+            assert status == 0 and int(st) == 0
+            np.testing.assert_array_equal(got.cpu().numpy(), slots)
+            assert len(np.unique(slots)) == slots.size           # no two beams write the same row
+            for pool, ref in zip((c.kp, c.vp), pools):
+                new = torch.randn(slots.shape + (64,), generator=gen(step)).to(BF16)
+                flat = torch.from_numpy(slots)
+                pool[(flat // ps).to(DEV), 0, (flat % ps).to(DEV)] = new.to(DEV)
+                ref[slots // ps, 0, slots % ps] = new.double().numpy()
+    status, table, lens, ring, state, pools = R.reorder(np.full((G, W), -1), table, lens, ring, state, ps, pools)
+    assert int(P.prefixkv_page_reorder(c, i32(np.full((G, W), -1)))) == 0
+    check_cache(c, table, lens, ring, state, ps, pools)
+    assert int(c.state[1]) == total
+    np.testing.assert_array_equal(np.sort(c.ring.cpu().numpy()), np.arange(total))
+
+
+@pytest.mark.parametrize("what,status", [("parent", 2), ("below", 2), ("long", 2), ("negative", 2), ("head", 2), ("count", 2), ("room", 2),
+                                         ("few", 1)])
+@pytest.mark.parametrize("G,layers", [(3, 2), (50, 40)])
+def test_reorderings_that_are_refused_on_the_device(what, status, G, layers):
+    W, ps, width = 3, 16, 6
+    S = G * W
+    lens, table, ring, state = page_state(5, S, layers, ps, width, 200, 80)
+    lens[0] = 33
+    table[0, :, :3] = np.arange(3 * layers).reshape(layers, 3)
+    parents = np.tile(np.arange(W), (G, 1))
+    parents[0] = [0, 0, -1]
+    if what == "parent":
+        parents[G - 1, 1] = W
+    elif what == "below":
+        parents[1, 0] = -2
+    elif what == "long":
+        lens[S - 1, layers - 1] = width * ps + 1
+    elif what == "negative":
+        lens[4, 0] = -3
+    elif what == "head":
+        state[0] = -1
+    elif what == "count":
+        state[1] = len(ring) + 1
+    elif what == "room":
+        state[1] = len(ring)                                     # pages come back, and the ring is full
+    else:
+        state[1] = layers - 1
+    c = as_cache(lens, table, ring, state, ps, 1, 64, BF16, 3)
+    pools = [f64(c.kp), f64(c.vp)]
+    assert R.reorder(parents, table, lens, ring, state, ps)[0] == status
+    kw = dict(table_out=torch.full_like(c.table, -7), lens_out=torch.empty_like(c.lens), state_out=torch.empty_like(c.state))
+    assert int(P.prefixkv_page_reorder(c, i32(parents), **kw)) == status
+    assert int(P.prefixkv_page_reorder(c, i32(parents))) == status
+    for x, y in ((c.table, table), (c.lens, lens), (c.ring, ring), (c.state, state), (kw["lens_out"], lens), (kw["state_out"], state)):
+        np.testing.assert_array_equal(x.cpu().numpy(), y)
+    held = np.arange(width) < np.clip(-(-lens // ps), 0, width)[..., None]
+    np.testing.assert_array_equal(kw["table_out"].cpu().numpy(), np.where(held, table, -7))
+    for x, y in zip((c.kp, c.vp), pools):
+        np.testing.assert_array_equal(f64(x), y)
+
+
+def test_reorder_leaves_pages_outside_the_pool_alone():
+    """Ids that are no page, held or in the ring: nothing is copied from or to them, and none goes to the ring."""
+    W, layers, ps = 4, 2, 16
+    lens, held = np.full((W, layers), 40), W * layers * 3
+    table = np.concatenate([np.arange(held).reshape(W, layers, 3), np.full((W, layers, 1), -1)], axis=2)
+    ring, state = np.full(held + 9, -1), np.array([5, 9])
+    ring[5:14] = held + np.arange(9)
+    table[0, 0, 2], table[1, 0, 1], table[3, 1, 0] = -1, len(ring), 1 << 30
+    ring[(state[0] + 1) % len(ring)] = -5
+    parents = np.array([[0, 0, 2, 2]])
+    c = as_cache(lens, table, ring, state, ps, 2, 64, BF16, 4)
+    pools = [f64(c.kp), f64(c.vp)]
+    assert int(P.prefixkv_page_reorder(c, i32(parents))) == 0
+    np.testing.assert_array_equal(c.lens.cpu().numpy(), lens)
+    now = c.ring.cpu().numpy()
+    new = [now[(state[0] + state[1] + i) % len(ring)] for i in range(int(c.state[1]) - (state[1] - 4))]
+    assert all(0 <= x < len(ring) for x in new)
+    # taken, in (place, layer) order: one page each for place 1 and place 3; the one copied from page -1 stays as it was
+    fresh = [ring[(state[0] + i) % len(ring)] for i in range(4)]
+    got = c.table.cpu().numpy()
+    assert [got[1, 0, 2], got[1, 1, 2], got[3, 0, 2], got[3, 1, 2]] == fresh
+    for x, y in zip((c.kp, c.vp), pools):
+        for dst, src in zip(fresh, (table[0, 0, 2], table[0, 1, 2], table[2, 0, 2], table[2, 1, 2])):
+            if 0 <= dst < len(ring) and 0 <= src < len(ring):
+                y[dst, :, :8] = y[src, :, :8]
+        np.testing.assert_array_equal(f64(x), y)
+
+
+def test_reorder_replays_from_a_graph():
+    """A captured reordering in place, replayed: every replay goes on from the last one's places."""
+    G, W, layers, ps = 2, 4, 3, 16
+    lens, table, ring, state = page_state(9, G * W, layers, ps, 5, 60, 70)
+    c = as_cache(lens, table, ring, state, ps, 2, 64, BF16, 5)
+    pools = [f64(c.kp), f64(c.vp)]
+    parents = i32(np.zeros((G, W)))
+    status = torch.empty(1, dtype=torch.int32, device=DEV)
+    ws = torch.empty(P.reorder_workspace_bytes(G * W, layers), dtype=torch.uint8, device=DEV)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        P.prefixkv_page_reorder(c, parents, status=status, ws=ws)
+    r = np.random.default_rng(1)
+    for i in range(8):
+        p = some_parents(r, G, W, empty=0.0)
+        parents.copy_(i32(p))
+        ws.fill_(255 * (i % 2))
+        g.replay()
+        torch.cuda.synchronize()
+        want, table, lens, ring, state, pools = R.reorder(p, table, lens, ring, state, ps, pools)
+        assert int(status) == want
+        check_cache(c, table, lens, ring, state, ps, pools)
