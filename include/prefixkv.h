@@ -440,6 +440,23 @@ int prefixkv_chunk_attn(const pkv_packed *shape, const void *q, pkv_strides qs, 
                         const int32_t *table, const int32_t *lens, const float *scale, int max_rows,
                         void *out, pkv_strides os, void *ws, size_t ws_bytes, pkv_stream stream);
 
+/* ---- Attention of packed rows to states of another length (those of an encoder: pictures, a recording), without a mask of
+ * causality: every row of sequence s attends to all states of s.  Rows that share states, such as the beams of a prompt, lie one
+ * behind the other and are one sequence of this call.
+ *   out[l,h,t,:] = sum_n softmax_n(scale[l] * q[l,h,t,:].k[l,g(h),n,:]) v[l,g(h),n,:],
+ *                  n over the states state_off[s] ... state_off[s+1]-1, with `seen` the first seen[t] of them
+ * A row that sees none gives zeros; keys and values that it does not see take no part, whatever they hold.
+ *   q, out [L,H,T,D] strides qs, os;  k, v [L,Hkv,M,D] strides ks, vs (n below 2^26);  scale [dev] fp32 [L]
+ *   row_off [dev] i32 [S+1];  state_off [dev] i32 [S+1], non-decreasing, 0 ... M: no states between equal ones
+ *   seen [dev] i32 [T] or NULL; below 0 is 0, above the number of states all of them
+ *   max_rows: no sequence has more rows in this call (1 <= max_rows <= T); further ones are left as they are.  It chooses the kernel.
+ *   ws [dev]: prefixkv_cross_workspace_bytes(shape, M, max_rows) bytes, 16-byte aligned (NULL if that is 0)
+ * 1 <= M <= 2^22.  The limits on T, S and the tiles are those of the two attention calls above; (M/32 + S) * L * Hkv < 2^31. */
+size_t prefixkv_cross_workspace_bytes(const pkv_packed *shape, int M, int max_rows);
+int prefixkv_cross_attn(const pkv_packed *shape, const void *q, pkv_strides qs, const int32_t *row_off, int M, const void *k,
+                        pkv_strides ks, const void *v, pkv_strides vs, const int32_t *state_off, const int32_t *seen,
+                        const float *scale, int max_rows, void *out, pkv_strides os, void *ws, size_t ws_bytes, pkv_stream stream);
+
 /* ==== Several continuations of a prompt (beam search) ==================================================
  * W beams of a prompt have W places of the paged cache, one behind the other.  After a step, prefixkv_beam_select names the W best
  * of all their continuations, and prefixkv_page_reorder makes the places what their new beams continue.

@@ -136,6 +136,10 @@ def load(path: Optional[str] = None) -> C.CDLL:
                                                sz, vp]
     L.prefixkv_chunk_attn.restype = C.c_int
     L.prefixkv_chunk_attn.argtypes = [packed, vp, _Strides, vp, paging, i32, vp, vp, vp, vp, vp, i32, vp, _Strides, vp, sz, vp]
+    L.prefixkv_cross_workspace_bytes.restype = sz
+    L.prefixkv_cross_workspace_bytes.argtypes = [packed, i32, i32]
+    L.prefixkv_cross_attn.restype = C.c_int
+    L.prefixkv_cross_attn.argtypes = [packed, vp, _Strides, vp, i32, vp, _Strides, vp, _Strides, vp, vp, vp, i32, vp, _Strides, vp, sz, vp]
     L.prefixkv_beam_workspace_bytes.restype = sz
     L.prefixkv_beam_workspace_bytes.argtypes = [i32, i32, i32, i32]
     L.prefixkv_beam_select.restype = C.c_int
@@ -935,6 +939,49 @@ def prefixkv_chunk_attn(cache: PagedCache, q: torch.Tensor, row_off: torch.Tenso
                                     out.data_ptr(), os_, w.data_ptr(), w.numel() * w.element_size(), stream)
     if rc != 0:
         raise PrefixKVError(rc, "prefixkv_chunk_attn")
+    return out
+
+
+def cross_workspace_bytes(S: int, L: int, H: int, Hkv: int, T: int, M: int, D: int, dtype: torch.dtype, max_rows: int) -> int:
+    return int(load().prefixkv_cross_workspace_bytes(C.byref(_packed(S, Hkv, (L, H, T, D), dtype)), _c_int(int(M), "M"),
+                                                     _c_int(int(max_rows), "max_rows")))
+
+
+@lru_cache(maxsize=512)
+def _cross_args(qsh, qst, qdt, ksh, kst, kdt, vsh, vst, vdt, osh, ost, odt, S, max_rows):
+    """Argument structs of rows q and out and of states k and v, and the call's workspace."""
+    qs, ks, vs, os_ = (_row_strides(*a) for a in ((qsh, qst, qdt), (ksh, kst, kdt), (vsh, vst, vdt), (osh, ost, odt)))
+    if osh != qsh or odt != qdt:
+        raise ValueError("out must have the shape and dtype of q")
+    if vsh != ksh or not (kdt == vdt == qdt) or (ksh[0], ksh[3]) != (qsh[0], qsh[3]):
+        raise ValueError("k, v must be [L,Hkv,M,D] with q's dtype")
+    return (C.byref(_packed(S, ksh[1], qsh, qdt)), qs, ks, vs, os_,
+            cross_workspace_bytes(S, qsh[0], qsh[1], ksh[1], qsh[2], ksh[2], qsh[3], qdt, max_rows))
+
+
+def prefixkv_cross_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_off: torch.Tensor, state_off: torch.Tensor,
+                        scale: torch.Tensor, max_rows: int, seen: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                        ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of packed rows to states of another length: q [L,H,T,D], k/v [L,Hkv,M,D] (bf16 or f32), row_off and state_off
+    [S+1] i32, scale [L] f32, max_rows = the most rows of a sequence, seen [T] i32 (how many of its sequence's states a row sees;
+    None: all) -> out [L,H,T,D].  Rows that belong to no sequence are left as they are."""
+    stream = _here(q.get_device(), k, v, row_off, state_off, scale, seen, out, ws)
+    out = torch.empty_like(q) if out is None else out
+    max_rows, S, qsh = _c_int(index(max_rows), "max_rows"), row_off.numel() - 1, q.shape
+    s, qs, ks, vs, os_, need = _cross_args(qsh, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype,
+                                           out.shape, out.stride(), out.dtype, S, max_rows)
+    _i32_like(row_off, (S + 1,), "row_off")
+    _i32_like(state_off, (S + 1,), "state_off")
+    if seen is not None:
+        _i32_like(seen, (qsh[2],), "seen")
+    if scale.dtype is not torch.float32 or scale.shape != qsh[:1] or not scale.is_contiguous():
+        raise ValueError("scale must be contiguous f32 [L]")
+    w = _ws(need, q.device, ws)
+    rc = load().prefixkv_cross_attn(s, q.data_ptr(), qs, row_off.data_ptr(), k.shape[2], k.data_ptr(), ks, v.data_ptr(), vs,
+                                    state_off.data_ptr(), _ptr(seen), scale.data_ptr(), max_rows, out.data_ptr(), os_, w.data_ptr(),
+                                    w.numel() * w.element_size(), stream)
+    if rc != 0:
+        raise PrefixKVError(rc, "prefixkv_cross_attn")
     return out
 
 

@@ -413,6 +413,36 @@ int prefixkv_chunk_attn(const pkv_packed* s, const void* q, pkv_strides qs, cons
     return e == hipSuccess ? PKV_OK : PKV_ERR_HIP;
 }
 
+static bool cross_ok(const pkv_packed* s, int M, int max_rows) {
+    return packed_ok(s) && M >= 1 && M <= kMaxT && max_rows >= 1 && max_rows <= s->T;
+}
+
+size_t prefixkv_cross_workspace_bytes(const pkv_packed* s, int M, int max_rows) {
+    if (!s || !cross_ok(s, M, max_rows) || (s->dtype != PKV_F32 && s->dtype != PKV_BF16)) return 0;
+    return cross_attn_ws_bytes(*s, M, max_rows);
+}
+
+int prefixkv_cross_attn(const pkv_packed* s, const void* q, pkv_strides qs, const int32_t* row_off, int M, const void* k,
+                        pkv_strides ks, const void* v, pkv_strides vs, const int32_t* state_off, const int32_t* seen,
+                        const float* scale, int max_rows, void* out, pkv_strides os, void* ws, size_t ws_bytes, pkv_stream stream) {
+    if (!s || !q || !row_off || !k || !v || !state_off || !scale || !out) return PKV_ERR_NULL;
+    if (!cross_ok(s, M, max_rows)) return PKV_ERR_DIM;
+    if (s->dtype != PKV_F32 && s->dtype != PKV_BF16) return PKV_ERR_DTYPE;
+    const int esize = s->dtype == PKV_F32 ? 4 : 2;
+    if (!row_strides_ok(qs, esize) || !row_strides_ok(ks, esize) || !row_strides_ok(vs, esize) || !out_strides_ok(os, esize, s->L, s->H) ||
+        !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out))
+        return PKV_ERR_STRIDE;
+    // the copies address 16 rows with 32-bit byte offsets
+    if (!cross_attn_fits(*s, M) || ks.n >= (1ll << 26) || vs.n >= (1ll << 26)) return PKV_ERR_UNSUPPORTED;
+    const size_t need = cross_attn_ws_bytes(*s, M, max_rows);
+    if (need > 0 && (!ws || ws_bytes < need || !aligned16(ws))) return PKV_ERR_WORKSPACE;
+    PackedAttn a{};
+    a.q = q; a.k = k; a.v = v; a.qs = to_strides(qs); a.ks = to_strides(ks); a.vs = to_strides(vs); a.os = to_strides(os);
+    a.row_off = row_off; a.state_off = state_off; a.seen = seen; a.M = M; a.scale = scale; a.out = out; a.max_rows = max_rows; a.ws = ws;
+    const hipError_t e = launch_packed_attn(*s, a, (hipStream_t)stream);
+    return e == hipSuccess ? PKV_OK : PKV_ERR_HIP;
+}
+
 size_t prefixkv_reorder_workspace_bytes(int S, int layers) {
     if (S < 1 || S > kMaxS || layers < 1 || layers > kMaxL) return 0;
     return reorder_ws_bytes(S, layers);

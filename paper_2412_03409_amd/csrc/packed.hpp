@@ -40,7 +40,8 @@ hipError_t launch_rope(const pkv_packed& s, const pkv_rope& r, const int32_t* po
                        Strides ks, const void* v, Strides vs, void* q_out, Strides qos, void* k_out, Strides kos,
                        const int64_t* slots, const pkv_paging* g, void* kp, void* vp, hipStream_t st);
 
-// Rows of packed sequences and the keys they attend to: packed rows themselves (k, v; table NULL) or the pages.
+// Rows of packed sequences and the keys they attend to: packed rows themselves (k, v; table and state_off NULL), the pages, or
+// states of another length (k, v; state_off).
 struct PackedAttn {
     const void *q, *k, *v;
     Strides qs, ks, vs, os;
@@ -50,10 +51,14 @@ struct PackedAttn {
     float* lse;           // packed prompts only
     pkv_paging g;
     int l0, max_rows;     // max_rows 0: packed prompts
+    int M;                // states
+    const int32_t *state_off, *seen;
     void* ws;
 };
 bool packed_attn_fits(const pkv_packed& s, const pkv_paging* g);
 size_t packed_attn_ws_bytes(const pkv_packed& s, int max_rows);
+bool cross_attn_fits(const pkv_packed& s, int M);
+size_t cross_attn_ws_bytes(const pkv_packed& s, int M, int max_rows);
 hipError_t launch_packed_attn(const pkv_packed& s, const PackedAttn& a, hipStream_t st);
 
 }  // namespace pkv

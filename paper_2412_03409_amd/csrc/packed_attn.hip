@@ -1,6 +1,6 @@
-// Causal attention of packed rows: whole prompts of different lengths over their own packed keys, and chunks of new rows over a
-// paged cache.  Both are one operator with two places to read keys from: row i of a sequence's n rows sees the keys
-// 0 ... len - n + i, where len = n for a prompt.  Query heads that share a KV head are rows of one tile, row = token * heads + head:
+// Attention of packed rows: whole prompts of different lengths over their own packed keys, chunks of new rows over a paged cache, and
+// rows over packed states of another length.  They are one operator with three places to read keys from: row i of a sequence's n rows
+// sees the keys 0 ... len - n + i of a prompt (len = n) or cache, and all states or the first `seen` of them.  Query heads that share a KV head are rows of one tile, row = token * heads + head:
 // the keys are read once for all of them, and a tile's diagonal is as narrow as its tokens are few.
 //
 //  attn_tiles_kernel  bf16, many rows.  A workgroup has 128 rows of one (sequence, KV head), a wavefront 32 of them.  Keys and
@@ -27,14 +27,20 @@
 
 namespace pkv {
 
+// where the keys and values are
+enum Keys { kPrompt, kPages, kStates };
+
 struct PackedParams {
     int S, L, H, Hkv, T;
     int grp;                        // H / Hkv
-    int num_pages, max_pages, shift, layers, l0, max_rows;
+    union { int num_pages, M; };    // M: states
+    int max_pages, shift, layers, l0, max_rows;
     const unsigned char *q, *k, *v;
     unsigned char* out;
     Strides qs, ks, vs, os;         // in bytes
-    const int32_t *row_off, *table, *lens;
+    const int32_t* row_off;
+    union { const int32_t *table, *state_off; };
+    union { const int32_t *lens, *seen; };    // seen: NULL, a row sees all states of its sequence
     const float* scale;
     float* lse;
 };
@@ -64,8 +70,12 @@ __device__ __forceinline__ int entries(const PackedParams& p, int s, int l) {
     return max(0, min(len, p.max_pages << p.shift));
 }
 
+// states of sequence s, and how many of its `all` row t sees
+__device__ __forceinline__ int states(const PackedParams& p, int s) { return new_rows(p.state_off[s], p.state_off[s + 1], p.M); }
+__device__ __forceinline__ int seen_by(const PackedParams& p, int64_t t, int all) { return p.seen ? max(0, min(p.seen[t], all)) : all; }
+
 // ---- fp32 ----------------------------------------------------------------------------------------------
-template <int D>
+template <int D, Keys KEYS>
 __global__ void __launch_bounds__(256)
 attn_rows_kernel(PackedParams p) {
     constexpr int LPR = D / 4, RG = kWave / LPR, U = 4, kRow = D * 4;
@@ -78,9 +88,15 @@ attn_rows_kernel(PackedParams p) {
     if (s >= p.S) return;
     const int first = p.row_off[s], n = p.row_off[s + 1] - first, i = t - first;
     if (first < 0 || i < 0 || i >= p.max_rows) return;
-    const int len = entries(p, s, l), count = min(len, i + 1 + len - n);    // keys that the row sees
-    const int32_t* pages = p.table + ((int64_t)s * p.layers + p.l0 + l) * p.max_pages;
+    const int len = KEYS == kStates ? states(p, s) : entries(p, s, l);
+    const int count = KEYS == kStates ? seen_by(p, t, len) : min(len, i + 1 + len - n);    // keys that the row sees
+    const int32_t* pages = KEYS == kStates ? nullptr : p.table + ((int64_t)s * p.layers + p.l0 + l) * p.max_pages;
     const int g = h / p.grp;
+    const unsigned char *kb = p.k, *vb = p.v;
+    if constexpr (KEYS == kStates) {
+        kb += p.ks.l * l + p.ks.h * g + p.ks.n * (int64_t)p.state_off[s] + sub * 16;
+        vb += p.vs.l * l + p.vs.h * g + p.vs.n * (int64_t)p.state_off[s] + sub * 16;
+    }
     float4 q = *(const float4*)(p.q + p.qs.l * l + p.qs.h * h + p.qs.n * t + sub * 16);
     const float sc0 = p.scale[l], scale = score_scale(sc0);
     if (sc0 < 0.f) q = make_float4(-q.x, -q.y, -q.z, -q.w);
@@ -93,10 +109,15 @@ attn_rows_kernel(PackedParams p) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int j = j0 + u * RG + rg;
-            const int id = j < count ? pages[j >> p.shift] : -1;
-            real[u] = (uint32_t)id < (uint32_t)p.num_pages;
+            const int id = KEYS == kStates ? 0 : j < count ? pages[j >> p.shift] : -1;
+            real[u] = KEYS == kStates ? j < count : (uint32_t)id < (uint32_t)p.num_pages;
             kr[u] = vr[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (real[u]) {
+            if (KEYS == kStates) {
+                if (real[u]) {
+                    kr[u] = *(const float4*)(kb + p.ks.n * (int64_t)j);
+                    vr[u] = *(const float4*)(vb + p.vs.n * (int64_t)j);
+                }
+            } else if (real[u]) {
                 const int64_t at = ((((int64_t)id * p.Hkv + g) << p.shift) + (j & ((1 << p.shift) - 1))) * kRow + sub * 16;
                 kr[u] = *(const float4*)(p.k + at);
                 vr[u] = *(const float4*)(p.v + at);
@@ -501,7 +522,7 @@ struct Work {
 struct Segment { int s, l, first, n, rows, len, before, end; };   // rows: of this call, times the heads of a KV head; keys; keys in front
                                                                   // of the first new row (below 0: the first rows see nothing); keys that some row sees (none without rows)
 
-template <bool PAGED>
+template <Keys KEYS>
 __device__ __forceinline__ Segment segment(const Work& p, int i) {
     Segment x;
     const DivMod sl = div_mod(i, p.by_layers);
@@ -509,16 +530,16 @@ __device__ __forceinline__ Segment segment(const Work& p, int i) {
     const int last = p.a.row_off[x.s + 1];
     x.first = p.a.row_off[x.s];
     x.n = new_rows(x.first, last, p.a.T);
-    x.len = PAGED ? entries(p.a, x.s, x.l) : x.n;
-    const int rows = PAGED ? min(x.n, p.a.max_rows) : x.n;
+    x.len = KEYS == kPages ? entries(p.a, x.s, x.l) : KEYS == kStates ? states(p.a, x.s) : x.n;
+    const int rows = KEYS == kPrompt ? x.n : min(x.n, p.a.max_rows);
     x.rows = rows * p.a.grp;
-    x.before = x.len - x.n;
-    x.end = keys_seen(rows, x.n, x.len);
+    x.before = KEYS == kStates ? x.len - 1 : x.len - x.n;
+    x.end = KEYS == kStates ? (rows > 0 ? x.len : 0) : keys_seen(rows, x.n, x.len);
     return x;
 }
-template <bool PAGED>
+template <Keys KEYS>
 __device__ __forceinline__ Segment uniform_segment(const Work& p, int i) {
-    Segment x = segment<PAGED>(p, i);
+    Segment x = segment<KEYS>(p, i);
     x.s = __builtin_amdgcn_readfirstlane(x.s); x.l = __builtin_amdgcn_readfirstlane(x.l);
     x.first = __builtin_amdgcn_readfirstlane(x.first); x.n = __builtin_amdgcn_readfirstlane(x.n);
     x.rows = __builtin_amdgcn_readfirstlane(x.rows); x.len = __builtin_amdgcn_readfirstlane(x.len);
@@ -540,7 +561,7 @@ __device__ __forceinline__ int64_t of_lane(int64_t x, int j) { return lane64(x, 
 
 // `count` segments, first + i * step, and their places (of type N).  Up to 64 of them (a layer of 64 sequences) are read once, a lane
 // each; beyond, they are read again where they are asked for.
-template <bool PAGED, class N, class F>
+template <Keys KEYS, class N, class F>
 struct Looked {
     const Work& p;
     int lane, count, first, step;
@@ -550,9 +571,9 @@ struct Looked {
 
     __device__ __forceinline__ Looked(const Work& work, int ln, int n, int from, int by, F f)
         : p(work), lane(ln), count(n), first(from), step(by), cost(f) {
-        mine = segment<PAGED>(p, first + min(lane, count - 1) * step);
+        mine = segment<KEYS>(p, first + min(lane, count - 1) * step);
         upto = lane < count ? cost(mine) : (N)0;
-        for (int i = lane + kWave; i < count; i += kWave) upto += cost(segment<PAGED>(p, first + i * step));
+        for (int i = lane + kWave; i < count; i += kWave) upto += cost(segment<KEYS>(p, first + i * step));
         for (int d = 1; d < min(count, kWave); d <<= 1) {
             const N before = up(upto, d);
             if (lane >= d) upto += before;
@@ -573,7 +594,7 @@ struct Looked {
         int j = 0;
         N base = 0;
         for (int c = 0; c < count; c += kWave) {
-            const N here = c + lane < count ? cost(segment<PAGED>(p, first + (c + lane) * step)) : (N)0;
+            const N here = c + lane < count ? cost(segment<KEYS>(p, first + (c + lane) * step)) : (N)0;
             N incl = here;
 #pragma unroll
             for (int d = 1; d < kWave; d <<= 1) {
@@ -588,7 +609,7 @@ struct Looked {
             }
             base += of_lane(incl, kWave - 1);
         }
-        sg = uniform_segment<PAGED>(p, first + j * step);
+        sg = uniform_segment<KEYS>(p, first + j * step);
         return j;
     }
 };
@@ -610,25 +631,48 @@ constexpr int kJoinStages = 3;      // what a cut costs: two parts written and r
 // long ones on an empty chip.  (600 rows over 6000 keys among shorter sequences, H32/8: 135 us so, 108 in
 // equal shares, of which 10 join the parts.)
 // A tile's cost is the keys that it sees, if it were full, and kStartKeys, in units of one key and row of grp; that has a closed sum.
-template <bool PAGED>
+template <Keys KEYS>
 struct TileCost {
     int64_t first;                  // of tile 0, without its rows
     int tiles;
     __device__ __forceinline__ TileCost(const Work& p, const Segment& x)
         : first((int64_t)p.a.grp * (max(x.before, 0) + kStartKeys)), tiles((x.rows + kTileRows - 1) / kTileRows) {}
-    __device__ __forceinline__ int64_t up_to(int i) const { return i * first + (int64_t)(kTileRows / 2) * i * (i + 1); }   // tiles 0 ... i-1
-    __device__ __forceinline__ int64_t of(int i) const { return first + (int64_t)kTileRows * (i + 1); }
+    __device__ __forceinline__ int64_t up_to(int i) const { return i * first + (KEYS == kStates ? 0 : (int64_t)(kTileRows / 2) * i * (i + 1)); }   // tiles 0 ... i-1
+    __device__ __forceinline__ int64_t of(int i) const { return first + (KEYS == kStates ? 0 : (int64_t)kTileRows * (i + 1)); }
 };
 // stages of tile i
+template <Keys KEYS>
 __device__ __forceinline__ int tile_end(const Work& p, const Segment& x, int i) {       // keys that its rows see
+    if constexpr (KEYS == kStates) return x.len;
     const int last = __builtin_amdgcn_readfirstlane(row_at(min(x.rows, (i + 1) * kTileRows) - 1, p.grp).token);
     return max(0, min(x.len, x.before + last + 1));
+}
+
+// How many states all of the rows row0 ... row0+ROWS-1 of a segment see, and some of them.
+struct Limits { int all, some; };
+template <int ROWS>
+__device__ __forceinline__ Limits limits(const Work& p, const Segment& x, int row0, int lane) {
+    if (!p.a.seen) return {x.len, x.len};
+    int lo = x.len, hi = 0;
+#pragma unroll
+    for (int i = 0; i < (ROWS + kWave - 1) / kWave; ++i) {
+        const int row = min(row0 + min(i * kWave + lane, ROWS - 1), max(x.rows - 1, 0));
+        const int n = seen_by(p.a, x.first + row_at(row, p.grp).token, x.len);
+        lo = min(lo, n);
+        hi = max(hi, n);
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+        lo = min(lo, __shfl_xor(lo, d, kWave));
+        hi = max(hi, __shfl_xor(hi, d, kWave));
+    }
+    return {__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(hi)};
 }
 
 struct Cut { int seg, head, tile, stage; };
 
 // What the workgroups share out.
-template <bool PAGED, class L>
+template <Keys KEYS, class L>
 struct Shares {
     const TileParams& p;
     const L& segs;
@@ -636,7 +680,7 @@ struct Shares {
 
     __device__ __forceinline__ Shares(const TileParams& params, const L& looked) : p(params), segs(looked) {
         int longest = segs.mine.end;
-        for (int i = segs.lane + kWave; i < p.segs; i += kWave) longest = max(longest, segment<PAGED>(p, i).end);
+        for (int i = segs.lane + kWave; i < p.segs; i += kWave) longest = max(longest, segment<KEYS>(p, i).end);
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) longest = max(longest, __shfl_xor(longest, d, kWave));
         // where a launch is small a long tile is cut into pieces of eight stages at least
@@ -651,7 +695,7 @@ struct Shares {
         Cut c;
         Segment sg;
         c.seg = segs.find(x, in, sg);
-        const TileCost<PAGED> t(p, sg);
+        const TileCost<KEYS> t(p, sg);
         const int64_t head = t.up_to(t.tiles);
         c.head = min(p.a.Hkv - 1, (int)((double)in / (double)head));       // (a quotient that is rounded up is corrected)
         in -= c.head * head;
@@ -662,7 +706,7 @@ struct Shares {
             if (t.up_to(mid) <= in) lo = mid; else hi = mid;
         }
         c.tile = lo;
-        const int nst = (tile_end(p, sg, lo) + kStage - 1) / kStage;
+        const int nst = (tile_end<KEYS>(p, sg, lo) + kStage - 1) / kStage;
         c.stage = min(nst, (int)((float)(in - t.up_to(lo)) / (float)t.of(lo) * (float)nst));
         if (c.stage <= kJoinStages && 2 * c.stage <= nst) c.stage = 0;
         else if (nst - c.stage <= kJoinStages) {                    // the next tile
@@ -685,7 +729,7 @@ __device__ __forceinline__ Cut uniform(const Cut& c) {
 // head run next to each other and read its keys at about the same time through that XCD's L2; the last heads of an XCD are taken
 // together, so that the launch does not end on the long tiles of a single one.  Else heads alternate.  Within a head: sequence by
 // sequence, the last tile first, whose rows see the most.
-template <bool PAGED>
+template <Keys KEYS>
 __device__ __forceinline__ Cut tile_of(const TileParams& p, int lane, int bid, Segment& sg) {
     int head, tt;
     if (p.heads_per_xcd > 0) {
@@ -700,14 +744,14 @@ __device__ __forceinline__ Cut tile_of(const TileParams& p, int lane, int bid, S
     }
     const DivMod lg = uniform_div_mod(head, p.by_hkv);
     auto tiles = [&](const Segment& x) { return (x.rows + kTileRows - 1) / kTileRows; };
-    const Looked<PAGED, int, decltype(tiles)> looked(p, lane, p.a.S, lg.q, p.a.L, tiles);      // the layer's sequences
+    const Looked<KEYS, int, decltype(tiles)> looked(p, lane, p.a.S, lg.q, p.a.L, tiles);      // the layer's sequences
     if (tt >= looked.all) return {p.segs, 0, 0, 0};
     int in;
     const int s = looked.find(tt, in, sg);
     return {s * p.a.L + lg.q, lg.r, in, 0};
 }
 
-template <int D, bool PAGED, bool WHOLE>
+template <int D, Keys KEYS, bool WHOLE>
 __global__ void __launch_bounds__(256, 2)
 attn_tiles_kernel(TileParams p) {
     constexpr int ROWB = D * 2, kInst = CopyLane<D>::kCopies;               // copies per wavefront, stage and tensor: 16 rows
@@ -722,16 +766,16 @@ attn_tiles_kernel(TileParams p) {
     Cut from, to;
     Segment sg;
     if constexpr (WHOLE) {
-        from = to = uniform(tile_of<PAGED>(p, lane, (int)blockIdx.x, sg));
+        from = to = uniform(tile_of<KEYS>(p, lane, (int)blockIdx.x, sg));
     } else {
         // neighbours in the order of the work run on one XCD and share keys through its L2
         wg = (int)xcd_swizzle(blockIdx.x, (uint32_t)p.workgroups);
         auto cost = [&](const Segment& x) {
-            const TileCost<PAGED> t(p, x);
+            const TileCost<KEYS> t(p, x);
             return t.up_to(t.tiles) * a.Hkv;
         };
-        const Looked<PAGED, int64_t, decltype(cost)> looked(p, lane, p.segs, 0, 1, cost);
-        const Shares<PAGED, decltype(looked)> sh(p, looked);
+        const Looked<KEYS, int64_t, decltype(cost)> looked(p, lane, p.segs, 0, 1, cost);
+        const Shares<KEYS, decltype(looked)> sh(p, looked);
         from = uniform(sh.cut(wg));
         to = uniform(sh.cut(wg + 1));
         if (threadIdx.x == 0) p.cut[wg] = make_int4(from.seg, from.head, from.tile, from.stage);
@@ -742,30 +786,49 @@ attn_tiles_kernel(TileParams p) {
     tl.offsets(lane);
     int seg = from.seg, g = from.head, tile = from.tile, stage = from.stage;
     while (seg < p.segs && seg <= to.seg) {                 // (`to` may be a segment without rows)
-        if constexpr (!WHOLE) sg = uniform_segment<PAGED>(p, seg);
+        if constexpr (!WHOLE) sg = uniform_segment<KEYS>(p, seg);
         const int tiles = (sg.rows + kTileRows - 1) / kTileRows;
         if (!WHOLE && tile >= tiles) { tile = 0; g = 0; ++seg; continue; }  // a segment without rows
         if constexpr (WHOLE) tile = tiles - 1 - tile;
         const bool last = !WHOLE && seg == to.seg && g == to.head && tile == to.tile;
         if (last && to.stage == 0) break;
-        const int end = tile_end(p, sg, tile), nst = (end + kStage - 1) / kStage;
-        const int st0 = stage, st1 = last ? to.stage : nst;
+        int end = tile_end<KEYS>(p, sg, tile);
+        const int nst = (end + kStage - 1) / kStage;
+        const int st0 = stage, to_stage = last ? to.stage : nst;
+        int st1 = to_stage;
 
         // this wavefront's rows
         const int r0 = tile * kTileRows + wv * 32, row = r0 + ln;
         const bool mine = r0 < sg.rows, real = row < sg.rows;
         const RowAt ra = row_at(real ? row : mine ? r0 : 0, p.grp);         // (rows that do not exist repeat one that does)
-        const int lim = sg.before + ra.token;                               // the last key that the row sees
-        const int lim_first = sg.before + __builtin_amdgcn_readfirstlane(row_at(mine ? r0 : 0, p.grp).token);
-        const int lim_last = sg.before + __builtin_amdgcn_readfirstlane(row_at(max(min(sg.rows, r0 + 32) - 1, 0), p.grp).token);
         const int h = g * a.grp + ra.head;
         const int64_t t = sg.first + ra.token;
+        // the last key that the row sees; those of the wavefront's first and last row, or the least and the most
+        int lim, lim_first, lim_last;
+        Limits tile_lim = {0, 0};                               // keys that all rows of the tile see, and that some row does
+        if constexpr (KEYS == kStates) {
+            tile_lim = limits<kTileRows>(p, sg, tile * kTileRows, lane);
+            const Limits w = a.seen ? limits<32>(p, sg, mine ? r0 : 0, lane) : tile_lim;
+            lim = seen_by(a, t, sg.len) - 1;
+            lim_first = w.all - 1;
+            lim_last = w.some - 1;
+        } else {
+            lim = sg.before + ra.token;
+            lim_first = sg.before + __builtin_amdgcn_readfirstlane(row_at(mine ? r0 : 0, p.grp).token);
+            lim_last = sg.before + __builtin_amdgcn_readfirstlane(row_at(max(min(sg.rows, r0 + 32) - 1, 0), p.grp).token);
+        }
 
         // Keys and values of a stage: a wavefront copies 16 rows of each, which lie in one page.
         const unsigned char *kb = a.k, *vb = a.v;
         const int32_t* pages = nullptr;
-        if constexpr (PAGED) {
+        if constexpr (KEYS == kPages) {
             pages = a.table + ((int64_t)sg.s * a.layers + a.l0 + sg.l) * a.max_pages;
+        } else if constexpr (KEYS == kStates) {
+            const int64_t from = a.state_off[sg.s];
+            kb += a.ks.l * sg.l + a.ks.h * g + a.ks.n * from;
+            vb += a.vs.l * sg.l + a.vs.h * g + a.vs.n * from;
+            end = tile_lim.some;                                // (a part of a tile may be past what its rows see: it is empty)
+            st1 = min(st1, (end + kStage - 1) / kStage);
         } else {
             kb += a.ks.l * sg.l + a.ks.h * g + a.ks.n * sg.first;
             vb += a.vs.l * sg.l + a.vs.h * g + a.vs.n * sg.first;
@@ -784,7 +847,7 @@ attn_tiles_kernel(TileParams p) {
             if (out) x = 0;
             return __builtin_amdgcn_ballot_w64(out);
         };
-        if constexpr (PAGED) {
+        if constexpr (KEYS == kPages) {
             ids = load_ids(ids0);
             next = load_ids(ids0 + kWave);
             const int to_page = (min(st1 * kStage, end) - 1) >> a.shift;
@@ -797,7 +860,7 @@ attn_tiles_kernel(TileParams p) {
             uint32_t bad = 0;
             const int key = min(st * kStage + wv * 16, end - 1);            // the group's first key, or the last one there is
             const uint32_t rest = (uint32_t)(end - 1 - key);
-            if constexpr (PAGED) {
+            if constexpr (KEYS == kPages) {
                 if (st * 4 >= ids0 + kWave) {
                     ids = next; bad_now = bad_next; ids0 += kWave;
                     next = load_ids(ids0 + kWave);
@@ -823,7 +886,7 @@ attn_tiles_kernel(TileParams p) {
             return bad;
         };
         uint32_t bad_a = 0, bad_b = 0;
-        const int seen = sg.before + __builtin_amdgcn_readfirstlane(row_at(tile * kTileRows, p.grp).token) + 1;
+        const int seen = KEYS == kStates ? tile_lim.all : sg.before + __builtin_amdgcn_readfirstlane(row_at(tile * kTileRows, p.grp).token) + 1;
         const int plain = hidden ? 0 : max(0, min(st1, seen / kStage) - st0);
         if (st0 < st1) {
             if (plain & 1) issue(st0, sKb, sVb);
@@ -873,9 +936,9 @@ attn_tiles_kernel(TileParams p) {
         }
         if (mine) {
             const float sum = tl.total();
-            if (WHOLE || (st0 == 0 && st1 == nst)) {
+            if (WHOLE || (st0 == 0 && to_stage == nst)) {
                 tl.store(a.out + a.os.l * sg.l + a.os.h * h + a.os.n * t, hf, sum == 0.f ? 0.f : 1.f / sum, real);
-                if (!PAGED && real && hf == 0)
+                if (KEYS == kPrompt && real && hf == 0)
                     a.lse[(int64_t)a.L * a.H * sg.first + (int64_t)(sg.l * a.H + h) * sg.n + ra.token] = fmaf(tl.m, size, kLn2 * __builtin_amdgcn_logf(sum));
             } else {
                 // a workgroup has at most two parts of tiles that others share: of one that began before it, and of one that goes on
@@ -896,7 +959,7 @@ attn_tiles_kernel(TileParams p) {
 // Joins the parts of the tiles that were cut: the first cut of a tile has all of its parts.  A wavefront has 32 columns of 32 rows, in
 // the registers' order, in which the parts were written.  Bound: reading the parts, two of 64 KB for each workgroup at most at D 128;
 // 9.6 us for 512 workgroups.
-template <int D, bool PAGED>
+template <int D, Keys KEYS>
 __global__ void __launch_bounds__(kWave)
 attn_merge_tiles_kernel(TileParams p) {
     const PackedParams& a = p.a;
@@ -922,7 +985,7 @@ attn_merge_tiles_kernel(TileParams p) {
         w1 = base + run - 1;
         if (run < kWave) break;
     }
-    const Segment sg = uniform_segment<PAGED>(p, c.x);
+    const Segment sg = uniform_segment<KEYS>(p, c.x);
     const int r0 = c.z * kTileRows + wv * 32, row = r0 + ln;
     if (r0 >= sg.rows) return;
     const float size = scale_size(a.scale[sg.l]), qs = size * kLog2e;
@@ -950,7 +1013,7 @@ attn_merge_tiles_kernel(TileParams p) {
     const RowAt ra = row_at(real ? row : r0, p.grp);
     const int h = c.y * a.grp + ra.head;
     store_columns(o, a.out + a.os.l * sg.l + a.os.h * h + a.os.n * (int64_t)(sg.first + ra.token) + 64 * dt, hf, sum == 0.f ? 0.f : 1.f / sum, real);
-    if (!PAGED && real && hf == 0 && dt == 0)
+    if (KEYS == kPrompt && real && hf == 0 && dt == 0)
         a.lse[(int64_t)a.L * a.H * sg.first + (int64_t)(sg.l * a.H + h) * sg.n + ra.token] = fmaf(m, size, kLn2 * __builtin_amdgcn_logf(sum));
 }
 
@@ -967,7 +1030,7 @@ constexpr int kLeastBlocks = 2;     // of a wavefront
 
 __device__ __forceinline__ int blocks_of(const Segment& x) { return (x.end + kBlockKeys - 1) / kBlockKeys; }
 
-template <int D>
+template <int D, Keys KEYS>
 __global__ void __launch_bounds__(128, 128 / D)
 attn_stream_kernel(StreamParams p) {
     constexpr int ROWB = D * 2, kBytes = kBlockKeys * ROWB, kInst = CopyLane<D>::kCopies;            // copies per 16 keys and tensor
@@ -981,7 +1044,7 @@ attn_stream_kernel(StreamParams p) {
 
     // the launch's blocks, and this wavefront's: segment by segment, KV head by KV head
     auto blocks = [&](const Segment& x) { return (int64_t)blocks_of(x) * a.Hkv; };
-    const Looked<true, int64_t, decltype(blocks)> looked(p, lane, p.segs, 0, 1, blocks);
+    const Looked<KEYS, int64_t, decltype(blocks)> looked(p, lane, p.segs, 0, 1, blocks);
     const int all_blocks = (int)looked.all;                                // (below 2^31: the call is refused otherwise)
     const int share = max(kLeastBlocks, (all_blocks + p.waves - 1) / p.waves);
     if (wave == 0 && lane == 0) *p.share = share;
@@ -1004,14 +1067,19 @@ attn_stream_kernel(StreamParams p) {
         c.blk = 0;
         if (++c.g < a.Hkv) return false;
         c.g = 0;
-        do { ++c.seg; x = uniform_segment<true>(p, c.seg); } while (x.end == 0);    // (a block is left, so a segment is)
+        do { ++c.seg; x = uniform_segment<KEYS>(p, c.seg); } while (x.end == 0);    // (a block is left, so a segment is)
         return true;
     };
     const CopyLane<D> cp(lane);
     // lane i has the page of the i-th group of 16 keys from ids0 on
     int ids = 0, ids0 = 0;
     unsigned long long bad_ids = 0;
+    int64_t from = 0;                                           // first state of the segment
     auto load_ids = [&]() {
+        if constexpr (KEYS == kStates) {
+            from = uniform_load(a.state_off + in.s);
+            return;
+        }
         const int32_t* pages = a.table + ((int64_t)in.s * a.layers + a.l0 + in.l) * a.max_pages;
         ids0 = 2 * ci.blk;
         ids = pages[min((ids0 + lane) * 16, in.end - 1) >> a.shift];
@@ -1021,6 +1089,21 @@ attn_stream_kernel(StreamParams p) {
     };
     load_ids();
     auto issue = [&](unsigned char* dK, unsigned char* dV) -> uint32_t {
+        if constexpr (KEYS == kStates) {
+            const unsigned char *kb = a.k + a.ks.l * in.l + a.ks.h * ci.g, *vb = a.v + a.vs.l * in.l + a.vs.h * ci.g;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int key = min(ci.blk * kBlockKeys + 16 * x, in.end - 1);
+                const uint32_t last = (uint32_t)(in.end - 1 - key);
+                const unsigned char *ka = kb + a.ks.n * (from + key), *va = vb + a.vs.n * (from + key);
+#pragma unroll
+                for (int i = 0; i < kInst; ++i) {
+                    copy_to_lds(ka + cp.at(i, last, (uint32_t)a.ks.n), dK + (x * kInst + i) * 1024);
+                    copy_to_lds(va + cp.at(i, last, (uint32_t)a.vs.n), dV + (x * kInst + i) * 1024);
+                }
+            }
+            return 0;
+        }
         const uint32_t bad = (uint32_t)((bad_ids >> (2 * ci.blk - ids0)) & 3u);
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -1042,7 +1125,7 @@ attn_stream_kernel(StreamParams p) {
     auto ask = [&](unsigned char* dK, unsigned char* dV) -> uint32_t {
         if (asked > b0) {
             const bool other = step(ci, in);
-            if (other || 2 * ci.blk + 1 >= ids0 + kWave || 2 * ci.blk < ids0) load_ids();
+            if (other || (KEYS == kPages && (2 * ci.blk + 1 >= ids0 + kWave || 2 * ci.blk < ids0))) load_ids();
         }
         ++asked;
         return issue(dK, dV);
@@ -1051,6 +1134,7 @@ attn_stream_kernel(StreamParams p) {
     RowTile<D> tl;
     tl.offsets(lane);
     float qs = 1.f;
+    [[maybe_unused]] int seen = 0;                              // keys that all rows see
     int lim = 0, piece = cw.blk;                                // piece: the unit's first block here
     unsigned char* out = nullptr;
     auto begin = [&]() {                                        // a unit: its queries
@@ -1061,7 +1145,12 @@ attn_stream_kernel(StreamParams p) {
         qs = score_scale(sc);
         tl.load_q(a.q + a.qs.l * sg.l + a.qs.h * h + a.qs.n * t, hf, sc < 0.f);
         out = a.out + a.os.l * sg.l + a.os.h * h + a.os.n * t;
-        lim = sg.before + ra.token;
+        if constexpr (KEYS == kStates) {
+            lim = seen_by(a, t, sg.len) - 1;
+            seen = limits<kFewRows>(p, sg, 0, lane).all;
+        } else {
+            lim = sg.before + ra.token;
+        }
         tl.clear();
         piece = cw.blk;
         if (cw.g == 0 && cw.blk == 0 && lane == 0) p.start[cw.seg] = seg_start;
@@ -1076,7 +1165,7 @@ attn_stream_kernel(StreamParams p) {
     };
     auto attend = [&](const unsigned char* sK, const unsigned char* sV, uint32_t bad) {
         const int key0 = cw.blk * kBlockKeys;
-        if (key0 + kBlockKeys - 1 <= sg.before && bad == 0) tl.template attend<1, false, true>(sK, sV, qs, lane, 0, 0u, 1, 1);
+        if ((KEYS == kStates ? key0 + kBlockKeys <= seen : key0 + kBlockKeys - 1 <= sg.before) && bad == 0) tl.template attend<1, false, true>(sK, sV, qs, lane, 0, 0u, 1, 1);
         else tl.template attend<1, true, true>(sK, sV, qs, lane, lim - key0, bad, 1, 0);
     };
     // one block of the work: `more` blocks are in flight behind it
@@ -1124,7 +1213,7 @@ attn_stream_kernel(StreamParams p) {
 // workgroup per row, whose groups of lanes share the row's pieces (one sequence of 8192 keys, H32/8: 128 pieces per unit); with more
 // rows there are few pieces, and a group has a row (a workgroup per row took 42 us for 1600 units of 20 rows that nobody shared).
 constexpr int kJoinThreads = 256;
-template <int D>
+template <int D, Keys KEYS>
 __global__ void __launch_bounds__(kJoinThreads)
 attn_merge_stream_kernel(StreamParams p) {
     constexpr int LPP = D / 4, GROUPS = kJoinThreads / LPP;
@@ -1134,7 +1223,7 @@ attn_merge_stream_kernel(StreamParams p) {
     const int i = (int)blockIdx.x / a.Hkv, g = (int)blockIdx.x % a.Hkv;
     const int share = max(1, *p.share), start = p.start[i];     // (asked for with the segment; `start` is looked at if it has blocks)
     const float qs = score_scale(a.scale[uniform_div_mod(i, p.by_layers).r]);
-    const Segment x = uniform_segment<true>(p, i);
+    const Segment x = uniform_segment<KEYS>(p, i);
     if ((int)blockIdx.y * p.join_rows >= x.rows) return;
     const int u0 = x.end == 0 ? 0 : start + g * blocks_of(x);
     const int w0 = u0 / share, w1 = (u0 + blocks_of(x) - 1) / share;
@@ -1207,10 +1296,13 @@ static long long most_tiles(const pkv_packed& s) { return (long long)s.T * (s.H 
 // What the lengths are is on the device, so the bounds are wide where the rows are several prompts' (T stands for the longest) or the
 // table is wider than its caches, and launches are cut that would be faster whole: prompts of H12/4, 6 x 500 21 / 31, H8/2, 12 x 500
 // 24 / 32, H4, 16 x 1000 41 / 57, H8/1, 64 x 100 13 / 20; H32/8, 8 x 64 rows over 1000 entries of a table of 8192 27 / 43.
-static bool cut_tiles(const pkv_packed& s, long long keys, bool paged) {
+static bool cut_tiles(const pkv_packed& s, long long keys, double filled) {
     const double stages = (double)((keys + kStage - 1) / kStage), tiles = (double)most_tiles(s) * s.L * s.Hkv;
-    return stages * (1.27 - (paged ? 0.75 : 0.5) * 2.0 * tiles / tile_workgroups()) > 30.0;
+    return stages * (1.27 - filled * 2.0 * tiles / tile_workgroups()) > 30.0;
 }
+constexpr double kPromptFilled = 0.5, kPagesFilled = 0.75, kStatesFilled = 0.67;
+// the longest of S texts of M states, taken to be half as long again as the average
+static long long longest_states(const pkv_packed& s, int M) { return 3ll * M / (2 * s.S) < M ? (3ll * M + 2 * s.S - 1) / (2 * s.S) : M; }
 
 // rows of a KV head and block numbers are 32 bits wide, and so are the threads of a grid (256 of a workgroup)
 bool packed_attn_fits(const pkv_packed& s, const pkv_paging* g) {
@@ -1219,13 +1311,30 @@ bool packed_attn_fits(const pkv_packed& s, const pkv_paging* g) {
     return !g || (double)s.S * s.L * s.Hkv * g->max_pages * g->page_size / kBlockKeys < 2147483648.0;
 }
 
+static size_t part_row(const pkv_packed& s) { return sizeof(float2) + s.D * sizeof(float); }     // (a part of a tile has two of the first per row)
+static size_t stream_bytes(const pkv_packed& s) {
+    return 256 + up256((size_t)s.S * s.L * 4) + (size_t)2 * stream_waves(s) * kFewRows * part_row(s);
+}
+static size_t cut_bytes(const pkv_packed& s) {
+    return up256(tile_workgroups() * sizeof(int4)) + (size_t)2 * tile_workgroups() * kTileRows * (part_row(s) + sizeof(float2));
+}
+
 size_t packed_attn_ws_bytes(const pkv_packed& s, int max_rows) {
     if (s.dtype != PKV_BF16) return 0;
-    const size_t row = sizeof(float2) + s.D * sizeof(float);                    // (a part of a tile has two of the first per row)
-    if (few_rows(s, max_rows)) return 256 + up256((size_t)s.S * s.L * 4) + (size_t)2 * stream_waves(s) * kFewRows * row;
+    if (few_rows(s, max_rows)) return stream_bytes(s);
     // (whether tiles are cut goes by the table's width too, which the size does not ask for: where the widest would not be, none is)
-    if (!cut_tiles(s, max_rows > 0 ? kMaxSegmentSlots : s.T, max_rows > 0)) return 0;
-    return up256(tile_workgroups() * sizeof(int4)) + (size_t)2 * tile_workgroups() * kTileRows * (row + sizeof(float2));
+    if (!cut_tiles(s, max_rows > 0 ? kMaxSegmentSlots : s.T, max_rows > 0 ? kPagesFilled : kPromptFilled)) return 0;
+    return cut_bytes(s);
+}
+
+// blocks of the stream kernel are 32 bits wide
+bool cross_attn_fits(const pkv_packed& s, int M) {
+    return packed_attn_fits(s, nullptr) && ((double)M / kBlockKeys + s.S) * s.L * s.Hkv < 2147483648.0;
+}
+size_t cross_attn_ws_bytes(const pkv_packed& s, int M, int max_rows) {
+    if (s.dtype != PKV_BF16) return 0;
+    if (few_rows(s, max_rows)) return stream_bytes(s);
+    return cut_tiles(s, longest_states(s, M), kStatesFilled) ? cut_bytes(s) : 0;
 }
 
 static Work work_of(const pkv_packed& s, const PackedParams& a) {
@@ -1236,7 +1345,7 @@ static Work work_of(const pkv_packed& s, const PackedParams& a) {
     return w;
 }
 
-template <int D, bool PAGED>
+template <int D, Keys KEYS>
 static hipError_t launch_tiles(const pkv_packed& s, const PackedParams& a, void* ws, hipStream_t st) {
     TileParams p;
     (Work&)p = work_of(s, a);
@@ -1249,17 +1358,19 @@ static hipError_t launch_tiles(const pkv_packed& s, const PackedParams& a, void*
     p.workgroups = tile_workgroups();
     p.part_o = (float*)((char*)ws + up256(p.workgroups * sizeof(int4)));
     p.part_ms = (float2*)(p.part_o + (size_t)2 * p.workgroups * kTileRows * D);
-    if (!cut_tiles(s, PAGED ? (long long)a.max_pages << a.shift : s.T, PAGED)) {
-        hipLaunchKernelGGL((attn_tiles_kernel<D, PAGED, true>), dim3((unsigned)(tiles * heads)), dim3(256), 0, st, p);
+    const bool cut = KEYS == kPages ? cut_tiles(s, (long long)a.max_pages << a.shift, kPagesFilled)
+                     : KEYS == kStates ? cut_tiles(s, longest_states(s, a.M), kStatesFilled) : cut_tiles(s, s.T, kPromptFilled);
+    if (!cut) {
+        hipLaunchKernelGGL((attn_tiles_kernel<D, KEYS, true>), dim3((unsigned)(tiles * heads)), dim3(256), 0, st, p);
     } else {
-        hipLaunchKernelGGL((attn_tiles_kernel<D, PAGED, false>), dim3((unsigned)p.workgroups), dim3(256), 0, st, p);
-        hipLaunchKernelGGL((attn_merge_tiles_kernel<D, PAGED>), dim3((unsigned)p.workgroups - 1, kTileRows / 32 * (D / 32)), dim3(kWave), 0,
+        hipLaunchKernelGGL((attn_tiles_kernel<D, KEYS, false>), dim3((unsigned)p.workgroups), dim3(256), 0, st, p);
+        hipLaunchKernelGGL((attn_merge_tiles_kernel<D, KEYS>), dim3((unsigned)p.workgroups - 1, kTileRows / 32 * (D / 32)), dim3(kWave), 0,
                            st, p);
     }
     return hipGetLastError();
 }
 
-template <int D>
+template <int D, Keys KEYS>
 static hipError_t launch_stream(const pkv_packed& s, const PackedParams& a, void* ws, hipStream_t st) {
     StreamParams p;
     (Work&)p = work_of(s, a);
@@ -1270,8 +1381,8 @@ static hipError_t launch_stream(const pkv_packed& s, const PackedParams& a, void
     p.part_ms = (float2*)(p.part_o + (size_t)2 * p.waves * kFewRows * D);
     const int rows = a.max_rows * a.grp;
     p.join_rows = rows <= 8 ? 1 : kJoinThreads / (D / 4);
-    hipLaunchKernelGGL(attn_stream_kernel<D>, dim3((unsigned)(p.waves / 2)), dim3(128), 0, st, p);
-    hipLaunchKernelGGL(attn_merge_stream_kernel<D>, dim3((unsigned)(p.segs * s.Hkv), (unsigned)((rows + p.join_rows - 1) / p.join_rows)),
+    hipLaunchKernelGGL((attn_stream_kernel<D, KEYS>), dim3((unsigned)(p.waves / 2)), dim3(128), 0, st, p);
+    hipLaunchKernelGGL((attn_merge_stream_kernel<D, KEYS>), dim3((unsigned)(p.segs * s.Hkv), (unsigned)((rows + p.join_rows - 1) / p.join_rows)),
                        dim3(kJoinThreads), 0, st, p);
     return hipGetLastError();
 }
@@ -1287,14 +1398,21 @@ hipError_t launch_packed_attn(const pkv_packed& s, const PackedAttn& a, hipStrea
     p.q = (const unsigned char*)a.q; p.k = (const unsigned char*)a.k; p.v = (const unsigned char*)a.v; p.out = (unsigned char*)a.out;
     p.qs = bytes(a.qs); p.ks = bytes(a.ks); p.vs = bytes(a.vs); p.os = bytes(a.os);
     p.row_off = a.row_off; p.table = a.table; p.lens = a.lens; p.scale = a.scale; p.lse = a.lse;
+    const bool states = a.state_off != nullptr, wide = s.D == 128;
+    if (states) { p.M = a.M; p.state_off = a.state_off; p.seen = a.seen; }
     if (s.dtype == PKV_BF16) {
-        if (few_rows(s, a.max_rows)) return s.D == 128 ? launch_stream<128>(s, p, a.ws, st) : launch_stream<64>(s, p, a.ws, st);
-        if (paged) return s.D == 128 ? launch_tiles<128, true>(s, p, a.ws, st) : launch_tiles<64, true>(s, p, a.ws, st);
-        return s.D == 128 ? launch_tiles<128, false>(s, p, a.ws, st) : launch_tiles<64, false>(s, p, a.ws, st);
+        if (few_rows(s, a.max_rows)) {
+            if (states) return wide ? launch_stream<128, kStates>(s, p, a.ws, st) : launch_stream<64, kStates>(s, p, a.ws, st);
+            return wide ? launch_stream<128, kPages>(s, p, a.ws, st) : launch_stream<64, kPages>(s, p, a.ws, st);
+        }
+        if (states) return wide ? launch_tiles<128, kStates>(s, p, a.ws, st) : launch_tiles<64, kStates>(s, p, a.ws, st);
+        if (paged) return wide ? launch_tiles<128, kPages>(s, p, a.ws, st) : launch_tiles<64, kPages>(s, p, a.ws, st);
+        return wide ? launch_tiles<128, kPrompt>(s, p, a.ws, st) : launch_tiles<64, kPrompt>(s, p, a.ws, st);
     }
     const dim3 grid((unsigned)s.T, (unsigned)s.H, (unsigned)s.L);
-    if (s.D == 128) hipLaunchKernelGGL(attn_rows_kernel<128>, grid, dim3(256), 0, st, p);
-    else hipLaunchKernelGGL(attn_rows_kernel<64>, grid, dim3(256), 0, st, p);
+    auto* rows = states ? (wide ? attn_rows_kernel<128, kStates> : attn_rows_kernel<64, kStates>)
+                        : (wide ? attn_rows_kernel<128, kPages> : attn_rows_kernel<64, kPages>);
+    hipLaunchKernelGGL(rows, grid, dim3(256), 0, st, p);
     return hipGetLastError();
 }
 

@@ -1,4 +1,4 @@
-"""Beam search over the paged cache: what the C entry points refuse, before anything is enqueued, and what the binding refuses;
+"""Beam search over the paged cache and attention to states of another length: what the C entry points refuse, before anything is enqueued, and what the binding refuses;
 the plain forms against hand-worked numbers."""
 import ctypes as C
 import math
@@ -10,7 +10,7 @@ import torch
 import beam_reference as R
 import paper_2412_03409_amd as P
 from paper_2412_03409_amd import binding as Bd
-from test_serving_boundary_cpu import A, BAD_PAGING, BIG, ODD, paging, with_null
+from test_serving_boundary_cpu import A, BAD_PACKED, BAD_PAGING, BIG, ODD, ST, packed, paging, with_null
 
 
 def but(args, i, x):
@@ -58,6 +58,65 @@ def test_reorder_refuses():
     # 4096 * 64 segments of 2048 heads: more workgroups than a launch has
     assert f(*but(but(but(args, 0, 4096), 2, 2048), 5, paging(layers=64, page_size=256, max_pages=1))) == 7
     assert P.reorder_workspace_bytes(0, 2) == 0 and P.reorder_workspace_bytes(4097, 1) == 0 and P.reorder_workspace_bytes(4, 65) == 0
+
+
+def test_cross_attention_refuses():
+    lib = P.load()
+    f = lib.prefixkv_cross_attn
+    args = [packed(), A, ST, A, 100, A, ST, A, ST, A, A, A, 10, A, ST, A, BIG, None]
+    for bad in with_null(args, optional=(10, 15)):
+        assert f(*bad) == 1
+    assert f(*but(args, 0, None)) == 1
+    for kw in BAD_PACKED:
+        assert f(*but(args, 0, packed(**kw))) == 2, kw
+    for i, xs in ((4, (0, -1, (1 << 22) + 1)), (12, (0, 11))):
+        for x in xs:
+            assert f(*but(args, i, x)) == 2
+    assert f(*but(args, 0, packed(dtype=5))) == 3
+    for i in (1, 5, 7, 13):
+        assert f(*but(args, i, ODD)) == 4
+    for i in (2, 6, 8, 14):
+        for bad in (Bd._Strides(0, 8192, 130, 4096), Bd._Strides(0, -8192, 128, 4096), Bd._Strides(0, 8192, 128, 0)):
+            assert f(*but(args, i, bad)) == 4
+    assert f(*but(but(args, 0, packed(L=2)), 14, Bd._Strides(0, 0, 128, 4096))) == 4
+    assert f(*but(args, 14, Bd._Strides(0, 8192, 0, 4096))) == 4
+    for i in (6, 8):
+        assert f(*but(args, i, Bd._Strides(0, 8192, 128, 1 << 26))) == 7
+    assert f(*but(args, 0, packed(T=1 << 22, H=2048, Hkv=1, S=1))) == 7
+    # (blocks of the states in more than 31 bits: so many layers and heads that tiles are too many first)
+    for S, rows in ((2, 10), (1, 10)):
+        need = P.cross_workspace_bytes(S, 1, 4, 2, 10, 100, 128, torch.bfloat16, rows)
+        if need:
+            for i, x in ((15, None), (15, C.c_void_p(4104)), (16, need - 1)):
+                assert f(*but(but(args, 0, packed(S=S)), i, x)) == 5
+    for bad in (dict(T=0), dict(D=96), dict(S=0), dict(M=0), dict(M=(1 << 22) + 1), dict(max_rows=0), dict(max_rows=11)):
+        d = {**dict(S=2, L=1, H=4, Hkv=2, T=10, M=100, D=128, max_rows=10), **bad}
+        assert P.cross_workspace_bytes(dtype=torch.bfloat16, **d) == 0
+    assert P.cross_workspace_bytes(2, 1, 4, 2, 10, 100, 128, torch.float32, 10) == 0
+
+
+def test_cross_binding_refuses(monkeypatch):
+    q, kv = torch.zeros((1, 4, 6, 64)), torch.zeros((1, 2, 30, 64))
+    off, to, scale = torch.tensor([0, 6], dtype=torch.int32), torch.tensor([0, 30], dtype=torch.int32), torch.ones(1)
+    good = dict(q=q, k=kv, v=kv, row_off=off, state_off=to, scale=scale, max_rows=6)
+    with pytest.raises(ValueError, match="GPU"):
+        P.prefixkv_cross_attn(**good)
+
+    class Library:
+        prefixkv_cross_workspace_bytes = P.load().prefixkv_cross_workspace_bytes
+
+        def __getattr__(self, name):
+            return lambda *a: pytest.fail(f"{name} was called")
+    monkeypatch.setattr(Bd, "_here", lambda *a: 0)
+    monkeypatch.setattr(Bd, "load", Library)
+    for bad in (dict(k=kv[:, :, :20]), dict(v=kv.bfloat16()), dict(k=kv.bfloat16(), v=kv.bfloat16()), dict(k=kv[0], v=kv[0]),
+                dict(k=kv[..., :32], v=kv[..., :32]), dict(q=q.half(), k=kv.half(), v=kv.half()), dict(out=q[:, :2]), dict(out=q.bfloat16()),
+                dict(row_off=off.long()), dict(state_off=to[:1]), dict(state_off=torch.zeros(3, dtype=torch.int32)),
+                dict(scale=scale.double()), dict(scale=torch.ones(2)), dict(seen=torch.zeros(5, dtype=torch.int32)),
+                dict(seen=torch.zeros(6, dtype=torch.int64)), dict(seen=torch.zeros(12, dtype=torch.int32)[::2]),
+                dict(max_rows=1 << 32), dict(q=q.transpose(2, 3).contiguous().transpose(2, 3))):
+        with pytest.raises((ValueError, TypeError)):
+            P.prefixkv_cross_attn(**{**good, **bad})
 
 
 def test_binding_refuses(monkeypatch):
