@@ -4,7 +4,8 @@ library.
 HotPath    one rectangular batch on pre-allocated buffers: importance -> select -> compact -> T
            decode steps.  Used by the benchmark, the smoke check and the end-to-end tests.
 PagedPath  sequences of different lengths that come, ask again and go: packed prompts -> rotation ->
-           attention -> importance and search per sequence -> pages -> further rows over the pages.
+           attention -> importance and search per sequence -> pages -> further rows over the pages; with
+           several beams per prompt, which share its pages and the states of its encoder.
 """
 from __future__ import annotations
 
@@ -116,16 +117,24 @@ class HotPath:
 
 
 _LONGEST = 8192      # positions of a prompt that the importance and the search take
+_MOST_BEAMS = 32     # that the choice among continuations takes
 
 
 class PagedPath:
     """S places for sequences over one pool of pages.  All layers of the model are called at once, as the queries, keys and
     values [L,heads,T,D] of the packed rows of all layers are given (bf16).  Nothing is read back: `status` [1] tells whether
     the last call that needed pages got them, `search` [S] what the search said (its status bits, 0 if nothing) of the last
-    prompt of every place: a prompt that it could not rank, with NaN in a query for instance, keeps no entries."""
+    prompt of every place: a prompt that it could not rank, with NaN in a query for instance, keeps no entries.
+
+    beams > 1: the places come in groups of so many, one behind the other, that hold the beams of a prompt.  A prompt begins in the
+    first place of a group, whose beams end with that (whatever becomes of the prompt); follow(zeros) makes them all continue it,
+    and advance() chooses every step's continuations."""
 
     def __init__(self, S: int, L: int, H: int, Hkv: int, D: int, scale: torch.Tensor, plan: B_.RopePlan, num_pages: int,
-                 max_pages: int, page_size: int = 64, device="cuda"):
+                 max_pages: int, page_size: int = 64, device="cuda", beams: int = 1):
+        beams = index(beams)
+        if not 1 <= beams <= _MOST_BEAMS or S % beams:
+            raise ValueError(f"a prompt has 1 ... {_MOST_BEAMS} beams, and S is a multiple of them")
         if scale.dtype != torch.float32 or scale.shape != (L,) or not scale.is_contiguous():
             raise ValueError("scale must be contiguous f32 [L]")
         self.S, self.L, self.H, self.Hkv, self.D = S, L, H, Hkv, D
@@ -135,6 +144,10 @@ class PagedPath:
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
         self.search = torch.zeros(S, dtype=torch.int32, device=device)
         self.page_ws = torch.empty(B_.page_workspace_bytes(S, L), dtype=torch.uint8, device=device)
+        self.beams = beams
+        if beams > 1:
+            self.stay = torch.arange(beams, dtype=torch.int32, device=device).repeat(S // beams, 1)
+            self.reorder_ws = torch.empty(B_.reorder_workspace_bytes(S, L), dtype=torch.uint8, device=device)
 
     def _offsets(self, lengths) -> torch.Tensor:
         off = [0]
@@ -162,12 +175,16 @@ class PagedPath:
         places, lengths = [index(s) for s in places], [index(n) for n in lengths]
         if len(set(places)) != len(places) or any(not 0 <= s < self.S for s in places):
             raise ValueError(f"places must be different numbers in 0 ... {self.S - 1}")
+        if any(s % self.beams for s in places):
+            raise ValueError("a prompt begins in the first place of a group of beams")
         if not 0 < len(places) == len(lengths) == len(budgets) or any(n < 1 for n in lengths) or sum(lengths) > q.shape[2]:
             raise ValueError("a length and a budget per place, rows for all of them")
         budgets = [int(b) for b in budgets]
         if any(n > _LONGEST for n in lengths) or any(not 1 <= b < 1 << 63 for b in budgets):
             raise ValueError(f"prompts of at most {_LONGEST} positions, budgets of at least 1")
         self._look_at(q, k, v, positions)
+        if self.beams > 1:
+            self.end(s + i for s in places for i in range(self.beams))
         off = self._offsets(lengths)
         B_.prefixkv_rope(q, k, positions, self.plan, q_out=q, k_out=k)
         out, lse = B_.prefixkv_prefill_attn_packed(q, k, v, off, self.scale)
@@ -216,6 +233,42 @@ class PagedPath:
         places = [index(s) for s in places]
         if any(not 0 <= s < self.S for s in places):
             raise ValueError(f"places must be in 0 ... {self.S - 1}")
+        if self.beams > 1:              # (pages that others hold too stay with them)
+            parents = self.stay.clone()
+            parents.view(-1)[places] = -1
+            self.follow(parents)
+            return
         self.target.copy_(self.cache.lens)
         self.target[places] = 0
         B_.prefixkv_page_resize(self.cache, self.target, status=self.status, ws=self.page_ws)
+
+    # ---- several beams per prompt ------------------------------------------------------------
+    def follow(self, parents):
+        """Place i of every group becomes what place parents[g,i] was: parents [S/beams,beams] i32 on the GPU, -1: empty.  Nothing
+        changes if `status` says that there were too few pages."""
+        if parents.shape != (self.S // self.beams, self.beams):
+            raise ValueError("parents must be [S/beams,beams]")
+        if self.beams == 1:
+            raise ValueError("a path with one beam per prompt has nothing to follow")
+        B_.prefixkv_page_reorder(self.cache, parents, status=self.status, ws=self.reorder_ws)
+
+    def advance(self, logits, scores, ended=None, end_token=None):
+        """The best continuations of every prompt, and the places that follow them: logits [S/beams,beams,V], scores [S/beams,beams]
+        f32, ended [S/beams,beams] bool or None -> (tokens, parents, scores, ended) as of prefixkv_beam_select.  If `status` says that
+        there were too few pages the places are as they were, and the beams have to be chosen again from fewer prompts."""
+        if logits.shape[:2] != (self.S // self.beams, self.beams):
+            raise ValueError("logits must be [S/beams,beams,V]")
+        if self.beams == 1:
+            raise ValueError("a path with one beam per prompt has nothing to follow")
+        chosen = B_.prefixkv_beam_select(logits, scores, ended=ended, end_token=end_token)
+        self.follow(chosen[1])
+        return chosen
+
+    def cross(self, lengths, q, k, v, state_off, seen=None):
+        """Attention of rows (lengths[s] of place s, packed) to their prompt's states k, v [L,Hkv,M,D], state_off [S/beams+1] i32 on
+        the GPU, which the beams of a group share; seen [T] i32: only the first ones -> [L,H,T,D]."""
+        lengths = [int(n) for n in lengths]
+        if len(lengths) != self.S or any(n < 0 for n in lengths) or sum(lengths) > q.shape[2]:
+            raise ValueError("a length per place, rows for all of them")
+        rows = [sum(lengths[s:s + self.beams]) for s in range(0, self.S, self.beams)]
+        return B_.prefixkv_cross_attn(q, k, v, self._offsets(rows), state_off, self.scale, max(1, max(rows)), seen=seen)

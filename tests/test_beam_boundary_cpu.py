@@ -151,6 +151,35 @@ def test_binding_refuses(monkeypatch):
             P.prefixkv_page_reorder(c, **{**dict(parents=par), **bad})
 
 
+def test_paths_refuse(monkeypatch):
+    import paper_2412_03409_amd.pipeline as pipeline
+
+    def path(**kw):
+        return pipeline.PagedPath(6, 1, 2, 1, 64, torch.ones(1), P.rope_plan(64, device="cpu"), num_pages=4, max_pages=2, device="cpu", **kw)
+    for beams in (0, 4, 33, -1):
+        with pytest.raises(ValueError, match="beams"):
+            path(beams=beams)
+    for name in ("prefixkv_rope", "prefixkv_page_reorder", "prefixkv_beam_select", "prefixkv_cross_attn"):
+        monkeypatch.setattr(pipeline.B_, name, lambda *a, **kw: pytest.fail("a step was made"))
+    three, one = path(beams=3), path()
+    q, k = torch.zeros((1, 2, 6, 64), dtype=torch.bfloat16), torch.zeros((1, 1, 6, 64), dtype=torch.bfloat16)
+    pos = torch.zeros((1, 6), dtype=torch.int32)
+    with pytest.raises(ValueError, match="first place"):
+        three.prefill([1], [5], q, k, k, pos, [5])
+    for bad in (torch.zeros((3, 2), dtype=torch.int32), torch.zeros(6, dtype=torch.int32)):
+        with pytest.raises(ValueError, match="parents"):
+            three.follow(bad)
+    with pytest.raises(ValueError, match="one beam"):
+        one.follow(torch.zeros((6, 1), dtype=torch.int32))
+    with pytest.raises(ValueError, match="one beam"):
+        one.advance(torch.zeros((6, 1, 9)), torch.zeros((6, 1)))
+    with pytest.raises(ValueError, match="logits"):
+        three.advance(torch.zeros((6, 9)), torch.zeros((2, 3)))
+    for lengths in ([1, 1], [1, 1, 1, 1, 1, 2], [-1, 1, 1, 1, 1, 1]):
+        with pytest.raises(ValueError, match="place"):
+            three.cross(lengths, q, k, k, torch.zeros(3, dtype=torch.int32))
+
+
 def test_plain_forms_on_hand_worked_numbers():
     inf = math.inf
     # two beams over two tokens: 1/4, 3/4 of the first, halves of the second; scores log 1/2 and log 1

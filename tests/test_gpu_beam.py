@@ -325,3 +325,101 @@ def test_reorder_replays_from_a_graph():
         want, table, lens, ring, state, pools = R.reorder(p, table, lens, ring, state, ps, pools)
         assert int(status) == want
         check_cache(c, table, lens, ring, state, ps, pools)
+
+
+# ---- together -----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("H,Hkv,D,ps,beams", [(4, 2, 64, 16, 3), (3, 3, 128, 32, 4)])
+def test_beam_search_of_a_path(H, Hkv, D, ps, beams):
+    """Prompts come into a path, their beams fork, extend, attend to the prompt's encoder's states, and are chosen and reordered for
+    some steps; a prompt ends and another comes.  Every output against the definitions in 64 bits, on keys and values that are
+    copied with their beam."""
+    from paper_2412_03409_amd.pipeline import PagedPath
+    from test_gpu_serving import close, projected
+    L, G, V, end, g = 2, 2, 301, 4, gen(H)
+    S = G * beams
+    scale = torch.tensor([0.15, 0.3])
+    plan = P.rope_plan(D, device=DEV)
+    axis = plan.axis.cpu().numpy()
+    path = PagedPath(S, L, H, Hkv, D, scale.to(DEV), plan, num_pages=260, max_pages=12, page_size=ps, device=DEV, beams=beams)
+    keys = [[None] * L for _ in range(S)]
+    m = [70, 131]
+    to = offsets(m)
+    kv = torch.randn((L, 2 * Hkv, sum(m), D), generator=g).to(BF16).to(DEV)
+    states = kv[:, :Hkv], kv[:, Hkv:]
+
+    def rows(T):
+        x = projected(g, L, H, Hkv, T, D, BF16)
+        pos = torch.randint(0, 3000, (1, T), generator=g).to(torch.int32).to(DEV)
+        return (*x, pos)
+
+    def rotated(x, pos):
+        return torch.from_numpy(RS.rope(f64(x), pos.cpu().numpy(), axis, 10000.0, D, False)).to(BF16).double().numpy()
+
+    def prompts(places, lengths, budgets):
+        q, k, v, pos = rows(sum(lengths))
+        kr, vr = rotated(k, pos), f64(v)
+        kept = []
+        path.prefill(places, lengths, q, k, v, pos, budgets, kept_pos=kept)
+        assert int(path.status) == 0
+        off = offsets(lengths)
+        for i, s in enumerate(places):
+            for b in range(beams):
+                keys[s + b] = [[x[l][:, :0] for x in (kr, vr)] for l in range(L)]
+            for l in range(L):
+                at = kept[i][l].cpu().numpy()
+                at = off[i] + at[at >= 0]
+                keys[s][l] = [x[l][:, at] for x in (kr, vr)]
+
+    def follow(parents):
+        old = list(keys)
+        for s in range(S):
+            p = parents[s // beams, s % beams]
+            keys[s] = [[x[:, :0] for x in seg] for seg in old[s]] if p < 0 else [list(seg) for seg in old[s // beams * beams + p]]
+        lens = np.array([[seg[0].shape[1] for seg in k] for k in keys])
+        np.testing.assert_array_equal(path.cache.lens.cpu().numpy(), lens)
+
+    def extend():
+        q, k, v, pos = rows(S)
+        qr, kr, vr = rotated(q, pos), rotated(k, pos), f64(v)
+        out = path.extend([1] * S, q, k, v, pos)
+        assert int(path.status) == 0
+        for s in range(S):
+            for l in range(L):
+                keys[s][l] = [np.concatenate([old, x[l][:, s:s + 1]], axis=1) for old, x in zip(keys[s][l], (kr, vr))]
+                kk, vv = keys[s][l]
+                for h in range(H):
+                    o, mag, _ = RS.attend(qr[l, h, s:s + 1], kk[h // (H // Hkv)], vv[h // (H // Hkv)], float(scale[l]), kk.shape[1] - 1)
+                    close(out[l:l + 1, h:h + 1, s:s + 1], o[None, None], mag[None, None], BF16)
+        crossed = path.cross([1] * S, q, *states, i32(to))
+        want, mag = R.cross(f64(q), offsets([beams] * G), f64(states[0]), f64(states[1]), to, scale.double().numpy())
+        close(crossed, want, mag, BF16)
+
+    def choose(scores, ended, step):
+        x, _, _ = select_inputs(100 * H + step, G, beams, V, BF16)
+        got = path.advance(x.to(DEV), scores, ended=ended, end_token=end)
+        assert int(path.status) == 0
+        check_select(x, scores.cpu(), None if ended is None else ended.cpu(), end, got)
+        follow(got[1].cpu().numpy())
+        return got[2], got[3]
+
+    prompts([0, beams], [90, 41], [120, 60])
+    path.follow(torch.zeros((G, beams), dtype=torch.int32, device=DEV))
+    follow(np.zeros((G, beams), dtype=int))
+    scores, ended = torch.full((G, beams), float("-inf"), device=DEV), None
+    scores[:, 0] = 0
+    for step in range(3):
+        extend()
+        scores, ended = choose(scores, ended, step)
+    path.end(range(beams))
+    follow(np.array([[-1] * beams, list(range(beams))]))
+    prompts([0], [60], [70])
+    first = np.array([[0] * beams, list(range(beams))])
+    path.follow(i32(first))
+    follow(first)
+    scores[0], ended[0] = float("-inf"), False
+    scores[0, 0] = 0
+    for step in range(3, 3 + ps):
+        extend()
+        scores, ended = choose(scores, ended, step)
+    path.end(range(S))
+    assert int(path.cache.state[1]) == 260 and np.array_equal(np.sort(path.cache.ring.cpu().numpy()), np.arange(260))
