@@ -18,34 +18,52 @@
 namespace pkv {
 
 constexpr int kScanThreads = 256;
-constexpr int kJoinThreads = 256;
+constexpr int kWaveCandidates = 128;    // of a wavefront's part of a piece
 
 struct BeamParams {
     int S, W, V, pieces;            // pieces of a row
+    int group;                      // pieces, rounded up to a power of two
     int64_t stride;                 // of a row, in elements
     const void* logits;
     const float* scores;
     const uint8_t* ended;
     int end_token;                  // -1: none
-    FastDiv by_pieces;
+    FastDiv by_pieces, by_w;
     int32_t *tokens, *parents;
     float* scores_out;
     uint8_t* ended_out;
-    float2* sums;                   // workspace [S*W][pieces]: {maximum, sum}
+    float2* sums;                   // workspace [S*W][pieces]: {maximum, sum of 2^(kLog2e x - base(maximum))}
     float* value;                   // workspace [S*W][pieces][W], descending
     int32_t* token;                 // the same, -1 behind the last
 };
 
-// NaN counts as -inf, +inf as the largest finite number, -0 as 0
-__device__ __forceinline__ float clean(float x) { return x != x ? -INFINITY : fminf(x, 3.402823466e38f) + 0.f; }
-// an order-preserving whole number above 0 of a finite value; 0 stands for -inf: no candidate
+// NaN counts as -inf, +inf as the largest finite number
+constexpr float kLargest = 3.402823466e38f;
+__device__ __forceinline__ float clean(float x) { return x != x ? -INFINITY : fminf(x, kLargest); }
+// an order-preserving whole number above 0 of a finite value, the same for both zeros; 0 stands for -inf: no candidate
 __device__ __forceinline__ uint32_t key_of(float x) {
-    const uint32_t u = __float_as_uint(x);
+    const uint32_t u = __float_as_uint(x + 0.f);
     return x == -INFINITY ? 0u : (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
+// (of a key that no finite value has: the lowest one)
+__device__ __forceinline__ float of_key(uint32_t k) {
+    k = max(k, ~__float_as_uint(-kLargest));
+    return __uint_as_float((k & 0x80000000u) ? k ^ 0x80000000u : ~k);
+}
 __device__ __forceinline__ uint64_t key_of(double x) {
-    const uint64_t u = (uint64_t)__double_as_longlong(x);
+    const uint64_t u = (uint64_t)__double_as_longlong(x + 0.0);
     return x == -(double)INFINITY ? 0ull : (u >> 63) ? ~u : u | (1ull << 63);
+}
+
+// Terms of a row's sum are 2^(kLog2e x - base), one fma and one rounding of the exponent each; base = kLog2e * maximum, rounded.
+// kLog2e is log2(e) (1 + kExcess): of a sum that stands for its maximum the logarithm is too large by kExcess * maximum (by up to
+// kExcess * log V < 2e-7 less where it does not), which is taken off behind it, in 64 bits.  Beyond kWideLogit, where the base would leave the range,
+// the difference from the maximum is scaled.
+constexpr float kLog2e = 1.44269502f, kWideLogit = 1e30f;
+constexpr double kLn2 = 0.693147180559945309417, kExcess = (double)kLog2e * kLn2 - 1.0;
+__device__ __forceinline__ float base_of(float m) { return m * kLog2e; }
+__device__ __forceinline__ double base_log(float m) {
+    return fabsf(m) > kWideLogit ? (double)m : (double)base_of(m) * kLn2 - kExcess * (double)m;
 }
 
 template <class K>
@@ -61,263 +79,421 @@ __device__ __forceinline__ K wave_min(K x) {
     return x;
 }
 
-// The W-th largest of `n` entries in LDS: {key, place}, larger keys first, equal ones by ascending place, key 0: none.  An entry is
-// among the W largest if its key is above `key` or equal and its place at most `place`.  Bisection over the keys that there are, by
-// counting with ballots: the first key that exactly W reach will do.  Every wavefront does it for itself.
+// A threshold that the W largest of `n` entries {key, place} reach, and at most `slack` others: larger keys first, equal ones by ascending
+// place, key 0: none.  Bisection over the keys that there are, by counting with ballots.  Every wavefront does it for itself, on entries
+// in LDS or, the first 256, in registers.
 template <class K>
 struct Threshold { K key; uint32_t place; };
 template <class K>
-__device__ __forceinline__ Threshold<K> nth_largest(const K* key, const uint32_t* place, int n, int W, int lane) {
+__device__ __forceinline__ bool reaches(K key, uint32_t place, const Threshold<K>& t) { return key > t.key || (key == t.key && place <= t.place); }
+
+template <class K, class C>
+__device__ __forceinline__ K nth_key(K lo, K hi, int W, int slack, C count) {       // count(k): entries of at least k; at least W reach lo
+    while (lo < hi) {
+        const K mid = lo + (hi - lo + 1) / 2;
+        const int c = count(mid);
+        if (c >= W && c <= W + slack) return mid;
+        if (c > W) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+// in registers: R of a lane
+template <int R, class K>
+__device__ __forceinline__ K nth_key(const K (&k)[R], int W, int slack) {
+    K lo = ~(K)0, hi = 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) { hi = max(hi, k[i]); lo = min(lo, k[i] - 1); }        // (0 - 1 is the largest)
+    hi = wave_max(hi);
+    lo = wave_min(lo) + 1;
+    auto count = [&](K x) {
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < R; ++i) c += __popcll(__builtin_amdgcn_ballot_w64(k[i] >= x));
+        return c;
+    };
+    return hi == 0 || count(1) <= W ? (K)1 : nth_key(lo, hi, W, slack, count);
+}
+template <class K>
+__device__ __forceinline__ Threshold<K> nth_largest(const K* key, const uint32_t* place, int n, int W, int slack, int lane) {
     auto count = [&](auto f) {
         int c = 0;
         for (int i = 0; i < n; i += kWave) c += __popcll(__builtin_amdgcn_ballot_w64(i + lane < n && f(min(i + lane, n - 1))));
         return c;
     };
-    K lo = ~(K)0, hi = 0;
-    for (int i = lane; i < n; i += kWave) {
-        const K k = key[i];
-        hi = max(hi, k);
-        lo = k != 0 ? min(lo, k) : lo;
+    K t;
+    if (n <= 4 * kWave) {
+        K k[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) k[i] = i * kWave + lane < n ? key[i * kWave + lane] : 0;
+        t = nth_key(k, W, slack);
+    } else {
+        K lo = ~(K)0, hi = 0;
+        for (int i = lane; i < n; i += kWave) { hi = max(hi, key[i]); lo = min(lo, key[i] - 1); }
+        hi = wave_max(hi);
+        lo = wave_min(lo) + 1;
+        auto at_least = [&](K x) { return count([&](int i) { return key[i] >= x; }); };
+        t = hi == 0 || at_least(1) <= W ? (K)1 : nth_key(lo, hi, W, slack, at_least);
     }
-    hi = wave_max(hi);
-    lo = wave_min(lo);
-    if (hi == 0 || count([&](int i) { return key[i] != 0; }) <= W) return {(K)1, ~0u};      // all there are
-    while (lo < hi) {                                                    // at least W reach lo, fewer than W pass hi
-        const K mid = lo + (hi - lo + 1) / 2;
-        const int c = count([&](int i) { return key[i] >= mid; });
-        if (c == W) return {mid, ~0u};
-        if (c > W) lo = mid; else hi = mid - 1;
-    }
-    const int above = count([&](int i) { return key[i] > lo; });
+    if (count([&](int i) { return key[i] >= t; }) <= W + slack) return {t, ~0u};
+    const int above = count([&](int i) { return key[i] > t; });
     uint32_t a = 0, b = ~0u;                                             // the lowest places of the equal ones
     while (a < b) {
         const uint32_t mid = a + (b - a) / 2;
-        if (above + count([&](int i) { return key[i] == lo && place[i] <= mid; }) >= W) b = mid; else a = mid + 1;
+        if (above + count([&](int i) { return key[i] == t && place[i] <= mid; }) >= W) b = mid; else a = mid + 1;
     }
-    return {lo, a};
+    return {t, a};
 }
-template <class K>
-__device__ __forceinline__ bool reaches(K key, uint32_t place, const Threshold<K>& t) { return key > t.key || (key == t.key && place <= t.place); }
 
+__device__ __forceinline__ uint32_t of_lane(uint32_t x, int j) { return (uint32_t)__builtin_amdgcn_readlane((int)x, j); }
+__device__ __forceinline__ uint64_t of_lane(uint64_t x, int j) { return ((uint64_t)of_lane((uint32_t)(x >> 32), j) << 32) | of_lane((uint32_t)x, j); }
+// how many of the n candidates come before this lane's, where a wavefront holds them all
+template <class K>
+__device__ __forceinline__ int rank_in_wave(int n, K key, uint32_t place) {
+    int r = 0;
+    for (int j = 0; j < n; ++j) {
+        const K k = of_lane(key, j);
+        const uint32_t a = of_lane(place, j);
+        r += (k > key) | ((k == key) & (a < place));
+    }
+    return r;
+}
 // how many of the n candidates come before {key, place}
 template <class K>
 __device__ __forceinline__ int rank_of(const K* keys, const uint32_t* places, int n, K key, uint32_t place) {
     int r = 0;
-    for (int i = 0; i < n; ++i) r += keys[i] > key || (keys[i] == key && places[i] < place);
+#pragma unroll 8
+    for (int i = 0; i < n; ++i) {
+        const K k = keys[i];
+        const uint32_t a = places[i];
+        r += (k > key) | ((k == key) & (a < place));
+    }
     return r;
-}
-
-// whether beam w of prompt s has continuations to look for
-__device__ __forceinline__ bool alive(const BeamParams& p, int64_t row) {
-    return !(p.ended && p.ended[row]) && clean(p.scores[row]) != -INFINITY;
 }
 
 // A piece is NV times 16 bytes of every thread.  Pieces and threads go by the token, so that equal rows have equal sums wherever they
 // begin: rows of an odd number of tokens are read from addresses that are multiples of an element's size only.
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4), aligned(2)));
 template <bool BF16, int NV>
-__global__ void __launch_bounds__(kScanThreads)
+__global__ void __launch_bounds__(kScanThreads, 4)
 beam_scan_kernel(BeamParams p) {
-    constexpr int E = BF16 ? 2 : 4, PER = 16 / E, kWaves = kScanThreads / kWave, kMost = kMaxBeams * NV * PER;
-    __shared__ float s_max[kWaves], s_sum[kWaves];
+    constexpr int E = BF16 ? 2 : 4, PER = 16 / E, N = NV * PER, kWaves = kScanThreads / kWave, kPiece = kScanThreads * N;
+    constexpr int kMost = kMaxBeams * N > kWaves * kWaveCandidates ? kMaxBeams * N : kWaves * kWaveCandidates;
+    __shared__ float s_sum[kWaves];
     __shared__ uint32_t s_key[kScanThreads], s_at[kScanThreads];
-    __shared__ uint32_t s_ck[kMost], s_ca[kMost];
-    __shared__ int s_count;
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = tid / kWave;
+    // candidates (two arrays: a store of both together would want every element in a pair of registers)
+    __shared__ float s_v[kMost];
+    __shared__ int s_t[kMost];
+    __shared__ int s_n[kWaves], s_count;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = __builtin_amdgcn_readfirstlane(tid / kWave);
     const DivMod rp = uniform_div_mod((int)blockIdx.x, p.by_pieces);
     const int64_t row = rp.q;
-    if (!alive(p, row)) return;
-    if (tid == 0) s_count = 0;
-
     const unsigned char* base = (const unsigned char*)p.logits + row * p.stride * E;
-    const int first = rp.r * (kScanThreads * NV * PER) + tid * PER;      // token of the thread's first element
-    float x[NV * PER];
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const int t0 = first + k * kScanThreads * PER;
-        const unsigned char* at = base + (int64_t)t0 * E;
-        uint32_t w[4] = {0, 0, 0, 0};
-        if (t0 + PER <= p.V) {
-            const u32x4_t y = *(const u32x4_t*)at;
-            w[0] = y[0]; w[1] = y[1]; w[2] = y[2]; w[3] = y[3];
-        } else {
-#pragma unroll
-            for (int e = 0; e < PER; ++e) {
-                const bool in = t0 + e < p.V;
-                if constexpr (BF16) w[e / 2] |= (in ? (uint32_t)((const uint16_t*)at)[e] : 0xff80u) << (16 * (e % 2));
-                else w[e] = in ? ((const uint32_t*)at)[e] : 0xff800000u;
-            }
-        }
+    const int first = rp.r * kPiece + tid * PER;                         // token of the thread's first element
+    auto token_of = [&](int i) { return first + i / PER * (kScanThreads * PER) + i % PER; };
+    auto load = [&](int t) {
+        if constexpr (BF16) return __uint_as_float((uint32_t)((const uint16_t*)base)[t] << 16);
+        else return ((const float*)base)[t];
+    };
+    // Where a launch is small its latency counts, and the logits are asked for ahead of whether they are needed.
+    const uint8_t over = p.ended ? p.ended[row] : 0;
+    const float score = p.scores[row];
+    auto dead = [&]() { return over != 0 || clean(score) == -INFINITY; };
+    if (NV > 2 && dead()) return;
+    float x[N];
+    auto unpack = [&](int k, const u32x4_t& y) {
 #pragma unroll
         for (int e = 0; e < PER; ++e) {
-            if constexpr (BF16) x[k * PER + e] = clean(__uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16));
-            else x[k * PER + e] = clean(__uint_as_float(w[e]));
+            if constexpr (BF16) x[k * PER + e] = __uint_as_float(e % 2 ? y[e / 2] & 0xffff0000u : y[e / 2] << 16);
+            else x[k * PER + e] = __uint_as_float(y[e]);
+        }
+    };
+    if (rp.r * kPiece + kPiece <= p.V) {                                 // a whole piece
+#pragma unroll
+        for (int k = 0; k < NV; ++k) unpack(k, *(const u32x4_t*)(base + (int64_t)token_of(k * PER) * E));
+    } else {
+        // threads begin at multiples of PER: one of them has the row's last elements
+        const int end = p.V - p.V % PER;
+        const uint32_t none = BF16 ? 0xff80ff80u : 0xff800000u;
+        u32x4_t last = {none, none, none, none};
+#pragma unroll
+        for (int e = 0; e + 1 < PER; ++e)
+            if (end + e < p.V) {
+                if constexpr (BF16) last[e / 2] = (last[e / 2] & (0xffffu << (16 * (1 - e % 2)))) | (uint32_t)((const uint16_t*)base)[end + e] << (16 * (e % 2));
+                else last[e] = ((const uint32_t*)base)[end + e];
+            }
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int t0 = token_of(k * PER);
+            u32x4_t y = {none, none, none, none};
+            if (t0 < end) y = *(const u32x4_t*)(base + (int64_t)t0 * E);
+            else if (t0 == end) y = last;
+            unpack(k, y);
         }
     }
-    // the thread's maximum and where it is first
-    float top = x[0];
-    int at = 0;
+    if (NV <= 2 && dead()) return;
+    // The largest, or NaN if there is one: one look tells whether the wavefront has any value that counts as another.
+    auto largest = [&]() {
+        float v = x[0];
 #pragma unroll
-    for (int i = 1; i < NV * PER; ++i)
-        if (x[i] > top) { top = x[i]; at = i; }
+        for (int i = 1; i < N; ++i) v = __builtin_elementwise_maximum(v, x[i]);
+        return v;
+    };
+    float top = largest();
+    if (__builtin_amdgcn_ballot_w64(!(top <= kLargest)) != 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = clean(x[i]);
+        top = largest();
+    }
     s_key[tid] = key_of(top);
-    auto token_of = [&](int i) { return (uint32_t)(first + i / PER * (kScanThreads * PER) + i % PER); };
-    s_at[tid] = token_of(at);
-    const float wm = wave_max(top);
-    if (lane == 0) s_max[wv] = wm;
     __syncthreads();
-    float m = s_max[0];
+    uint32_t keys[kWaves], most = 0;
 #pragma unroll
-    for (int i = 1; i < kWaves; ++i) m = fmaxf(m, s_max[i]);
-    const float ref = m == -INFINITY ? 0.f : m;
+    for (int i = 0; i < kWaves; ++i) {
+        keys[i] = s_key[i * kWave + lane];
+        most = max(most, keys[i]);
+    }
+    most = wave_max(most);
+    const float m = most == 0 ? -INFINITY : of_key(most);
+
     float part[4] = {0.f, 0.f, 0.f, 0.f};
+    if (fabsf(m) > kWideLogit) {
+        const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
-    for (int i = 0; i < NV * PER; ++i) part[i % 4] += __builtin_amdgcn_exp2f((x[i] - ref) * 1.4426950408889634f);
+        for (int i = 0; i < N; ++i) part[i % 4] += __builtin_amdgcn_exp2f((x[i] - ref) * kLog2e);
+    } else {
+        const float ref = base_of(m);
+#pragma unroll
+        for (int i = 0; i < N; ++i) part[i % 4] += __builtin_amdgcn_exp2f(fmaf(x[i], kLog2e, -ref));
+    }
     float sum = (part[0] + part[1]) + (part[2] + part[3]);
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, kWave);
-    if (lane == 0) s_sum[wv] = sum;
 
-    const Threshold<uint32_t> t = nth_largest(s_key, s_at, kScanThreads, p.W, lane);
-    if (reaches(s_key[tid], s_at[tid], t)) {
+    // Candidates are what reaches the W-th largest of the threads' maxima: few more than W.
+    const uint32_t t = nth_key(keys, p.W, p.W / 2);
+    const float least = of_key(t);
+    int got = 0;                                                         // of the wavefront
 #pragma unroll
-        for (int i = 0; i < NV * PER; ++i) {
-            const uint32_t k = key_of(x[i]), a = token_of(i);
-            if (k != 0 && reaches(k, a, t)) {
-                const int c = atomicAdd(&s_count, 1);
-                s_ck[c] = k;
-                s_ca[c] = a;
+    for (int i = 0; i < N; ++i) {
+        const bool is = x[i] >= least;
+        const unsigned long long who = __builtin_amdgcn_ballot_w64(is);
+        if (who != 0) {
+            const int at = got + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+            if (is && at < kWaveCandidates) {
+                s_v[wv * kWaveCandidates + at] = x[i];
+                s_t[wv * kWaveCandidates + at] = token_of(i);
+            }
+            got += (int)__popcll(who);
+        }
+    }
+    if (lane == 0) { s_sum[wv] = sum; s_n[wv] = got; }
+    __syncthreads();
+    const int64_t list = (row * p.pieces + rp.r) * p.W;
+    int n[kWaves], all = 0;
+    bool many = false;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) { n[i] = s_n[i]; all += n[i]; many = many || n[i] > kWaveCandidates; }
+    auto give = [&](float v, int tk, int r) {
+        if (r < p.W) {
+            p.value[list + r] = v;
+            p.token[list + r] = tk;
+        }
+    };
+    auto before = [&](float v, int tk, int from, int count) {            // candidates that come before
+        int r = 0;
+#pragma unroll 4
+        for (int j = from; j < from + count; ++j) r += (s_v[j] > v) | ((s_v[j] == v) & (s_t[j] < tk));
+        return r;
+    };
+    if (!many && all <= kWave) {
+        // one wavefront has them all
+        if (wv != 0) return;
+        float v = 0.f;
+        int tk = 0, at = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (lane >= at && lane < at + n[w]) {
+                v = s_v[w * kWaveCandidates + lane - at];
+                tk = s_t[w * kWaveCandidates + lane - at];
+            }
+            at += n[w];
+        }
+        const int r = rank_in_wave(all, key_of(v), (uint32_t)tk);
+        if (lane < all) give(v, tk, r);
+    } else if (!many) {
+        // a quarter of the candidates at a time: rank by counting
+        for (int i = lane; i < n[wv]; i += kWave) {
+            const float v = s_v[wv * kWaveCandidates + i];
+            const int tk = s_t[wv * kWaveCandidates + i];
+            int r = 0;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) r += before(v, tk, w * kWaveCandidates, n[w]);
+            give(v, tk, r);
+        }
+    } else {
+        // Many equal logits: of those the lowest tokens, W threads' at most, whose elements are read again.
+        int at = 0;
+#pragma unroll
+        for (int i = N - 1; i >= 0; --i) at = x[i] == top ? i : at;
+        s_at[tid] = (uint32_t)token_of(at);
+        if (tid == 0) s_count = 0;
+        __syncthreads();
+        const Threshold<uint32_t> te = nth_largest(s_key, s_at, kScanThreads, p.W, 0, lane);
+        if (reaches(s_key[tid], s_at[tid], te)) {
+#pragma unroll 4
+            for (int i = 0; i < N; ++i) {
+                const int tk = token_of(i);
+                const float v = tk < p.V ? clean(load(tk)) : -INFINITY;
+                if (v != -INFINITY && reaches(key_of(v), (uint32_t)tk, te)) {
+                    const int at = atomicAdd(&s_count, 1);
+                    s_v[at] = v;
+                    s_t[at] = tk;
+                }
             }
         }
+        __syncthreads();
+        all = s_count;
+        for (int i = tid; i < all; i += kScanThreads) give(s_v[i], s_t[i], before(s_v[i], s_t[i], 0, all));
     }
-    __syncthreads();
-    const int n = s_count;
-    const int64_t list = (row * p.pieces + rp.r) * p.W;
-    for (int i = tid; i < n; i += kScanThreads) {
-        const uint32_t k = s_ck[i], a = s_ca[i];
-        const int r = rank_of(s_ck, s_ca, n, k, a);
-        if (r < p.W) {
-            p.value[list + r] = __uint_as_float((k & 0x80000000u) ? k ^ 0x80000000u : ~k);
-            p.token[list + r] = (int32_t)a;
-        }
-    }
-    for (int i = n + tid; i < p.W; i += kScanThreads) p.token[list + i] = -1;
-    if (tid == 0) {
-        float all = s_sum[0];
-#pragma unroll
-        for (int i = 1; i < kWaves; ++i) all += s_sum[i];
-        p.sums[row * p.pieces + rp.r] = make_float2(m, all);
-    }
+    for (int i = all + tid; i < p.W; i += kScanThreads) p.token[list + i] = -1;
+    if (tid == 0) p.sums[row * p.pieces + rp.r] = make_float2(m, (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]));
 }
 
-__global__ void __launch_bounds__(kJoinThreads)
+// A group of lanes, a power of two of them, has the pieces of a row.
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS)
 beam_join_kernel(BeamParams p) {
-    constexpr int kWaves = kJoinThreads / kWave;
-    __shared__ double s_off[kMaxBeams], s_score[kMaxBeams];
-    __shared__ uint8_t s_ended[kMaxBeams];
-    __shared__ uint64_t s_head[kMaxBeams * kMaxPieces], s_ck[kMaxBeams * kMaxBeams];
-    __shared__ uint32_t s_place[kMaxBeams * kMaxPieces], s_ca[kMaxBeams * kMaxBeams];
-    __shared__ int s_count;
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = tid / kWave, W = p.W, n = W * p.pieces;
+    constexpr int kHeads = (kMaxBeams * kMaxPieces + 1023) / 1024;       // of a thread, at most
+    constexpr int kLists = kMaxBeams * 3 / 2;
+    __shared__ double s_lse[kMaxBeams], s_score[kMaxBeams];
+    __shared__ uint8_t s_kind[kMaxBeams];                                // 0: goes on, 1: has ended, 2: no candidates
+    __shared__ uint64_t s_head[kMaxBeams * kMaxPieces], s_ck[kLists * kMaxBeams];
+    __shared__ uint32_t s_place[kMaxBeams * kMaxPieces], s_ca[kLists * kMaxBeams];
+    __shared__ Threshold<uint64_t> s_t;
+    __shared__ int s_list[kLists], s_lists, s_count;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), W = p.W, n = W * p.pieces;
+    const bool first_wave = tid < kWave;
     const int64_t row0 = (int64_t)blockIdx.x * W;
     if (tid == 0) s_count = 0;
-    for (int w = wv; w < W; w += kWaves) {
-        const double score = (double)clean(p.scores[row0 + w]);
-        const bool over = p.ended && p.ended[row0 + w], live = alive(p, row0 + w);
-        double lse = 0.0;
-        if (live) {
-            float m = -INFINITY;
-            for (int c = lane; c < p.pieces; c += kWave) m = fmaxf(m, p.sums[(row0 + w) * p.pieces + c].x);
-            m = wave_max(m);
-            double z = 0.0;
-            for (int c = lane; c < p.pieces; c += kWave) {
-                const float2 y = p.sums[(row0 + w) * p.pieces + c];
-                if (y.x != -INFINITY) z += (double)y.y * exp((double)y.x - (double)m);
-            }
+    // the lists' first entries are asked for ahead of the sums (those of rows that are not looked at hold anything)
+    float hv[kHeads];
+    int32_t ht[kHeads];
 #pragma unroll
-            for (int d = 32; d > 0; d >>= 1) z += __shfl_xor(z, d, kWave);
-            lse = (double)m + log(z);
-        }
-        if (lane == 0) {
-            s_off[w] = lse;
+    for (int i = 0; i < kHeads; ++i) {
+        const int64_t at = (row0 * p.pieces + min(tid + i * THREADS, n - 1)) * W;
+        hv[i] = p.value[at];
+        ht[i] = p.token[at];
+    }
+    const int c = tid & (p.group - 1);
+    for (int w = tid / p.group; w < W; w += THREADS / p.group) {         // (a wavefront's lanes leave the loop together or by groups)
+        const double score = (double)clean(p.scores[row0 + w]);
+        const bool over = p.ended && p.ended[row0 + w], live = !over && score != -(double)INFINITY;
+        float2 y = make_float2(-INFINITY, 0.f);
+        if (live && c < p.pieces) y = p.sums[(row0 + w) * p.pieces + c];
+        float m = y.x;                                                   // (a row without candidates: its log-sum-exp is not used)
+        for (int d = p.group / 2; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, kWave));
+        double z = y.x != -INFINITY ? (double)y.y * exp(base_log(y.x) - (double)m) : 0.0;
+        for (int d = p.group / 2; d > 0; d >>= 1) z += __shfl_xor(z, d, kWave);
+        if (c == 0) {
+            s_lse[w] = live ? (double)m + log(z) : 0.0;
             s_score[w] = score;
-            s_ended[w] = over ? 1 : live ? 0 : 2;                        // 2: no candidates
+            s_kind[w] = over ? 1 : live ? 0 : 2;
         }
     }
     __syncthreads();
-    auto key = [&](int w, float x) { return key_of(((double)x - s_off[w]) + s_score[w]); };
-    const uint32_t end = (uint32_t)max(p.end_token, 0);
-    for (int i = tid; i < n; i += kJoinThreads) {
-        const int w = i / p.pieces, c = i - w * p.pieces;
+    auto key = [&](int w, float x) { return key_of(((double)x - s_lse[w]) + s_score[w]); };
+    auto place = [&](int w, int v) { return (uint32_t)w * (uint32_t)p.V + (uint32_t)v; };
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i) {
+        const int l = tid + i * THREADS;
+        if (l >= n) break;
+        const DivMod wc = div_mod(l, p.by_pieces);
+        const int w = wc.q;
         uint64_t k = 0;
         uint32_t a = 0;
-        if (s_ended[w] == 0) {
-            const int64_t list = ((row0 + w) * p.pieces + c) * W;
-            const int32_t t = p.token[list];
-            if (t >= 0) { k = key(w, p.value[list]); a = (uint32_t)w * (uint32_t)p.V + (uint32_t)t; }
-        } else if (s_ended[w] == 1 && c == 0) {
+        if (s_kind[w] == 0 && ht[i] >= 0) {
+            k = key(w, hv[i]);
+            a = place(w, ht[i]);
+        } else if (s_kind[w] == 1 && wc.r == 0) {
             k = key_of(s_score[w]);
-            a = (uint32_t)w * (uint32_t)p.V + end;
+            a = place(w, max(p.end_token, 0));
         }
-        s_head[i] = k;
-        s_place[i] = a;
+        s_head[l] = k;
+        s_place[l] = a;
     }
     __syncthreads();
-    const Threshold<uint64_t> t = nth_largest(s_head, s_place, n, W, lane);
-    // (at most W lists have a first entry that reaches it, of W entries each)
-    for (int i = tid; i < n * W; i += kJoinThreads) {
-        const int l = i / W, e = i - l * W;
-        if (s_head[l] == 0 || !reaches(s_head[l], s_place[l], t)) continue;
-        const int w = l / p.pieces;
+    if (first_wave) {
+        const Threshold<uint64_t> t = nth_largest(s_head, s_place, n, W, W / 2, lane);
+        int got = 0;                                                     // W + W/2 lists at most
+        for (int i = 0; i < n; i += kWave) {
+            const int l = min(i + lane, n - 1);
+            const bool is = i + lane < n && s_head[l] != 0 && reaches(s_head[l], s_place[l], t);
+            const unsigned long long who = __builtin_amdgcn_ballot_w64(is);
+            if (is) s_list[got + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = l;
+            got += (int)__popcll(who);
+        }
+        if (lane == 0) { s_t = t; s_lists = got; }
+    }
+    __syncthreads();
+    const Threshold<uint64_t> t = s_t;
+    const int all = s_lists * W;
+    for (int i = tid; i < all; i += THREADS) {
+        const DivMod le = div_mod(i, p.by_w);
+        const int l = s_list[le.q], w = div_mod(l, p.by_pieces).q;
         uint64_t k = s_head[l];
         uint32_t a = s_place[l];
-        if (e > 0) {
-            if (s_ended[w] != 0) continue;
-            const int64_t at = ((row0 + w) * p.pieces + (l - w * p.pieces)) * W + e;
-            const int32_t tk = p.token[at];
-            if (tk < 0) continue;
-            k = key(w, p.value[at]);
-            a = (uint32_t)w * (uint32_t)p.V + (uint32_t)tk;
+        if (le.r > 0) {
+            if (s_kind[w] != 0) continue;
+            const int64_t at = (row0 * p.pieces + l) * W + le.r;
+            const int32_t v = p.token[at];
+            const float x = p.value[at];
+            if (v < 0) continue;
+            k = key(w, x);
+            a = place(w, v);
             if (k == 0 || !reaches(k, a, t)) continue;
         }
-        const int c = atomicAdd(&s_count, 1);
-        s_ck[c] = k;
-        s_ca[c] = a;
+        const int at = atomicAdd(&s_count, 1);
+        s_ck[at] = k;
+        s_ca[at] = a;
     }
     __syncthreads();
     const int found = s_count;
-    for (int i = tid; i < found; i += kJoinThreads) {
-        const uint64_t k = s_ck[i];
-        const uint32_t a = s_ca[i];
-        const int r = rank_of(s_ck, s_ca, found, k, a);
-        if (r >= W) continue;
+    auto give = [&](uint64_t k, uint32_t a, int r) {
+        if (r >= W) return;
         const int w = (int)(a / (uint32_t)p.V), v = (int)(a - (uint32_t)w * (uint32_t)p.V);
-        const bool over = s_ended[w] == 1;
+        const bool over = s_kind[w] == 1;
         p.tokens[row0 + r] = over ? p.end_token : v;
         p.parents[row0 + r] = w;
         const uint64_t u = (k >> 63) ? k ^ (1ull << 63) : ~k;
         p.scores_out[row0 + r] = (float)__longlong_as_double((long long)u);
         if (p.ended_out) p.ended_out[row0 + r] = over || v == p.end_token;
+    };
+    if (found <= kWave) {
+        if (!first_wave) return;
+        const uint64_t k = lane < found ? s_ck[lane] : 0;
+        const uint32_t a = lane < found ? s_ca[lane] : 0;
+        const int r = rank_in_wave(found, k, a);
+        if (lane < found) give(k, a, r);
+    } else {
+        for (int i = tid; i < found; i += THREADS) give(s_ck[i], s_ca[i], rank_of(s_ck, s_ca, found, s_ck[i], s_ca[i]));
     }
-    for (int i = found + tid; i < W; i += kJoinThreads) {                // fewer continuations than beams
+    for (int i = found + tid; i < W; i += THREADS) {                     // fewer continuations than beams (and than lanes)
         p.tokens[row0 + i] = p.parents[row0 + i] = -1;
         p.scores_out[row0 + i] = -INFINITY;
         if (p.ended_out) p.ended_out[row0 + i] = 0;
     }
 }
 
-// Bytes of a piece over 4096
-static int piece_vectors(int rows, int V, int esize) {
-    for (int nv : {16, 8, 4})
-        if ((int64_t)rows * V * esize >= (int64_t)nv * 4096 * 4 * compute_units()) return nv;
-    return 2;
-}
-static int piece_count(int V, int esize, int nv) { return (int)(((int64_t)V * esize + nv * 4096 - 1) / (nv * 4096)); }
+// A piece is nv * 4096 bytes: 64 elements of a thread at most, which are registers, fewer where the launch would have less than four
+// workgroups for each compute unit.
 struct Pieces { int nv, count; };
 static Pieces pieces_of(int rows, int V, int esize) {
-    int nv = piece_vectors(rows, V, esize);
-    while (piece_count(V, esize, nv) > kMaxPieces) nv *= 2;             // (16 always serves: kMaxV)
-    return {nv, piece_count(V, esize, nv)};
+    const int most = esize == 4 ? 16 : 8;
+    int nv = most;
+    while (nv > 2 && (int64_t)rows * V * esize < (int64_t)nv * 4096 * 4 * compute_units()) nv /= 2;
+    auto count = [&]() { return (int)(((int64_t)V * esize + nv * 4096 - 1) / (nv * 4096)); };
+    while (count() > kMaxPieces) nv *= 2;                               // (not beyond `most`: kMaxV)
+    return {nv, count()};
 }
 
 bool beam_fits(int S, int W, int V, int esize) { return (int64_t)S * W * pieces_of(S * W, V, esize).count < 1 << 24; }
@@ -334,7 +510,9 @@ hipError_t launch_beam(int S, int W, int V, bool bf16, const void* logits, int64
     BeamParams p;
     p.S = S; p.W = W; p.V = V; p.pieces = pc.count; p.stride = stride;
     p.logits = logits; p.scores = scores; p.ended = ended; p.end_token = end_token;
-    p.by_pieces = fast_div(pc.count);
+    p.by_pieces = fast_div(pc.count); p.by_w = fast_div(W);
+    p.group = 1;
+    while (p.group < pc.count) p.group *= 2;
     p.tokens = tokens; p.parents = parents; p.scores_out = scores_out; p.ended_out = ended_out;
     const int64_t lists = (int64_t)S * W * pc.count;
     p.sums = (float2*)ws;
@@ -342,10 +520,11 @@ hipError_t launch_beam(int S, int W, int V, bool bf16, const void* logits, int64
     p.token = (int32_t*)(p.value + lists * W);
     const dim3 grid((unsigned)lists), block(kScanThreads);
 #define SCAN(NV) (bf16 ? beam_scan_kernel<true, NV> : beam_scan_kernel<false, NV>)
-    auto* scan = pc.nv == 2 ? SCAN(2) : pc.nv == 4 ? SCAN(4) : pc.nv == 8 ? SCAN(8) : SCAN(16);
+    auto* scan = pc.nv == 2 ? SCAN(2) : pc.nv == 4 ? SCAN(4) : pc.nv == 8 ? SCAN(8) : beam_scan_kernel<false, 16>;
 #undef SCAN
     hipLaunchKernelGGL(scan, grid, block, 0, st, p);
-    hipLaunchKernelGGL(beam_join_kernel, dim3((unsigned)S), dim3(kJoinThreads), 0, st, p);
+    if (W <= 4) hipLaunchKernelGGL(beam_join_kernel<256>, dim3((unsigned)S), dim3(256), 0, st, p);
+    else hipLaunchKernelGGL(beam_join_kernel<1024>, dim3((unsigned)S), dim3(1024), 0, st, p);
     return hipGetLastError();
 }
 

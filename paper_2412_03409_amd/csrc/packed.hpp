@@ -9,7 +9,7 @@ constexpr int kMaxS = 4096;        // sequences of a packed call
 constexpr int kMaxT = 1 << 22;     // rows of a packed call
 constexpr int kMaxBeams = 32;      // of a prompt
 constexpr int kMaxPieces = 64;     // of a row of logits
-constexpr int kMaxV = 1 << 20;     // tokens: 64 pieces of 64 KB
+constexpr int kMaxV = 1 << 20;     // tokens: 64 pieces of 16384
 
 hipError_t launch_compact_paged(const pkv_shape& s, const void* k, Strides ks, const void* v, Strides vs, const int32_t* order,
                                 const int32_t* lengths, const pkv_paging& g, int l0, const int32_t* table, void* kp, void* vp,

@@ -42,10 +42,15 @@ struct ReorderParams {
     int32_t *table_out, *lens_out, *state_out;
     unsigned char *kp, *vp;
     int32_t* status;
-    int4* head;                         // workspace: {head, count, taken, given} (the latter two: of all segments), {accepted, status, 0, 0}
-    int4* rec;                          // workspace [n]: {taken (-1: a number that cannot be), given, page to copy from, rows}
-    int2* first;                        // workspace [n]: sums of both over the segments before
+    // workspace, in whole fours of segments
+    int4* head;                         // {head, count, taken, given} (the latter two of all segments), {status, 0, 0, 0}
+    int4* quarters;                     // pages that the wavefronts' columns of a segment give back
+    int4* given;                        // their sums, four segments
+    uint32_t* flags;                    // of four segments, a byte each: kTakes, kWrong
+    int2* from;                         // where kTakes: the page to copy from, rows
+    int2* first;                        // pages taken and given back by the segments before (reorder_sums_kernel)
 };
+constexpr uint32_t kTakes = 1, kWrong = 2;
 
 // What a lane knows of its place: in every column the same.
 struct Place {
@@ -118,31 +123,38 @@ __device__ __forceinline__ int count_given(const ReorderParams& p, const Place& 
 
 __global__ void __launch_bounds__(kReorderThreads)
 reorder_count_kernel(ReorderParams p) {
-    __shared__ int s_given[kReorderWaves][kMaxBeams];
+    __shared__ __attribute__((aligned(16))) int s_given[kMaxBeams][kReorderWaves];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = tid / kWave;
     const DivMod gl = uniform_div_mod((int)blockIdx.x, p.by_layers);
     const int g = gl.q, l = gl.r;
-    if (blockIdx.x == 0 && tid == 0) p.head[0] = make_int4(p.state[0], p.state[1], 0, 0);
+    if (blockIdx.x == 0) {
+        if (tid == 0) p.head[0] = make_int4(p.state[0], p.state[1], 0, 0);
+        if (tid >= p.n % 4 && tid < 4 && p.n % 4 != 0) {            // the last four's places behind the end
+            ((uint8_t*)p.flags)[p.n - p.n % 4 + tid] = 0;
+            ((int*)p.given)[p.n - p.n % 4 + tid] = 0;
+        }
+    }
     Place x;
     const bool ok = look(p, g, l, lane, x);
     if (ok) {
         const int given = count_given(p, x, l, lane, columns_of(p, x, wv));
-        if (x.real && x.col == 0) s_given[wv][x.w] = given;
+        if (x.real && x.col == 0) s_given[x.w][wv] = given;
     }
     __syncthreads();
     if (wv != 0 || !x.real || x.col != 0) return;
-    int4 r = make_int4(-1, 0, -1, 0);
+    const int64_t seg = (int64_t)x.s * p.layers + l;
+    uint32_t flags = kWrong;
+    int4 q = make_int4(0, 0, 0, 0);
     if (ok) {
-        r.y = 0;
-#pragma unroll
-        for (int i = 0; i < kReorderWaves; ++i) r.y += s_given[i][x.w];
-        r.x = copies(p, x) ? 1 : 0;
-        if (r.x) {
-            r.z = p.table[((int64_t)(g * p.W + x.parent) * p.layers + l) * p.max_pages + (x.new_len >> p.shift)];
-            r.w = x.new_len & ((1 << p.shift) - 1);
-        }
+        q = *(const int4*)s_given[x.w];
+        flags = copies(p, x) ? kTakes : 0;
+        if (flags)
+            p.from[seg] = make_int2(p.table[((int64_t)(g * p.W + x.parent) * p.layers + l) * p.max_pages + (x.new_len >> p.shift)],
+                                    x.new_len & ((1 << p.shift) - 1));
     }
-    p.rec[(int64_t)x.s * p.layers + l] = r;
+    ((uint8_t*)p.flags)[seg] = (uint8_t)flags;
+    ((int*)p.given)[seg] = q.x + q.y + q.z + q.w;
+    p.quarters[seg] = q;
 }
 
 struct Sums { int bad, taken, given; };
@@ -152,6 +164,16 @@ __device__ __forceinline__ int verdict(const ReorderParams& p, const int4& hd, c
     return all.taken > hd.y ? PKV_PAGES_SHORT : 0;
 }
 
+__device__ __forceinline__ int2 scanned(int2 x, int lane) {
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        const int ux = __shfl_up(x.x, d, kWave), uy = __shfl_up(x.y, d, kWave);
+        if (lane >= d) { x.x += ux; x.y += uy; }
+    }
+    return x;
+}
+__device__ __forceinline__ int2 of_four(uint32_t f, const int4& g) { return make_int2(__popc(f & 0x01010101u), g.x + g.y + g.z + g.w); }
+
 __global__ void __launch_bounds__(kSumThreads)
 reorder_sums_kernel(ReorderParams p) {
     __shared__ int2 s_sum[kSumThreads / kWave];
@@ -159,22 +181,15 @@ reorder_sums_kernel(ReorderParams p) {
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = tid / kWave;
     if (tid == 0) s_bad = 0;
     int2 carry = make_int2(0, 0);
-    bool bad = false;
-    for (int base = 0; base < p.n; base += kSumThreads) {
-        const int i = base + tid;
-        int2 mine = make_int2(0, 0);
-        if (i < p.n) {
-            const int4 r = p.rec[i];
-            bad = bad || r.x < 0;
-            mine = make_int2(max(r.x, 0), r.y);
-        }
-        int2 incl = mine;
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) {
-            const int ux = __shfl_up(incl.x, d, kWave), uy = __shfl_up(incl.y, d, kWave);
-            if (lane >= d) { incl.x += ux; incl.y += uy; }
-        }
-        __syncthreads();                                        // (the round before has read its sums)
+    uint32_t bad = 0;
+    for (int base = 0; base < p.n; base += 4 * kSumThreads) {
+        const int i = base + 4 * tid;
+        uint32_t f = 0;
+        int4 g = make_int4(0, 0, 0, 0);
+        if (i < p.n) { f = p.flags[i / 4]; g = p.given[i / 4]; }
+        bad |= f & (0x01010101u * kWrong);
+        const int2 mine = of_four(f, g), incl = scanned(mine, lane);
+        __syncthreads();                                            // (the round before has read its sums)
         if (lane == kWave - 1) s_sum[wv] = incl;
         __syncthreads();
         int2 before = make_int2(carry.x + incl.x - mine.x, carry.y + incl.y - mine.y);
@@ -183,7 +198,13 @@ reorder_sums_kernel(ReorderParams p) {
             if (w < wv) { before.x += y.x; before.y += y.y; }
             carry.x += y.x; carry.y += y.y;
         }
-        if (i < p.n) p.first[i] = before;
+        const int ge[4] = {g.x, g.y, g.z, g.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (i + e < p.n) p.first[i + e] = before;
+            before.x += (f >> (8 * e)) & 1u;
+            before.y += ge[e];
+        }
     }
     if (bad) s_bad = 1;
     __syncthreads();
@@ -199,80 +220,77 @@ reorder_sums_kernel(ReorderParams p) {
 template <bool OWN>
 __global__ void __launch_bounds__(kReorderThreads)
 reorder_apply_kernel(ReorderParams p) {
-    __shared__ int s_row[kMaxBeams][2], s_part[kMaxBeams][2];       // a place's layers, those in front of this one
-    __shared__ int s_sum[5], s_given[kReorderWaves][kMaxBeams];
+    __shared__ int2 s_sum[kReorderWaves], s_before[kMaxBeams];
+    __shared__ uint32_t s_bad[kReorderWaves];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = tid / kWave;
     const bool tables = (int)blockIdx.x < p.units;
-    int g, l, seg = 0, split = 0;
-    int4 r = make_int4(0, 0, -1, 0);
+    int g = 0, l = 0, seg = 0, split = 0;
+    int2 from = make_int2(-1, 0);
+    const int4 hd = p.head[0];
+    Place x;
+    bool known = true;
     if (tables) {
         const DivMod gl = uniform_div_mod((int)blockIdx.x, p.by_layers);
         g = gl.q; l = gl.r;
+        known = look(p, g, l, lane, x);
     } else {
         const DivMod ss = uniform_div_mod((int)blockIdx.x - p.units, p.by_splits);
         seg = ss.q; split = ss.r;
-        r = p.rec[seg];
-        if (r.x <= 0) return;                                       // nothing to copy
-        const DivMod sl = uniform_div_mod(seg, p.by_layers);
-        g = sl.q / p.W; l = sl.r;
+        const uint8_t flags = ((const uint8_t*)p.flags)[seg];
+        from = p.from[seg];
+        if (!(flags & kTakes)) return;                              // nothing to copy
     }
-    const int4 hd = p.head[0];
     Sums all;
-    int2 before = make_int2(0, 0);                                  // of this place's segment (tables: of lane's)
+    int2 before;                                                    // of this segment (tables: of the lane's)
     int status;
-    const int w = tables ? lane & (p.lanes - 1) : seg / p.layers - g * p.W;
     if constexpr (OWN) {
-        for (int i = tid; i < kMaxBeams * 2; i += kReorderThreads) { (&s_row[0][0])[i] = 0; (&s_part[0][0])[i] = 0; }
-        if (tid < 5) s_sum[tid] = 0;
-        __syncthreads();
-        const int from = g * p.W * p.layers, to = from + p.W * p.layers;
-        int bad = 0, tx = 0, ty = 0, bx = 0, by = 0;
-        for (int i = tid; i < p.n; i += kReorderThreads) {
-            const int2 y = *(const int2*)(p.rec + i);
-            const int taken = max(y.x, 0);
-            bad |= y.x < 0;
-            tx += taken; ty += y.y;
-            if (i < from) { bx += taken; by += y.y; }
-            else if (i < to && (taken | y.y) != 0) {
-                const DivMod sl = div_mod(i - from, p.by_layers);
-                atomicAdd(&s_row[sl.q][0], taken);
-                atomicAdd(&s_row[sl.q][1], y.y);
-                if (sl.r < l) { atomicAdd(&s_part[sl.q][0], taken); atomicAdd(&s_part[sl.q][1], y.y); }
-            }
+        const int per = (p.n + 4 * kReorderThreads - 1) / (4 * kReorderThreads) * 4, i0 = tid * per;      // segments of a thread
+        int2 mine = make_int2(0, 0);
+        uint32_t bad = 0;
+        for (int i = i0; i < min(i0 + per, p.n); i += 4) {
+            const uint32_t f = p.flags[i / 4];
+            const int2 y = of_four(f, p.given[i / 4]);
+            bad |= f & (0x01010101u * kWrong);
+            mine.x += y.x; mine.y += y.y;
         }
+        const int2 incl = scanned(mine, lane);
+        const bool wrong = __builtin_amdgcn_ballot_w64(bad != 0) != 0;
+        if (lane == kWave - 1) { s_sum[wv] = incl; s_bad[wv] = wrong; }
+        __syncthreads();
+        int2 start = make_int2(incl.x - mine.x, incl.y - mine.y);
+        all = Sums{0, 0, 0};
 #pragma unroll
-        for (int d = 32; d > 0; d >>= 1) {
-            bad |= __shfl_xor(bad, d, kWave);
-            tx += __shfl_xor(tx, d, kWave); ty += __shfl_xor(ty, d, kWave);
-            bx += __shfl_xor(bx, d, kWave); by += __shfl_xor(by, d, kWave);
+        for (int w = 0; w < kReorderWaves; ++w) {
+            const int2 y = s_sum[w];
+            if (w < wv) { start.x += y.x; start.y += y.y; }
+            all.taken += y.x; all.given += y.y; all.bad |= (int)s_bad[w];
         }
-        if (lane == 0) {
-            if (bad) atomicOr(&s_sum[0], 1);
-            atomicAdd(&s_sum[1], tx); atomicAdd(&s_sum[2], ty);
-            atomicAdd(&s_sum[3], bx); atomicAdd(&s_sum[4], by);
+        for (int w = 0; w < (tables ? p.W : 1); ++w) {
+            const int at = tables ? (g * p.W + w) * p.layers + l : seg;
+            if (at < i0 || at >= i0 + per) continue;
+            int2 y = start;
+            for (int i = i0; i < at; ++i) { y.x += ((const uint8_t*)p.flags)[i] & kTakes; y.y += ((const int*)p.given)[i]; }
+            s_before[w] = y;
         }
         __syncthreads();
-        all = Sums{s_sum[0], s_sum[1], s_sum[2]};
-        before = make_int2(s_sum[3], s_sum[4]);
-        for (int i = 0; i < min(w, p.W); ++i) { before.x += s_row[i][0]; before.y += s_row[i][1]; }
-        if (w < p.W) { before.x += s_part[w][0]; before.y += s_part[w][1]; }
+        before = s_before[tables ? min(x.w, p.W - 1) : 0];
         status = verdict(p, hd, all);
     } else {
         all = Sums{0, hd.z, hd.w};
         status = p.head[1].x;
-        before = p.first[tables ? (int64_t)(g * p.W + min(w, p.W - 1)) * p.layers + l : seg];
+        before = p.first[tables ? (int64_t)x.s * p.layers + l : seg];
     }
 
     if (!tables) {
         if (status != 0) return;
         const int dst = p.ring[ring_place((uint32_t)hd.x + (uint32_t)before.x, p.num_pages)];
-        if ((uint32_t)dst >= (uint32_t)p.num_pages || (uint32_t)r.z >= (uint32_t)p.num_pages) return;
+        if ((uint32_t)dst >= (uint32_t)p.num_pages || (uint32_t)from.x >= (uint32_t)p.num_pages) return;
         // the used rows of a head lie together: heads h0 ... h1-1, pieces of 16 bytes
         const int h0 = split * p.heads_per, heads = min(p.Hkv - h0, p.heads_per);
-        const uint32_t pieces = (uint32_t)r.w << p.row_shift;       // (above 1)
-        const FastDiv by_pieces = {pieces, (uint32_t)((1ull << 32) / pieces)};
+        const uint32_t pieces = (uint32_t)from.y << p.row_shift;
+        const FastDiv by_pieces = {pieces, 0xffffffffu / pieces};   // (one less than it could be for powers of two: corrected by div_mod)
         const int64_t page = (int64_t)p.row_bytes << p.shift;       // of one head
-        const int64_t src = ((int64_t)r.z * p.Hkv + h0) * page, to = ((int64_t)dst * p.Hkv + h0) * page;
+        const int64_t src = ((int64_t)from.x * p.Hkv + h0) * page, to = ((int64_t)dst * p.Hkv + h0) * page;
         const int all_pieces = heads * (int)pieces;
         constexpr int U = 4;                                        // in flight, of both tensors
         for (int i0 = tid; i0 < all_pieces; i0 += U * kReorderThreads) {
@@ -300,7 +318,7 @@ reorder_apply_kernel(ReorderParams p) {
         p.state_out[1] = status ? hd.y : hd.y - all.taken + all.given;
         *p.status = status;
     }
-    if (status != 0) {
+    if (status != 0 || !known) {
         // everything stays: outputs of their own get what there was
         for (int i = wv; i < p.W; i += kReorderWaves) {
             const int64_t row = (int64_t)(g * p.W + i) * p.layers + l;
@@ -311,21 +329,16 @@ reorder_apply_kernel(ReorderParams p) {
         }
         return;
     }
-    Place x;
-    look(p, g, l, lane, x);
-    const Range range = columns_of(p, x, wv);
-    const int mine = count_given(p, x, l, lane, range);
-    if (x.real && x.col == 0) s_given[wv][x.w] = mine;
-    __syncthreads();                                                // (all four have read the lengths)
-    if (wv == 0 && x.real && x.col == 0) p.lens_out[(int64_t)x.s * p.layers + l] = x.new_len;
-    int to = before.y;
-    for (int i = 0; i < wv; ++i) to += s_given[i][min(x.w, p.W - 1)];
+    const int4 q = p.quarters[(int64_t)x.s * p.layers + l];
     const bool copied = copies(p, x);
     const int fresh = copied && x.real ? p.ring[ring_place((uint32_t)hd.x + (uint32_t)before.x, p.num_pages)] : -1;
-    unsigned long long lower = 0;                                   // lanes of the place in the columns before
-    for (int c = 0; c < x.col; ++c) lower |= 1ull << (x.w + c * p.lanes);
-    unsigned long long same = 0;
+    const Range range = columns_of(p, x, wv);
+    if constexpr (!OWN) __syncthreads();                            // (all four have read the lengths)
+    if (wv == 0 && x.real && x.col == 0) p.lens_out[(int64_t)x.s * p.layers + l] = x.new_len;
+    int to = before.y + (wv > 0 ? q.x : 0) + (wv > 1 ? q.y : 0) + (wv > 2 ? q.z : 0);
+    unsigned long long same = 0;                                    // lanes of the place
     for (int c = 0; c < kWave / p.lanes; ++c) same |= 1ull << (x.w + c * p.lanes);
+    const unsigned long long lower = same & ((1ull << lane) - 1);   // in the columns before
     int32_t* row = p.table_out + ((int64_t)x.s * p.layers + l) * p.max_pages;
     for (int j0 = range.begin; j0 < range.end; j0 += range.step) {
         const int j = j0 + x.col;
@@ -351,7 +364,8 @@ bool reorder_fits(int S, int W, int Hkv, int row_bytes, const pkv_paging& g) {
     return (int64_t)S / W * g.layers + (int64_t)S * g.layers * ((Hkv + per - 1) / per) < 1 << 24;
 }
 
-size_t reorder_ws_bytes(int S, int layers) { return 256 + (size_t)S * layers * (sizeof(int4) + sizeof(int2)); }
+static size_t in_fours(int S, int layers) { return ((size_t)S * layers + 3) / 4 * 4; }
+size_t reorder_ws_bytes(int S, int layers) { return 256 + in_fours(S, layers) * (sizeof(int4) + sizeof(int) + 1 + 2 * sizeof(int2)); }
 
 hipError_t launch_reorder(int S, int W, int Hkv, int row_bytes, const pkv_paging& g, const int32_t* parents, const int32_t* table,
                           const int32_t* lens, int32_t* ring, const int32_t* state, int32_t* table_out, int32_t* lens_out,
@@ -370,7 +384,13 @@ hipError_t launch_reorder(int S, int W, int Hkv, int row_bytes, const pkv_paging
     p.parents = parents; p.table = table; p.lens = lens; p.ring = ring; p.state = state;
     p.table_out = table_out; p.lens_out = lens_out; p.state_out = state_out;
     p.kp = (unsigned char*)kp; p.vp = (unsigned char*)vp; p.status = status;
-    p.head = (int4*)ws; p.rec = (int4*)((char*)ws + 256); p.first = (int2*)(p.rec + p.n);
+    const size_t n4 = in_fours(S, g.layers);
+    p.head = (int4*)ws;
+    p.quarters = (int4*)((char*)ws + 256);
+    p.given = p.quarters + n4;
+    p.from = (int2*)(p.given + n4 / 4);
+    p.first = p.from + n4;
+    p.flags = (uint32_t*)(p.first + n4);
     // (a single place has nobody to share with: nothing is copied)
     const dim3 grid((unsigned)(p.units + (W > 1 ? p.n * p.splits : 0)));
     hipLaunchKernelGGL(reorder_count_kernel, dim3((unsigned)p.units), dim3(kReorderThreads), 0, st, p);

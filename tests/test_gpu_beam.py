@@ -115,6 +115,23 @@ def test_select_values_at_the_ends():
     assert got[1][4, 0] == 3 and not bool(torch.isnan(got[2]).any())
 
 
+@pytest.mark.parametrize("V", [50, 4096, 5001])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_select_every_kind_of_nan_is_no_candidate(V, dtype):
+    """Quiet and signalling, of both signs, in logits and scores."""
+    x, _, _ = select_inputs(V, 1, 3, V, dtype)
+    bits = x.view(torch.int16 if dtype == BF16 else torch.int32)
+    quiet, sign = ((0x7fc0, 1 << 15) if dtype == BF16 else (0x7fc00000, 1 << 31))
+    inf = 0x7f80 if dtype == BF16 else 0x7f800000
+    for i, b in enumerate((inf + 1, quiet, inf + 1 - sign, quiet - sign, inf + 5)):
+        bits[0, :, 3 + 7 * i] = b
+    assert int(torch.isnan(x[0, 0]).sum()) >= 5
+    scores = torch.tensor([[-3.0, -3.5, -4.0]])
+    check_select(x, scores, None, None, P.prefixkv_beam_select(x.to(DEV), scores.to(DEV)))
+    scores.view(torch.int32)[0, 1] = 0x7f800001
+    check_select(x, scores, None, None, P.prefixkv_beam_select(x.to(DEV), scores.to(DEV)))
+
+
 def test_select_is_repeatable_and_replays_from_a_graph():
     S, W, V, end = 5, 4, 20011, 3
     x, scores, ended = (t.to(DEV) for t in select_inputs(8, S, W, V, BF16, end))
