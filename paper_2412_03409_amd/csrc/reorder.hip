@@ -51,6 +51,7 @@ struct ReorderParams {
     int2* first;                        // pages taken and given back by the segments before (reorder_sums_kernel)
 };
 constexpr uint32_t kTakes = 1, kWrong = 2;
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 // What a lane knows of its place: in every column the same.
 struct Place {
@@ -294,21 +295,20 @@ reorder_apply_kernel(ReorderParams p) {
         const int all_pieces = heads * (int)pieces;
         constexpr int U = 4;                                        // in flight, of both tensors
         for (int i0 = tid; i0 < all_pieces; i0 += U * kReorderThreads) {
-            uint4 k[U], v[U];
+            u32x4_t k[U], v[U];
             int64_t off[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const DivMod x = div_mod(min(i0 + u * kReorderThreads, all_pieces - 1), by_pieces);
                 off[u] = x.q * page + 16 * (int64_t)x.r;
-                k[u] = *(const uint4*)(p.kp + src + off[u]);
-                v[u] = *(const uint4*)(p.vp + src + off[u]);
+                k[u] = *(const u32x4_t*)(p.kp + src + off[u]);
+                v[u] = *(const u32x4_t*)(p.vp + src + off[u]);
             }
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (i0 + u * kReorderThreads < all_pieces) {
-                    *(uint4*)(p.kp + to + off[u]) = k[u];
-                    *(uint4*)(p.vp + to + off[u]) = v[u];
-                }
+            for (int u = 0; u < U; ++u) {                           // (the last piece more than once)
+                *(u32x4_t*)(p.kp + to + off[u]) = k[u];
+                *(u32x4_t*)(p.vp + to + off[u]) = v[u];
+            }
         }
         return;
     }
