@@ -125,6 +125,17 @@ __device__ __forceinline__ Threshold<K> nth_largest(const K* key, const uint32_t
         K k[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) k[i] = i * kWave + lane < n ? key[i * kWave + lane] : 0;
+        if constexpr (sizeof(K) == 8) {
+            // the upper halves will mostly do
+            uint32_t u[4];
+            int c = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u[i] = (uint32_t)(k[i] >> 32);
+            const uint32_t h = nth_key(u, W, slack);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c += __popcll(__builtin_amdgcn_ballot_w64(u[i] >= h));
+            if (c <= W + slack) return {(K)h << 32, ~0u};
+        }
         t = nth_key(k, W, slack);
     } else {
         K lo = ~(K)0, hi = 0;
@@ -157,19 +168,6 @@ __device__ __forceinline__ int rank_in_wave(int n, K key, uint32_t place) {
     }
     return r;
 }
-// how many of the n candidates come before {key, place}
-template <class K>
-__device__ __forceinline__ int rank_of(const K* keys, const uint32_t* places, int n, K key, uint32_t place) {
-    int r = 0;
-#pragma unroll 8
-    for (int i = 0; i < n; ++i) {
-        const K k = keys[i];
-        const uint32_t a = places[i];
-        r += (k > key) | ((k == key) & (a < place));
-    }
-    return r;
-}
-
 // A piece is NV times 16 bytes of every thread.  Pieces and threads go by the token, so that equal rows have equal sums wherever they
 // begin: rows of an odd number of tokens are read from addresses that are multiples of an element's size only.
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4), aligned(2)));
@@ -475,7 +473,19 @@ beam_join_kernel(BeamParams p) {
         const int r = rank_in_wave(found, k, a);
         if (lane < found) give(k, a, r);
     } else {
-        for (int i = tid; i < found; i += THREADS) give(s_ck[i], s_ca[i], rank_of(s_ck, s_ca, found, s_ck[i], s_ca[i]));
+        // as many lanes as there are have a candidate, up to eight
+        int g = 8;
+        while (g > 1 && found * g > THREADS) g /= 2;
+        for (int i0 = 0; i0 < found; i0 += THREADS / g) {
+            const int i = i0 + tid / g;
+            const uint64_t k = s_ck[min(i, found - 1)];
+            const uint32_t a = s_ca[min(i, found - 1)];
+            int r = 0;
+#pragma unroll 4
+            for (int j = tid & (g - 1); j < found; j += g) r += (s_ck[j] > k) | ((s_ck[j] == k) & (s_ca[j] < a));
+            for (int d = 1; d < g; d <<= 1) r += __shfl_xor(r, d, kWave);
+            if ((tid & (g - 1)) == 0 && i < found) give(k, a, r);
+        }
     }
     for (int i = found + tid; i < W; i += THREADS) {                     // fewer continuations than beams (and than lanes)
         p.tokens[row0 + i] = p.parents[row0 + i] = -1;
