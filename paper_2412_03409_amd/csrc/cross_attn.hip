@@ -1,0 +1,381 @@
+// Attention of many bf16 rows to states of another length: every row of a sequence sees all of its states, or the first seen[t] of them.
+// Query heads that share a KV head are rows of one tile, row = token * heads + head.
+//
+//  cross_tiles_kernel  A workgroup has 128 rows of one (sequence, KV head) and a piece of the states, which stream through LDS 64 at a
+//                      time (asynchronous copies, two buffer pairs); a wavefront has 32 rows.  Bound: the matrix cores and the softmax
+//                      next to them.
+//  cross_merge_kernel  joins the pieces of a tile.
+//
+// How long the sequences and their states are is known on the device only, and a launch of a workgroup per tile takes as long as its
+// longest one.  So every workgroup adds up the stages of all tiles, one lane per sequence, and takes the same cap: no piece has more than
+// a kPieces-th of all stages (kLeastStages at least).  Then there are kPieces pieces more than tiles at most, which bounds the grid, and at most
+// 2 kPieces of tiles that are cut, which bounds the workspace.
+//
+// Stages that some rows see and others do not are masked, and a probability of 0 times an infinite or NaN value that such a row must not
+// see would spoil it.  To look for such values in every masked stage costs a third of it, so a tile is worked on without, and again with
+// the look if a row of it came out infinite or NaN.
+#include "attn_tile.hpp"
+
+#include <type_traits>
+
+namespace pkv {
+
+struct CrossParams {
+    int S, L, H, Hkv, T, M, grp, max_rows;
+    int heads, heads_per_xcd;           // heads: L * Hkv; heads_per_xcd: 0 if they do not divide up
+    FastDiv by_grp, by_hkv, by_heads;
+    const unsigned char *q, *k, *v;
+    unsigned char* out;
+    Strides qs, ks, vs, os;             // in bytes
+    const int32_t *row_off, *state_off, *seen;
+    const float* scale;
+    float* part_o;                      // workspace [2 * kPieces][4 wavefronts][32 * D], as registers are
+    float2* part_ms;                    // [2 * kPieces][4 wavefronts][64]: {maximum, sum}; sum 0: nothing seen, no numerators
+};
+constexpr int kPieces = 512;
+constexpr int kLeastStages = 4;
+
+struct Text { int s, first, rows, from, len; };     // rows: of the call, times the heads of a KV head; from, len: its states
+__device__ __forceinline__ Text text_of(const CrossParams& p, int s) {
+    const int first = p.row_off[s], last = p.row_off[s + 1], from = p.state_off[s], to = p.state_off[s + 1];
+    return {s, first, min(new_rows(first, last, p.T), p.max_rows) * p.grp, from, new_rows(from, to, p.M)};
+}
+__device__ __forceinline__ int tiles_of(const Text& x) { return (x.rows + kTileRows - 1) / kTileRows; }
+__device__ __forceinline__ int stages_of(const Text& x) { return (x.len + kStage - 1) / kStage; }
+__device__ __forceinline__ int pieces_of(const Text& x, int cap) { return x.rows == 0 ? 0 : max(1, (stages_of(x) + cap - 1) / cap); }
+
+// The texts of a head, one per lane (beyond 64 they are read again): the cap on a piece, and the places of a head, which are the pieces of
+// all tiles or (MERGE) the tiles that are cut.
+template <bool MERGE>
+struct Plan {
+    const CrossParams& p;
+    int lane, cap;
+    Text mine;
+    int upto, cut_upto;                 // places of the first 64 texts up to this lane's; pieces of cut tiles
+    int places, cuts;                   // of all (below 2^24; 2 kPieces)
+
+    __device__ __forceinline__ Plan(const CrossParams& params, int ln) : p(params), lane(ln) {
+        mine = text_of(p, min(lane, p.S - 1));
+        int64_t all = lane < p.S ? (int64_t)tiles_of(mine) * stages_of(mine) : 0;
+        for (int s = lane + kWave; s < p.S; s += kWave) {
+            const Text x = text_of(p, s);
+            all += (int64_t)tiles_of(x) * stages_of(x);
+        }
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) {
+            const int lo = __shfl_xor((int)(uint32_t)all, d, kWave), hi = __shfl_xor((int)(all >> 32), d, kWave);
+            all += (int64_t)(((uint64_t)(uint32_t)hi << 32) | (uint32_t)lo);
+        }
+        cap = __builtin_amdgcn_readfirstlane(max(kLeastStages, (int)fmin((double)all * p.heads / kPieces, 1e9) + 1));
+        places = cuts = 0;
+        for (int s0 = 0; s0 < p.S; s0 += kWave) {
+            int a, b;
+            scan(s0, s0 == 0 ? mine : text_of(p, min(s0 + lane, p.S - 1)), a, b);
+            if (s0 == 0) { upto = a; cut_upto = b; }
+            places += __builtin_amdgcn_readlane(a, kWave - 1);
+            cuts += __builtin_amdgcn_readlane(b, kWave - 1);
+        }
+    }
+    __device__ __forceinline__ int size(const Text& x) const {
+        const int pieces = pieces_of(x, cap);
+        return MERGE ? (pieces > 1 ? tiles_of(x) : 0) : pieces * tiles_of(x);
+    }
+    __device__ __forceinline__ int cut_size(const Text& x) const {
+        const int pieces = pieces_of(x, cap);
+        return pieces > 1 ? pieces * tiles_of(x) : 0;
+    }
+    // sums over the texts s0 ... s0 + lane
+    __device__ __forceinline__ void scan(int s0, const Text& x, int& a, int& b) const {
+        const bool real = s0 + lane < p.S;
+        a = real ? size(x) : 0;
+        b = real ? cut_size(x) : 0;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            const int ua = __shfl_up(a, d, kWave), ub = __shfl_up(b, d, kWave);
+            if (lane >= d) { a += ua; b += ub; }
+        }
+    }
+    // the text that holds place x (below `places`), the place in it, and the pieces of cut tiles before it
+    __device__ __forceinline__ Text find(int x, int& in, int& cut_before) const {
+        int s0 = 0, base = 0, cut = 0, a = upto, b = cut_upto;
+        Text y = mine;
+        while (s0 + kWave < p.S && __builtin_amdgcn_ballot_w64(base + a > x) == 0) {
+            base += __builtin_amdgcn_readlane(a, kWave - 1);
+            cut += __builtin_amdgcn_readlane(b, kWave - 1);
+            s0 += kWave;
+            y = text_of(p, min(s0 + lane, p.S - 1));
+            scan(s0, y, a, b);
+        }
+        const unsigned long long at = __builtin_amdgcn_ballot_w64(base + a > x);
+        Text t = {0, 0, 0, 0, 0};
+        in = cut_before = 0;
+        if (at == 0) return t;                                  // (offsets that descend may add up to more places than there are numbers)
+        const int j = __builtin_ctzll(at);
+        t.s = s0 + j;
+        t.first = __builtin_amdgcn_readlane(y.first, j); t.rows = __builtin_amdgcn_readlane(y.rows, j);
+        t.from = __builtin_amdgcn_readlane(y.from, j); t.len = __builtin_amdgcn_readlane(y.len, j);
+        in = x - base - __builtin_amdgcn_readlane(a, j) + size(t);
+        cut_before = cut + __builtin_amdgcn_readlane(b, j) - cut_size(t);
+        return t;
+    }
+};
+
+// how many of its text's states row `row` of it sees
+__device__ __forceinline__ int seen_by(const CrossParams& p, const Text& x, int row) {
+    return max(0, min(p.seen[x.first + row_at(row, p.by_grp).token], x.len));
+}
+// how many all of the rows row0 ... row0+ROWS-1 see, and how many some row does
+struct Limits { int all, some; };
+template <int ROWS>
+__device__ __forceinline__ Limits limits(const CrossParams& p, const Text& x, int row0, int lane) {
+    int lo = x.len, hi = 0;
+#pragma unroll
+    for (int i = 0; i < (ROWS + kWave - 1) / kWave; ++i) {
+        const int n = seen_by(p, x, min(row0 + min(i * kWave + lane, ROWS - 1), x.rows - 1));
+        lo = min(lo, n);
+        hi = max(hi, n);
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+        lo = min(lo, __shfl_xor(lo, d, kWave));
+        hi = max(hi, __shfl_xor(hi, d, kWave));
+    }
+    return {__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(hi)};
+}
+
+// SEEN: rows see the first states only.
+template <int D, bool SEEN>
+__global__ void __launch_bounds__(256, 2)
+cross_tiles_kernel(CrossParams p) {
+    constexpr int ROWB = D * 2, kInst = CopyLane<D>::kCopies;               // copies per wavefront, stage and tensor: 16 rows
+    __shared__ __attribute__((aligned(1024))) unsigned char sKa[kStage * ROWB];
+    __shared__ __attribute__((aligned(1024))) unsigned char sVa[kStage * ROWB];
+    __shared__ __attribute__((aligned(1024))) unsigned char sKb[kStage * ROWB];
+    __shared__ __attribute__((aligned(1024))) unsigned char sVb[kStage * ROWB];
+    __shared__ int s_wild;
+    const int lane = threadIdx.x & (kWave - 1), wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int ln = lane & 31, hf = lane >> 5;
+    if (SEEN && threadIdx.x == 0) s_wild = 0;
+
+    // Which tile and piece.  With heads in eighths every head stays on one XCD, else they alternate; in a head text by text, the tiles of
+    // a piece of the states one after the other, so that they are read through the same L2 at about the same time.
+    const Plan<false> plan(p, lane);
+    if (plan.places <= 0) return;
+    int head, x;
+    if (p.heads_per_xcd > 0) {
+        const uint32_t j = blockIdx.x / kXcds, h = j / (uint32_t)plan.places;
+        if (h >= (uint32_t)p.heads_per_xcd) return;
+        head = (int)(blockIdx.x % kXcds) * p.heads_per_xcd + (int)h;
+        x = (int)(j - h * (uint32_t)plan.places);
+    } else {
+        const DivMod hx = uniform_div_mod((int)blockIdx.x, p.by_heads);
+        if (hx.q >= plan.places) return;
+        head = hx.r; x = hx.q;
+    }
+    int in, cut_before;
+    const Text t = plan.find(x, in, cut_before);
+    if (t.rows == 0) return;
+    const DivMod lg = uniform_div_mod(head, p.by_hkv);                      // layer, KV head
+    const int tiles = tiles_of(t), stages = stages_of(t), pieces = pieces_of(t, plan.cap);
+    const int piece = __builtin_amdgcn_readfirstlane((uint32_t)in / (uint32_t)tiles), tile = in - piece * tiles;
+    const int st0 = piece * stages / pieces;
+    int st1 = (piece + 1) * stages / pieces;
+
+    // this wavefront's rows (those that do not exist repeat one that does)
+    const int r0 = tile * kTileRows + wv * 32, row = r0 + ln;
+    const bool mine = r0 < t.rows, real = row < t.rows;
+    const int rr = real ? row : mine ? r0 : 0;
+    const RowAt ra = row_at(rr, p.by_grp);
+    int end = t.len, all = t.len, lim = t.len - 1, lim_first = lim, lim_last = lim;     // states that some, and all rows of the tile see; the last one of the row, and of the wavefront's
+    if constexpr (SEEN) {
+        const Limits tl = limits<kTileRows>(p, t, tile * kTileRows, lane), w = limits<32>(p, t, mine ? r0 : 0, lane);
+        end = tl.some; all = tl.all;
+        lim = seen_by(p, t, rr) - 1;
+        lim_first = w.all - 1; lim_last = w.some - 1;
+        st1 = min(st1, (end + kStage - 1) / kStage);
+    }
+    const int n = max(0, st1 - st0), plain = max(0, min(st1, all / kStage) - st0);
+
+    const unsigned char* kb = p.k + p.ks.l * lg.q + p.ks.h * lg.r + p.ks.n * (int64_t)t.from;
+    const unsigned char* vb = p.v + p.vs.l * lg.q + p.vs.h * lg.r + p.vs.n * (int64_t)t.from;
+    const CopyLane<D> cp(lane);
+    auto issue = [&](int st, unsigned char* dK, unsigned char* dV) {        // a wavefront copies 16 rows of each
+        const int key = min(st * kStage + wv * 16, end - 1);                // the group's first state, or the last one there is
+        const uint32_t rest = (uint32_t)(end - 1 - key);
+        const unsigned char *ka = kb + p.ks.n * (int64_t)key, *va = vb + p.vs.n * (int64_t)key;
+#pragma unroll
+        for (int i = 0; i < kInst; ++i) {
+            copy_to_lds(ka + cp.at(i, rest, (uint32_t)p.ks.n), dK + (wv * kInst + i) * 1024);
+            copy_to_lds(va + cp.at(i, rest, (uint32_t)p.vs.n), dV + (wv * kInst + i) * 1024);
+        }
+    };
+    auto sync = [&]() {
+        __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0): this wavefront's part of the stage has landed
+        __syncthreads();                                     // ... and everybody's; the other pair is free again
+    };
+    // The last stage is in pair a, so the first one is there if they are odd.
+    bool half = (n & 1) != 0;
+    if (n > 0) {
+        if (half) issue(st0, sKa, sVa);
+        else issue(st0, sKb, sVb);
+    }
+    const float sc = p.scale[lg.q], qs = score_scale(sc);
+    const int h = lg.r * p.grp + ra.head;
+    const int64_t token = t.first + ra.token;
+    RowTile<D> tl;
+    tl.offsets(lane);
+    tl.load_q(p.q + p.qs.l * lg.q + p.qs.h * h + p.qs.n * token, hf, sc < 0.f);
+    tl.clear();
+
+    // Stages that every row of the tile sees, two at a time, without a branch between them.  A wavefront without rows works along on rows
+    // that are not stored.
+    int st = st0;
+    if (half && plain > 0) {
+        sync();
+        if (st + 1 < st1) issue(st + 1, sKb, sVb);
+        tl.template attend<2, false>(sKa, sVa, qs, lane, 0, 0u, 2, 2);
+        ++st;
+        half = false;
+    }
+    if (!half) {
+        for (; st + 1 < st0 + plain; st += 2) {
+            sync();
+            issue(st + 1, sKa, sVa);
+            tl.template attend<2, false>(sKb, sVb, qs, lane, 0, 0u, 2, 2);
+            sync();
+            if (st + 2 < st1) issue(st + 2, sKb, sVb);
+            tl.template attend<2, false>(sKa, sVa, qs, lane, 0, 0u, 2, 2);
+        }
+    }
+    auto masked = [&](int st, const unsigned char* sK, const unsigned char* sV, auto check) {
+        const int key0 = st * kStage;
+        if (mine && key0 <= lim_last)
+            tl.template attend<2, true, false, decltype(check)::value>(sK, sV, qs, lane, lim - key0, 0u, key0 + 32 <= lim_last ? 2 : 1,
+                                                                      (max(lim_first - key0, -1) + 1) / 32);
+    };
+    // the others: with SEEN any, else the last one behind one that is like those before
+    while (st < st1) {
+        if (!half) {
+            sync();
+            issue(st + 1, sKa, sVa);
+            if constexpr (SEEN) masked(st, sKb, sVb, std::false_type{});
+            else tl.template attend<2, false>(sKb, sVb, qs, lane, 0, 0u, 2, 2);
+            ++st;
+        }
+        half = false;
+        sync();
+        if (st + 1 < st1) issue(st + 1, sKb, sVb);
+        if constexpr (SEEN) masked(st, sKa, sVa, std::false_type{});
+        else masked(st, sKa, sVa, std::true_type{});
+        ++st;
+    }
+    if constexpr (SEEN) {
+        // 0 times what is infinite or NaN is NaN
+        float z = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) z = fmaf(tl.o[dt][r], 0.f, z);
+        if (n > plain) {
+            if (mine && __builtin_amdgcn_ballot_w64(z != z) != 0) s_wild = 1;
+            __syncthreads();
+            if (__builtin_expect(s_wild, 0)) {
+                tl.clear();
+                for (st = st0; st < st1; ++st) {
+                    issue(st, sKa, sVa);
+                    sync();
+                    masked(st, sKa, sVa, std::true_type{});
+                    __syncthreads();
+                }
+            }
+        }
+    }
+    if (!mine) return;
+    const float sum = tl.total();
+    if (pieces == 1) {
+        tl.store(p.out + p.os.l * lg.q + p.os.h * h + p.os.n * token, hf, sum == 0.f ? 0.f : 1.f / sum, real);
+    } else {
+        const int64_t slot = ((int64_t)head * plan.cuts + cut_before + tile * pieces + piece) * 4 + wv;
+        if (n > 0) tl.store_tile(p.part_o + slot * 32 * D, p.part_ms + slot * kWave, lane, sum);
+        else p.part_ms[slot * kWave + lane] = make_float2(-INFINITY, 0.f);
+    }
+}
+
+// Joins the pieces of a tile: a wavefront has 32 columns of 32 rows, in the registers' order, in which the pieces were written.
+template <int D>
+__global__ void __launch_bounds__(256)
+cross_merge_kernel(CrossParams p) {
+    const int lane = threadIdx.x & (kWave - 1), wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), dt = (int)blockIdx.y;
+    const int ln = lane & 31, hf = lane >> 5;
+    const Plan<true> plan(p, lane);
+    if (plan.places <= 0) return;
+    const int head = __builtin_amdgcn_readfirstlane(blockIdx.x / (uint32_t)plan.places);
+    if (head >= p.heads) return;
+    int in, cut_before;
+    const Text t = plan.find((int)blockIdx.x - head * plan.places, in, cut_before);
+    if (t.rows == 0) return;
+    const int pieces = pieces_of(t, plan.cap), r0 = in * kTileRows + wv * 32, row = r0 + ln;
+    if (r0 >= t.rows) return;
+    const DivMod lg = uniform_div_mod(head, p.by_hkv);
+    const float qs = score_scale(p.scale[lg.q]);
+    const int64_t first = (int64_t)head * plan.cuts + cut_before + in * pieces;
+    float m = -INFINITY, sum = 0.f;
+    f32x16_t o;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[r] = 0.f;
+    for (int i = 0; i < pieces; ++i) {                           // a running maximum: every piece is read once
+        const int64_t slot = (first + i) * 4 + wv;
+        const float2 x = p.part_ms[slot * kWave + lane];
+        if (__builtin_amdgcn_ballot_w64(x.y != 0.f) == 0) continue;       // nothing seen
+        const float4* from = (const float4*)(p.part_o + slot * 32 * D) + dt * 4 * kWave + lane;
+        const float4 y[4] = {from[0], from[kWave], from[2 * kWave], from[3 * kWave]};
+        const float mx = fmaxf(m, x.x), ref = mx == -INFINITY ? 0.f : mx;
+        const float c0 = __builtin_amdgcn_exp2f((m - ref) * qs), c1 = __builtin_amdgcn_exp2f((x.x - ref) * qs);
+        sum = fmaf(sum, c0, x.y * c1);
+        m = mx;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            o[4 * e] = fmaf(o[4 * e], c0, y[e].x * c1); o[4 * e + 1] = fmaf(o[4 * e + 1], c0, y[e].y * c1);
+            o[4 * e + 2] = fmaf(o[4 * e + 2], c0, y[e].z * c1); o[4 * e + 3] = fmaf(o[4 * e + 3], c0, y[e].w * c1);
+        }
+    }
+    const bool real = row < t.rows;
+    const RowAt ra = row_at(real ? row : r0, p.by_grp);
+    store_columns(o, p.out + p.os.l * lg.q + p.os.h * (lg.r * p.grp + ra.head) + p.os.n * (int64_t)(t.first + ra.token) + 64 * dt, hf,
+                  sum == 0.f ? 0.f : 1.f / sum, real);
+}
+
+// whether a tile may be cut
+static bool may_cut(int M) { return M > kLeastStages * kStage; }
+
+size_t cross_tiles_ws_bytes(const pkv_packed& s, int M) {
+    return may_cut(M) ? (size_t)2 * kPieces * kTileRows * (s.D * sizeof(float) + 2 * sizeof(float2)) : 0;
+}
+
+template <int D>
+static hipError_t launch(const CrossParams& p, long long tiles, int M, hipStream_t st) {
+    const dim3 grid((unsigned)(tiles * p.heads + (may_cut(M) ? kPieces : 0)));
+    if (p.seen) hipLaunchKernelGGL((cross_tiles_kernel<D, true>), grid, dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((cross_tiles_kernel<D, false>), grid, dim3(256), 0, st, p);
+    if (may_cut(M)) hipLaunchKernelGGL(cross_merge_kernel<D>, dim3(kPieces, D / 32), dim3(256), 0, st, p);
+    return hipGetLastError();
+}
+
+hipError_t launch_cross_tiles(const pkv_packed& s, const PackedAttn& a, hipStream_t st) {
+    auto bytes = [](Strides x) { return Strides{0, x.l * 2, x.h * 2, x.n * 2}; };
+    CrossParams p;
+    p.S = s.S; p.L = s.L; p.H = s.H; p.Hkv = s.Hkv; p.T = s.T; p.M = a.M; p.grp = s.H / s.Hkv; p.max_rows = a.max_rows;
+    p.heads = s.L * s.Hkv;
+    p.heads_per_xcd = p.heads % kXcds == 0 ? p.heads / kXcds : 0;
+    p.by_grp = fast_div(p.grp); p.by_hkv = fast_div(s.Hkv); p.by_heads = fast_div(p.heads);
+    p.q = (const unsigned char*)a.q; p.k = (const unsigned char*)a.k; p.v = (const unsigned char*)a.v; p.out = (unsigned char*)a.out;
+    p.qs = bytes(a.qs); p.ks = bytes(a.ks); p.vs = bytes(a.vs); p.os = bytes(a.os);
+    p.row_off = a.row_off; p.state_off = a.state_off; p.seen = a.seen; p.scale = a.scale;
+    p.part_o = (float*)a.ws;
+    p.part_ms = (float2*)(p.part_o + (size_t)2 * kPieces * kTileRows * s.D);
+    // tiles of all texts of a head, at most
+    const long long tiles = (long long)s.T * p.grp / kTileRows + (s.S < s.T ? s.S : s.T);
+    return s.D == 128 ? launch<128>(p, tiles, a.M, st) : launch<64>(p, tiles, a.M, st);
+}
+
+}  // namespace pkv

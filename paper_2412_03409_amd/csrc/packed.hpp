@@ -59,6 +59,9 @@ bool packed_attn_fits(const pkv_packed& s, const pkv_paging* g);
 size_t packed_attn_ws_bytes(const pkv_packed& s, int max_rows);
 bool cross_attn_fits(const pkv_packed& s, int M);
 size_t cross_attn_ws_bytes(const pkv_packed& s, int M, int max_rows);
+// ... of many bf16 rows over states
+size_t cross_tiles_ws_bytes(const pkv_packed& s, int M);
+hipError_t launch_cross_tiles(const pkv_packed& s, const PackedAttn& a, hipStream_t st);
 hipError_t launch_packed_attn(const pkv_packed& s, const PackedAttn& a, hipStream_t st);
 
 }  // namespace pkv
