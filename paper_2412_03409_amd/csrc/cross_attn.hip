@@ -32,7 +32,8 @@ struct CrossParams {
     float* part_o;                      // workspace [2 * kPieces][4 wavefronts][32 * D], as registers are
     float2* part_ms;                    // [2 * kPieces][4 wavefronts][64]: {maximum, sum}; sum 0: nothing seen, no numerators
 };
-constexpr int kPieces = 512;
+// (320, 384, 512, 768, 1024 pieces: 21.9, 21.8, 22.3, 22.8, 23.3 us, the geometric mean of 70 calls of all sizes; at least 8 stages a piece: 22.2)
+constexpr int kPieces = 384;
 constexpr int kLeastStages = 4;
 
 struct Text { int s, first, rows, from, len; };     // rows: of the call, times the heads of a KV head; from, len: its states
@@ -46,7 +47,7 @@ __device__ __forceinline__ int pieces_of(const Text& x, int cap) { return x.rows
 
 // The texts of a head, one per lane (beyond 64 they are read again): the cap on a piece, and the places of a head, which are the pieces of
 // all tiles or (MERGE) the tiles that are cut.
-template <bool MERGE>
+template <bool MERGE, bool CUT>
 struct Plan {
     const CrossParams& p;
     int lane, cap;
@@ -56,31 +57,37 @@ struct Plan {
 
     __device__ __forceinline__ Plan(const CrossParams& params, int ln) : p(params), lane(ln) {
         mine = text_of(p, min(lane, p.S - 1));
-        int64_t all = lane < p.S ? (int64_t)tiles_of(mine) * stages_of(mine) : 0;
-        for (int s = lane + kWave; s < p.S; s += kWave) {
-            const Text x = text_of(p, s);
-            all += (int64_t)tiles_of(x) * stages_of(x);
-        }
+        cap = 1 << 30;
+        if constexpr (CUT) {
+            int64_t all = lane < p.S ? (int64_t)tiles_of(mine) * stages_of(mine) : 0;
+            for (int s = lane + kWave; s < p.S; s += kWave) {
+                const Text x = text_of(p, s);
+                all += (int64_t)tiles_of(x) * stages_of(x);
+            }
 #pragma unroll
-        for (int d = 32; d > 0; d >>= 1) {
-            const int lo = __shfl_xor((int)(uint32_t)all, d, kWave), hi = __shfl_xor((int)(all >> 32), d, kWave);
-            all += (int64_t)(((uint64_t)(uint32_t)hi << 32) | (uint32_t)lo);
+            for (int d = 32; d > 0; d >>= 1) {
+                const int lo = __shfl_xor((int)(uint32_t)all, d, kWave), hi = __shfl_xor((int)(all >> 32), d, kWave);
+                all += (int64_t)(((uint64_t)(uint32_t)hi << 32) | (uint32_t)lo);
+            }
+            cap = __builtin_amdgcn_readfirstlane(max(kLeastStages, (int)fmin((double)all * p.heads / kPieces, 1e9) + 1));
         }
-        cap = __builtin_amdgcn_readfirstlane(max(kLeastStages, (int)fmin((double)all * p.heads / kPieces, 1e9) + 1));
         places = cuts = 0;
         for (int s0 = 0; s0 < p.S; s0 += kWave) {
             int a, b;
             scan(s0, s0 == 0 ? mine : text_of(p, min(s0 + lane, p.S - 1)), a, b);
             if (s0 == 0) { upto = a; cut_upto = b; }
-            places += __builtin_amdgcn_readlane(a, kWave - 1);
-            cuts += __builtin_amdgcn_readlane(b, kWave - 1);
+            const int last = min(p.S - s0, kWave) - 1;
+            places += __builtin_amdgcn_readlane(a, last);
+            cuts += __builtin_amdgcn_readlane(b, last);
         }
     }
     __device__ __forceinline__ int size(const Text& x) const {
+        if constexpr (!CUT) return tiles_of(x);
         const int pieces = pieces_of(x, cap);
         return MERGE ? (pieces > 1 ? tiles_of(x) : 0) : pieces * tiles_of(x);
     }
     __device__ __forceinline__ int cut_size(const Text& x) const {
+        if constexpr (!CUT) return 0;
         const int pieces = pieces_of(x, cap);
         return pieces > 1 ? pieces * tiles_of(x) : 0;
     }
@@ -91,7 +98,8 @@ struct Plan {
         b = real ? cut_size(x) : 0;
 #pragma unroll
         for (int d = 1; d < kWave; d <<= 1) {
-            const int ua = __shfl_up(a, d, kWave), ub = __shfl_up(b, d, kWave);
+            if (d >= p.S) break;
+            const int ua = __shfl_up(a, d, kWave), ub = CUT ? __shfl_up(b, d, kWave) : 0;
             if (lane >= d) { a += ua; b += ub; }
         }
     }
@@ -106,7 +114,7 @@ struct Plan {
             y = text_of(p, min(s0 + lane, p.S - 1));
             scan(s0, y, a, b);
         }
-        const unsigned long long at = __builtin_amdgcn_ballot_w64(base + a > x);
+        const unsigned long long at = __builtin_amdgcn_ballot_w64(s0 + lane < p.S && base + a > x);
         Text t = {0, 0, 0, 0, 0};
         in = cut_before = 0;
         if (at == 0) return t;                                  // (offsets that descend may add up to more places than there are numbers)
@@ -143,8 +151,8 @@ __device__ __forceinline__ Limits limits(const CrossParams& p, const Text& x, in
     return {__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(hi)};
 }
 
-// SEEN: rows see the first states only.
-template <int D, bool SEEN>
+// SEEN: rows see the first states only.  CUT: tiles may be cut.
+template <int D, bool SEEN, bool CUT>
 __global__ void __launch_bounds__(256, 2)
 cross_tiles_kernel(CrossParams p) {
     constexpr int ROWB = D * 2, kInst = CopyLane<D>::kCopies;               // copies per wavefront, stage and tensor: 16 rows
@@ -159,7 +167,7 @@ cross_tiles_kernel(CrossParams p) {
 
     // Which tile and piece.  With heads in eighths every head stays on one XCD, else they alternate; in a head text by text, the tiles of
     // a piece of the states one after the other, so that they are read through the same L2 at about the same time.
-    const Plan<false> plan(p, lane);
+    const Plan<false, CUT> plan(p, lane);
     if (plan.places <= 0) return;
     int head, x;
     if (p.heads_per_xcd > 0) {
@@ -176,10 +184,10 @@ cross_tiles_kernel(CrossParams p) {
     const Text t = plan.find(x, in, cut_before);
     if (t.rows == 0) return;
     const DivMod lg = uniform_div_mod(head, p.by_hkv);                      // layer, KV head
-    const int tiles = tiles_of(t), stages = stages_of(t), pieces = pieces_of(t, plan.cap);
-    const int piece = __builtin_amdgcn_readfirstlane((uint32_t)in / (uint32_t)tiles), tile = in - piece * tiles;
-    const int st0 = piece * stages / pieces;
-    int st1 = (piece + 1) * stages / pieces;
+    const int tiles = tiles_of(t), stages = stages_of(t), pieces = CUT ? pieces_of(t, plan.cap) : 1;
+    const int piece = CUT ? __builtin_amdgcn_readfirstlane((uint32_t)in / (uint32_t)tiles) : 0, tile = in - piece * tiles;
+    const int st0 = CUT ? piece * stages / pieces : 0;
+    int st1 = CUT ? (piece + 1) * stages / pieces : stages;
 
     // this wavefront's rows (those that do not exist repeat one that does)
     const int r0 = tile * kTileRows + wv * 32, row = r0 + ln;
@@ -292,7 +300,7 @@ cross_tiles_kernel(CrossParams p) {
     }
     if (!mine) return;
     const float sum = tl.total();
-    if (pieces == 1) {
+    if (!CUT || pieces == 1) {
         tl.store(p.out + p.os.l * lg.q + p.os.h * h + p.os.n * token, hf, sum == 0.f ? 0.f : 1.f / sum, real);
     } else {
         const int64_t slot = ((int64_t)head * plan.cuts + cut_before + tile * pieces + piece) * 4 + wv;
@@ -307,7 +315,7 @@ __global__ void __launch_bounds__(256)
 cross_merge_kernel(CrossParams p) {
     const int lane = threadIdx.x & (kWave - 1), wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), dt = (int)blockIdx.y;
     const int ln = lane & 31, hf = lane >> 5;
-    const Plan<true> plan(p, lane);
+    const Plan<true, true> plan(p, lane);
     if (plan.places <= 0) return;
     const int head = __builtin_amdgcn_readfirstlane(blockIdx.x / (uint32_t)plan.places);
     if (head >= p.heads) return;
@@ -345,19 +353,29 @@ cross_merge_kernel(CrossParams p) {
                   sum == 0.f ? 0.f : 1.f / sum, real);
 }
 
-// whether a tile may be cut
-static bool may_cut(int M) { return M > kLeastStages * kStage; }
+// tiles of all texts and heads, at most
+static long long all_tiles(const pkv_packed& s) {
+    return ((long long)s.T * (s.H / s.Hkv) / kTileRows + (s.S < s.T ? s.S : s.T)) * s.L * s.Hkv;
+}
+// Whether tiles may be cut: where texts are long (half as long again as the average is taken for the longest, as lengths are on the device) and
+// the tiles would not fill the chip several times over.  Joining costs 4 to 5 us where nothing was cut.  us, whole / cut: H12/4, 14 texts of
+// up to 3350 states and 20 rows 71 / 31; H16/8, one of 1827 and 238 rows 39 / 27; H40/40, 3 of up to 186 and 2872 rows 46 / 54; H32/4, 44
+// of up to 179 and 5 rows 8.6 / 13; H40/40, 3 of up to 839 and 3909 rows, D 64, 69 / 74 (cut all the same).
+constexpr double kCutStages = 8.0;
+constexpr int kManyTiles = 2048;
+static bool may_cut(const pkv_packed& s, int M) { return 1.5 * M / s.S / kStage > kCutStages && all_tiles(s) < kManyTiles; }
 
 size_t cross_tiles_ws_bytes(const pkv_packed& s, int M) {
-    return may_cut(M) ? (size_t)2 * kPieces * kTileRows * (s.D * sizeof(float) + 2 * sizeof(float2)) : 0;
+    return may_cut(s, M) ? (size_t)2 * kPieces * kTileRows * (s.D * sizeof(float) + 2 * sizeof(float2)) : 0;
 }
 
 template <int D>
-static hipError_t launch(const CrossParams& p, long long tiles, int M, hipStream_t st) {
-    const dim3 grid((unsigned)(tiles * p.heads + (may_cut(M) ? kPieces : 0)));
-    if (p.seen) hipLaunchKernelGGL((cross_tiles_kernel<D, true>), grid, dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((cross_tiles_kernel<D, false>), grid, dim3(256), 0, st, p);
-    if (may_cut(M)) hipLaunchKernelGGL(cross_merge_kernel<D>, dim3(kPieces, D / 32), dim3(256), 0, st, p);
+static hipError_t launch(const CrossParams& p, long long tiles, bool cut, hipStream_t st) {
+    const dim3 grid((unsigned)(tiles + (cut ? kPieces : 0)));
+    auto* kernel = cut ? (p.seen ? cross_tiles_kernel<D, true, true> : cross_tiles_kernel<D, false, true>)
+                       : (p.seen ? cross_tiles_kernel<D, true, false> : cross_tiles_kernel<D, false, false>);
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, p);
+    if (cut) hipLaunchKernelGGL(cross_merge_kernel<D>, dim3(kPieces, D / 32), dim3(256), 0, st, p);
     return hipGetLastError();
 }
 
@@ -373,9 +391,8 @@ hipError_t launch_cross_tiles(const pkv_packed& s, const PackedAttn& a, hipStrea
     p.row_off = a.row_off; p.state_off = a.state_off; p.seen = a.seen; p.scale = a.scale;
     p.part_o = (float*)a.ws;
     p.part_ms = (float2*)(p.part_o + (size_t)2 * kPieces * kTileRows * s.D);
-    // tiles of all texts of a head, at most
-    const long long tiles = (long long)s.T * p.grp / kTileRows + (s.S < s.T ? s.S : s.T);
-    return s.D == 128 ? launch<128>(p, tiles, a.M, st) : launch<64>(p, tiles, a.M, st);
+    const bool cut = may_cut(s, a.M);
+    return s.D == 128 ? launch<128>(p, all_tiles(s), cut, st) : launch<64>(p, all_tiles(s), cut, st);
 }
 
 }  // namespace pkv
