@@ -19,6 +19,7 @@ namespace pkv {
 
 constexpr int kScanThreads = 256;
 constexpr int kWaveCandidates = 128;    // of a wavefront's part of a piece
+constexpr int kManyFound = 512;         // candidates of a prompt beyond which those that cannot be are sorted out (4 prompts of 32 beams, 2729 tokens: 68 -> 20 us; 200 candidates: 24.5, 28.1 so)
 
 struct BeamParams {
     int S, W, V, pieces;            // pieces of a row
@@ -357,18 +358,57 @@ beam_scan_kernel(BeamParams p) {
     if (tid == 0) p.sums[row * p.pieces + rp.r] = make_float2(m, (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]));
 }
 
+// Which of the candidates of a workgroup, R of a thread, are among the W best, and at most 64 - W others: bisection over the upper halves
+// of the scores, where equal ones are too many over the lower halves, and then over the places.  Every step is a count of the whole workgroup.
+template <int THREADS, int R>
+struct Best {
+    int* counts;                        // LDS, 0
+    int lane, step, W;
+    // v: larger ones first; in: whether it takes part; above: how many come before those.  -> which take part, at least W - above of them
+    __device__ __forceinline__ bool narrow(const uint32_t (&v)[R], bool (&in)[R], int& above) {
+        uint32_t lo = 0, hi = ~0u;
+        int at_lo = -1;                                                  // how many reach lo
+        while (lo < hi) {
+            const uint32_t mid = lo + (hi - lo) / 2 + 1;
+            int c = 0;
+#pragma unroll
+            for (int r = 0; r < R; ++r) c += __popcll(__builtin_amdgcn_ballot_w64(in[r] && v[r] >= mid));
+            c = above + all(c);
+            if (c >= W) { lo = mid; at_lo = c; } else hi = mid - 1;
+            if (c >= W && c <= kWave) break;
+        }
+        const bool enough = at_lo >= 0 && at_lo <= kWave;
+        int more = 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            more += enough ? 0 : __popcll(__builtin_amdgcn_ballot_w64(in[r] && v[r] > lo));
+            sure[r] = sure[r] || (in[r] && (enough ? v[r] >= lo : v[r] > lo));
+            in[r] = !enough && in[r] && v[r] == lo;
+        }
+        if (!enough) above += all(more);
+        return enough;
+    }
+    __device__ __forceinline__ int all(int c) {                          // sum over the workgroup's wavefronts
+        if (lane == 0) atomicAdd(counts + step, c);
+        __syncthreads();
+        return counts[step++];
+    }
+    bool sure[R];                       // the verdict
+};
+
 // A group of lanes, a power of two of them, has the pieces of a row.
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS)
 beam_join_kernel(BeamParams p) {
     constexpr int kHeads = (kMaxBeams * kMaxPieces + 1023) / 1024;       // of a thread, at most
-    constexpr int kLists = kMaxBeams * 3 / 2;
+    constexpr int kLists = kMaxBeams * 3 / 2, R = 2, kSteps = 3 * 34;
+    static_assert(1024 * R >= kLists * kMaxBeams, "a thread has R of what the lists hold");
     __shared__ double s_lse[kMaxBeams], s_score[kMaxBeams];
     __shared__ uint8_t s_kind[kMaxBeams];                                // 0: goes on, 1: has ended, 2: no candidates
     __shared__ uint64_t s_head[kMaxBeams * kMaxPieces], s_ck[kLists * kMaxBeams];
     __shared__ uint32_t s_place[kMaxBeams * kMaxPieces], s_ca[kLists * kMaxBeams];
     __shared__ Threshold<uint64_t> s_t;
-    __shared__ int s_list[kLists], s_lists, s_count;
+    __shared__ int s_list[kLists], s_lists, s_count, s_counts[kSteps];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), W = p.W, n = W * p.pieces;
     const bool first_wave = tid < kWave;
     const int64_t row0 = (int64_t)blockIdx.x * W;
@@ -455,7 +495,7 @@ beam_join_kernel(BeamParams p) {
         s_ca[at] = a;
     }
     __syncthreads();
-    const int found = s_count;
+    int found = s_count;
     auto give = [&](uint64_t k, uint32_t a, int r) {
         if (r >= W) return;
         const int w = (int)(a / (uint32_t)p.V), v = (int)(a - (uint32_t)w * (uint32_t)p.V);
@@ -466,6 +506,45 @@ beam_join_kernel(BeamParams p) {
         p.scores_out[row0 + r] = (float)__longlong_as_double((long long)u);
         if (p.ended_out) p.ended_out[row0 + r] = over || v == p.end_token;
     };
+    if (THREADS == 1024 && found > kManyFound) {
+        // a few beams have most of them: what is not among the W best leaves
+        uint64_t k[R];
+        uint32_t a[R], part[R];
+        Best<THREADS, R> best{s_counts, lane, 0, W, {}};
+        bool in[R];
+        int above = 0;
+        for (int i = tid; i < kSteps; i += THREADS) s_counts[i] = 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int i = tid + r * THREADS;
+            in[r] = i < found;
+            best.sure[r] = false;
+            k[r] = in[r] ? s_ck[i] : 0;
+            a[r] = in[r] ? s_ca[i] : 0;
+            part[r] = (uint32_t)(k[r] >> 32);
+        }
+        __syncthreads();
+        if (!best.narrow(part, in, above)) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) part[r] = (uint32_t)k[r];
+            if (!best.narrow(part, in, above)) {
+#pragma unroll
+                for (int r = 0; r < R; ++r) part[r] = ~a[r];
+                best.narrow(part, in, above);
+            }
+        }
+        if (tid == 0) s_count = 0;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (best.sure[r]) {
+                const int at = atomicAdd(&s_count, 1);
+                s_ck[at] = k[r];
+                s_ca[at] = a[r];
+            }
+        __syncthreads();
+        found = s_count;
+    }
     if (found <= kWave) {
         if (!first_wave) return;
         const uint64_t k = lane < found ? s_ck[lane] : 0;
