@@ -309,6 +309,7 @@ cross_tiles_kernel(CrossParams p) {
     }
 }
 
+typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 // Joins the pieces of a tile: a wavefront has 32 columns of 32 rows, in the registers' order, in which the pieces were written.
 template <int D>
 __global__ void __launch_bounds__(256)
@@ -331,20 +332,32 @@ cross_merge_kernel(CrossParams p) {
     f32x16_t o;
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[r] = 0.f;
-    for (int i = 0; i < pieces; ++i) {                           // a running maximum: every piece is read once
-        const int64_t slot = (first + i) * 4 + wv;
-        const float2 x = p.part_ms[slot * kWave + lane];
-        if (__builtin_amdgcn_ballot_w64(x.y != 0.f) == 0) continue;       // nothing seen
-        const float4* from = (const float4*)(p.part_o + slot * 32 * D) + dt * 4 * kWave + lane;
-        const float4 y[4] = {from[0], from[kWave], from[2 * kWave], from[3 * kWave]};
-        const float mx = fmaxf(m, x.x), ref = mx == -INFINITY ? 0.f : mx;
-        const float c0 = __builtin_amdgcn_exp2f((m - ref) * qs), c1 = __builtin_amdgcn_exp2f((x.x - ref) * qs);
-        sum = fmaf(sum, c0, x.y * c1);
-        m = mx;
+    constexpr int U = 4;                                         // pieces that are asked for together
+    for (int i0 = 0; i0 < pieces; i0 += U) {                     // a running maximum: every piece is read once
+        float2 x[U];
+        f32x4_t y[U][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            o[4 * e] = fmaf(o[4 * e], c0, y[e].x * c1); o[4 * e + 1] = fmaf(o[4 * e + 1], c0, y[e].y * c1);
-            o[4 * e + 2] = fmaf(o[4 * e + 2], c0, y[e].z * c1); o[4 * e + 3] = fmaf(o[4 * e + 3], c0, y[e].w * c1);
+        for (int u = 0; u < U; ++u) {
+            x[u] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[u][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            if (i0 + u >= pieces) continue;
+            const int64_t slot = (first + i0 + u) * 4 + wv;
+            x[u] = p.part_ms[slot * kWave + lane];
+            const f32x4_t* from = (const f32x4_t*)(p.part_o + slot * 32 * D) + dt * 4 * kWave + lane;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[u][e] = from[e * kWave];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            // (of a piece that nothing was seen in the numerators were not written)
+            const bool any = x[u].y != 0.f;
+            const float mx = any ? fmaxf(m, x[u].x) : m, ref = mx == -INFINITY ? 0.f : mx;
+            const float c0 = any ? __builtin_amdgcn_exp2f((m - ref) * qs) : 1.f, c1 = __builtin_amdgcn_exp2f((x[u].x - ref) * qs);
+            sum = any ? fmaf(sum, c0, x[u].y * c1) : sum;
+            m = mx;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = any ? fmaf(o[e], c0, y[u][e / 4][e % 4] * c1) : o[e];
         }
     }
     const bool real = row < t.rows;

@@ -172,7 +172,7 @@ struct Work {
 struct Segment { int s, l, first, n, rows, len, before, end; };   // rows: of this call, times the heads of a KV head; keys; keys in front
                                                                   // of the first new row (below 0: the first rows see nothing); keys that some row sees (none without rows)
 
-template <Keys KEYS>
+template <Keys KEYS, bool ALL = false>          // ALL: as if every row saw all states
 __device__ __forceinline__ Segment segment(const Work& p, int i) {
     Segment x;
     const DivMod sl = div_mod(i, p.by_layers);
@@ -184,12 +184,28 @@ __device__ __forceinline__ Segment segment(const Work& p, int i) {
     const int rows = KEYS == kPrompt ? x.n : min(x.n, p.a.max_rows);
     x.rows = rows * p.a.grp;
     x.before = KEYS == kStates ? x.len - 1 : x.len - x.n;
-    x.end = KEYS == kStates ? (rows > 0 ? x.len : 0) : keys_seen(rows, x.n, x.len);
+    if constexpr (KEYS == kStates) {
+        x.end = rows > 0 ? x.len : 0;
+        if (!ALL && p.a.seen && rows > 0) {                     // (32 rows at most)
+            int most = 0;
+            for (int t = 0; t < rows; ++t) most = max(most, p.a.seen[x.first + t]);
+            x.end = min(x.len, most);
+        }
+    } else {
+        x.end = keys_seen(rows, x.n, x.len);
+    }
     return x;
 }
 template <Keys KEYS>
 __device__ __forceinline__ Segment uniform_segment(const Work& p, int i) {
-    Segment x = segment<KEYS>(p, i);
+    Segment x = segment<KEYS, KEYS == kStates>(p, i);
+    if (KEYS == kStates && p.a.seen && x.rows > 0) {            // a row for a lane
+        const int rows = min(x.n, p.a.max_rows), lane = threadIdx.x & (kWave - 1);
+        int most = lane < rows ? p.a.seen[x.first + lane] : 0;
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) most = max(most, __shfl_xor(most, d, kWave));
+        x.end = max(0, min(x.len, most));
+    }
     x.s = __builtin_amdgcn_readfirstlane(x.s); x.l = __builtin_amdgcn_readfirstlane(x.l);
     x.first = __builtin_amdgcn_readfirstlane(x.first); x.n = __builtin_amdgcn_readfirstlane(x.n);
     x.rows = __builtin_amdgcn_readfirstlane(x.rows); x.len = __builtin_amdgcn_readfirstlane(x.len);
@@ -647,7 +663,10 @@ attn_merge_tiles_kernel(TileParams p) {
 }
 
 // ---- few rows: the keys of a launch shared out evenly over the wavefronts ---------------------------------
+// (States are the same in every layer: there a segment is a sequence, and its heads are those of all layers.)
 struct StreamParams : Work {
+    int heads;                      // of a segment
+    FastDiv by_hkv;
     int waves;
     int join_rows;                  // rows of a workgroup that joins: 1, or all of its groups of lanes
     int* share;                     // workspace: blocks of a wavefront
@@ -672,7 +691,8 @@ attn_stream_kernel(StreamParams p) {
     const int wave = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 2 + wv), ln = lane & 31, hf = lane >> 5;
 
     // the launch's blocks, and this wavefront's: segment by segment, KV head by KV head
-    auto blocks = [&](const Segment& x) { return (int64_t)blocks_of(x) * a.Hkv; };
+    const int heads = KEYS == kStates ? p.heads : a.Hkv;
+    auto blocks = [&](const Segment& x) { return (int64_t)blocks_of(x) * heads; };
     const Looked<KEYS, int64_t, decltype(blocks)> looked(p, lane, p.segs, 0, 1, blocks);
     const int all_blocks = (int)looked.all;                                // (below 2^31: the call is refused otherwise)
     const int share = max(kLeastBlocks, (all_blocks + p.waves - 1) / p.waves);
@@ -694,7 +714,7 @@ attn_stream_kernel(StreamParams p) {
     auto step = [&](Cursor& c, Segment& x) -> bool {            // true: another segment
         if (++c.blk < blocks_of(x)) return false;
         c.blk = 0;
-        if (++c.g < a.Hkv) return false;
+        if (++c.g < heads) return false;
         c.g = 0;
         do { ++c.seg; x = uniform_segment<KEYS>(p, c.seg); } while (x.end == 0);    // (a block is left, so a segment is)
         return true;
@@ -719,7 +739,8 @@ attn_stream_kernel(StreamParams p) {
     load_ids();
     auto issue = [&](unsigned char* dK, unsigned char* dV) -> uint32_t {
         if constexpr (KEYS == kStates) {
-            const unsigned char *kb = a.k + a.ks.l * in.l + a.ks.h * ci.g, *vb = a.v + a.vs.l * in.l + a.vs.h * ci.g;
+            const DivMod lg = uniform_div_mod(ci.g, p.by_hkv);
+            const unsigned char *kb = a.k + a.ks.l * lg.q + a.ks.h * lg.r, *vb = a.v + a.vs.l * lg.q + a.vs.h * lg.r;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 const int key = min(ci.blk * kBlockKeys + 16 * x, in.end - 1);
@@ -768,12 +789,13 @@ attn_stream_kernel(StreamParams p) {
     unsigned char* out = nullptr;
     auto begin = [&]() {                                        // a unit: its queries
         const RowAt ra = row_at(ln < sg.rows ? ln : 0, p.grp);
-        const int h = cw.g * a.grp + ra.head;
+        const DivMod lg = KEYS == kStates ? uniform_div_mod(cw.g, p.by_hkv) : DivMod{sg.l, cw.g};
+        const int h = lg.r * a.grp + ra.head;
         const int64_t t = sg.first + ra.token;
-        const float sc = a.scale[sg.l];
+        const float sc = a.scale[lg.q];
         qs = score_scale(sc);
-        tl.load_q(a.q + a.qs.l * sg.l + a.qs.h * h + a.qs.n * t, hf, sc < 0.f);
-        out = a.out + a.os.l * sg.l + a.os.h * h + a.os.n * t;
+        tl.load_q(a.q + a.qs.l * lg.q + a.qs.h * h + a.qs.n * t, hf, sc < 0.f);
+        out = a.out + a.os.l * lg.q + a.os.h * h + a.os.n * t;
         if constexpr (KEYS == kStates) {
             lim = seen_by(a, t, sg.len) - 1;
             seen = limits<kFewRows>(p, sg, 0, lane).all;
@@ -805,7 +827,7 @@ attn_stream_kernel(StreamParams p) {
             end(whole);
             if (b + 1 < b1) {
                 const int old = blocks_of(sg);
-                if (step(cw, sg)) seg_start += old * a.Hkv;
+                if (step(cw, sg)) seg_start += old * heads;
                 begin();
             }
         } else {
@@ -849,9 +871,11 @@ attn_merge_stream_kernel(StreamParams p) {
     __shared__ float2 s_ms[GROUPS];
     __shared__ float4 s_o[GROUPS][LPP];
     const PackedParams& a = p.a;
-    const int i = (int)blockIdx.x / a.Hkv, g = (int)blockIdx.x % a.Hkv;
+    const int heads = KEYS == kStates ? p.heads : a.Hkv;
+    const int i = (int)blockIdx.x / heads, g = (int)blockIdx.x % heads;
+    const DivMod lg = KEYS == kStates ? uniform_div_mod(g, p.by_hkv) : DivMod{0, g};
     const int share = max(1, *p.share), start = p.start[i];     // (asked for with the segment; `start` is looked at if it has blocks)
-    const float qs = score_scale(a.scale[uniform_div_mod(i, p.by_layers).r]);
+    const float qs = score_scale(a.scale[KEYS == kStates ? lg.q : uniform_div_mod(i, p.by_layers).r]);
     const Segment x = uniform_segment<KEYS>(p, i);
     if ((int)blockIdx.y * p.join_rows >= x.rows) return;
     const int u0 = x.end == 0 ? 0 : start + g * blocks_of(x);
@@ -897,8 +921,8 @@ attn_merge_stream_kernel(StreamParams p) {
     if (mine == 0 && row < x.rows) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         const RowAt ra = row_at(row, p.grp);
-        const int h = g * a.grp + ra.head;
-        *(uint2*)(a.out + a.os.l * x.l + a.os.h * h + a.os.n * (int64_t)(x.first + ra.token) + 8 * c) =
+        const int h = lg.r * a.grp + ra.head, l = KEYS == kStates ? lg.q : x.l;
+        *(uint2*)(a.out + a.os.l * l + a.os.h * h + a.os.n * (int64_t)(x.first + ra.token) + 8 * c) =
             make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
     }
 }
@@ -1001,6 +1025,13 @@ template <int D, Keys KEYS>
 static hipError_t launch_stream(const pkv_packed& s, const PackedParams& a, void* ws, hipStream_t st) {
     StreamParams p;
     (Work&)p = work_of(s, a);
+    p.heads = s.Hkv;
+    p.by_hkv = fast_div(s.Hkv);
+    if (KEYS == kStates) {
+        p.heads = s.L * s.Hkv;
+        p.segs = s.S;
+        p.by_layers = fast_div(1);
+    }
     p.waves = stream_waves(s);
     p.share = (int*)ws;
     p.start = (int*)((char*)ws + 256);
@@ -1009,7 +1040,7 @@ static hipError_t launch_stream(const pkv_packed& s, const PackedParams& a, void
     const int rows = a.max_rows * a.grp;
     p.join_rows = rows <= 8 ? 1 : kJoinThreads / (D / 4);
     hipLaunchKernelGGL((attn_stream_kernel<D, KEYS>), dim3((unsigned)(p.waves / 2)), dim3(128), 0, st, p);
-    hipLaunchKernelGGL((attn_merge_stream_kernel<D, KEYS>), dim3((unsigned)(p.segs * s.Hkv), (unsigned)((rows + p.join_rows - 1) / p.join_rows)),
+    hipLaunchKernelGGL((attn_merge_stream_kernel<D, KEYS>), dim3((unsigned)(p.segs * p.heads), (unsigned)((rows + p.join_rows - 1) / p.join_rows)),
                        dim3(kJoinThreads), 0, st, p);
     return hipGetLastError();
 }
