@@ -158,6 +158,29 @@ def test_select_is_repeatable_and_replays_from_a_graph():
         assert all(torch.equal(a, b) for a, b in zip(P.prefixkv_beam_select(x, scores, ended=ended, end_token=end), want))
 
 
+def test_select_beams_that_have_all_ended_and_the_first_step():
+    """Ended beams go on as they are, the best first; a beam among dead ones fills all places."""
+    W, V, end = 6, 5000, 4999
+    x, scores, _ = select_inputs(21, 2, W, V, F32)
+    scores = torch.tensor([[-5.0, -1.0, -3.0, -1.0, -9.0, -2.0], [0.0] + [float("-inf")] * 5])
+    ended = torch.tensor([[True] * W, [False] * W])
+    got = P.prefixkv_beam_select(x.to(DEV), scores.to(DEV), ended=ended.to(DEV), end_token=end)
+    assert got[0][0].tolist() == [end] * W and got[1][0].tolist() == [1, 3, 5, 2, 0, 4] and bool(got[3][0].all())
+    assert got[2][0].tolist() == [-1.0, -1.0, -2.0, -3.0, -5.0, -9.0]
+    assert got[1][1].tolist() == [0] * W
+    check_select(x, scores, ended, end, got, ties=True)
+
+
+@pytest.mark.parametrize("S,W,V", [(2, 32, 3000), (1, 32, 600), (3, 16, 1500)])
+def test_select_one_beam_has_all_the_best(S, W, V):
+    """Scores far apart: a single beam's list holds the W best, more than a wavefront's worth of candidates around them."""
+    x, _, _ = select_inputs(S * V, S, W, V, BF16)
+    for scores in (torch.arange(W).float().expand(S, W) * -50.0, torch.zeros((S, W)) - 7.0):
+        x2 = x if scores[0, 1] < -40 else x[:, :1].expand(S, W, V).contiguous()      # equal beams: ties all over
+        scores = scores.contiguous()
+        check_select(x2, scores, None, None, P.prefixkv_beam_select(x2.to(DEV), scores.to(DEV)), ties=True)
+
+
 # ---- places -------------------------------------------------------------------------------------------
 def some_parents(r, G, W, empty=0.1):
     p = np.minimum((r.exponential(size=(G, W)) * W / 2.5).astype(np.int64), W - 1)
@@ -440,3 +463,53 @@ def test_beam_search_of_a_path(H, Hkv, D, ps, beams):
         scores, ended = choose(scores, ended, step)
     path.end(range(S))
     assert int(path.cache.state[1]) == 260 and np.array_equal(np.sort(path.cache.ring.cpu().numpy()), np.arange(260))
+
+
+def test_calls_on_two_streams_at_once():
+    """Each with outputs and workspaces of its own: the same bits as one after the other."""
+    S, W, V, layers, ps = 6, 4, 30011, 8, 16
+    x, scores, _ = (t if t is None else t.to(DEV) for t in select_inputs(31, S, W, V, BF16))
+    states = [page_state(40 + i, S * W, layers, ps, 8, 600, 100) for i in range(2)]
+    parents = i32(some_parents(np.random.default_rng(3), S, W, empty=0.0))
+    caches = [as_cache(*st, ps, 4, 128, BF16, 9 + i) for i, st in enumerate(states)]
+    want = P.prefixkv_beam_select(x, scores)
+    refs = []
+    for st, c in zip(states, caches):
+        refs.append(R.reorder(parents.cpu().numpy(), st[1], st[0], st[2], st[3], ps, [f64(c.kp), f64(c.vp)]))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for stream, c in zip(streams, caches):
+        with torch.cuda.stream(stream):
+            for _ in range(3):
+                got.append(P.prefixkv_beam_select(x, scores))
+            assert P.prefixkv_page_reorder(c, parents) is not None
+    torch.cuda.synchronize()
+    for g in got:
+        assert all(torch.equal(a, b) for a, b in zip(g[:3], want[:3]))
+    for (status, *ref), c in zip(refs, caches):
+        assert status == 0
+        check_cache(c, *ref[:4], ps, ref[4])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_reorder_pages_behind_the_first_four_gigabytes(dtype):
+    """A fork in the last pages of a pool of more than 2^32 bytes: rows of every head are copied, nothing else is touched."""
+    Hkv, D, ps, W, n = 4, 128, 256, 3, 700
+    page = Hkv * ps * D * torch.finfo(dtype).bits // 8
+    pages = (1 << 32) // page + 9
+    c = P.paged_cache(W, 1, Hkv, D, ps, pages, 4, dtype, DEV)
+    c.state.copy_(i32([pages - 8, 8]))                 # only the last eight pages are free
+    assert int(P.prefixkv_page_resize(c, i32([[n], [0], [0]]))) == 0
+    held = c.table[0, 0, :3].long()
+    for x, seed in ((c.kp, 1), (c.vp, 2)):
+        x[held] = torch.randn((3, Hkv, ps, D), generator=gen(seed)).to(dtype).to(DEV)
+        x[pages - 5:] = 7.0
+    assert int(P.prefixkv_page_reorder(c, i32([[0, 0, 0]]))) == 0
+    t = c.table[:, 0, :3].cpu()
+    assert bool((t[:, :2] == t[0, :2]).all()) and len(set(t[:, 2].tolist())) == 3 and int(t.min()) >= pages - 8
+    for x in (c.kp, c.vp):
+        for w in (1, 2):
+            assert torch.equal(x[int(t[w, 2]), :, :n - 2 * ps], x[int(t[0, 2]), :, :n - 2 * ps])
+            assert bool((x[int(t[w, 2]), :, n - 2 * ps:] == 7.0).all())
+        assert bool((x[pages - 3:] == 7.0).all())
