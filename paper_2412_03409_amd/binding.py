@@ -198,6 +198,9 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+# The current GPU's number without torch's look at whether it has been set up (there are tensors on it).
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
 # The current stream's handle without a Stream object around it (1.2 us a call), where torch has that.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -652,7 +655,7 @@ def _here(d: int, *ts) -> int:
     """The current stream's handle; d (a tensor's or a cache's GPU) has to be the current one, and every tensor on it."""
     if d < 0:
         raise ValueError("all tensors must be on the GPU")
-    if d != torch.cuda.current_device():
+    if d != _current_device():
         raise ValueError("all tensors must be on the current GPU")
     for t in ts:
         if t is not None and t.get_device() != d:
@@ -947,15 +950,28 @@ def cross_workspace_bytes(S: int, L: int, H: int, Hkv: int, T: int, M: int, D: i
                                                      _c_int(int(max_rows), "max_rows")))
 
 
+def _flat(t: torch.Tensor):
+    """What a check of a small tensor looks at."""
+    return t.shape, t.dtype, t.is_contiguous()
+
+
 @lru_cache(maxsize=512)
-def _cross_args(qsh, qst, qdt, ksh, kst, kdt, vsh, vst, vdt, osh, ost, odt, S, max_rows):
+def _cross_args(qsh, qst, qdt, ksh, kst, kdt, vsh, vst, vdt, osh, ost, odt, offs, states, scale, seen, max_rows):
     """Argument structs of rows q and out and of states k and v, and the call's workspace."""
     qs, ks, vs, os_ = (_row_strides(*a) for a in ((qsh, qst, qdt), (ksh, kst, kdt), (vsh, vst, vdt), (osh, ost, odt)))
     if osh != qsh or odt != qdt:
         raise ValueError("out must have the shape and dtype of q")
     if vsh != ksh or not (kdt == vdt == qdt) or (ksh[0], ksh[3]) != (qsh[0], qsh[3]):
         raise ValueError("k, v must be [L,Hkv,M,D] with q's dtype")
-    return (C.byref(_packed(S, ksh[1], qsh, qdt)), qs, ks, vs, os_,
+    for x, what in ((offs, "row_off"), (states, "state_off")):
+        if len(x[0]) != 1 or x != (offs[0], torch.int32, True):
+            raise ValueError(f"{what} must be contiguous i32 [S+1]")
+    if seen is not None and seen != (qsh[2:3], torch.int32, True):
+        raise ValueError("seen must be contiguous i32 [T]")
+    if scale != (qsh[:1], torch.float32, True):
+        raise ValueError("scale must be contiguous f32 [L]")
+    S, max_rows = offs[0][0] - 1, _c_int(max_rows, "max_rows")
+    return (C.byref(_packed(S, ksh[1], qsh, qdt)), qs, ks, vs, os_, ksh[2],
             cross_workspace_bytes(S, qsh[0], qsh[1], ksh[1], qsh[2], ksh[2], qsh[3], qdt, max_rows))
 
 
@@ -967,19 +983,18 @@ def prefixkv_cross_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_o
     None: all) -> out [L,H,T,D].  Rows that belong to no sequence are left as they are."""
     stream = _here(q.get_device(), k, v, row_off, state_off, scale, seen, out, ws)
     out = torch.empty_like(q) if out is None else out
-    max_rows, S, qsh = _c_int(index(max_rows), "max_rows"), row_off.numel() - 1, q.shape
-    s, qs, ks, vs, os_, need = _cross_args(qsh, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype,
-                                           out.shape, out.stride(), out.dtype, S, max_rows)
-    _i32_like(row_off, (S + 1,), "row_off")
-    _i32_like(state_off, (S + 1,), "state_off")
-    if seen is not None:
-        _i32_like(seen, (qsh[2],), "seen")
-    if scale.dtype is not torch.float32 or scale.shape != qsh[:1] or not scale.is_contiguous():
-        raise ValueError("scale must be contiguous f32 [L]")
-    w = _ws(need, q.device, ws)
-    rc = load().prefixkv_cross_attn(s, q.data_ptr(), qs, row_off.data_ptr(), k.shape[2], k.data_ptr(), ks, v.data_ptr(), vs,
-                                    state_off.data_ptr(), _ptr(seen), scale.data_ptr(), max_rows, out.data_ptr(), os_, w.data_ptr(),
-                                    w.numel() * w.element_size(), stream)
+    max_rows = index(max_rows)
+    s, qs, ks, vs, os_, M, need = _cross_args(q.shape, q.stride(), q.dtype, k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype,
+                                              out.shape, out.stride(), out.dtype, _flat(row_off), _flat(state_off), _flat(scale),
+                                              None if seen is None else _flat(seen), max_rows)
+    if ws is None:
+        ws = _ws(need, q.device, None)
+    nbytes = ws.numel() * ws.element_size()
+    if nbytes < need:
+        raise ValueError("workspace too small")
+    rc = load().prefixkv_cross_attn(s, q.data_ptr(), qs, row_off.data_ptr(), M, k.data_ptr(), ks, v.data_ptr(), vs, state_off.data_ptr(),
+                                    None if seen is None else seen.data_ptr(), scale.data_ptr(), max_rows, out.data_ptr(), os_,
+                                    ws.data_ptr(), nbytes, stream)
     if rc != 0:
         raise PrefixKVError(rc, "prefixkv_cross_attn")
     return out
@@ -987,30 +1002,31 @@ def prefixkv_cross_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_o
 
 # ---- several continuations of a prompt ---------------------------------------------------------------------
 @lru_cache(maxsize=256)
-def _beam_args(lsh, lst, ldt, ssh, sdt):
-    """Sizes, dtype, row stride and workspace of logits [S,W,V] with these scores."""
+def _beam_args(lsh, lst, ldt, scores, ended, end_token, tokens, parents, scores_out, ended_out):
+    """Sizes, dtype, row stride, the end token's number and the workspace, of logits [S,W,V] and of what _flat says of the others."""
     if len(lsh) != 3 or 0 in lsh or (lsh[2] > 1 and lst[2] != 1) or (lsh[0] > 1 and lsh[1] > 1 and lst[0] != lsh[1] * lst[1]):
         raise ValueError("logits must be [S,W,V], rows one stride apart, with V contiguous")
     if ldt not in _CODES:
         raise TypeError(f"unsupported storage dtype {ldt}")
-    if sdt is not torch.float32 or ssh != lsh[:2]:
+    if scores != (lsh[:2], torch.float32, True):
         raise ValueError("scores must be contiguous f32 [S,W]")
+    for x, dtype, what in ((ended, torch.bool, "ended"), (tokens, torch.int32, "tokens"), (parents, torch.int32, "parents"),
+                           (scores_out, torch.float32, "scores_out"), (ended_out, torch.bool, "ended_out")):
+        if x is not None and x != (lsh[:2], dtype, True):
+            raise ValueError(f"{what} must be contiguous {dtype} [S,W]")
+    if end_token is None and (ended is not None or ended_out is not None):
+        raise ValueError("beams end by an end_token")
+    if end_token is not None and not 0 <= end_token < lsh[2]:
+        raise ValueError("end_token must be a token")
     S, W, V = lsh
-    return S, W, V, _CODES[ldt], lst[1] if W > 1 else lst[0] if S > 1 else V, beam_workspace_bytes(S, W, V, ldt)
+    stride = lst[1] if W > 1 else lst[0] if S > 1 else V
+    return S, W, V, _CODES[ldt], stride, -1 if end_token is None else end_token, beam_workspace_bytes(S, W, V, ldt)
 
 
 def beam_workspace_bytes(S: int, W: int, V: int, dtype: torch.dtype) -> int:
     if dtype not in _CODES:
         raise TypeError(f"unsupported storage dtype {dtype}")
     return int(load().prefixkv_beam_workspace_bytes(_c_int(index(S), "S"), _c_int(index(W), "W"), _c_int(index(V), "V"), _CODES[dtype]))
-
-
-def _like(t: Optional[torch.Tensor], shape, dtype, device, what: str) -> torch.Tensor:
-    if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{what} must be contiguous {dtype} {list(shape)}")
-    return t
 
 
 def prefixkv_beam_select(logits: torch.Tensor, scores: torch.Tensor, ended: Optional[torch.Tensor] = None,
@@ -1020,27 +1036,25 @@ def prefixkv_beam_select(logits: torch.Tensor, scores: torch.Tensor, ended: Opti
     """The W best continuations of every prompt: logits [S,W,V] (bf16 or f32), scores [S,W] f32, ended [S,W] bool (with an
     end_token) -> (tokens [S,W] i32, parents [S,W] i32, scores_out [S,W] f32, ended_out [S,W] bool or None).  -1 where there are
     fewer; scores_out may be scores, ended_out may be ended."""
-    d = logits.get_device()
-    stream = _here(d, scores, ended, tokens, parents, scores_out, ended_out, ws)
-    S, W, V, code, stride, need = _beam_args(logits.shape, logits.stride(), logits.dtype, scores.shape, scores.dtype)
-    if not scores.is_contiguous():
-        raise ValueError("scores must be contiguous f32 [S,W]")
-    end = -1 if end_token is None else _c_int(index(end_token), "end_token")
-    if end_token is None and (ended is not None or ended_out is not None):
-        raise ValueError("beams end by an end_token")
-    if end_token is not None and not 0 <= end < V:
-        raise ValueError("end_token must be a token")
-    shape, dev = scores.shape, logits.device
-    if ended is not None:
-        _like(ended, shape, torch.bool, dev, "ended")
-    tokens = _like(tokens, shape, torch.int32, dev, "tokens")
-    parents = _like(parents, shape, torch.int32, dev, "parents")
-    scores_out = _like(scores_out, shape, torch.float32, dev, "scores_out")
-    ended_out = None if end < 0 else _like(ended_out, shape, torch.bool, dev, "ended_out")
-    w = _ws(need, dev, ws)
+    stream = _here(logits.get_device(), scores, ended, tokens, parents, scores_out, ended_out, ws)
+    S, W, V, code, stride, end, need = _beam_args(
+        logits.shape, logits.stride(), logits.dtype, _flat(scores), None if ended is None else _flat(ended),
+        None if end_token is None else index(end_token), None if tokens is None else _flat(tokens),
+        None if parents is None else _flat(parents), None if scores_out is None else _flat(scores_out),
+        None if ended_out is None else _flat(ended_out))
+    if tokens is None or parents is None or scores_out is None or (ended_out is None and end >= 0) or ws is None:
+        new = lambda dtype: torch.empty((S, W), dtype=dtype, device=logits.device)
+        tokens = new(torch.int32) if tokens is None else tokens
+        parents = new(torch.int32) if parents is None else parents
+        scores_out = new(torch.float32) if scores_out is None else scores_out
+        ended_out = new(torch.bool) if ended_out is None and end >= 0 else ended_out
+        ws = _ws(need, logits.device, ws)
+    nbytes = ws.numel() * ws.element_size()
+    if nbytes < need:
+        raise ValueError("workspace too small")
     rc = load().prefixkv_beam_select(S, W, V, code, logits.data_ptr(), stride, scores.data_ptr(), _ptr(ended), end,
-                                     tokens.data_ptr(), parents.data_ptr(), scores_out.data_ptr(), _ptr(ended_out), w.data_ptr(),
-                                     w.numel() * w.element_size(), stream)
+                                     tokens.data_ptr(), parents.data_ptr(), scores_out.data_ptr(), _ptr(ended_out), ws.data_ptr(),
+                                     nbytes, stream)
     if rc != 0:
         raise PrefixKVError(rc, "prefixkv_beam_select")
     return tokens, parents, scores_out, ended_out
