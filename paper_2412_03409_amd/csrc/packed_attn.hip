@@ -675,6 +675,10 @@ struct StreamParams : Work {
     float2* part_ms;
 };
 constexpr int kLeastBlocks = 2;     // of a wavefront
+// Over states: one, and up to four where a unit would be cut into more parts than these.  us, one / two / four blocks at least: a row over 577
+// states, H32/8, 10.3 / 12.2 / 15.4; 4 rows of 4 sequences over up to 3882, H32/4, 28.0 / 21.6 / 22.3; 8 rows of 2 over up to 4141, H32/8,
+// 33.0 / 23.7 / 23.5.
+constexpr int kManyParts = 40;
 
 __device__ __forceinline__ int blocks_of(const Segment& x) { return (x.end + kBlockKeys - 1) / kBlockKeys; }
 
@@ -695,7 +699,15 @@ attn_stream_kernel(StreamParams p) {
     auto blocks = [&](const Segment& x) { return (int64_t)blocks_of(x) * heads; };
     const Looked<KEYS, int64_t, decltype(blocks)> looked(p, lane, p.segs, 0, 1, blocks);
     const int all_blocks = (int)looked.all;                                // (below 2^31: the call is refused otherwise)
-    const int share = max(kLeastBlocks, (all_blocks + p.waves - 1) / p.waves);
+    int least = kLeastBlocks;
+    if constexpr (KEYS == kStates) {
+        int longest = blocks_of(looked.mine);
+        for (int i = lane + kWave; i < p.segs; i += kWave) longest = max(longest, blocks_of(segment<KEYS>(p, i)));
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) longest = max(longest, __shfl_xor(longest, d, kWave));
+        least = max(1, min(4, __builtin_amdgcn_readfirstlane(longest) / kManyParts));
+    }
+    const int share = max(least, (all_blocks + p.waves - 1) / p.waves);
     if (wave == 0 && lane == 0) *p.share = share;
     const int b0 = (int)min((int64_t)wave * share, (int64_t)all_blocks), b1 = (int)min((int64_t)b0 + share, (int64_t)all_blocks);
     if (b0 >= b1) return;
