@@ -4,11 +4,13 @@
 // of one pass, before its log-sum-exp is known; beams meet in a second, small launch.
 //
 //  beam_scan_kernel   a workgroup has a piece of a row, in registers: its maximum, the sum of its exponentials and its W largest logits.
-//                     Which these are: the W-th largest of the threads' maxima is below W logits at least, so only the W threads
-//                     that reach it hold candidates, a few more than W on the whole; each finds its rank by counting.
-//                     Bound: HBM, one read of the logits.
+//                     Which these are: W logits at least reach the W-th largest of the threads' maxima (or one up to W / 2 places
+//                     below it, which is found in fewer steps), so only the threads whose maximum reaches it hold candidates, little more
+//                     than W on the whole; each finds its rank by counting.
+//                     Bound: HBM, one read of the logits; with 32 beams the choice beside it (590 vector instructions of a wavefront).
+//                     64 x 4 rows of 128000 in fp32 22.7 us (5.8 TB/s); 8 x 32 rows of 100003 in bf16 19.7 (2.6 TB/s); 4 rows of 32000 5.9.
 //  beam_join_kernel   a workgroup has a prompt: log-sum-exp of the rows from their pieces, then the same choice among the pieces'
-//                     lists (the W-th largest of their first entries leaves W lists of W entries).
+//                     lists by their first entries.  Bound: dependent steps of one workgroup.  The same calls: 5.9, 10.4, 5.0 us.
 //
 // A sum of exponentials of a piece is held in 32 bits (terms of a thread, then a tree); pieces, logarithms and scores in 64, because
 // beams are told apart by differences that 32 bits of a score of -10^2 do not hold.

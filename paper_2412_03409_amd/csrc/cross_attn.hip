@@ -3,8 +3,8 @@
 //
 //  cross_tiles_kernel  A workgroup has 128 rows of one (sequence, KV head) and a piece of the states, which stream through LDS 64 at a
 //                      time (asynchronous copies, two buffer pairs); a wavefront has 32 rows.  Bound: the matrix cores and the softmax
-//                      next to them.
-//  cross_merge_kernel  joins the pieces of a tile.
+//                      next to them.  Two texts of up to 4001 rows over up to 6001 states, H32/8: 444 GFLOP in 455 ... 490 us.
+//  cross_merge_kernel  joins the pieces of a tile.  Bound: HBM, 66 KB of a part, and the launch: 5 ... 10 us.
 //
 // How long the sequences and their states are is known on the device only, and a launch of a workgroup per tile takes as long as its
 // longest one.  So every workgroup adds up the stages of all tiles, one lane per sequence, and takes the same cap: no piece has more than

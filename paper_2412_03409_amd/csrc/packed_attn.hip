@@ -10,7 +10,8 @@
 //  attn_stream_kernel bf16, at most 32 rows per (sequence, KV head): decode steps.  A wavefront streams 32 keys at a time through
 //                     LDS of its own.  All keys of a launch are one sequence of blocks that the wavefronts share out evenly,
 //                     wherever the units begin and end.  Bound: HBM; 467 MB of keys and values of 32 sequences in 90 us, 5.2 TB/s
-//                     (a plain read reaches 5.8), and 5 us to join.
+//                     (a plain read reaches 5.8), and 5 us to join.  States of 32 sequences of up to 2880, 4 rows of 32 heads each, 777 MB:
+//                     144 ... 149 us and 10 to join; 577 states for one row, 32 heads: 7.3 + 4.8, the latency of both launches.
 //  attn_merge_*       join the parts of a tile or unit that several workgroups or wavefronts worked on.
 //  attn_rows_kernel   fp32: a workgroup per (row, head, layer).  The keys stream past one row: LPR lanes hold a key
 //                     row, scores meet by shuffles, softmax online (running maximum and sum, everything fp32); the four
