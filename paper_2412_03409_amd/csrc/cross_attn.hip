@@ -9,7 +9,9 @@
 // How long the sequences and their states are is known on the device only, and a launch of a workgroup per tile takes as long as its
 // longest one.  So every workgroup adds up the stages of all tiles, one lane per sequence, and takes the same cap: no piece has more than
 // a kPieces-th of all stages (kLeastStages at least).  Then there are kPieces pieces more than tiles at most, which bounds the grid, and at most
-// 2 kPieces of tiles that are cut, which bounds the workspace.
+// 2 kPieces of tiles that are cut, which bounds the workspace.  Rows that see the first states only leave such a plan uneven: where the work
+// is large, a launch of its own (cross_plan_kernel, 6 to 7 us) looks at what each tile sees first, gives its pieces that length, and begins with the longest.
+// 6 texts of up to 700 rows over up to 2885 states, H32/8, 13.7 GFLOP: 6.5 + 32 + 8.5 us (without 49 + 10).
 //
 // Stages that some rows see and others do not are masked, and a probability of 0 times an infinite or NaN value that such a row must not
 // see would spoil it.  To look for such values in every masked stage costs a third of it, so a tile is worked on without, and again with
@@ -31,10 +33,12 @@ struct CrossParams {
     const float* scale;
     float* part_o;                      // workspace [2 * kPieces][4 wavefronts][32 * D], as registers are
     float2* part_ms;                    // [2 * kPieces][4 wavefronts][64]: {maximum, sum}; sum 0: nothing seen, no numerators
+    int4* planned;                      // {places, pieces of cut tiles, cut tiles, 0} of a head, then two a place, then two a cut tile
 };
 // (320, 384, 512, 768, 1024 pieces: 21.9, 21.8, 22.3, 22.8, 23.3 us, the geometric mean of 70 calls of all sizes; at least 8 stages a piece: 22.2)
 constexpr int kPieces = 384;
 constexpr int kLeastStages = 4;
+constexpr int kManyTiles = 2048;        // from which on no tile is cut
 
 struct Text { int s, first, rows, from, len; };     // rows: of the call, times the heads of a KV head; from, len: its states
 __device__ __forceinline__ Text text_of(const CrossParams& p, int s) {
@@ -151,8 +155,132 @@ __device__ __forceinline__ Limits limits(const CrossParams& p, const Text& x, in
     return {__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(hi)};
 }
 
-// SEEN: rows see the first states only.  CUT: tiles may be cut.
-template <int D, bool SEEN, bool CUT>
+// The same plan where rows see the first states only, by what some row of each tile sees: written out, a list of places and one of cut tiles.
+struct Place { Text text; int tile, pieces, piece, slot, end, all; };       // slot: of the tile's first part; end, all: states that some, and all of its rows see
+constexpr int kPlanThreads = 1024;      // texts at most
+constexpr int kPlaces = kManyTiles + kPieces;
+constexpr size_t kPlanBytes = (1 + 2 * (kPlaces + kPieces)) * sizeof(int4);
+static_assert(kPieces < 512 && kManyTiles == 2 * kPlanThreads, "nine bits in a place; two tiles a thread");
+__device__ __forceinline__ void write_place(int4* to, const Place& x) {
+    to[0] = make_int4(x.text.first, x.text.rows, x.text.from, x.text.len);
+    to[1] = make_int4(x.tile, x.pieces | x.piece << 9 | x.slot << 18, x.end, x.all);
+}
+__device__ __forceinline__ Place read_place(const int4* from) {
+    const int4 a = from[0], b = from[1];
+    return {{0, a.x, a.y, a.z, a.w}, b.x, b.y & 511, b.y >> 9 & 511, b.y >> 18, b.z, b.w};
+}
+// sums of x over the threads 0 ... threadIdx.x, and of all
+template <typename T>
+__device__ __forceinline__ T block_sums(T x, T* cells, T& all) {
+    const int lane = threadIdx.x & (kWave - 1), wv = threadIdx.x / kWave;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        const T up = __shfl_up(x, d, kWave);
+        if (lane >= d) x += up;
+    }
+    if (lane == kWave - 1) cells[wv] = x;
+    __syncthreads();
+    T before = 0;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < kPlanThreads / kWave; ++w) {
+        if (w < wv) before += cells[w];
+        all += cells[w];
+    }
+    return before + x;
+}
+__global__ void __launch_bounds__(kPlanThreads)
+cross_plan_kernel(CrossParams p) {
+    constexpr int kGroup = 16;          // lanes that look at a tile's rows
+    constexpr int kLengths = 16;        // classes of pieces, the longest first
+    __shared__ Text s_text[kPlanThreads];
+    __shared__ int s_upto[kPlanThreads], s_at[kManyTiles], s_end[kManyTiles], s_all[kManyTiles];
+    __shared__ int s_tiles[kPlanThreads / kWave];
+    __shared__ double s_work[kPlanThreads / kWave];
+    __shared__ uint32_t s_sums[kPlanThreads / kWave];
+    __shared__ int s_length[kLengths], s_next[kLengths];
+    const int tid = threadIdx.x;
+    if (tid < kLengths) s_length[tid] = s_next[tid] = 0;
+    int tiles = 0;
+    if (tid < p.S) {
+        s_text[tid] = text_of(p, tid);
+        tiles = tiles_of(s_text[tid]);
+    }
+    int all;
+    s_upto[tid] = block_sums(tiles, s_tiles, all);
+    all = min(all, kManyTiles);                                 // (more only where texts overlap)
+    __syncthreads();
+    for (int i = tid / kGroup; i < all; i += kPlanThreads / kGroup) {
+        int s = 0, behind = p.S - 1;                            // the first text whose sum is above i
+        while (s < behind) {
+            const int mid = (s + behind) / 2;
+            if (s_upto[mid] > i) behind = mid;
+            else s = mid + 1;
+        }
+        const Text t = s_text[s];
+        const int tile = i - (s == 0 ? 0 : s_upto[s - 1]), r0 = tile * kTileRows;
+        const int from = row_at(r0, p.by_grp).token, to = row_at(min(r0 + kTileRows, t.rows) - 1, p.by_grp).token;
+        int lo = t.len, hi = 0;
+#pragma unroll 4
+        for (int k = from + tid % kGroup; k <= to; k += kGroup) {
+            const int n = max(0, min(p.seen[t.first + k], t.len));
+            lo = min(lo, n);
+            hi = max(hi, n);
+        }
+#pragma unroll
+        for (int d = kGroup / 2; d > 0; d >>= 1) {
+            lo = min(lo, __shfl_xor(lo, d, kWave));
+            hi = max(hi, __shfl_xor(hi, d, kWave));
+        }
+        if (tid % kGroup == 0) {
+            s_at[i] = s;
+            s_end[i] = hi;
+            s_all[i] = lo;
+        }
+    }
+    __syncthreads();
+    int stages[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) stages[k] = 2 * tid + k < all ? (s_end[2 * tid + k] + kStage - 1) / kStage : 0;
+    double work;
+    block_sums((double)stages[0] + (double)stages[1], s_work, work);
+    const int cap = max(kLeastStages, (int)fmin(work * p.heads / kPieces, 1e9) + 1);
+    // pieces of cut tiles and cut tiles in one sum; all pieces by their length, so that a launch does not end with its longest
+    uint32_t n[2];
+    int pieces[2], length[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        pieces[k] = 2 * tid + k < all ? max(1, (stages[k] + cap - 1) / cap) : 0;
+        n[k] = pieces[k] > 1 ? (uint32_t)pieces[k] | 1u << 16 : 0u;
+        const int most = pieces[k] > 1 ? (stages[k] + pieces[k] - 1) / pieces[k] : stages[k];
+        length[k] = most == 0 ? kLengths - 1 : kLengths - 2 - (int)((float)most * (kLengths - 1) / ((float)cap + 1.f));
+        if (pieces[k] > 0) atomicAdd(&s_length[length[k]], pieces[k]);
+    }
+    uint32_t sums, before = block_sums(n[0] + n[1], s_sums, sums) - n[0] - n[1];
+    int upto[kLengths], places = 0;
+#pragma unroll
+    for (int c = 0; c < kLengths; ++c) {
+        upto[c] = places;
+        places += s_length[c];
+    }
+    if (tid == 0) p.planned[0] = make_int4(places, (int)(sums & 0xffff), (int)(sums >> 16), 0);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        if (pieces[k] == 0) break;
+        const int i = 2 * tid + k, s = s_at[i];
+        Place x = {s_text[s], i - (s == 0 ? 0 : s_upto[s - 1]), pieces[k], 0, (int)(before & 0xffff), s_end[i], s_all[i]};
+        int first = 0;
+#pragma unroll
+        for (int c = 0; c < kLengths; ++c) first = c == length[k] ? upto[c] : first;
+        int4* to = p.planned + 1 + 2 * (first + atomicAdd(&s_next[length[k]], pieces[k]));
+        if (pieces[k] > 1) write_place(p.planned + 1 + 2 * (kPlaces + (int)(before >> 16)), x);
+        for (; x.piece < x.pieces; ++x.piece, to += 2) write_place(to, x);
+        before += n[k];
+    }
+}
+
+// SEEN: rows see the first states only.  CUT: tiles may be cut.  PLANNED: as cross_plan_kernel says.
+template <int D, bool SEEN, bool CUT, bool PLANNED>
 __global__ void __launch_bounds__(256, 2)
 cross_tiles_kernel(CrossParams p) {
     constexpr int ROWB = D * 2, kInst = CopyLane<D>::kCopies;               // copies per wavefront, stage and tensor: 16 rows
@@ -167,40 +295,60 @@ cross_tiles_kernel(CrossParams p) {
 
     // Which tile and piece.  With heads in eighths every head stays on one XCD, else they alternate; in a head text by text, the tiles of
     // a piece of the states one after the other, so that they are read through the same L2 at about the same time.
-    const Plan<false, CUT> plan(p, lane);
-    if (plan.places <= 0) return;
     int head, x;
-    if (p.heads_per_xcd > 0) {
-        const uint32_t j = blockIdx.x / kXcds, h = j / (uint32_t)plan.places;
-        if (h >= (uint32_t)p.heads_per_xcd) return;
-        head = (int)(blockIdx.x % kXcds) * p.heads_per_xcd + (int)h;
-        x = (int)(j - h * (uint32_t)plan.places);
-    } else {
+    auto place = [&](int places) {                                          // whether there is one
+        if (places <= 0) return false;
+        if (p.heads_per_xcd > 0) {
+            const uint32_t j = blockIdx.x / kXcds, h = j / (uint32_t)places;
+            head = (int)(blockIdx.x % kXcds) * p.heads_per_xcd + (int)h;
+            x = (int)(j - h * (uint32_t)places);
+            return h < (uint32_t)p.heads_per_xcd;
+        }
         const DivMod hx = uniform_div_mod((int)blockIdx.x, p.by_heads);
-        if (hx.q >= plan.places) return;
         head = hx.r; x = hx.q;
+        return hx.q < places;
+    };
+    Place at;
+    int cuts = 0;
+    if constexpr (PLANNED) {
+        const int4 sums = p.planned[0];
+        if (!place(sums.x)) return;
+        cuts = sums.y;
+        at = read_place(p.planned + 1 + 2 * x);
+    } else {
+        const Plan<false, CUT> plan(p, lane);
+        if (!place(plan.places)) return;
+        int in, cut_before;
+        at.text = plan.find(x, in, cut_before);
+        if (at.text.rows == 0) return;
+        const int tiles = tiles_of(at.text);
+        at.pieces = CUT ? pieces_of(at.text, plan.cap) : 1;
+        at.piece = CUT ? __builtin_amdgcn_readfirstlane((uint32_t)in / (uint32_t)tiles) : 0;
+        at.tile = in - at.piece * tiles;
+        at.slot = cut_before + at.tile * at.pieces;
+        cuts = plan.cuts;
+        at.end = at.all = at.text.len;
+        if constexpr (SEEN) {
+            const Limits tl = limits<kTileRows>(p, at.text, at.tile * kTileRows, lane);
+            at.end = tl.some; at.all = tl.all;
+        }
     }
-    int in, cut_before;
-    const Text t = plan.find(x, in, cut_before);
-    if (t.rows == 0) return;
+    const Text t = at.text;
+    const int tile = at.tile, pieces = at.pieces, piece = at.piece, end = at.end, all = at.all, ends = (end + kStage - 1) / kStage;
+    const int stages = PLANNED ? ends : stages_of(t);
     const DivMod lg = uniform_div_mod(head, p.by_hkv);                      // layer, KV head
-    const int tiles = tiles_of(t), stages = stages_of(t), pieces = CUT ? pieces_of(t, plan.cap) : 1;
-    const int piece = CUT ? __builtin_amdgcn_readfirstlane((uint32_t)in / (uint32_t)tiles) : 0, tile = in - piece * tiles;
-    const int st0 = CUT ? piece * stages / pieces : 0;
-    int st1 = CUT ? (piece + 1) * stages / pieces : stages;
+    const int st0 = CUT ? piece * stages / pieces : 0, st1 = CUT ? min((piece + 1) * stages / pieces, ends) : ends;
 
     // this wavefront's rows (those that do not exist repeat one that does)
     const int r0 = tile * kTileRows + wv * 32, row = r0 + ln;
     const bool mine = r0 < t.rows, real = row < t.rows;
     const int rr = real ? row : mine ? r0 : 0;
     const RowAt ra = row_at(rr, p.by_grp);
-    int end = t.len, all = t.len, lim = t.len - 1, lim_first = lim, lim_last = lim;     // states that some, and all rows of the tile see; the last one of the row, and of the wavefront's
+    int lim = t.len - 1, lim_first = lim, lim_last = lim;                   // the last state that the row sees, and the wavefront's rows
     if constexpr (SEEN) {
-        const Limits tl = limits<kTileRows>(p, t, tile * kTileRows, lane), w = limits<32>(p, t, mine ? r0 : 0, lane);
-        end = tl.some; all = tl.all;
+        const Limits w = limits<32>(p, t, mine ? r0 : 0, lane);
         lim = seen_by(p, t, rr) - 1;
         lim_first = w.all - 1; lim_last = w.some - 1;
-        st1 = min(st1, (end + kStage - 1) / kStage);
     }
     const int n = max(0, st1 - st0), plain = max(0, min(st1, all / kStage) - st0);
 
@@ -303,7 +451,7 @@ cross_tiles_kernel(CrossParams p) {
     if (!CUT || pieces == 1) {
         tl.store(p.out + p.os.l * lg.q + p.os.h * h + p.os.n * token, hf, sum == 0.f ? 0.f : 1.f / sum, real);
     } else {
-        const int64_t slot = ((int64_t)head * plan.cuts + cut_before + tile * pieces + piece) * 4 + wv;
+        const int64_t slot = ((int64_t)head * cuts + at.slot + piece) * 4 + wv;
         if (n > 0) tl.store_tile(p.part_o + slot * 32 * D, p.part_ms + slot * kWave, lane, sum);
         else p.part_ms[slot * kWave + lane] = make_float2(-INFINITY, 0.f);
     }
@@ -311,23 +459,38 @@ cross_tiles_kernel(CrossParams p) {
 
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 // Joins the pieces of a tile: a wavefront has 32 columns of 32 rows, in the registers' order, in which the pieces were written.
-template <int D>
+template <int D, bool PLANNED>
 __global__ void __launch_bounds__(256)
 cross_merge_kernel(CrossParams p) {
     const int lane = threadIdx.x & (kWave - 1), wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), dt = (int)blockIdx.y;
     const int ln = lane & 31, hf = lane >> 5;
-    const Plan<true, true> plan(p, lane);
-    if (plan.places <= 0) return;
-    const int head = __builtin_amdgcn_readfirstlane(blockIdx.x / (uint32_t)plan.places);
-    if (head >= p.heads) return;
-    int in, cut_before;
-    const Text t = plan.find((int)blockIdx.x - head * plan.places, in, cut_before);
-    if (t.rows == 0) return;
-    const int pieces = pieces_of(t, plan.cap), r0 = in * kTileRows + wv * 32, row = r0 + ln;
+    int head, cuts;
+    Place at;
+    if constexpr (PLANNED) {
+        const int4 sums = p.planned[0];
+        if (sums.z <= 0) return;
+        head = __builtin_amdgcn_readfirstlane(blockIdx.x / (uint32_t)sums.z);
+        if (head >= p.heads) return;
+        cuts = sums.y;
+        at = read_place(p.planned + 1 + 2 * (kPlaces + (int)blockIdx.x - head * sums.z));
+    } else {
+        const Plan<true, true> plan(p, lane);
+        if (plan.places <= 0) return;
+        head = __builtin_amdgcn_readfirstlane(blockIdx.x / (uint32_t)plan.places);
+        if (head >= p.heads) return;
+        int cut_before;
+        at.text = plan.find((int)blockIdx.x - head * plan.places, at.tile, cut_before);
+        if (at.text.rows == 0) return;
+        at.pieces = pieces_of(at.text, plan.cap);
+        at.slot = cut_before + at.tile * at.pieces;
+        cuts = plan.cuts;
+    }
+    const Text t = at.text;
+    const int pieces = at.pieces, r0 = at.tile * kTileRows + wv * 32, row = r0 + ln;
     if (r0 >= t.rows) return;
     const DivMod lg = uniform_div_mod(head, p.by_hkv);
     const float qs = score_scale(p.scale[lg.q]);
-    const int64_t first = (int64_t)head * plan.cuts + cut_before + in * pieces;
+    const int64_t first = (int64_t)head * cuts + at.slot;
     float m = -INFINITY, sum = 0.f;
     f32x16_t o;
 #pragma unroll
@@ -375,20 +538,30 @@ static long long all_tiles(const pkv_packed& s) {
 // up to 3350 states and 20 rows 71 / 31; H16/8, one of 1827 and 238 rows 39 / 27; H40/40, 3 of up to 186 and 2872 rows 46 / 54; H32/4, 44
 // of up to 179 and 5 rows 8.6 / 13; H40/40, 3 of up to 839 and 3909 rows, D 64, 69 / 74 (cut all the same).
 constexpr double kCutStages = 8.0;
-constexpr int kManyTiles = 2048;
 static bool may_cut(const pkv_packed& s, int M) { return 1.5 * M / s.S / kStage > kCutStages && all_tiles(s) < kManyTiles; }
 
 size_t cross_tiles_ws_bytes(const pkv_packed& s, int M) {
-    return may_cut(s, M) ? (size_t)2 * kPieces * kTileRows * (s.D * sizeof(float) + 2 * sizeof(float2)) : 0;
+    return may_cut(s, M) ? (size_t)2 * kPieces * kTileRows * (s.D * sizeof(float) + 2 * sizeof(float2)) + kPlanBytes : 0;
+}
+
+// Whether what the rows see is looked at first.  The launch costs 4 to 6 us; pieces of one length, and the longest first, are worth more where
+// the compute units' 512 workgroups have 16 stages each, if rows saw all.  us, without / with: H28/4, 25 rows over 2859 states 26 / 30; 5 texts of up
+// to 35 rows over 4377, H12/4, 25 / 31; 6 of up to 700 over 2885, H32/8, 59 / 48; 10 of up to 343 over 7463, H32/4, 88 / 67; of 70 calls, the 33 above: 0.94.
+constexpr double kPlanStages = 512 * 16.0;
+static bool look_first(const pkv_packed& s, int M) {
+    return s.S <= kPlanThreads && (double)all_tiles(s) * M / s.S / kStage >= kPlanStages;
 }
 
 template <int D>
-static hipError_t launch(const CrossParams& p, long long tiles, bool cut, hipStream_t st) {
+static hipError_t launch(const CrossParams& p, long long tiles, bool cut, bool look, hipStream_t st) {
     const dim3 grid((unsigned)(tiles + (cut ? kPieces : 0)));
-    auto* kernel = cut ? (p.seen ? cross_tiles_kernel<D, true, true> : cross_tiles_kernel<D, false, true>)
-                       : (p.seen ? cross_tiles_kernel<D, true, false> : cross_tiles_kernel<D, false, false>);
+    auto* kernel = look ? cross_tiles_kernel<D, true, true, true>
+                 : cut ? (p.seen ? cross_tiles_kernel<D, true, true, false> : cross_tiles_kernel<D, false, true, false>)
+                       : (p.seen ? cross_tiles_kernel<D, true, false, false> : cross_tiles_kernel<D, false, false, false>);
+    auto* merge = look ? cross_merge_kernel<D, true> : cross_merge_kernel<D, false>;
+    if (look) hipLaunchKernelGGL(cross_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, p);
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, p);
-    if (cut) hipLaunchKernelGGL(cross_merge_kernel<D>, dim3(kPieces, D / 32), dim3(256), 0, st, p);
+    if (cut) hipLaunchKernelGGL(merge, dim3(kPieces, D / 32), dim3(256), 0, st, p);
     return hipGetLastError();
 }
 
@@ -404,8 +577,9 @@ hipError_t launch_cross_tiles(const pkv_packed& s, const PackedAttn& a, hipStrea
     p.row_off = a.row_off; p.state_off = a.state_off; p.seen = a.seen; p.scale = a.scale;
     p.part_o = (float*)a.ws;
     p.part_ms = (float2*)(p.part_o + (size_t)2 * kPieces * kTileRows * s.D);
-    const bool cut = may_cut(s, a.M);
-    return s.D == 128 ? launch<128>(p, all_tiles(s), cut, st) : launch<64>(p, all_tiles(s), cut, st);
+    p.planned = (int4*)(p.part_ms + (size_t)2 * kPieces * 4 * kWave);
+    const bool cut = may_cut(s, a.M), look = cut && a.seen && look_first(s, a.M);
+    return s.D == 128 ? launch<128>(p, all_tiles(s), cut, look, st) : launch<64>(p, all_tiles(s), cut, look, st);
 }
 
 }  // namespace pkv

@@ -209,3 +209,110 @@ def test_states_behind_the_first_four_gigabytes(dtype):
         far.append(y)
     assert torch.equal(P.prefixkv_cross_attn(q, *far, i32(off), i32(to), scale, 67), want)
     assert torch.equal(P.prefixkv_cross_attn(q, *far, i32([0, 3, 6]), i32(to), scale, 3)[:, :, :6], few[:, :, :6])
+
+
+def large(seed, n, m, H, Hkv, D, heads_tiles=230, **kw):
+    """Inputs with so many rows and states of nobody that a call looks at what the rows see before it shares them out."""
+    S, grp = len(n), H // Hkv
+    T = heads_tiles // Hkv * 128 // grp
+    M = S * 64 * (8192 // heads_tiles + 3)
+    q, k, v, off, to, scale = inputs(seed, 1, H, Hkv, n, m, D, BF16, pad=max(0, T - sum(n)), behind=max(0, M - sum(m)), **kw)
+    tiles = (q.shape[2] * grp // 128 + min(S, q.shape[2])) * Hkv
+    assert tiles < 2048 and tiles * k.shape[2] / S / 64 >= 8192
+    return q, k, v, off, to, scale
+
+
+LARGE = [  # rows, states, H, Hkv, D
+    ([40], [2600], 2, 2, 128), ([33, 1, 129], [64, 1, 2130], 6, 2, 64), ([200, 0, 70], [0, 3000, 900], 3, 3, 128), ([128, 64], [65, 6000], 2, 1, 64),
+    ([5, 90], [700, 2], 12, 4, 128), ([17, 100, 3, 64], [1300, 1000, 10, 4097], 8, 1, 64), ([1, 34], [5000, 3], 8, 8, 64),
+]
+
+
+@pytest.mark.parametrize("n,m,H,Hkv,D", LARGE)
+@pytest.mark.parametrize("what", ["any", "rising", "few", "none", "all"])
+def test_cross_attn_shared_out_by_what_rows_see(n, m, H, Hkv, D, what):
+    q, k, v, off, to, scale = large(sum(n) + H, n, m, H, Hkv, D, first=3, before=7)
+    T = q.shape[2]
+    r = np.random.default_rng(sum(m))
+    seen = {"any": r.integers(-3, max(m) + 5, size=T), "rising": (np.arange(T) - 3) * max(m) // sum(n), "few": np.minimum(3, r.integers(0, 40, size=T)),
+            "none": np.full(T, -1), "all": np.full(T, 1 << 30)}[what].clip(-(1 << 31), 1 << 30)
+    for s in range(len(n)):                                     # what no row sees
+        rows = seen[off[s]:off[s + 1]]
+        most = int(np.clip(rows, 0, m[s]).max()) if len(rows) else 0
+        k[:, :, to[s] + most:to[s + 1]] = float("nan")
+        v[:, :, to[s] + most:to[s + 1]] = float("inf")
+    check(q, k, v, off, to, scale, max(n), seen)
+    check(q, k, v, off, to, scale, 35, seen, max_rows=35)
+
+
+def test_cross_attn_shared_out_values_that_some_rows_must_not_see():
+    n, m = [64, 40], [3000, 500]
+    q, k, v, off, to, scale = large(21, n, m, 4, 2, 64)
+    seen = np.full(q.shape[2], 1 << 20)
+    seen[:30], seen[70:90] = 1111, 130
+    v[:, :, 1111, ::3] = float("inf")
+    v[:, :, to[1] + 130, 5] = float("nan")
+    out = P.prefixkv_cross_attn(q, k, v, i32(off), i32(to), scale, 64, seen=i32(seen))
+    want, mag = R.cross(f64(q), off, f64(k), f64(v), to, scale.double().cpu().numpy(), seen)
+    want, mag, out = want[:, :, :104], mag[:, :, :104], out[:, :, :104]
+    finite = np.isfinite(want) & np.isfinite(mag)
+    assert not finite.all() and finite[:, :, :30].all() and finite[:, :, 70:90].all()
+    here = torch.from_numpy(finite).to(DEV)
+    assert bool((~torch.isfinite(out.float()))[~here].all())
+    close(torch.where(here, out, torch.zeros_like(out)), np.where(finite, want, 0.0), np.where(finite, mag, 0.0), BF16)
+
+
+def test_cross_attn_shared_out_among_many_texts():
+    """More texts than there are lanes, most of them short; and as many as a call is shared out for, and one more."""
+    n = [1 + i % 4 for i in range(100)]
+    n[41], n[99] = 150, 40
+    m = [(37 * i) % 200 for i in range(100)]
+    m[41], m[99] = 2500, 300
+    for S in (100, 1024, 1025):
+        rows, states = n + [1] * (S - 100), m + [9] * (S - 100)
+        q, k, v, off, to, scale = inputs(22, 1, 1, 1, rows, states, 64, BF16, pad=20000, behind=S * 64 * (8192 // (20000 // 128 + S) + 2))
+        assert (q.shape[2] // 128 + S) * k.shape[2] / S / 64 >= 8192 and q.shape[2] // 128 + S < 2048
+        check(q, k, v, off, to, scale, 150, np.arange(q.shape[2]) % 2000)
+
+
+def test_cross_attn_shared_out_offsets_that_cannot_be():
+    q, k, v, _, _, scale = large(23, [50, 50, 50], [900, 900, 900], 2, 2, 64)
+    T, M = q.shape[2], k.shape[2]
+    seen = np.arange(T) * 7
+    for off, to, good in (([0, 60, 40, 150], [0, 900, 1800, 2700], {0: (0, 60), 2: (40, 150)}), ([-1, 50, 100, T + 1], [0, 900, 1800, 2700], {1: (50, 100)}),
+                          ([0, 50, 100, 150], [0, 900, 800, M + 1], {0: (0, 50)}), ([0, 50, 100, 150], [-5, 900, 1800, M], {1: (50, 100), 2: (100, 150)})):
+        out = torch.full_like(q, 9.0)
+        P.prefixkv_cross_attn(q, k, v, i32(off), i32(to), scale, 110, seen=i32(seen), out=out)
+        for s in range(3):
+            a, b, x, y = off[s], off[s + 1], to[s], to[s + 1]
+            if s not in good:
+                if 0 <= a < b <= T:
+                    assert bool((out[:, :, a:b] == 0).all())
+                continue
+            if off[1] > off[2]:                                 # rows of two texts: either's answer
+                a, b = (a, 40) if s == 0 else (60, b)
+            want, mag = R.cross(f64(q), [a, b], f64(k), f64(v), [x, y], scale.double().cpu().numpy(), seen)
+            close(out[:, :, a:b], want[:, :, a:b], mag[:, :, a:b], BF16)
+        assert bool((out[:, :, 150:] == 9).all())
+
+
+def test_cross_attn_shared_out_is_repeatable_and_replays_from_a_graph():
+    n, m, H, Hkv, D = [150, 9, 40], [3000, 500, 2000], 8, 2, 128
+    q, k, v, off, to, scale = large(24, n, m, H, Hkv, D)
+    T, M = q.shape[2], k.shape[2]
+    off, to = i32(off), i32(to)
+    lims = [i32(np.arange(T) * 20), i32(3000 - np.arange(T) * 17)]
+    wants = [P.prefixkv_cross_attn(q, k, v, off, to, scale, 150, seen=x, out=torch.zeros_like(q)) for x in lims]
+    ws = torch.empty(P.cross_workspace_bytes(3, 1, H, Hkv, T, M, D, BF16, 150), dtype=torch.uint8, device=DEV)
+    out, seen = torch.zeros_like(q), lims[0].clone()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        P.prefixkv_cross_attn(q, k, v, off, to, scale, 150, seen=seen, out=out, ws=ws)
+    for i in range(6):
+        seen.copy_(lims[i % 2])
+        out.zero_()
+        ws.fill_(255 * (i // 2 % 2))
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, wants[i % 2])
+        assert torch.equal(P.prefixkv_cross_attn(q, k, v, off, to, scale, 150, seen=lims[i % 2], out=torch.zeros_like(q)), wants[i % 2])
