@@ -450,7 +450,8 @@ int prefixkv_chunk_attn(const pkv_packed *shape, const void *q, pkv_strides qs, 
  *   row_off [dev] i32 [S+1];  state_off [dev] i32 [S+1], non-decreasing, 0 ... M: no states between equal ones
  *   seen [dev] i32 [T] or NULL; below 0 is 0, above the number of states all of them
  *   max_rows: no sequence has more rows in this call (1 <= max_rows <= T); further ones are left as they are.  It chooses the kernel.
- *   ws [dev]: prefixkv_cross_workspace_bytes(shape, M, max_rows) bytes, 16-byte aligned (NULL if that is 0)
+ *   ws [dev]: prefixkv_cross_workspace_bytes(shape, M, max_rows) bytes, any contents, 16-byte aligned (NULL if that is 0).  Calls on
+ *       different streams need workspaces of their own.
  * 1 <= M <= 2^22.  The limits on T, S and the tiles are those of the two attention calls above; (M/32 + S) * L * Hkv < 2^31. */
 size_t prefixkv_cross_workspace_bytes(const pkv_packed *shape, int M, int max_rows);
 int prefixkv_cross_attn(const pkv_packed *shape, const void *q, pkv_strides qs, const int32_t *row_off, int M, const void *k,
@@ -459,7 +460,8 @@ int prefixkv_cross_attn(const pkv_packed *shape, const void *q, pkv_strides qs, 
 
 /* ==== Several continuations of a prompt (beam search) ==================================================
  * W beams of a prompt have W places of the paged cache, one behind the other.  After a step, prefixkv_beam_select names the W best
- * of all their continuations, and prefixkv_page_reorder makes the places what their new beams continue.
+ * of all their continuations, and prefixkv_page_reorder makes the places what their new beams continue.  Calls on different streams
+ * need workspaces of their own.
  *
  * prefixkv_beam_select: beam w of prompt s by token v has the score
  *   scores[s,w] + x[v] - log sum_u exp x[u],   x = logits[s,w,:].
