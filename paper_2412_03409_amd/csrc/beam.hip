@@ -7,8 +7,9 @@
 //                     Which these are: W logits at least reach the W-th largest of the threads' maxima (or one up to W / 2 places
 //                     below it, which is found in fewer steps), so only the threads whose maximum reaches it hold candidates, little more
 //                     than W on the whole; each finds its rank by counting.
-//                     Bound: HBM, one read of the logits; with 32 beams the choice beside it (590 vector instructions of a wavefront).
-//                     64 x 4 rows of 128000 in fp32 22.7 us (5.8 TB/s); 8 x 32 rows of 100003 in bf16 19.7 (2.6 TB/s); 4 rows of 32000 5.9.
+//                     Bound: HBM, one read of the logits; with 32 beams the choice beside it (about 590 vector instructions of a wavefront
+//                     for 64 elements a lane).
+//                     64 x 4 rows of 128000 in fp32 22.7 us (5.8 TB/s); 8 x 32 rows of 100003 in bf16 18.7 (2.7 TB/s); 4 rows of 32000 5.9.
 //  beam_join_kernel   a workgroup has a prompt: log-sum-exp of the rows from their pieces, then the same choice among the pieces'
 //                     lists by their first entries.  Bound: dependent steps of one workgroup.  The same calls: 5.9, 10.4, 5.0 us.
 //
@@ -585,7 +586,12 @@ static Pieces pieces_of(int rows, int V, int esize) {
     while (nv > 2 && (int64_t)rows * V * esize < (int64_t)nv * 4096 * compute_units()) nv /= 2;
     auto count = [&]() { return (int)(((int64_t)V * esize + nv * 4096 - 1) / (nv * 4096)); };
     while (count() > kMaxPieces) nv *= 2;                               // (not beyond `most`: kMaxV)
-    return {nv, count()};
+    // as few as that number of pieces needs (in fp32 an even number): all elements take part in the choice, also those that are not there.
+    // (us, at most / as few: 352 rows of 26754 in fp32 29.8 / 25.9, 232 of 35111 17.4 / 15.3, 256 of 100003 in bf16 29.6 / 27.8)
+    const int pieces = count(), step = esize == 4 ? 2 : 1;
+    while (nv > 2 && (nv -= step, count() == pieces)) {}
+    if (count() != pieces) nv += step;
+    return {nv, pieces};
 }
 
 bool beam_fits(int S, int W, int V, int esize) { return (int64_t)S * W * pieces_of(S * W, V, esize).count < 1 << 24; }
@@ -611,9 +617,11 @@ hipError_t launch_beam(int S, int W, int V, bool bf16, const void* logits, int64
     p.value = (float*)(p.sums + lists);
     p.token = (int32_t*)(p.value + lists * W);
     const dim3 grid((unsigned)lists), block(kScanThreads);
-#define SCAN(NV) (bf16 ? beam_scan_kernel<true, NV> : beam_scan_kernel<false, NV>)
-    auto* scan = pc.nv == 2 ? SCAN(2) : pc.nv == 4 ? SCAN(4) : pc.nv == 8 ? SCAN(8) : beam_scan_kernel<false, 16>;
-#undef SCAN
+    static constexpr void (*kScan16[])(BeamParams) = {beam_scan_kernel<true, 2>, beam_scan_kernel<true, 3>, beam_scan_kernel<true, 4>, beam_scan_kernel<true, 5>,
+                                                      beam_scan_kernel<true, 6>, beam_scan_kernel<true, 7>, beam_scan_kernel<true, 8>};
+    static constexpr void (*kScan32[])(BeamParams) = {beam_scan_kernel<false, 2>, beam_scan_kernel<false, 4>, beam_scan_kernel<false, 6>, beam_scan_kernel<false, 8>,
+                                                      beam_scan_kernel<false, 10>, beam_scan_kernel<false, 12>, beam_scan_kernel<false, 14>, beam_scan_kernel<false, 16>};
+    auto* scan = bf16 ? kScan16[pc.nv - 2] : kScan32[pc.nv / 2 - 1];
     hipLaunchKernelGGL(scan, grid, block, 0, st, p);
     if (W <= 4) hipLaunchKernelGGL(beam_join_kernel<256>, dim3((unsigned)S), dim3(256), 0, st, p);
     else hipLaunchKernelGGL(beam_join_kernel<1024>, dim3((unsigned)S), dim3(1024), 0, st, p);

@@ -62,6 +62,15 @@ def test_select(S, W, V, dtype, end):
     check_select(x, scores, ended, end, got)
 
 
+# pieces of 3, 5, 6 and 7 (bf16) and of 6, 10, 12 and 14 (fp32) times 16 bytes a thread, full to the last element or not
+@pytest.mark.parametrize("S,W,V,dtype", [(105, 4, 5000, BF16), (16, 32, 9001, BF16), (70, 5, 12288, BF16), (38, 4, 28000, BF16), (95, 4, 5555, F32),
+                                         (14, 32, 10001, F32), (44, 4, 24000, F32), (98, 3, 14336, F32)])
+def test_select_pieces_that_divide_the_row(S, W, V, dtype):
+    x, scores, ended = select_inputs(S + V, S, W, V, dtype, 3)
+    got = P.prefixkv_beam_select(x.to(DEV), scores.to(DEV), ended=ended.to(DEV), end_token=3)
+    check_select(x, scores, ended, 3, got)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_select_rows_that_begin_anywhere(dtype):
     """The last step of several, rows of odd length among others; outputs in the inputs' place."""
