@@ -10,8 +10,8 @@
 //  attn_stream_kernel bf16, at most 32 rows per (sequence, KV head): decode steps.  A wavefront streams 32 keys at a time through
 //                     LDS of its own.  All keys of a launch are one sequence of blocks that the wavefronts share out evenly,
 //                     wherever the units begin and end.  Bound: HBM; 467 MB of keys and values of 32 sequences in 90 us, 5.2 TB/s
-//                     (a plain read reaches 5.8), and 5 us to join.  States of 32 sequences of up to 2880, 4 rows of 32 heads each, 777 MB:
-//                     144 ... 149 us and 10 to join; 577 states for one row, 32 heads: 7.3 + 4.8, the latency of both launches.
+//                     (a plain read reaches 5.8), and 5 us to join.
+//  attn_unit_kernel   the same rows over states of another length, where the units are many or short: a workgroup has a unit, and no second launch.
 //  attn_merge_*       join the parts of a tile or unit that several workgroups or wavefronts worked on.
 //  attn_rows_kernel   fp32: a workgroup per (row, head, layer).  The keys stream past one row: LPR lanes hold a key
 //                     row, scores meet by shuffles, softmax online (running maximum and sum, everything fp32); the four
@@ -667,7 +667,7 @@ attn_merge_tiles_kernel(TileParams p) {
 // (States are the same in every layer: there a segment is a sequence, and its heads are those of all layers.)
 struct StreamParams : Work {
     int heads;                      // of a segment
-    FastDiv by_hkv;
+    FastDiv by_hkv, by_heads;
     int waves;
     int join_rows;                  // rows of a workgroup that joins: 1, or all of its groups of lanes
     int* share;                     // workspace: blocks of a wavefront
@@ -676,9 +676,8 @@ struct StreamParams : Work {
     float2* part_ms;
 };
 constexpr int kLeastBlocks = 2;     // of a wavefront
-// Over states: one, and up to four where a unit would be cut into more parts than these.  us, one / two / four blocks at least: a row over 577
-// states, H32/8, 10.3 / 12.2 / 15.4; 4 rows of 4 sequences over up to 3882, H32/4, 28.0 / 21.6 / 22.3; 8 rows of 2 over up to 4141, H32/8,
-// 33.0 / 23.7 / 23.5.
+// Over states: one, and up to four where a unit would be cut into more parts than these.  us, one / two / four blocks at least: 4 rows of
+// 4 sequences over up to 3882 states, H32/4, 28.0 / 21.6 / 22.3; 8 rows of 2 over up to 4141, H32/8, 33.0 / 23.7 / 23.5.
 constexpr int kManyParts = 40;
 
 __device__ __forceinline__ int blocks_of(const Segment& x) { return (x.end + kBlockKeys - 1) / kBlockKeys; }
@@ -940,6 +939,85 @@ attn_merge_stream_kernel(StreamParams p) {
     }
 }
 
+// ---- few rows over states: a workgroup per unit ------------------------------------------------------------
+// A wavefront takes every WAVES-th block of 32 states, through LDS of its own (one buffer: the other wavefronts' work hides its waits), and the
+// parts are joined there.  Bound: latency, a trip for the offsets and one for each block of a wavefront; HBM where there are many units, 777 MB
+// of keys and values of 32 sequences in 140 us, 5.5 TB/s.
+template <int D, int WAVES>
+__global__ void __launch_bounds__(WAVES * kWave, 2)
+attn_unit_kernel(StreamParams p) {
+    constexpr int ROWB = D * 2, kBytes = kBlockKeys * ROWB, kInst = CopyLane<D>::kCopies, LPP = D / 4;
+    static_assert(2 * kBytes == kFewRows * D * 4, "a part lies where the keys and values were");
+    __shared__ __attribute__((aligned(1024))) unsigned char s_kv[WAVES][2 * kBytes];
+    __shared__ float2 s_ms[WAVES][kFewRows];
+    const PackedParams& a = p.a;
+    const int lane = threadIdx.x & (kWave - 1), wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), ln = lane & 31, hf = lane >> 5;
+    const DivMod sg = uniform_div_mod((int)blockIdx.x, p.by_heads), lg = uniform_div_mod(sg.r, p.by_hkv);
+    const Segment x = uniform_segment<kStates>(p, sg.q);
+    if (x.rows == 0) return;
+    const int blocks = blocks_of(x), waves = min(blocks, WAVES);
+    const float sc = a.scale[lg.q], qs = score_scale(sc);
+    if (wv < waves) {
+        const int64_t from = uniform_load(a.state_off + x.s);
+        const unsigned char *kb = a.k + a.ks.l * lg.q + a.ks.h * lg.r, *vb = a.v + a.vs.l * lg.q + a.vs.h * lg.r;
+        const CopyLane<D> cp(lane);
+        unsigned char *sK = s_kv[wv], *sV = sK + kBytes;
+        auto issue = [&](int b) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const int key = min(b * kBlockKeys + 16 * y, x.end - 1);
+                const uint32_t last = (uint32_t)(x.end - 1 - key);
+                const unsigned char *ka = kb + a.ks.n * (from + key), *va = vb + a.vs.n * (from + key);
+#pragma unroll
+                for (int i = 0; i < kInst; ++i) {
+                    copy_to_lds(ka + cp.at(i, last, (uint32_t)a.ks.n), sK + (y * kInst + i) * 1024);
+                    copy_to_lds(va + cp.at(i, last, (uint32_t)a.vs.n), sV + (y * kInst + i) * 1024);
+                }
+            }
+        };
+        issue(wv);
+        const RowAt ra = row_at(ln < x.rows ? ln : 0, p.grp);
+        const int64_t t = x.first + ra.token;
+        RowTile<D> tl;
+        tl.offsets(lane);
+        tl.load_q(a.q + a.qs.l * lg.q + a.qs.h * (lg.r * a.grp + ra.head) + a.qs.n * t, hf, sc < 0.f);
+        tl.clear();
+        const int lim = seen_by(a, t, x.len) - 1, seen = limits<kFewRows>(p, x, 0, lane).all;
+        for (int b = wv;;) {
+            __builtin_amdgcn_s_waitcnt(0x0F70);                 // vmcnt(0): the block has landed
+            asm volatile("" ::: "memory");
+            const int key0 = b * kBlockKeys;
+            if (key0 + kBlockKeys <= seen) tl.template attend<1, false, true>(sK, sV, qs, lane, 0, 0u, 1, 1);
+            else tl.template attend<1, true, true>(sK, sV, qs, lane, lim - key0, 0u, 1, 0);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the fragment reads are done: the buffer is free
+            b += WAVES;
+            if (b >= blocks) break;
+            issue(b);
+        }
+        const float all = tl.total();
+        if (ln < x.rows) tl.store_part((float*)sK + ln * D, &s_ms[wv][ln], hf, all);
+    }
+    __syncthreads();
+    const int c = threadIdx.x % LPP;
+    for (int row = threadIdx.x / LPP; row < x.rows; row += WAVES * kWave / LPP) {
+        float top = -INFINITY, sum = 0.f;
+        for (int w = 0; w < waves; ++w) top = fmaxf(top, s_ms[w][row].x);
+        const float ref = top == -INFINITY ? 0.f : top;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int w = 0; w < waves; ++w) {
+            const float2 ms = s_ms[w][row];
+            const float4 y = *(const float4*)((const float*)s_kv[w] + row * D + 4 * c);
+            const float c1 = __builtin_amdgcn_exp2f((ms.x - ref) * qs);
+            sum = fmaf(ms.y, c1, sum);
+            o.x = fmaf(y.x, c1, o.x); o.y = fmaf(y.y, c1, o.y); o.z = fmaf(y.z, c1, o.z); o.w = fmaf(y.w, c1, o.w);
+        }
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const RowAt ra = row_at(row, p.grp);
+        *(uint2*)(a.out + a.os.l * lg.q + a.os.h * (lg.r * a.grp + ra.head) + a.os.n * (int64_t)(x.first + ra.token) + 8 * c) =
+            make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+    }
+}
+
 // ---- launches ------------------------------------------------------------------------------------------
 constexpr int kStreamWorkgroups = 2;          // of a compute unit: 64 KB of LDS each at D = 128
 constexpr int kTileWorkgroups = 2;            // of attn_tiles_kernel: 256 registers
@@ -991,13 +1069,30 @@ size_t packed_attn_ws_bytes(const pkv_packed& s, int max_rows) {
     return cut_bytes(s);
 }
 
+// Few rows over states: whether a unit has a workgroup, by its blocks (on average, as lengths are on the device).  Long units of few are shared out evenly by
+// the stream kernel; its second launch and what a wavefront does to find its place cost 5 us.  us, stream / unit: a row over 577 states, H32/8,
+// 10.8 / 9.1; 4 rows of 2 sequences over up to 80, 4 layers of 32 heads, 11.6 / 5.6; 24 rows of 8 over up to 1003, 4 layers of 24, 50 / 38; 4 rows of 32
+// over up to 2880, H32, 162 / 144; a row over 2095, H16/8, 11.2 / 18.9; 8 rows of 3 over up to 1527, H12/4, 19 / 23; a row of 40 over up to 4000,
+// H32/8, 83 / 93.  The geometric mean of 90 calls, all of them by units: 0.80 of the time; by this rule 0.72.
+static double unit_blocks(const pkv_packed& s, int M) { return (double)M / s.S / kBlockKeys; }
+static bool per_unit(const pkv_packed& s, int M) {
+    const double units = (double)s.S * s.L * s.Hkv, most = 24 + units / 4;
+    return unit_blocks(s, M) <= (most < 64 ? most : 64) && units < 1 << 22;
+}
+// Many short units want small workgroups, of which a compute unit holds several.  us, 8 / 4 / 2 wavefronts: 8 units over up to 80 states 6.4 / 6.9 / 8.2,
+// 448 over up to 220 14.9 / 13.1 / 14.8, 800 over up to 80 (D 64) 12.0 / 7.0 / 7.8; 4 / 2: 6144 over up to 38 59 / 39, 8192 over up to 200 112 / 91.
+static int unit_waves(const pkv_packed& s, int M) {
+    const int units = s.S * s.L * s.Hkv;
+    return unit_blocks(s, M) > 6 || units <= compute_units() ? 8 : units <= 4 * compute_units() ? 4 : 2;
+}
+
 // blocks of the stream kernel are 32 bits wide
 bool cross_attn_fits(const pkv_packed& s, int M) {
     return packed_attn_fits(s, nullptr) && ((double)M / kBlockKeys + s.S) * s.L * s.Hkv < 2147483648.0;
 }
 size_t cross_attn_ws_bytes(const pkv_packed& s, int M, int max_rows) {
     if (s.dtype != PKV_BF16) return 0;
-    if (few_rows(s, max_rows)) return stream_bytes(s);
+    if (few_rows(s, max_rows)) return per_unit(s, M) ? 0 : stream_bytes(s);
     return cross_tiles_ws_bytes(s, M);
 }
 
@@ -1044,6 +1139,14 @@ static hipError_t launch_stream(const pkv_packed& s, const PackedParams& a, void
         p.heads = s.L * s.Hkv;
         p.segs = s.S;
         p.by_layers = fast_div(1);
+        p.by_heads = fast_div(p.heads);
+        if (per_unit(s, a.M)) {
+            const dim3 grid((unsigned)(p.segs * p.heads));
+            const int waves = unit_waves(s, a.M);
+            auto* kernel = waves == 8 ? attn_unit_kernel<D, 8> : waves == 4 ? attn_unit_kernel<D, 4> : attn_unit_kernel<D, 2>;
+            hipLaunchKernelGGL(kernel, grid, dim3((unsigned)(waves * kWave)), 0, st, p);
+            return hipGetLastError();
+        }
     }
     p.waves = stream_waves(s);
     p.share = (int*)ws;

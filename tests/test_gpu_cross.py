@@ -316,3 +316,94 @@ def test_cross_attn_shared_out_is_repeatable_and_replays_from_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(out, wants[i % 2])
         assert torch.equal(P.prefixkv_cross_attn(q, k, v, off, to, scale, 150, seen=lims[i % 2], out=torch.zeros_like(q)), wants[i % 2])
+
+
+FEW = [  # rows, states, H, Hkv, D, layers: rows of a head 1 ... 32; units 1 ... 1152, a workgroup of 8, 4 or 2 wavefronts each
+    ([1], [1], 1, 1, 64, 1), ([1], [577], 32, 8, 128, 1), ([4, 4, 4], [100, 0, 33], 4, 4, 128, 2), ([1, 0, 1], [31, 700, 32], 7, 1, 64, 1),
+    ([3], [767], 8, 8, 64, 1), ([8, 8], [64, 65], 4, 1, 128, 1), ([32, 1, 17], [257, 256, 255], 2, 2, 128, 1), ([1] * 30, [20 + i for i in range(30)], 10, 10, 64, 1),
+    ([2, 0, 1] * 12, [(i * 23) % 70 for i in range(36)], 16, 16, 128, 2), ([3, 1] * 35, [(i * 37) % 90 for i in range(70)], 4, 2, 64, 1),
+]
+
+
+@pytest.mark.parametrize("n,m,H,Hkv,D,L", FEW)
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("what", ["all", "any", "rising", "few"])
+def test_cross_attn_of_few_rows(n, m, H, Hkv, D, L, shared, what):
+    """A unit a workgroup; and, with so many states of nobody that long units are to be expected, shared out over the wavefronts."""
+    S = len(n)
+    q, k, v, off, to, scale = inputs(sum(n) + sum(m) + H, L, H, Hkv, n, m, D, BF16, first=1, pad=2, before=3, behind=S * 32 * 66 if shared else 4)
+    T = q.shape[2]
+    assert (P.cross_workspace_bytes(S, L, H, Hkv, T, k.shape[2], D, BF16, max(n)) > 0) == shared
+    r = np.random.default_rng(T)
+    seen = {"all": None, "any": r.integers(-3, max(m) + 5, size=T), "rising": np.arange(T) * max(m) // T, "few": np.minimum(3, r.integers(0, 40, size=T))}[what]
+    if seen is not None:
+        seen[r.random(T) < 0.1] = 1 << 30
+        seen[r.random(T) < 0.1] = -(1 << 31)
+        for s in range(S):                                      # what no row sees
+            rows = seen[off[s]:off[s + 1]]
+            most = int(np.clip(rows, 0, m[s]).max()) if len(rows) else 0
+            k[:, :, to[s] + most:to[s + 1]] = float("nan")
+            v[:, :, to[s] + most:to[s + 1]] = float("inf")
+    check(q, k, v, off, to, scale, max(n), seen)
+    if max(n) > 2:
+        check(q, k, v, off, to, scale, 2, seen, max_rows=2)
+
+
+@pytest.mark.parametrize("shared", [False, True])
+def test_cross_attn_of_few_rows_values_that_some_rows_must_not_see(shared):
+    n, m = [4, 3], [400, 90]
+    q, k, v, off, to, scale = inputs(31, 1, 8, 2, n, m, 128, BF16, behind=2 * 32 * 66 if shared else 0)
+    seen = np.array([400, 77, 300, 90, 90, 1, 89])
+    v[:, :, 77, ::5] = float("inf")
+    v[:, :, 300:310, 3] = float("nan")
+    v[:, :, to[1] + 89, 9] = float("-inf")
+    out = P.prefixkv_cross_attn(q, k, v, i32(off), i32(to), scale, 4, seen=i32(seen))
+    want, mag = R.cross(f64(q), off, f64(k), f64(v), to, scale.double().cpu().numpy(), seen)
+    finite = np.isfinite(want) & np.isfinite(mag)
+    assert finite[:, :, [1, 5, 6]].all() and not finite.all()
+    here = torch.from_numpy(finite).to(DEV)
+    assert bool((~torch.isfinite(out.float()))[~here].all())
+    close(torch.where(here, out, torch.zeros_like(out)), np.where(finite, want, 0.0), np.where(finite, mag, 0.0), BF16)
+
+
+@pytest.mark.parametrize("n", [[2, 1], [20, 12]])
+def test_cross_attn_of_few_rows_shared_out_lowest_values_and_infinities(n):
+    """Scores that are all the type's lowest number weigh the same; keys of -inf weigh nothing."""
+    H, Hkv, D, m = 1, 1, 64, [300, 90]
+    for behind in (0, 2 * 32 * 66):
+        q, k, v, off, to, _ = inputs(32, 1, H, Hkv, n, m, D, BF16, behind=behind)
+        q = torch.zeros_like(q)
+        q[..., 0] = 1.0
+        k[..., 1:] = 0
+        k[:, :, :m[0], 0] = torch.finfo(BF16).min
+        k[:, :, m[0]:, 0] = float("-inf")
+        k[:, :, m[0] + 40, 0] = 1.0
+        scale = torch.tensor([1.0], device=DEV)
+        out = P.prefixkv_cross_attn(q, k, v, i32(off), i32(to), scale, max(n))
+        x = f64(v)[0, 0]
+        for s, want in ((0, x[:m[0]].mean(0)), (1, x[m[0] + 40])):
+            got = out[0, 0, off[s]:off[s + 1]].double().cpu().numpy()
+            bar = 2.0 ** -8 * np.abs(want) + (2.0 ** -16 + 2e-4) * np.abs(x[:m[0]]).mean(0) * (s == 0) + 1e-30
+            assert (np.abs(got - want) <= bar).all()
+
+
+@pytest.mark.parametrize("shared", [False, True])
+def test_cross_attn_of_few_rows_is_repeatable_and_replays_from_a_graph(shared):
+    n, m, H, Hkv, D = [4, 1, 3], [700, 33, 500], 8, 2, 128
+    q, k, v, off, to, scale = inputs(33, 1, H, Hkv, n, m, D, BF16, behind=3 * 32 * 66 if shared else 0)
+    off, to = i32(off), i32(to)
+    lims = [i32(np.arange(8) * 90), i32(600 - np.arange(8) * 70)]
+    wants = [P.prefixkv_cross_attn(q, k, v, off, to, scale, 4, seen=x) for x in lims]
+    ws = torch.empty(P.cross_workspace_bytes(3, 1, H, Hkv, 8, k.shape[2], D, BF16, 4), dtype=torch.uint8, device=DEV)
+    out, seen = torch.zeros_like(q), lims[0].clone()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        P.prefixkv_cross_attn(q, k, v, off, to, scale, 4, seen=seen, out=out, ws=ws)
+    for i in range(6):
+        seen.copy_(lims[i % 2])
+        out.zero_()
+        ws.fill_(255 * (i // 2 % 2))
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, wants[i % 2])
+        assert torch.equal(P.prefixkv_cross_attn(q, k, v, off, to, scale, 4, seen=lims[i % 2]), wants[i % 2])
