@@ -1079,11 +1079,13 @@ static bool per_unit(const pkv_packed& s, int M) {
     const double units = (double)s.S * s.L * s.Hkv, most = 24 + units / 4;
     return unit_blocks(s, M) <= (most < 64 ? most : 64) && units < 1 << 22;
 }
-// Many short units want small workgroups, of which a compute unit holds several.  us, 8 / 4 / 2 wavefronts: 8 units over up to 80 states 6.4 / 6.9 / 8.2,
-// 448 over up to 220 14.9 / 13.1 / 14.8, 800 over up to 80 (D 64) 12.0 / 7.0 / 7.8; 4 / 2: 6144 over up to 38 59 / 39, 8192 over up to 200 112 / 91.
+// Many units want small workgroups, of which a compute unit holds several, the short ones sooner.  us, 8 / 4 / 2 wavefronts: 8 units over up to 80 states
+// 6.4 / 6.9 / 8.2, 448 over up to 220 14.9 / 13.1 / 14.8, 800 over up to 80 (D 64) 12.0 / 7.0 / 7.8; 8 / 4: 384 over up to 469 11.1 / 12.5, 768 over up to 1003
+// 37.8 / 35.3; 4 / 2: 6144 over up to 38 59 / 39; 8 / 2: 1248 over up to 1761 66 / 77, 2048 over 500 115 / 101, 16384 over 300 612 / 489, 51200 of
+// which 1600 have a row 128 / 51, 2048 of which 32 have one 7.2 / 10.3.
 static int unit_waves(const pkv_packed& s, int M) {
-    const int units = s.S * s.L * s.Hkv;
-    return unit_blocks(s, M) > 6 || units <= compute_units() ? 8 : units <= 4 * compute_units() ? 4 : 2;
+    const int units = s.S * s.L * s.Hkv, many = compute_units() * (unit_blocks(s, M) > 6 ? 2 : 1);
+    return units >= 4 * many ? 2 : units >= many ? 4 : 8;
 }
 
 // blocks of the stream kernel are 32 bits wide
