@@ -10,7 +10,7 @@
 //                     Bound: HBM, one read of the logits; with 32 beams the choice beside it (about 590 vector instructions of a wavefront
 //                     for 64 elements a lane).
 //                     64 x 4 rows of 128000 in fp32 22.7 us (5.8 TB/s); 8 x 32 rows of 100003 in bf16 18.7 (2.7 TB/s); 4 rows of 32000 5.9.
-//  beam_join_kernel   a workgroup has a prompt: log-sum-exp of the rows from their pieces, then the same choice among the pieces'
+//  beam_join_kernel   a workgroup has a prompt: maxima and sums of the rows from their pieces, then the same choice among the pieces'
 //                     lists by their first entries.  Bound: dependent steps of one workgroup.  The same calls: 5.9, 10.4, 5.0 us.
 //
 // A sum of exponentials of a piece is held in 32 bits (terms of a thread, then a tree); pieces, logarithms and scores in 64, because
@@ -59,16 +59,16 @@ __device__ __forceinline__ uint64_t key_of(double x) {
     return x == -(double)INFINITY ? 0ull : (u >> 63) ? ~u : u | (1ull << 63);
 }
 
-// Terms of a row's sum are 2^(kLog2e x - base), one fma and one rounding of the exponent each; base = kLog2e * maximum, rounded.
-// kLog2e is log2(e) (1 + kExcess): of a sum that stands for its maximum the logarithm is too large by kExcess * maximum (by up to
-// kExcess * log V < 2e-7 less where it does not), which is taken off behind it, in 64 bits.  Beyond kWideLogit, where the base would leave the range,
-// the difference from the maximum is scaled.
+// Terms of a row's sum are 2^(kLog2e x - base), one fma and one rounding of the exponent each; base = kLog2e * maximum, rounded, whose
+// residue (exact in 32 bits) is taken off behind the sum.  Beyond kWideLogit, where the base would leave the range, the difference from
+// the maximum is scaled.  (kLog2e is log2(e) but for 1.4e-8 of it: a sum's logarithm is off by that times the terms' mean distance from the
+// maximum, which is log V at most: below 2e-7.)
+// Nothing is added to a maximum: at 10^17 and beyond 64 bits would not hold the sum's logarithm next to it.
 constexpr float kLog2e = 1.44269502f, kWideLogit = 1e30f;
-constexpr double kLn2 = 0.693147180559945309417, kExcess = (double)kLog2e * kLn2 - 1.0;
+constexpr double kLn2 = 0.693147180559945309417;
 __device__ __forceinline__ float base_of(float m) { return m * kLog2e; }
-__device__ __forceinline__ double base_log(float m) {
-    return fabsf(m) > kWideLogit ? (double)m : (double)base_of(m) * kLn2 - kExcess * (double)m;
-}
+// log of how much larger a sum is than that of exp(x - m)
+__device__ __forceinline__ double residue_log(float m) { return fabsf(m) > kWideLogit ? 0.0 : (double)fmaf(m, kLog2e, -base_of(m)) * kLn2; }
 
 template <class K>
 __device__ __forceinline__ K wave_max(K x) {
@@ -406,7 +406,8 @@ beam_join_kernel(BeamParams p) {
     constexpr int kHeads = (kMaxBeams * kMaxPieces + 1023) / 1024;       // of a thread, at most
     constexpr int kLists = kMaxBeams * 3 / 2, R = 2, kSteps = 3 * 34;
     static_assert(1024 * R >= kLists * kMaxBeams, "a thread has R of what the lists hold");
-    __shared__ double s_lse[kMaxBeams], s_score[kMaxBeams];
+    __shared__ double s_log[kMaxBeams], s_score[kMaxBeams];             // log of the sum of exp(x - maximum)
+    __shared__ float s_max[kMaxBeams];
     __shared__ uint8_t s_kind[kMaxBeams];                                // 0: goes on, 1: has ended, 2: no candidates
     __shared__ uint64_t s_head[kMaxBeams * kMaxPieces], s_ck[kLists * kMaxBeams];
     __shared__ uint32_t s_place[kMaxBeams * kMaxPieces], s_ca[kLists * kMaxBeams];
@@ -431,18 +432,19 @@ beam_join_kernel(BeamParams p) {
         const bool over = p.ended && p.ended[row0 + w], live = !over && score != -(double)INFINITY;
         float2 y = make_float2(-INFINITY, 0.f);
         if (live && c < p.pieces) y = p.sums[(row0 + w) * p.pieces + c];
-        float m = y.x;                                                   // (a row without candidates: its log-sum-exp is not used)
+        float m = y.x;                                                   // (a row without candidates: its sum is not used)
         for (int d = p.group / 2; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, kWave));
-        double z = y.x != -INFINITY ? (double)y.y * exp(base_log(y.x) - (double)m) : 0.0;
+        double z = y.x != -INFINITY ? (double)y.y * exp(((double)y.x - (double)m) - residue_log(y.x)) : 0.0;
         for (int d = p.group / 2; d > 0; d >>= 1) z += __shfl_xor(z, d, kWave);
         if (c == 0) {
-            s_lse[w] = live ? (double)m + log(z) : 0.0;
+            s_max[w] = m;
+            s_log[w] = live ? log(z) : 0.0;
             s_score[w] = score;
             s_kind[w] = over ? 1 : live ? 0 : 2;
         }
     }
     __syncthreads();
-    auto key = [&](int w, float x) { return key_of(((double)x - s_lse[w]) + s_score[w]); };
+    auto key = [&](int w, float x) { return key_of((((double)x - (double)s_max[w]) - s_log[w]) + s_score[w]); };
     auto place = [&](int w, int v) { return (uint32_t)w * (uint32_t)p.V + (uint32_t)v; };
 #pragma unroll
     for (int i = 0; i < kHeads; ++i) {
