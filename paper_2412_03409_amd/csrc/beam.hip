@@ -60,11 +60,11 @@ __device__ __forceinline__ uint64_t key_of(double x) {
 }
 
 // Terms of a row's sum are 2^(kLog2e x - base), one fma and one rounding of the exponent each; base = kLog2e * maximum, rounded, whose
-// residue (exact in 32 bits) is taken off behind the sum.  Beyond kWideLogit, where the base would leave the range, the difference from
-// the maximum is scaled.  (kLog2e is log2(e) but for 1.4e-8 of it: a sum's logarithm is off by that times the terms' mean distance from the
+// residue (exact in 32 bits) is taken off behind the sum.  Beyond kWideLogit the difference from the maximum is scaled: the residue, up to
+// 2^-24 of the base, is an exponent of every term, which past 10^9 leaves the range and up to here stays below 2^-7.  (kLog2e is log2(e) but for 1.4e-8 of it: a sum's logarithm is off by that times the terms' mean distance from the
 // maximum, which is log V at most: below 2e-7.)
 // Nothing is added to a maximum: at 10^17 and beyond 64 bits would not hold the sum's logarithm next to it.
-constexpr float kLog2e = 1.44269502f, kWideLogit = 1e30f;
+constexpr float kLog2e = 1.44269502f, kWideLogit = 65536.f;
 constexpr double kLn2 = 0.693147180559945309417;
 __device__ __forceinline__ float base_of(float m) { return m * kLog2e; }
 // log of how much larger a sum is than that of exp(x - m)

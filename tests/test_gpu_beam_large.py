@@ -59,7 +59,7 @@ def among_ordinary_beams(V, dtype, g):
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("V", [777, 32000, 100003])
-@pytest.mark.parametrize("value", ["lowest", "largest", 1e38, -1e38])
+@pytest.mark.parametrize("value", ["lowest", "largest", 1e38, -1e38, -1e30, 3e17])
 def test_rows_of_one_huge_value(value, V, dtype):
     """A beam whose tokens are all hidden by the type's lowest value has each of them with the probability 1 / V."""
     x, scores = among_ordinary_beams(V, dtype, gen(V))
@@ -83,7 +83,7 @@ def test_rows_with_several_infinities(V, count, dtype):
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("V", [777, 32000])
-@pytest.mark.parametrize("value", [6e4, -7e4, 1e6, -3e7, 1e9, -1e9])
+@pytest.mark.parametrize("value", [6e4, -7e4, 1e6, -3e7, 1e9, -1e9, 6e9, 1e12, 1e17, -1e17, 1e25, -9e29])
 def test_rows_around_a_large_value(value, V, dtype):
     """Logits a few steps of the type apart, where a step is less than a few units, else equal."""
     x, scores = among_ordinary_beams(V, dtype, gen(V + 1))
