@@ -255,13 +255,19 @@ class PagedPath:
     def advance(self, logits, scores, ended=None, end_token=None):
         """The best continuations of every prompt, and the places that follow them: logits [S/beams,beams,V], scores [S/beams,beams]
         f32, ended [S/beams,beams] bool or None -> (tokens, parents, scores, ended) as of prefixkv_beam_select.  If `status` says that
-        there were too few pages the places are as they were, and the beams have to be chosen again from fewer prompts."""
+        there were too few pages the places are as they were and no prompt has a continuation (tokens and parents -1, scores -inf):
+        the beams have to be chosen again, from these logits and scores, with fewer prompts."""
         if logits.shape[:2] != (self.S // self.beams, self.beams):
             raise ValueError("logits must be [S/beams,beams,V]")
         if self.beams == 1:
             raise ValueError("a path with one beam per prompt has nothing to follow")
         chosen = B_.prefixkv_beam_select(logits, scores, ended=ended, end_token=end_token)
         self.follow(chosen[1])
+        refused = self.status != 0
+        # (a later call sets `status` anew: what did not happen must not look chosen by then)
+        for x, none in zip(chosen, (-1, -1, float("-inf"), False)):
+            if x is not None:
+                x.masked_fill_(refused, none)
         return chosen
 
     def cross(self, lengths, q, k, v, state_off, seen=None):
