@@ -270,11 +270,13 @@ class PagedPath:
                 x.masked_fill_(refused, none)
         return chosen
 
-    def cross(self, lengths, q, k, v, state_off, seen=None):
+    def cross(self, lengths, q, k, v, state_off, seen=None, scale=None):
         """Attention of rows (lengths[s] of place s, packed) to their prompt's states k, v [L,Hkv,M,D], state_off [S/beams+1] i32 on
-        the GPU, which the beams of a group share; seen [T] i32: only the first ones -> [L,H,T,D]."""
+        the GPU, which the beams of a group share; seen [T] i32: only the first ones -> [L,H,T,D].  L: the layers that the call is
+        for, all of the path's or any others; scale [L] f32: theirs (None: the path's)."""
         lengths = [int(n) for n in lengths]
         if len(lengths) != self.S or any(n < 0 for n in lengths) or sum(lengths) > q.shape[2]:
             raise ValueError("a length per place, rows for all of them")
         rows = [sum(lengths[s:s + self.beams]) for s in range(0, self.S, self.beams)]
-        return B_.prefixkv_cross_attn(q, k, v, self._offsets(rows), state_off, self.scale, max(1, max(rows)), seen=seen)
+        return B_.prefixkv_cross_attn(q, k, v, self._offsets(rows), state_off, self.scale if scale is None else scale,
+                                      max(1, max(rows)), seen=seen)

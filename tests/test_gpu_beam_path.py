@@ -1,11 +1,12 @@
-"""PagedPath with several beams per prompt: a step that gets no pages."""
+"""PagedPath with several beams per prompt: a step that gets no pages, and attention to states in some of the layers only."""
 import pytest
 import torch
 
+import beam_reference as R
 import paper_2412_03409_amd as P
 from paper_2412_03409_amd.pipeline import PagedPath
 from test_gpu_beam import select_inputs
-from test_gpu_serving import BF16, DEV, gen, projected
+from test_gpu_serving import BF16, DEV, close, f64, gen, i32, offsets, projected
 
 pytestmark = pytest.mark.gpu
 L, H, HKV, D, PS, BEAMS, G, V, END = 2, 2, 1, 64, 16, 2, 2, 101, 7
@@ -57,3 +58,20 @@ def test_a_step_that_gets_its_pages_is_the_choice():
     want = P.prefixkv_beam_select(x, scores, ended=ended, end_token=END)
     got = path.advance(x, scores, ended=ended, end_token=END)
     assert int(path.status) == 0 and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("layers", [[0], [1], [1, 0, 1]])
+def test_attention_to_states_in_other_layers_than_the_paths(layers):
+    """A model may attend to its encoder's states in some of its layers, all at once or one after the other, and with a scale of its own."""
+    path, g = path_of(8), gen(len(layers))
+    lengths, m = [1, 3, 0, 2], [40, 70]
+    q, _, _ = projected(g, len(layers), H, HKV, sum(lengths), D, BF16)
+    kv = torch.randn((len(layers), 2 * HKV, sum(m), D), generator=g).to(BF16).to(DEV)
+    k, v, to = kv[:, :HKV], kv[:, HKV:], offsets(m)
+    for scale in (path.scale[layers], torch.full((len(layers),), -0.3, device=DEV)):
+        out = path.cross(lengths, q, k, v, i32(to), scale=scale)
+        want, mag = R.cross(f64(q), offsets([4, 2]), f64(k), f64(v), to, scale.double().cpu().numpy())
+        close(out, want, mag, BF16)
+    if len(layers) != L:
+        with pytest.raises(ValueError, match="scale"):
+            path.cross(lengths, q, k, v, i32(to))
