@@ -315,7 +315,8 @@ int prefixkv_decode_attn_evict(const pkv_shape *shape, int l0, int l1, const voi
  * For programs that serve sequences of different lengths.  S sequences are packed one behind the
  * other into T rows: row_off [dev] i32 [S+1] is non-decreasing, sequence s owns the rows
  * row_off[s] ... row_off[s+1]-1 (none is a sequence without rows), rows in front of row_off[0] and from
- * row_off[S] on belong to nobody and are left as they are.  Row tensors are [L, heads, T, D] with
+ * row_off[S] on belong to nobody and are left as they are.  (To the attention calls a sequence whose offsets descend
+ * or are not in 0 ... T has no rows; of a row that two have because others descend, either's answer comes out.)  Row tensors are [L, heads, T, D] with
  * element strides l, h and n (b is not looked at, n may be any multiple of 16 bytes), so that a
  * projection's token-major [T, heads, D] output is passed as it is.  Inputs may repeat a layer or head (a stride of 0); the rows of
  * an output are its own (PKV_ERR_STRIDE).

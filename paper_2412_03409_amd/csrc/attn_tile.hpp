@@ -21,12 +21,6 @@ __device__ __forceinline__ float scale_size(float sc) {
 // value weigh them equally.
 __device__ __forceinline__ float score_scale(float sc) { return scale_size(sc) * kLog2e; }
 
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d, kWave);
-    return x;
-}
-
 // ---- bf16: the matrix cores ----------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;

@@ -61,13 +61,17 @@ attn_rows_kernel(PackedParams p) {
     constexpr int LPR = D / 4, RG = kWave / LPR, U = 4, kRow = D * 4;
     const int lane = threadIdx.x & (kWave - 1), wv = threadIdx.x / kWave, sub = lane % LPR, rg = lane / LPR;
     const int t = blockIdx.x, h = blockIdx.y, l = blockIdx.z;
-    // the sequence of row t: how many end at t or before it
-    int s = 0;
-    for (int i = lane; i < p.S; i += kWave) s += p.row_off[i + 1] <= t;
-    s = wave_sum(s);
-    if (s >= p.S) return;
+    // the sequence of row t: the last one that has it
+    int s = -1;
+    for (int i = lane; i < p.S; i += kWave) {
+        const int from = p.row_off[i], to = p.row_off[i + 1];
+        s = from <= t && t < to && new_rows(from, to, p.T) > 0 ? i : s;
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) s = max(s, __shfl_xor(s, d, kWave));
+    if (s < 0) return;
     const int first = p.row_off[s], n = p.row_off[s + 1] - first, i = t - first;
-    if (first < 0 || i < 0 || i >= p.max_rows) return;
+    if (i >= p.max_rows) return;
     const int len = KEYS == kStates ? states(p, s) : entries(p, s, l);
     const int count = KEYS == kStates ? seen_by(p, t, len) : min(len, i + 1 + len - n);    // keys that the row sees
     const int32_t* pages = KEYS == kStates ? nullptr : p.table + ((int64_t)s * p.layers + p.l0 + l) * p.max_pages;
