@@ -448,7 +448,8 @@ int prefixkv_chunk_attn(const pkv_packed *shape, const void *q, pkv_strides qs, 
  *                  n over the states state_off[s] ... state_off[s+1]-1, with `seen` the first seen[t] of them
  * A row that sees none gives zeros; keys and values that it does not see take no part, whatever they hold.
  *   q, out [L,H,T,D] strides qs, os;  k, v [L,Hkv,M,D] strides ks, vs (n below 2^26);  scale [dev] fp32 [L]
- *   row_off [dev] i32 [S+1];  state_off [dev] i32 [S+1], non-decreasing, 0 ... M: no states between equal ones
+ *   row_off [dev] i32 [S+1];  state_off [dev] i32 [S+1], non-decreasing, 0 ... M: no states between equal ones (nor between offsets that
+ *       descend or are not in 0 ... M; where sequences share states by such, out may be left as it is)
  *   seen [dev] i32 [T] or NULL; below 0 is 0, above the number of states all of them
  *   max_rows: no sequence has more rows in this call (1 <= max_rows <= T); further ones are left as they are.  It chooses the kernel.
  *   ws [dev]: prefixkv_cross_workspace_bytes(shape, M, max_rows) bytes, any contents, 16-byte aligned (NULL if that is 0).  Calls on

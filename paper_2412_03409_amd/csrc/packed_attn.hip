@@ -674,7 +674,7 @@ struct StreamParams : Work {
     FastDiv by_hkv, by_heads;
     int waves;
     int join_rows;                  // rows of a workgroup that joins: 1, or all of its groups of lanes
-    int* share;                     // workspace: blocks of a wavefront
+    int* share;                     // workspace: blocks of a wavefront; 0: nothing was done
     int* start;                     // [segs]: first block of a segment (segments that have blocks)
     float* part_o;                  // [2 * waves][32][D]
     float2* part_ms;
@@ -702,7 +702,10 @@ attn_stream_kernel(StreamParams p) {
     const int heads = KEYS == kStates ? p.heads : a.Hkv;
     auto blocks = [&](const Segment& x) { return (int64_t)blocks_of(x) * heads; };
     const Looked<KEYS, int64_t, decltype(blocks)> looked(p, lane, p.segs, 0, 1, blocks);
-    const int all_blocks = (int)looked.all;                                // (below 2^31: the call is refused otherwise)
+    // (Below 2^31, or the call is refused; but states that several sequences name, by offsets that descend, count more than once.  Nothing
+    // is done then: the numbers of blocks would begin anew, and the second launch would look for parts that are none.)
+    const bool fits = looked.all >> 31 == 0;
+    const int all_blocks = fits ? (int)looked.all : 0;
     int least = kLeastBlocks;
     if constexpr (KEYS == kStates) {
         int longest = blocks_of(looked.mine);
@@ -712,7 +715,7 @@ attn_stream_kernel(StreamParams p) {
         least = max(1, min(4, __builtin_amdgcn_readfirstlane(longest) / kManyParts));
     }
     const int share = max(least, (all_blocks + p.waves - 1) / p.waves);
-    if (wave == 0 && lane == 0) *p.share = share;
+    if (wave == 0 && lane == 0) *p.share = fits ? share : 0;
     const int b0 = (int)min((int64_t)wave * share, (int64_t)all_blocks), b1 = (int)min((int64_t)b0 + share, (int64_t)all_blocks);
     if (b0 >= b1) return;
     int64_t in_seg;
@@ -890,10 +893,10 @@ attn_merge_stream_kernel(StreamParams p) {
     const int heads = KEYS == kStates ? p.heads : a.Hkv;
     const int i = (int)blockIdx.x / heads, g = (int)blockIdx.x % heads;
     const DivMod lg = KEYS == kStates ? uniform_div_mod(g, p.by_hkv) : DivMod{0, g};
-    const int share = max(1, *p.share), start = p.start[i];     // (asked for with the segment; `start` is looked at if it has blocks)
+    const int share = *p.share, start = p.start[i];             // (asked for with the segment; `start` is looked at if it has blocks)
     const float qs = score_scale(a.scale[KEYS == kStates ? lg.q : uniform_div_mod(i, p.by_layers).r]);
     const Segment x = uniform_segment<KEYS>(p, i);
-    if ((int)blockIdx.y * p.join_rows >= x.rows) return;
+    if (share <= 0 || (int)blockIdx.y * p.join_rows >= x.rows) return;
     const int u0 = x.end == 0 ? 0 : start + g * blocks_of(x);
     const int w0 = u0 / share, w1 = (u0 + blocks_of(x) - 1) / share;
     if (x.end > 0 && w0 == w1) return;                          // one wavefront has written it

@@ -73,3 +73,23 @@ def test_chunk_attn(off, whose, dtype):
     P.prefixkv_chunk_attn(cache, q, i32(good), scale, T, out=ok)
     assert torch.equal(out, ok)
     rest_is_left(out, off, whose)
+
+
+def test_states_that_many_sequences_name():
+    """Offsets that go to and fro name all states 512 times, 2^31 blocks of them: more than are counted.  Nothing is written, and the
+    next call, with the same workspace, is as ever."""
+    S, heads, most = 1024, 32, 1 << 22
+    q, _, _ = projected(gen(4), 1, heads, heads, S, 64, BF16)
+    states = torch.zeros((1, 1, most, 64), dtype=BF16, device=DEV)
+    states[:, :, :S] = torch.randn((S, 64), generator=gen(5)).to(BF16).to(DEV)
+    k = v = states.expand(1, heads, most, 64)
+    scale, off = torch.full((1,), 0.2, device=DEV), i32(np.arange(S + 1))
+    ws = torch.zeros(P.cross_workspace_bytes(S, 1, heads, heads, S, most, 64, BF16, 1), dtype=torch.uint8, device=DEV)
+    assert ws.numel() > 0                                       # units long enough for blocks that are shared out
+    ws.fill_(127)
+    out = torch.full_like(q, 9.0)
+    P.prefixkv_cross_attn(q, k, v, off, i32([most * (i % 2) for i in range(S + 1)]), scale, 1, out=out, ws=ws)
+    torch.cuda.synchronize()
+    assert bool((out == 9).all())
+    P.prefixkv_cross_attn(q, k, v, off, off, scale, 1, out=out, ws=ws)
+    assert torch.equal(out, v[:, :, :S])                        # one state each
