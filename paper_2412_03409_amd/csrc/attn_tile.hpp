@@ -353,4 +353,7 @@ __device__ __forceinline__ RowAt row_at(int row, FastDiv grp) {
     return {x.q, x.r};
 }
 
+// How many states all of some rows see, and how many some of them do
+struct Limits { int all, some; };
+
 }  // namespace pkv

@@ -136,8 +136,7 @@ struct Plan {
 __device__ __forceinline__ int seen_by(const CrossParams& p, const Text& x, int row) {
     return max(0, min(p.seen[x.first + row_at(row, p.by_grp).token], x.len));
 }
-// how many all of the rows row0 ... row0+ROWS-1 see, and how many some row does
-struct Limits { int all, some; };
+// Limits of the rows row0 ... row0+ROWS-1
 template <int ROWS>
 __device__ __forceinline__ Limits limits(const CrossParams& p, const Text& x, int row0, int lane) {
     int lo = x.len, hi = 0;

@@ -317,8 +317,7 @@ __device__ __forceinline__ int tile_end(const Work& p, const Segment& x, int i) 
     return max(0, min(x.len, x.before + last + 1));
 }
 
-// How many states all of the rows row0 ... row0+ROWS-1 of a segment see, and some of them.
-struct Limits { int all, some; };
+// Limits of the rows row0 ... row0+ROWS-1 of a segment
 template <int ROWS>
 __device__ __forceinline__ Limits limits(const Work& p, const Segment& x, int row0, int lane) {
     if (!p.a.seen) return {x.len, x.len};
@@ -669,7 +668,7 @@ attn_merge_tiles_kernel(TileParams p) {
 
 // ---- few rows: the keys of a launch shared out evenly over the wavefronts ---------------------------------
 // (States are the same in every layer: there a segment is a sequence, and its heads are those of all layers.)
-struct StreamParams : Work {
+struct FewRowsParams : Work {
     int heads;                      // of a segment
     FastDiv by_hkv, by_heads;
     int waves;
@@ -688,7 +687,7 @@ __device__ __forceinline__ int blocks_of(const Segment& x) { return (x.end + kBl
 
 template <int D, Keys KEYS>
 __global__ void __launch_bounds__(128, 128 / D)
-attn_stream_kernel(StreamParams p) {
+attn_stream_kernel(FewRowsParams p) {
     constexpr int ROWB = D * 2, kBytes = kBlockKeys * ROWB, kInst = CopyLane<D>::kCopies;            // copies per 16 keys and tensor
     __shared__ __attribute__((aligned(1024))) unsigned char sKa[2][kBytes];
     __shared__ __attribute__((aligned(1024))) unsigned char sVa[2][kBytes];
@@ -885,7 +884,7 @@ attn_stream_kernel(StreamParams p) {
 constexpr int kJoinThreads = 256;
 template <int D, Keys KEYS>
 __global__ void __launch_bounds__(kJoinThreads)
-attn_merge_stream_kernel(StreamParams p) {
+attn_merge_stream_kernel(FewRowsParams p) {
     constexpr int LPP = D / 4, GROUPS = kJoinThreads / LPP;
     __shared__ float2 s_ms[GROUPS];
     __shared__ float4 s_o[GROUPS][LPP];
@@ -952,7 +951,7 @@ attn_merge_stream_kernel(StreamParams p) {
 // of keys and values of 32 sequences in 140 us, 5.5 TB/s.
 template <int D, int WAVES>
 __global__ void __launch_bounds__(WAVES * kWave, 2)
-attn_unit_kernel(StreamParams p) {
+attn_unit_kernel(FewRowsParams p) {
     constexpr int ROWB = D * 2, kBytes = kBlockKeys * ROWB, kInst = CopyLane<D>::kCopies, LPP = D / 4;
     static_assert(2 * kBytes == kFewRows * D * 4, "a part lies where the keys and values were");
     __shared__ __attribute__((aligned(1024))) unsigned char s_kv[WAVES][2 * kBytes];
@@ -1140,7 +1139,7 @@ static hipError_t launch_tiles(const pkv_packed& s, const PackedParams& a, void*
 
 template <int D, Keys KEYS>
 static hipError_t launch_stream(const pkv_packed& s, const PackedParams& a, void* ws, hipStream_t st) {
-    StreamParams p;
+    FewRowsParams p;
     (Work&)p = work_of(s, a);
     p.heads = s.Hkv;
     p.by_hkv = fast_div(s.Hkv);

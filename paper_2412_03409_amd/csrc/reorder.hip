@@ -55,7 +55,7 @@ constexpr uint32_t kTakes = 1, kWrong = 2;
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 // What a lane knows of its place: in every column the same.
-struct Place {
+struct GroupPlace {
     int w, col, s, parent;              // parent: lane of its column, -1
     bool real, again;                   // again: a lower place continues the same one
     int old_len, new_len;
@@ -64,7 +64,7 @@ struct Place {
 __device__ __forceinline__ int pages_in(const ReorderParams& p, int len) { return (len + (1 << p.shift) - 1) >> p.shift; }
 
 // -> false where a parent or a length cannot be (of the whole group's)
-__device__ __forceinline__ bool look(const ReorderParams& p, int g, int l, int lane, Place& x) {
+__device__ __forceinline__ bool look(const ReorderParams& p, int g, int l, int lane, GroupPlace& x) {
     x.w = lane & (p.lanes - 1);
     x.col = lane / p.lanes;
     x.real = x.w < p.W;
@@ -83,10 +83,10 @@ __device__ __forceinline__ bool look(const ReorderParams& p, int g, int l, int l
     }
     return true;
 }
-__device__ __forceinline__ bool copies(const ReorderParams& p, const Place& x) { return x.again && (x.new_len & ((1 << p.shift) - 1)) != 0; }
+__device__ __forceinline__ bool copies(const ReorderParams& p, const GroupPlace& x) { return x.again && (x.new_len & ((1 << p.shift) - 1)) != 0; }
 
 struct Column { int id, next; bool in_old, in_new, given; };     // old and new entry (next: of a copied page the one copied from)
-__device__ __forceinline__ Column column(const ReorderParams& p, const Place& x, int l, int lane, int j) {
+__device__ __forceinline__ Column column(const ReorderParams& p, const GroupPlace& x, int l, int lane, int j) {
     Column c;
     c.in_old = j < pages_in(p, x.old_len);
     c.in_new = j < pages_in(p, x.new_len);
@@ -105,7 +105,7 @@ __device__ __forceinline__ Column column(const ReorderParams& p, const Place& x,
 }
 // the columns of a wavefront: a quarter, in steps of 64 / lanes
 struct Range { int begin, end, step; };
-__device__ __forceinline__ Range columns_of(const ReorderParams& p, const Place& x, int wv) {
+__device__ __forceinline__ Range columns_of(const ReorderParams& p, const GroupPlace& x, int wv) {
     int most = max(pages_in(p, x.old_len), pages_in(p, x.new_len));
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) most = max(most, __shfl_xor(most, d, kWave));
@@ -113,7 +113,7 @@ __device__ __forceinline__ Range columns_of(const ReorderParams& p, const Place&
     return {min(most, wv * each), min(most, (wv + 1) * each), step};
 }
 // pages that this wavefront's columns give back, of each place (in the lanes of column 0)
-__device__ __forceinline__ int count_given(const ReorderParams& p, const Place& x, int l, int lane, const Range& r) {
+__device__ __forceinline__ int count_given(const ReorderParams& p, const GroupPlace& x, int l, int lane, const Range& r) {
     int given = 0;
     for (int j = r.begin; j < r.end; j += r.step) {
         const Column c = column(p, x, l, lane, j + x.col);
@@ -136,7 +136,7 @@ reorder_count_kernel(ReorderParams p) {
             ((int*)p.given)[p.n - p.n % 4 + tid] = 0;
         }
     }
-    Place x;
+    GroupPlace x;
     const bool ok = look(p, g, l, lane, x);
     if (ok) {
         const int given = count_given(p, x, l, lane, columns_of(p, x, wv));
@@ -229,7 +229,7 @@ reorder_apply_kernel(ReorderParams p) {
     int g = 0, l = 0, seg = 0, split = 0;
     int2 from = make_int2(-1, 0);
     const int4 hd = p.head[0];
-    Place x;
+    GroupPlace x;
     bool known = true;
     if (tables) {
         const DivMod gl = uniform_div_mod((int)blockIdx.x, p.by_layers);
