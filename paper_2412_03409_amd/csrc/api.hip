@@ -479,7 +479,6 @@ int prefixkv_beam_select(int S, int W, int V, int dtype, const void* logits, int
     if (dtype != PKV_F32 && dtype != PKV_BF16) return PKV_ERR_DTYPE;
     const int esize = dtype == PKV_F32 ? 4 : 2;
     if (row_stride < 0 || ((uintptr_t)logits & (uintptr_t)(esize - 1))) return PKV_ERR_STRIDE;
-    if (!beam_fits(S, W, V, esize)) return PKV_ERR_UNSUPPORTED;
     if (!ws || ws_bytes < beam_ws_bytes(S, W, V, esize) || !aligned16(ws)) return PKV_ERR_WORKSPACE;
     const hipError_t e = launch_beam(S, W, V, dtype == PKV_BF16, logits, row_stride, scores, ended, end_token, tokens, parents,
                                      scores_out, ended_out, ws, (hipStream_t)stream);

@@ -25,7 +25,7 @@ constexpr int kWaveCandidates = 128;    // of a wavefront's part of a piece
 constexpr int kManyFound = 512;         // candidates of a prompt beyond which those that cannot be are sorted out (4 prompts of 32 beams, 2729 tokens: 68 -> 20 us; 200 candidates: 24.5, 28.1 so)
 
 struct BeamParams {
-    int S, W, V, pieces;            // pieces of a row
+    int W, V, pieces;               // pieces of a row
     int group;                      // pieces, rounded up to a power of two
     int64_t stride;                 // of a row, in elements
     const void* logits;
@@ -596,7 +596,8 @@ static Pieces pieces_of(int rows, int V, int esize) {
     return {nv, pieces};
 }
 
-bool beam_fits(int S, int W, int V, int esize) { return (int64_t)S * W * pieces_of(S * W, V, esize).count < 1 << 24; }
+// workgroups are counted in 24 bits, as a grid's threads (256 of a workgroup) are in 32
+static_assert((int64_t)kMaxS * kMaxBeams * kMaxPieces < 1 << 24, "any call's pieces are a grid");
 
 size_t beam_ws_bytes(int S, int W, int V, int esize) {
     const int64_t lists = (int64_t)S * W * pieces_of(S * W, V, esize).count;
@@ -608,7 +609,7 @@ hipError_t launch_beam(int S, int W, int V, bool bf16, const void* logits, int64
                        hipStream_t st) {
     const Pieces pc = pieces_of(S * W, V, bf16 ? 2 : 4);
     BeamParams p;
-    p.S = S; p.W = W; p.V = V; p.pieces = pc.count; p.stride = stride;
+    p.W = W; p.V = V; p.pieces = pc.count; p.stride = stride;
     p.logits = logits; p.scores = scores; p.ended = ended; p.end_token = end_token;
     p.by_pieces = fast_div(pc.count); p.by_w = fast_div(W);
     p.group = 1;

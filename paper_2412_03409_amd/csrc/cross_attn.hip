@@ -23,7 +23,7 @@
 namespace pkv {
 
 struct CrossParams {
-    int S, L, H, Hkv, T, M, grp, max_rows;
+    int S, T, M, grp, max_rows;
     int heads, heads_per_xcd;           // heads: L * Hkv; heads_per_xcd: 0 if they do not divide up
     FastDiv by_grp, by_hkv, by_heads;
     const unsigned char *q, *k, *v;
@@ -567,7 +567,7 @@ static hipError_t launch(const CrossParams& p, long long tiles, bool cut, bool l
 hipError_t launch_cross_tiles(const pkv_packed& s, const PackedAttn& a, hipStream_t st) {
     auto bytes = [](Strides x) { return Strides{0, x.l * 2, x.h * 2, x.n * 2}; };
     CrossParams p;
-    p.S = s.S; p.L = s.L; p.H = s.H; p.Hkv = s.Hkv; p.T = s.T; p.M = a.M; p.grp = s.H / s.Hkv; p.max_rows = a.max_rows;
+    p.S = s.S; p.T = s.T; p.M = a.M; p.grp = s.H / s.Hkv; p.max_rows = a.max_rows;
     p.heads = s.L * s.Hkv;
     p.heads_per_xcd = p.heads % kXcds == 0 ? p.heads / kXcds : 0;
     p.by_grp = fast_div(p.grp); p.by_hkv = fast_div(s.Hkv); p.by_heads = fast_div(p.heads);

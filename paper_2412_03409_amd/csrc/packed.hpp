@@ -29,7 +29,6 @@ hipError_t launch_reorder(int S, int W, int Hkv, int row_bytes, const pkv_paging
                           int32_t* state_out, void* kp, void* vp, int32_t* status, void* ws, hipStream_t st);
 
 // the best continuations of S prompts of W beams
-bool beam_fits(int S, int W, int V, int esize);
 size_t beam_ws_bytes(int S, int W, int V, int esize);
 hipError_t launch_beam(int S, int W, int V, bool bf16, const void* logits, int64_t stride, const float* scores, const uint8_t* ended,
                        int end_token, int32_t* tokens, int32_t* parents, float* scores_out, uint8_t* ended_out, void* ws,

@@ -30,7 +30,7 @@ constexpr int kOwnSums = 1024;          // segments up to which a workgroup sums
 constexpr int kCopyBytes = 32768;       // of a tensor that a workgroup copies
 
 struct ReorderParams {
-    int S, W, layers, n;                // n = S * layers segments
+    int W, layers, n;                   // n = S * layers segments
     int lanes;                          // of a column: W, rounded up to a power of two
     int num_pages, max_pages, shift;
     int units, splits;                  // units: groups * layers; splits: workgroups that copy a segment's rows
@@ -372,7 +372,7 @@ hipError_t launch_reorder(int S, int W, int Hkv, int row_bytes, const pkv_paging
                           const int32_t* lens, int32_t* ring, const int32_t* state, int32_t* table_out, int32_t* lens_out,
                           int32_t* state_out, void* kp, void* vp, int32_t* status, void* ws, hipStream_t st) {
     ReorderParams p;
-    p.S = S; p.W = W; p.layers = g.layers; p.n = S * g.layers;
+    p.W = W; p.layers = g.layers; p.n = S * g.layers;
     p.lanes = 1;
     while (p.lanes < W) p.lanes *= 2;
     p.num_pages = g.num_pages; p.max_pages = g.max_pages; p.shift = __builtin_ctz((unsigned)g.page_size);
