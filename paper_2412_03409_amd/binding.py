@@ -678,7 +678,7 @@ def _i32_like(t: torch.Tensor, shape, what: str) -> torch.Tensor:
 
 @lru_cache(maxsize=256, typed=True)
 def page_workspace_bytes(S: int, layers: int) -> int:
-    return int(load().prefixkv_page_workspace_bytes(S, layers))
+    return int(load().prefixkv_page_workspace_bytes(_c_int(index(S), "S"), _c_int(index(layers), "layers")))
 
 
 def _page_out(cache: PagedCache, status, lens_out, state_out, ws):
@@ -794,7 +794,8 @@ _CODES = {torch.float32: PKV_F32, torch.bfloat16: PKV_BF16}
 def _packed(S, Hkv, qsh, dtype) -> _Packed:
     if dtype not in _CODES:
         raise TypeError(f"unsupported storage dtype {dtype}")
-    return _Packed(S, qsh[0], qsh[1], Hkv, qsh[2], qsh[3], _CODES[dtype])
+    return _Packed(*(_c_int(index(x), what) for x, what in ((S, "S"), (qsh[0], "L"), (qsh[1], "H"), (Hkv, "Hkv"), (qsh[2], "T"), (qsh[3], "D"))),
+                   _CODES[dtype])
 
 
 @lru_cache(maxsize=512)
@@ -1062,7 +1063,7 @@ def prefixkv_beam_select(logits: torch.Tensor, scores: torch.Tensor, ended: Opti
 
 @lru_cache(maxsize=256, typed=True)
 def reorder_workspace_bytes(S: int, layers: int) -> int:
-    return int(load().prefixkv_reorder_workspace_bytes(S, layers))
+    return int(load().prefixkv_reorder_workspace_bytes(_c_int(index(S), "S"), _c_int(index(layers), "layers")))
 
 
 def prefixkv_page_reorder(cache: PagedCache, parents: torch.Tensor, status: Optional[torch.Tensor] = None,
