@@ -476,7 +476,8 @@ int prefixkv_cross_attn(const pkv_packed *shape, const void *q, pkv_strides qs, 
  *   tokens, parents [dev] i32 [S,W], scores_out [dev] fp32 [S,W], ended_out [dev] u8 [S,W]: the beam had ended or its token is
  *       end_token.  scores_out may be scores, ended_out may be ended.
  *   ws [dev]: prefixkv_beam_workspace_bytes(S, W, V, dtype) bytes, any contents, 16-byte aligned
- * 1 <= S <= 4096, 1 <= W <= 32, 1 <= V <= 2^20.  Sums of exponentials in fp32 by pieces of a row, all else in fp64. */
+ * 1 <= S <= 4096, 1 <= W <= 32, 1 <= V <= 2^20.  Sums of exponentials in fp32 by pieces of a row, all else in fp64: equal rows of a call have
+ * equal sums, but how rows are cut goes by S, W and V, and a score may differ by a few 2^-24 between calls of other sizes. */
 size_t prefixkv_beam_workspace_bytes(int S, int W, int V, int dtype);
 int prefixkv_beam_select(int S, int W, int V, int dtype, const void *logits, int64_t row_stride, const float *scores,
                          const uint8_t *ended, int end_token, int32_t *tokens, int32_t *parents, float *scores_out,

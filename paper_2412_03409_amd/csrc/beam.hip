@@ -9,9 +9,9 @@
 //                     than W on the whole; each finds its rank by counting.
 //                     Bound: HBM, one read of the logits; with 32 beams the choice beside it (about 590 vector instructions of a wavefront
 //                     for 64 elements a lane).
-//                     64 x 4 rows of 128000 in fp32 22.7 us (5.8 TB/s); 8 x 32 rows of 100003 in bf16 18.7 (2.7 TB/s); 4 rows of 32000 5.9.
+//                     64 x 4 rows of 128000 in fp32 22.7 us (5.8 TB/s); 8 x 32 rows of 100003 in bf16 19.0 (2.7 TB/s); 4 rows of 32000 5.9.
 //  beam_join_kernel   a workgroup has a prompt: maxima and sums of the rows from their pieces, then the same choice among the pieces'
-//                     lists by their first entries.  Bound: dependent steps of one workgroup.  The same calls: 5.9, 10.4, 5.0 us.
+//                     lists by their first entries.  Bound: dependent steps of one workgroup.  The same calls: 5.9, 10.3, 4.9 us.
 //
 // A sum of exponentials of a piece is held in 32 bits (terms of a thread, then a tree); pieces, logarithms and scores in 64, because
 // beams are told apart by differences that 32 bits of a score of -10^2 do not hold.
@@ -61,8 +61,8 @@ __device__ __forceinline__ uint64_t key_of(double x) {
 
 // Terms of a row's sum are 2^(kLog2e x - base), one fma and one rounding of the exponent each; base = kLog2e * maximum, rounded, whose
 // residue (exact in 32 bits) is taken off behind the sum.  Beyond kWideLogit the difference from the maximum is scaled: the residue, up to
-// 2^-24 of the base, is an exponent of every term, which past 10^9 leaves the range and up to here stays below 2^-7.  (kLog2e is log2(e) but for 1.4e-8 of it: a sum's logarithm is off by that times the terms' mean distance from the
-// maximum, which is log V at most: below 2e-7.)
+// 2^-24 of the base, is an exponent of every term, which past 10^9 leaves the range and up to here stays below 2^-7.  (kLog2e is log2(e)
+// but for 1.4e-8 of it: a sum's logarithm is off by that times the terms' mean distance from the maximum, which is log V at most: below 2e-7.)
 // Nothing is added to a maximum: at 10^17 and beyond 64 bits would not hold the sum's logarithm next to it.
 constexpr float kLog2e = 1.44269502f, kWideLogit = 65536.f;
 constexpr double kLn2 = 0.693147180559945309417;

@@ -13,6 +13,10 @@
 // is large, a launch of its own (cross_plan_kernel, 6 to 7 us) looks at what each tile sees first, gives its pieces that length, and begins with the longest.
 // 6 texts of up to 700 rows over up to 2885 states, H32/8, 13.7 GFLOP: 6.5 + 32 + 8.5 us (without 49 + 10).
 //
+// Probabilities are rounded to bf16 for the second product, against the running maximum, as for prompts (attn_tile.hpp): with twice the
+// second products they would hold 16 bits, which matrix cores that bound the kernel have no room for.  The outputs are 0.0004 to 0.0013 from those of 32-bit
+// probabilities, relative over all elements, and 0.0014 to 0.0017 from 64 bits, as those are: most of it is their own rounding to bf16.
+//
 // Stages that some rows see and others do not are masked, and a probability of 0 times an infinite or NaN value that such a row must not
 // see would spoil it.  To look for such values in every masked stage costs a third of it, so a tile is worked on without, and again with
 // the look if a row of it came out infinite or NaN.
@@ -535,7 +539,8 @@ static long long all_tiles(const pkv_packed& s) {
 // Whether tiles may be cut: where texts are long (half as long again as the average is taken for the longest, as lengths are on the device) and
 // the tiles would not fill the chip several times over.  Joining costs 4 to 5 us where nothing was cut.  us, whole / cut: H12/4, 14 texts of
 // up to 3350 states and 20 rows 71 / 31; H16/8, one of 1827 and 238 rows 39 / 27; H40/40, 3 of up to 186 and 2872 rows 46 / 54; H32/4, 44
-// of up to 179 and 5 rows 8.6 / 13; H40/40, 3 of up to 839 and 3909 rows, D 64, 69 / 74 (cut all the same).
+// of up to 179 and 5 rows 8.6 / 13; H40/40, 3 of up to 839 and 3909 rows, D 64, 69 / 74 (cut all the same).  One long text among many short ones stays
+// whole, H32/8: 150 rows over 5000 states and 31 texts of 40 over 40 95 / 41, 300 over 2500 and 15 of 40 over 30 53 / 39; 700 over 8000 and 31 of 40 over 20 150 / 147.
 constexpr double kCutStages = 8.0;
 static bool may_cut(const pkv_packed& s, int M) { return 1.5 * M / s.S / kStage > kCutStages && all_tiles(s) < kManyTiles; }
 

@@ -1080,6 +1080,8 @@ size_t packed_attn_ws_bytes(const pkv_packed& s, int max_rows) {
 // 10.8 / 9.1; 4 rows of 2 sequences over up to 80, 4 layers of 32 heads, 11.6 / 5.6; 24 rows of 8 over up to 1003, 4 layers of 24, 50 / 38; 4 rows of 32
 // over up to 2880, H32, 162 / 144; a row over 2095, H16/8, 11.2 / 18.9; 8 rows of 3 over up to 1527, H12/4, 19 / 23; a row of 40 over up to 4000,
 // H32/8, 83 / 93.  The geometric mean of 90 calls, all of them by units: 0.80 of the time; by this rule 0.72.
+// The average says nothing of a long sequence among short ones, whose units then take as long as it does (1.8 us for every 256 states): 4 rows of 16, one over
+// 28000 and the others over 40 states, H32/8, 49 / 195, over 8000 29 / 62, of 32 over 2880 and 100 22 / 35; of 8 over 14000 36 / 36 (shared out by the rule).
 static double unit_blocks(const pkv_packed& s, int M) { return (double)M / s.S / kBlockKeys; }
 static bool per_unit(const pkv_packed& s, int M) {
     const double units = (double)s.S * s.L * s.Hkv, most = 24 + units / 4;

@@ -26,7 +26,10 @@ namespace pkv {
 constexpr int kReorderThreads = 256;
 constexpr int kReorderWaves = kReorderThreads / kWave;
 constexpr int kSumThreads = 1024;
-constexpr int kOwnSums = 1024;          // segments up to which a workgroup sums them up itself (3456 segments 42.9 us so, 28.8 with a launch of its own; 128: 10.4, 12.1)
+// Segments up to which a workgroup sums them up itself.  us, so / with a launch of its own, 4 places a group: 8 heads of 128, 512 segments 14.9 / 17.3,
+// 1024 18.5 / 21.7, 1280 19.9 / 22.0, 1536 26.4 / 28.5, 2048 37.8 / 37.6, 4096 65.4 / 56.5; a head of 64, 128 segments 10.9 / 14.2, 1024 11.3 / 14.0, 1536 12.7 / 13.9,
+// 2048 13.8 / 15.2, 4096 19.7 / 17.5 (groups of 8: 24.2 / 17.5).  They meet at about 2048: up to there this is 1 to 2 us too careful.
+constexpr int kOwnSums = 1024;
 constexpr int kCopyBytes = 32768;       // of a tensor that a workgroup copies
 
 struct ReorderParams {
