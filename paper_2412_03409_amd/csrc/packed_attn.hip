@@ -1089,7 +1089,7 @@ static bool per_unit(const pkv_packed& s, int M) {
 }
 // Many units want small workgroups, of which a compute unit holds several, the short ones sooner.  us, 8 / 4 / 2 wavefronts: 8 units over up to 80 states
 // 6.4 / 6.9 / 8.2, 448 over up to 220 14.9 / 13.1 / 14.8, 800 over up to 80 (D 64) 12.0 / 7.0 / 7.8; 8 / 4: 384 over up to 469 11.1 / 12.5, 768 over up to 1003
-// 37.8 / 35.3, 1024 over up to 2880 140 / 146; 4 / 2: 6144 over up to 38 59 / 39; 8 / 2: 1248 over up to 1761 66 / 77, 3072 over 1000 289 / 278,
+// 37.8 / 35.3, 1024 over up to 2880 140 / 146; 4 / 2: 6144 over up to 38 59 / 39; 8 / 2: 1248 over up to 1761 66 / 77,
 // 2048 over 500 115 / 101, 16384 over 300 612 / 489, 51200 of which 1600 have a row 128 / 51, 2048 of which 32 have one 7.2 / 10.3.
 static int unit_waves(const pkv_packed& s, int M) {
     const int units = s.S * s.L * s.Hkv, many = compute_units() * (unit_blocks(s, M) > 24 ? 8 : unit_blocks(s, M) > 6 ? 2 : 1);
